@@ -428,6 +428,133 @@ cm_status cm_context_kernel_times(cm_context *ctx, cm_kernel_times *out, int32_t
  * The calling thread's current device is restored on return. */
 cm_status cm_measure_int_alu(int32_t device, double *xor3_tops, double *compress_tops);
 
+/* ------------------------------------------------------------------ 8-bit paged cache
+ *
+ * What follows a render: the merged cache (and the tokens decoded after it) held in 8 bits in
+ * a paged pool, and attention that reads it. The paper has no counterpart; Section 4.5 names
+ * block-addressable caches as what the merge feeds. A step of a serving loop is
+ *     cm_qcache_schedule   block tables, slots and row starts from the requests' lengths
+ *     cm_qcache_append     K and V rows (a render's, or a layer's new tokens) into their slots
+ *     cm_qcache_attend     softmax(scale q K^T) V over each request's own tokens
+ * All three enqueue one kernel on `stream` and return without waiting; they allocate nothing and
+ * keep nothing between calls, so they can be captured in a CUDA graph. Lengths, tables and slots
+ * are DEVICE arrays that the host never reads; entries that name no block of the pool, and lengths
+ * beyond the buffers, are left out rather than followed. Distinct arguments must not overlap
+ * unless said otherwise. */
+
+typedef enum cm_qcache_format {
+    CM_QCACHE_E4M3 = 0,           /* 8-bit floating point, 4 exponent and 3 mantissa bits, to 448 */
+    CM_QCACHE_INT8 = 1            /* two's complement, -127 .. 127 are written */
+} cm_qcache_format;
+
+/* A paged 8-bit cache. Token t of block b (layer l, kv head h) has head_dim codes, contiguous, at
+ * byte b * stride_block + l * stride_layer + h * stride_head + t * stride_token of k_codes (K) and
+ * v_codes (V), and the scales at element b * scale_stride_block + l * scale_stride_layer
+ * + h * scale_stride_head of k_scales and v_scales: one scale for each block of tokens, layer and
+ * head. The stored value is code * scale. cm_qcache_append writes scales that are powers of two in
+ * [2^-60, 2^60]; cm_qcache_attend takes any finite positive scale (V scales beyond that range are
+ * read as its ends). Limits: layers, heads in [1, 65535]; head_dim a power of two in [16, 512]
+ * (cm_qcache_attend: 32, 64, 128 or 256); block_size a power of two in [16, 256]; num_blocks in
+ * [1, 2^31 - 1]; code strides positive multiples of 16; scale strides positive; code pointers
+ * 16-byte aligned. */
+typedef struct cm_qcache {
+    void *k_codes, *v_codes;             /* DEVICE */
+    float *k_scales, *v_scales;          /* DEVICE */
+    int32_t format;                      /* cm_qcache_format */
+    int32_t num_layers, num_kv_heads, head_dim, block_size;
+    int32_t reserved;                    /* 0 */
+    int64_t num_blocks;
+    int64_t stride_block, stride_layer, stride_head, stride_token;
+    int64_t scale_stride_block, scale_stride_layer, scale_stride_head;
+} cm_qcache;
+
+/* The requests of a step, in DEVICE memory. */
+typedef struct cm_qcache_batch {
+    int32_t num_requests;                /* R >= 0 */
+    int32_t block_size;                  /* the cache's */
+    int64_t table_width;                 /* entries of a request's row of block_table */
+    int32_t *block_table;                /* [R][table_width]: block of token t at entry t / block_size */
+    int32_t *row_starts;                 /* [R + 1]: first row of each request's new tokens; ascending */
+    int32_t *kv_lens;                    /* [R]: tokens cached, the new ones included */
+} cm_qcache_batch;
+
+/* Block tables and slot maps from request lengths. Request r holds context_lens[r] tokens, whose
+ * blocks its table row names, and gets new_lens[r] more (negative lengths count as 0). The blocks
+ * that it needs beyond those it has, ceil((context + new) / B) - ceil(context / B) for B tokens to
+ * a block, are taken from free_blocks, in request order.
+ *   batch           block_table: the entries of the new blocks are written, the others kept;
+ *                   row_starts, kv_lens: written (R + 1 and R entries)
+ *   free_blocks     [num_free] block indices, taken from the front; an entry for which none is
+ *                   left becomes -1
+ *   slot_map        [max_rows]: the slot, block * block_size + place in the block, of each new row
+ *                   (row_starts[r] + i is token context_lens[r] + i of request r); -1 for rows past
+ *                   the last and rows without a block
+ *   counts          [2]: blocks needed (taken from the front of free_blocks, if there were as many)
+ *                   and rows
+ * Tokens beyond the table's width get no block (kv_lens stops there); rows beyond max_rows are not
+ * written (row_starts stops there). context_lens must not be batch->kv_lens. Limits:
+ * R <= 16384, max_rows < 2^31, block_size as for cm_qcache. */
+cm_status cm_qcache_schedule(cm_context *ctx, const cm_qcache_batch *batch, const int32_t *context_lens,
+                             const int32_t *new_lens, const int32_t *free_blocks, int64_t num_free,
+                             int64_t *slot_map, int64_t max_rows, int64_t *counts, cm_stream_t stream);
+
+/* K and V rows into their slots, for layers [layer, layer + num_layers) of the cache. Row i of
+ * head h of the j-th of those layers has head_dim bf16 values, contiguous, at element
+ * j * stride_layer + h * stride_head + i * stride_row of k and v (a rendered cache's strides are
+ * H * capacity * d, capacity * d and d; a layer's projections [rows][H][d] are fine too).
+ * For each block, layer and head that gets rows, and for K and V on their own: let p be the place of
+ * its first new token and m the largest finite |x| of its new values. The scale becomes the
+ * smallest 2^k, k in [-60, 60], with m <= 448 * 2^k (e4m3) or 127 * 2^k (int8), or stays if p > 0
+ * and it is larger; codes are x / scale to nearest even, clamped to +-448 or +-127, NaN to 0; where
+ * the scale grew, the codes of tokens 0 .. p - 1 are rounded again to it. The result is exactly that,
+ * whatever the launch.
+ *   slot_map    [num_rows] DEVICE: slots as cm_qcache_schedule writes them; one below 0 or beyond
+ *               the pool is skipped. The rows of one block must be consecutive with ascending slots:
+ *               a block that gets rows in two separate runs of one call ends up undefined.
+ *   k, v        DEVICE, 16-byte aligned; strides multiples of 8 */
+cm_status cm_qcache_append(cm_context *ctx, const cm_qcache *cache, int32_t layer, int32_t num_layers,
+                           const void *k, const void *v, int64_t stride_layer, int64_t stride_head,
+                           int64_t stride_row, const int64_t *slot_map, int64_t num_rows,
+                           cm_stream_t stream);
+
+/* Query rows and results of cm_qcache_attend. Row i, query head h has head_dim bf16 values at
+ * element i * q_stride_row + h * q_stride_head of q; out likewise. Query head h reads kv head
+ * h / (num_q_heads / num_kv_heads). */
+typedef struct cm_qcache_query {
+    const void *q;                       /* DEVICE, 16-byte aligned, bf16 */
+    void *out;                           /* DEVICE, 16-byte aligned, bf16 */
+    float *lse;                          /* nullable DEVICE [total_rows][num_q_heads] */
+    int64_t q_stride_row, q_stride_head, out_stride_row, out_stride_head;   /* multiples of 8 */
+    int32_t total_rows;                  /* rows of q, out and lse */
+    int32_t num_q_heads;                 /* a multiple of num_kv_heads */
+    int32_t max_rows_per_request;        /* the most query rows of one request that are expected;
+                                            it chooses the kernel, not the result */
+    int32_t causal;                      /* nonzero: row i of a request's n rows sees its first
+                                            kv_len - n + i + 1 tokens; 0: all kv_len */
+    float softmax_scale;                 /* finite; 1 / sqrt(head_dim) as a rule */
+    int32_t reserved;                    /* 0 */
+} cm_qcache_query;
+
+/* Attention of each request's rows (row_starts) over its own cached tokens (kv_lens, block_table):
+ * out = softmax(softmax_scale * q K^T) V with K and V the cache's values, and, if asked,
+ * lse = log sum exp of the scaled scores. A row that sees no token (no tokens, or causal with more
+ * rows than tokens) gives out = 0 and lse = -inf. Tokens whose table entry names no block of the pool
+ * are not attended. Rows of no request are left untouched. Codes of a request's tokens must be
+ * finite (an e4m3 NaN in V makes the rows near it NaN); codes and scales behind its last token may be
+ * anything. Sums and softmax statistics are fp32, weights fp16, the result is rounded once to bf16.
+ * Bit for bit reproducible on one GPU.
+ *   workspace   DEVICE, 16-byte aligned, at least cm_qcache_workspace() bytes: zeroed by the caller
+ *               once, before its first use; each call leaves it ready for the next. Calls that may
+ *               run at the same time (several streams) need one each.
+ * Limits: R <= 4096; head_dim 32, 64, 128 or 256; num_q_heads / num_kv_heads <= 128; the step's work
+ * (row tiles x tiles of 64 tokens of table_width) below 2^31. */
+cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t layer,
+                           const cm_qcache_batch *batch, const cm_qcache_query *query, void *workspace,
+                           int64_t workspace_bytes, cm_stream_t stream);
+
+/* Bytes of workspace that cm_qcache_attend needs on ctx's device at a head_dim. */
+cm_status cm_qcache_workspace(cm_context *ctx, int32_t head_dim, int64_t *out_bytes);
+
 /* Static name of a status code. */
 const char *cm_status_string(cm_status status);
 

@@ -9,6 +9,14 @@ loudly if the library has not been built; nothing here computes on the CPU.
     S = cm.FragmentSet(ctx)
     fid, absorbed = S.ingest(K, V)          # Algorithm 2, Ingest
     n, order = S.render(k_out, v_out)       # Algorithm 2, Render (= Algorithm 1)
+
+What decodes from a merged cache reads it in 8 bits (QCache, QBatch):
+
+    cache = cm.QCache(ctx, num_blocks, 16, L, H, d)           # e4m3 codes, a scale per block and head
+    batch = cm.QBatch(ctx, requests, table_width, max_rows, 16)
+    batch.schedule(context_lens, new_lens, free_blocks)       # block tables and slots
+    cache.append(k_out, v_out, batch.slot_map)                # the merged cache into its blocks
+    out, lse = cache.attend(q, batch, layer=0)                # softmax(q K^T / sqrt(d)) V
 """
 from ._binding import (  # noqa: F401
     CMError, Status, cm_id, cm_fragment, lib, LIB_PATH, EXPORTED,
@@ -21,4 +29,7 @@ from ._binding import (  # noqa: F401
     cm_context_set_timing, cm_context_kernel_times, cm_kernel_times, cm_union, cm_set_size, cm_set_seq_len, cm_set_ids,
     cm_render, cm_render_incremental, cm_render_paged, cm_paged_cache, cm_bagmerge,
     fragment_from_tensors, Context, FragmentSet,
+    cm_qcache, cm_qcache_batch, cm_qcache_query,
+    cm_qcache_schedule, cm_qcache_append, cm_qcache_attend, cm_qcache_workspace,
 )
+from .qcache import QBatch, QCache  # noqa: F401

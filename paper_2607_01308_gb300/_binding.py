@@ -79,6 +79,34 @@ class cm_render_job(ctypes.Structure):
                 ("capacity_tokens", ctypes.c_int64)]
 
 
+class cm_qcache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("format", ctypes.c_int32), ("num_layers", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("block_size", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("num_blocks", ctypes.c_int64),
+                ("stride_block", ctypes.c_int64), ("stride_layer", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64), ("stride_token", ctypes.c_int64),
+                ("scale_stride_block", ctypes.c_int64), ("scale_stride_layer", ctypes.c_int64),
+                ("scale_stride_head", ctypes.c_int64)]
+
+
+class cm_qcache_batch(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_int32), ("block_size", ctypes.c_int32),
+                ("table_width", ctypes.c_int64), ("block_table", ctypes.c_void_p),
+                ("row_starts", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p)]
+
+
+class cm_qcache_query(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("q_stride_row", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+                ("out_stride_row", ctypes.c_int64), ("out_stride_head", ctypes.c_int64),
+                ("total_rows", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+                ("max_rows_per_request", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
 _c = ctypes
 _P = ctypes.c_void_p
 _SIGS = {
@@ -130,6 +158,14 @@ _SIGS = {
     "cm_render_incremental": (_c.c_int, [_P, _P, _P, _c.c_int64, _c.POINTER(cm_id), _c.c_int64, _P,
                                          _c.POINTER(_c.c_int64), _c.POINTER(cm_id),
                                          _c.POINTER(_c.c_int64)]),
+    "cm_qcache_schedule": (_c.c_int, [_P, _c.POINTER(cm_qcache_batch), _P, _P, _P, _c.c_int64, _P,
+                                      _c.c_int64, _P, _P]),
+    "cm_qcache_append": (_c.c_int, [_P, _c.POINTER(cm_qcache), _c.c_int32, _c.c_int32, _P, _P,
+                                    _c.c_int64, _c.c_int64, _c.c_int64, _P, _c.c_int64, _P]),
+    "cm_qcache_attend": (_c.c_int, [_P, _c.POINTER(cm_qcache), _c.c_int32,
+                                    _c.POINTER(cm_qcache_batch), _c.POINTER(cm_qcache_query), _P,
+                                    _c.c_int64, _P]),
+    "cm_qcache_workspace": (_c.c_int, [_P, _c.c_int32, _c.POINTER(_c.c_int64)]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(lib, _name)
@@ -430,6 +466,34 @@ def cm_bagmerge(ctx: int, frags: Sequence[cm_fragment], k_out: int, v_out: int,
     _check(lib.cm_bagmerge(ctx, arr, len(frags), k_out, v_out, capacity_tokens,
                            _stream_handle(stream), ctypes.byref(seq)))
     return seq.value
+
+
+def cm_qcache_schedule(ctx: int, batch: cm_qcache_batch, context_lens: int, new_lens: int,
+                       free_blocks: int, num_free: int, slot_map: int, max_rows: int, counts: int,
+                       stream=None) -> None:
+    _check(lib.cm_qcache_schedule(ctx, ctypes.byref(batch), context_lens, new_lens, free_blocks,
+                                  num_free, slot_map, max_rows, counts, _stream_handle(stream)))
+
+
+def cm_qcache_append(ctx: int, cache: cm_qcache, layer: int, num_layers: int, k: int, v: int,
+                     stride_layer: int, stride_head: int, stride_row: int, slot_map: int,
+                     num_rows: int, stream=None) -> None:
+    _check(lib.cm_qcache_append(ctx, ctypes.byref(cache), layer, num_layers, k, v, stride_layer,
+                                stride_head, stride_row, slot_map, num_rows, _stream_handle(stream)))
+
+
+def cm_qcache_attend(ctx: int, cache: cm_qcache, layer: int, batch: cm_qcache_batch,
+                     query: cm_qcache_query, workspace: int, workspace_bytes: int,
+                     stream=None) -> None:
+    _check(lib.cm_qcache_attend(ctx, ctypes.byref(cache), layer, ctypes.byref(batch),
+                                ctypes.byref(query), workspace, workspace_bytes,
+                                _stream_handle(stream)))
+
+
+def cm_qcache_workspace(ctx: int, head_dim: int) -> int:
+    out = ctypes.c_int64()
+    _check(lib.cm_qcache_workspace(ctx, head_dim, ctypes.byref(out)))
+    return out.value
 
 
 # ---------------------------------------------------------------- torch-facing helpers

@@ -1,11 +1,15 @@
 """Builds libcm.so in-tree (next to this file) for sm_103a with nvcc and g++.
 
-Five translation units compiled in parallel, then one shared-library link:
+Nine translation units compiled in parallel, then one shared-library link:
   csrc/cm_host.cpp       host core (g++, C++17, no floating-point contraction)
   csrc/blake2s_tree.cu   content-address kernels (nvcc, sm_103a)
   csrc/render.cu         render kernel (nvcc, sm_103a)
   csrc/dedup.cu          byte comparison of the re-delivery fast path (nvcc, sm_103a)
   csrc/readback.cu       small device-to-host results written by the SMs (nvcc, sm_103a)
+  csrc/cm_qcache.cpp     8-bit paged cache: argument checks and launches (g++)
+  csrc/qcache_tables.cu  block tables and slot maps (nvcc, sm_103a)
+  csrc/qcache_append.cu  rows into the 8-bit cache (nvcc, sm_103a)
+  csrc/qcache_attention.cu  attention over the 8-bit cache, few rows per request (nvcc, sm_103a)
 The CUDA runtime is linked statically into libcm.so and only the cm_* symbols
 are exported (csrc/libcm.map).
 
@@ -36,8 +40,9 @@ NVCC_FLAGS = ["-std=c++17", "-O3", "-lineinfo", "-fmad=false", "-Xcompiler", "-f
 CXX_FLAGS = ["-std=c++17", "-O2", "-fPIC", "-ffp-contract=off", "-Wall", "-Wextra",
              "-I" + INCLUDE, "-I" + CSRC]
 
-CUDA_SOURCES = ["blake2s_tree.cu", "render.cu", "dedup.cu", "readback.cu"]
-CXX_SOURCES = ["cm_host.cpp"]
+CUDA_SOURCES = ["blake2s_tree.cu", "render.cu", "dedup.cu", "readback.cu", "qcache_tables.cu",
+                "qcache_append.cu", "qcache_attention.cu"]
+CXX_SOURCES = ["cm_host.cpp", "cm_qcache.cpp"]
 
 
 def _cuda_home() -> str:

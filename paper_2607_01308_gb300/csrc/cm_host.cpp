@@ -1922,4 +1922,9 @@ cm_status check_fragment(const cm_fragment *f) { return validate_fragment(f); }
 
 cm_status report_error(cm_status st, const char *msg) { return fail(st, msg); }
 
+// For the 8-bit cache calls (cm_qcache.cpp).
+int context_device(const cm_context *ctx) { return ctx->device; }
+
+int context_num_sms(const cm_context *ctx) { return ctx->num_sms; }
+
 }  // namespace cm
