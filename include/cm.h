@@ -352,11 +352,11 @@ cm_status cm_bagmerge(cm_context *ctx, const cm_fragment *frags, int32_t n, void
                       void *v_out, int64_t capacity_tokens, cm_stream_t stream,
                       int64_t *out_seq_len);
 
-/* Synchronise `stream` and report whether any render launched from ctx since the
- * last check had a device-side wait run out (render kernels bound every wait on
- * their own TMA copies to about one second, then record the failure and return
- * instead of hanging). Returns CM_ERR_TIMEOUT once per such event and clears it;
- * the output of the affected render is incomplete. CM_OK otherwise. */
+/* Synchronise `stream` and report whether any render or attention launched from ctx
+ * since the last check had a device-side wait run out (their kernels bound every wait
+ * on their own copies and matrix instructions to about one second, then record the
+ * failure and return instead of hanging). Returns CM_ERR_TIMEOUT once per such event and
+ * clears it; the output of the affected call is incomplete. CM_OK otherwise. */
 cm_status cm_context_check(cm_context *ctx, cm_stream_t stream);
 
 /* Re-delivery fast path for every later cm_ingest, cm_ingest_batch and cm_ingest_many

@@ -1,6 +1,6 @@
 """Builds libcm.so in-tree (next to this file) for sm_103a with nvcc and g++.
 
-Nine translation units compiled in parallel, then one shared-library link:
+Ten translation units compiled in parallel, then one shared-library link:
   csrc/cm_host.cpp       host core (g++, C++17, no floating-point contraction)
   csrc/blake2s_tree.cu   content-address kernels (nvcc, sm_103a)
   csrc/render.cu         render kernel (nvcc, sm_103a)
@@ -10,6 +10,7 @@ Nine translation units compiled in parallel, then one shared-library link:
   csrc/qcache_tables.cu  block tables and slot maps (nvcc, sm_103a)
   csrc/qcache_append.cu  rows into the 8-bit cache (nvcc, sm_103a)
   csrc/qcache_attention.cu  attention over the 8-bit cache, few rows per request (nvcc, sm_103a)
+  csrc/qcache_prefill.cu    the same, many rows per request (nvcc, sm_103a)
 The CUDA runtime is linked statically into libcm.so and only the cm_* symbols
 are exported (csrc/libcm.map).
 
@@ -41,7 +42,7 @@ CXX_FLAGS = ["-std=c++17", "-O2", "-fPIC", "-ffp-contract=off", "-Wall", "-Wextr
              "-I" + INCLUDE, "-I" + CSRC]
 
 CUDA_SOURCES = ["blake2s_tree.cu", "render.cu", "dedup.cu", "readback.cu", "qcache_tables.cu",
-                "qcache_append.cu", "qcache_attention.cu"]
+                "qcache_append.cu", "qcache_attention.cu", "qcache_prefill.cu"]
 CXX_SOURCES = ["cm_host.cpp", "cm_qcache.cpp"]
 
 

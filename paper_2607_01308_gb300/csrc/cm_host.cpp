@@ -509,8 +509,8 @@ cm_status take_device_error(cm_context *ctx, cudaStream_t stream) {
     if (e == 0) return CM_OK;
     CM_CUDA_TRY(cudaMemsetAsync(ctx->d_error, 0, sizeof(unsigned int), stream), "error word reset");
     CM_CUDA_TRY(cudaStreamSynchronize(stream), "error word synchronisation");
-    return fail(CM_ERR_TIMEOUT, "a bounded wait inside a render kernel timed out; that render's "
-                                "output is incomplete");
+    return fail(CM_ERR_TIMEOUT, "a bounded wait inside a kernel timed out; the output of the render or "
+                                "attention that ran it is incomplete");
 }
 
 // Byte comparison of a new fragment against a stored record with the same id.
@@ -1926,5 +1926,7 @@ cm_status report_error(cm_status st, const char *msg) { return fail(st, msg); }
 int context_device(const cm_context *ctx) { return ctx->device; }
 
 int context_num_sms(const cm_context *ctx) { return ctx->num_sms; }
+
+unsigned int *context_error_word(const cm_context *ctx) { return ctx->d_error; }
 
 }  // namespace cm

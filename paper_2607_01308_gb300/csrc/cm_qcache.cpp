@@ -17,6 +17,7 @@ namespace cm {
 // cm_host.cpp
 int context_device(const cm_context *ctx);
 int context_num_sms(const cm_context *ctx);
+unsigned int *context_error_word(const cm_context *ctx);
 }  // namespace cm
 
 namespace {
@@ -274,6 +275,7 @@ cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t laye
         p.total_rows = query->total_rows;
         p.causal = query->causal != 0;
         p.format = cache->format;
+        p.error = cm::context_error_word(ctx);
         cm::qcache_workspace_split(p, workspace, num_sms);
         const int64_t rows = (int64_t)(query->max_rows_per_request ? query->max_rows_per_request : query->total_rows) * group;
         return on_device(ctx, "attention launch", [&] {

@@ -171,11 +171,11 @@ __device__ __forceinline__ void write_row(const QcacheAttentionParams &p, const 
             l == 0.f ? -INFINITY : (m - headroom + __log2f(l)) * 0.693147180559945309f;
 }
 
-// The parts of a segment's whole range, held by thread blocks c0 .. c1, in that order.
-template <int ROWS, int D>
+// The parts of row n of a segment's whole range, held by thread blocks c0 .. c1, in that order;
+// at(c): the workspace row of block c's part.
+template <int D, class At>
 __device__ __forceinline__ void join_parts(const QcacheAttentionParams &p, const AttentionSegment &w, int n, int d, uint32_t c0,
-                                           uint32_t c1, float headroom) {
-    auto at = [&](uint32_t c) { return ((2 * (int64_t)c + (c == c0)) * ROWS + n); };
+                                           uint32_t c1, float headroom, At at) {
     float m = -INFINITY;
 #pragma unroll 8
     for (uint32_t c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(p.part_ml + at(c) * 2));
@@ -186,7 +186,7 @@ __device__ __forceinline__ void join_parts(const QcacheAttentionParams &p, const
         const float2 ml = __ldcg(reinterpret_cast<const float2 *>(p.part_ml + at(c) * 2));
         join(acc, l, __ldcg(reinterpret_cast<const float4 *>(p.part_o + at(c) * D + d)), ml.y, ml.x, m);
     }
-    write_row(p, w, w.row_tile * ROWS + n, d, acc, m, l, headroom);
+    write_row(p, w, n, d, acc, m, l, headroom);
 }
 
 }  // namespace

@@ -61,13 +61,14 @@ struct QcacheAttentionParams {
     float *part_o;                // workspace: partial outputs, then their (maximum, sum) pairs
     float *part_ml;
     unsigned int *arrived;
+    unsigned int *error;          // the context's word: bit 0 set when a bounded wait ran out
     float scale_log2;             // softmax scale * log2(e)
     int32_t requests, heads, group, head_dim, log2_block;
     int32_t total_rows, causal, format;
 };
 
-// The workspace holds, for every thread block of a launch, two partial results of `rows` rows
-// and an arrival counter.
+// The workspace holds, for every thread block of a launch, two partial results and an arrival
+// counter (for each of a block's row tiles).
 constexpr int kQcacheDecodeBlocksPerSm = 4;
 constexpr int kQcacheMaxAttentionRequests = 4096;   // a word of shared memory each
 size_t qcache_workspace_bytes(int head_dim, int num_sms);
@@ -75,5 +76,8 @@ void qcache_workspace_split(QcacheAttentionParams &p, void *workspace, int num_s
 // `rows_per_request`: the largest number of query rows of one request that is expected.
 cudaError_t launch_qcache_attention(const QcacheAttentionParams &p, int rows_per_request, int num_sms, int device,
                                     cudaStream_t stream);
+// The kernel for more rows per request, and the part rows of one of its thread blocks.
+cudaError_t launch_qcache_prefill(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream);
+size_t qcache_prefill_part_rows(int head_dim);
 
 }  // namespace cm

@@ -308,7 +308,8 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
                 __threadfence();
                 for (int x = tid; x < rows * (D / 4); x += kThreads) {
                     const int n = x / (D / 4), d = x % (D / 4) * 4;
-                    join_parts<C::kRows, D>(p, w, n, d, c0, c1, kHeadroom);
+                    join_parts<D>(p, w, w.row_tile * C::kRows + n, d, c0, c1, kHeadroom,
+                                  [&](uint32_t c) { return (2 * (int64_t)c + (c == c0)) * C::kRows + n; });
                 }
             }
         }
@@ -333,16 +334,20 @@ cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cuda
 
 }  // namespace
 
+// Part rows of a whole launch, of either kernel.
+static size_t part_rows(int head_dim, int num_sms) {
+    const size_t decode = (size_t)num_sms * kQcacheDecodeBlocksPerSm * 16, prefill = num_sms * qcache_prefill_part_rows(head_dim);
+    return 2 * (decode > prefill ? decode : prefill);
+}
+
 size_t qcache_workspace_bytes(int head_dim, int num_sms) {
-    const size_t blocks = (size_t)num_sms * kQcacheDecodeBlocksPerSm;
-    return blocks * 2 * 16 * ((size_t)head_dim + 2) * 4 + blocks * 4;
+    return part_rows(head_dim, num_sms) * ((size_t)head_dim + 2) * 4 + (size_t)num_sms * kQcacheDecodeBlocksPerSm * 4;
 }
 
 void qcache_workspace_split(QcacheAttentionParams &p, void *workspace, int num_sms) {
-    const size_t blocks = (size_t)num_sms * kQcacheDecodeBlocksPerSm;
     p.part_o = static_cast<float *>(workspace);
-    p.part_ml = p.part_o + blocks * 2 * 16 * p.head_dim;
-    p.arrived = reinterpret_cast<unsigned int *>(p.part_ml + blocks * 2 * 16 * 2);
+    p.part_ml = p.part_o + part_rows(p.head_dim, num_sms) * p.head_dim;
+    p.arrived = reinterpret_cast<unsigned int *>(p.part_ml + part_rows(p.head_dim, num_sms) * 2);
 }
 
 #define CM_EACH_DECODE(X) \
@@ -351,6 +356,7 @@ void qcache_workspace_split(QcacheAttentionParams &p, void *workspace, int num_s
 
 cudaError_t launch_qcache_attention(const QcacheAttentionParams &p, int rows_per_request, int num_sms, int device,
                                     cudaStream_t stream) {
+    if (rows_per_request > 16) return launch_qcache_prefill(p, num_sms, device, stream);
 #define CM_LAUNCH(D, F) \
     if (p.head_dim == D && p.format == F) \
         return rows_per_request <= 8 ? launch<D, F, 1>(p, num_sms, device, stream) : launch<D, F, 2>(p, num_sms, device, stream);

@@ -1,0 +1,622 @@
+// Attention over the 8-bit paged cache for many query rows per request (prompts, chunks of them).
+// The mathematics and the roundings are those of qcache_attention.cu: codes enter the matrix
+// instructions as fp16, the K scale multiplies the finished score, the V scale joins the exponent.
+//
+// One thread block per SM, on the tcgen05 tensor cores, with up to 256 query rows (rows are query
+// tokens x heads of a group) in two tiles of 128, so that each K and V tile that is brought in and
+// taken to fp16 serves both:
+//   warps 0-3, 4-7   softmax of query tile 0 and 1, one row per thread: scores from tensor memory,
+//                    weights back into the same columns as fp16, the output rescaled when the
+//                    running maximum is raised, the row normalised and written at the end
+//   warps 8-11       K and V tiles: 16 codes per load from their blocks, to fp16, into shared
+//                    memory in the 128-byte swizzle (two stages each)
+//   warp 12          one thread issues the matrix instructions: S = Q K^T (both operands from
+//                    shared memory), O += P V (P from tensor memory, V as it lies, tokens x head_dim)
+// While one tile's softmax runs, the tensor cores work on the other tile. Work is cut as in
+// qcache_attention.cu, over kv tiles that the rows of a tile may see at all.
+#include "cm_qcache_kernels.h"
+
+#include <atomic>
+
+#include "cm_qcache_attention.h"
+#include "cm_qcache_codes.h"
+
+namespace cm {
+namespace {
+
+constexpr int kSoftmaxWarps = 8, kLoadWarps = 4, kMmaWarp = kSoftmaxWarps + kLoadWarps;
+constexpr int kThreads = (kMmaWarp + 1) * 32;
+constexpr int kLoadThreads = kLoadWarps * 32;
+constexpr int kStages = 2;
+constexpr int kScaleStages = 4;             // softmax reads a tile's scales after its K has been given up
+constexpr float kRaise = 8.f, kHeadroom = 7.f;
+
+template <int D>
+struct Shape {
+    static constexpr int kQTiles = D == 256 ? 1 : 2;          // tensor memory: scores and outputs, 512 columns
+    static constexpr int kRows = 128 * kQTiles;
+    static constexpr int kTile = D == 256 ? 64 : 128;         // tokens of a kv tile
+    static constexpr int kPanels = D < 64 ? 1 : D / 64;       // 64 columns (128 bytes) of fp16 each
+    static constexpr int kQPanel = 128 * 128, kKvPanel = kTile * 128;   // bytes
+    static constexpr int kQBytes = kQTiles * kPanels * kQPanel;
+    static constexpr int kKvBytes = kPanels * kKvPanel;       // one tile of K or V
+    static constexpr int kBlocks = kTile / 16;                // scale entries of a tile
+    static constexpr int kChunks = kTile * D / 16 / kLoadThreads;   // 16-code loads of a thread for K (and for V)
+    static constexpr int kSColumns = 128;                     // tensor memory columns between score tiles
+    static constexpr int kOColumn = kQTiles * kSColumns;
+    static constexpr size_t kSmem = 1024 + kQBytes + 2 * kStages * kKvBytes;
+    static_assert(kChunks >= 1, "every load thread has work");
+    static_assert(kOColumn + kQTiles * D <= 512, "tensor memory");
+};
+
+// ---------------------------------------------------------------- barriers, bounded
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void bar_init(uint64_t *b, int n) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(n) : "memory");
+}
+
+__device__ __forceinline__ void bar_arrive(uint64_t *b) {
+    asm volatile("{\n.reg .b64 t;\nmbarrier.arrive.shared::cta.b64 t, [%0];\n}" ::"r"(smem_u32(b)) : "memory");
+}
+
+__device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000000;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+    return ok != 0;
+}
+
+// Waits for the phase of the given parity. A wait that runs out (about a second) is recorded, and
+// every later one then gives up at once, so that the block runs to its end with a wrong result that
+// the host can learn of.
+__device__ __noinline__ void bar_wait_slow(uint64_t *b, uint32_t parity, volatile int *failed, unsigned int *error) {
+    const long long t0 = clock64();
+    while (!bar_try(b, parity)) {
+        if (*failed) return;
+        if (clock64() - t0 > 2000000000ll) {
+            *failed = 1;
+            atomicOr(error, 1u);
+            return;
+        }
+    }
+}
+
+struct Waiter {
+    int *failed;
+    unsigned int *error;
+    __device__ __forceinline__ void operator()(uint64_t *b, uint32_t parity) const {
+        if (!bar_try(b, parity)) bar_wait_slow(b, parity, failed, error);
+    }
+    // of a whole warp, which goes on together
+    __device__ __forceinline__ void warp(uint64_t *b, uint32_t parity) const {
+        (*this)(b, parity);
+        __syncwarp();
+    }
+};
+
+// ---------------------------------------------------------------- tcgen05
+
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void commit(uint64_t *b) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+
+#define CM_REGS16(x, i) \
+    "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7]), \
+    "=r"(x[i + 8]), "=r"(x[i + 9]), "=r"(x[i + 10]), "=r"(x[i + 11]), "=r"(x[i + 12]), "=r"(x[i + 13]), "=r"(x[i + 14]), "=r"(x[i + 15])
+#define CM_IN16(x, i) \
+    "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7]), \
+    "r"(x[i + 8]), "r"(x[i + 9]), "r"(x[i + 10]), "r"(x[i + 11]), "r"(x[i + 12]), "r"(x[i + 13]), "r"(x[i + 14]), "r"(x[i + 15])
+
+// 32 columns of the warp's 32 lanes, one row per thread; the values are there after ld_wait.
+__device__ __forceinline__ void tmem_ld32(uint32_t (&x)[32], uint32_t at) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : CM_REGS16(x, 0), CM_REGS16(x, 16) : "r"(at));
+}
+__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&x)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(at), CM_IN16(x, 0), CM_IN16(x, 16) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&x)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(at), CM_IN16(x, 0) : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared memory operand in 128-byte swizzled atoms of 8 rows x 128 bytes. Rows of K (and Q) are
+// tokens (query rows) and the contraction runs along a row; for V the contraction runs over rows.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading, uint32_t stride) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+
+// fp32 accumulator, fp16 operands; b_rows: B's contraction runs over rows.
+__host__ __device__ constexpr uint32_t instruction(int m, int n, bool b_rows) {
+    return 1u << 4 | (b_rows ? 1u << 16 : 0u) | (uint32_t)(n / 8) << 17 | (uint32_t)(m / 16) << 24;
+}
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// ---------------------------------------------------------------- work
+
+// kv tiles that row tile rt of a request may see (one at least: its rows are written).
+template <int ROWS, int TILE>
+__device__ __forceinline__ int visible_tiles(const QcacheAttentionParams &p, const RequestShape &s, int rt) {
+    int limit = s.kv;
+    if (p.causal) limit = min(limit, max(0, s.kv - s.q_len + (min(s.rows, (rt + 1) * ROWS) - 1) / p.group + 1));
+    return max(1, (limit + TILE - 1) / TILE);
+}
+
+// Where a block's share begins, and the walk through it that every role makes for itself.
+template <int ROWS, int TILE>
+struct Walk {
+    RequestShape s;
+    int request, row_tile, head, tile, tiles;
+    uint64_t u, end;              // units: the next one, and the share's end
+
+    __device__ __forceinline__ bool next(const QcacheAttentionParams &p, AttentionSegment &w) {
+        if (u >= end) return false;
+        if (tile == tiles) {
+            tile = 0;
+            if (++head == p.heads) {
+                head = 0;
+                if (++row_tile == s.row_tiles) {
+                    row_tile = 0;
+                    do s = request_shape<ROWS, TILE>(p, ++request); while (s.row_tiles == 0);
+                }
+                tiles = visible_tiles<ROWS, TILE>(p, s, row_tile);
+            }
+        }
+        const int n = (int)min((uint64_t)(tiles - tile), end - u);
+        w.request = request; w.head = head; w.row_tile = row_tile;
+        w.t0 = tile; w.t1 = tile + n;
+        w.row0 = s.row0; w.q_len = s.q_len; w.kv = s.kv; w.rows = s.rows; w.tiles = tiles;
+        w.unit0 = u - tile;
+        tile += n;
+        u += n;
+        return true;
+    }
+};
+
+struct Start {
+    uint64_t u, end, per;
+    int request, row_tile, head, tile;
+};
+
+struct Barriers {
+    uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+    uint64_t scale_full[kScaleStages];
+    uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
+};
+
+template <int D, int FORMAT>
+__global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_constant__ QcacheAttentionParams p) {
+    using C = Shape<D>;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ Barriers bars;
+    __shared__ float4 scales[kScaleStages][C::kBlocks];   // k_scale, log2 v_scale, 1 / v_scale of 16 tokens each
+    __shared__ uint32_t scan[kThreads / 32];
+    __shared__ Start start;
+    __shared__ uint32_t tmem_base;
+    __shared__ uint32_t last_one[2];
+    __shared__ int failed;
+    unsigned char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + kStages * C::kKvBytes;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+
+    // the plan: one thread per request, prefix sums in the (still unused) tile memory
+    uint32_t *prefix = reinterpret_cast<uint32_t *>(smem);
+    uint32_t total = 0;
+    for (int r0 = 0; r0 < p.requests; r0 += kThreads) {
+        const int r = r0 + tid;
+        uint32_t n = 0;
+        if (r < p.requests) {
+            const RequestShape s = request_shape<C::kRows, C::kTile>(p, r);
+            for (int rt = 0; rt < s.row_tiles; ++rt) n += visible_tiles<C::kRows, C::kTile>(p, s, rt);
+        }
+        uint32_t a = n;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const uint32_t x = __shfl_up_sync(~0u, a, d);
+            if (lane >= d) a += x;
+        }
+        if (lane == 31) scan[warp] = a;
+        __syncthreads();
+        uint32_t before = total;
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) before += scan[w];
+            total += scan[w];
+        }
+        if (r < p.requests) prefix[r] = before + a - n;
+        __syncthreads();
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "n"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (tid == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            bar_init(&bars.k_full[i], kLoadWarps);
+            bar_init(&bars.v_full[i], kLoadWarps);
+            bar_init(&bars.k_empty[i], 1);
+            bar_init(&bars.v_empty[i], 1);
+        }
+        for (int i = 0; i < kScaleStages; ++i) bar_init(&bars.scale_full[i], 1);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&bars.q_full[i], 128);
+            bar_init(&bars.p_full[i], 128);
+            bar_init(&bars.s_full[i], 1);
+            bar_init(&bars.o_full[i], 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        failed = 0;
+        const uint64_t units = (uint64_t)total * (uint32_t)p.heads;
+        Start s;
+        s.per = units_per_block(units, gridDim.x);
+        s.u = (uint64_t)blockIdx.x * s.per;
+        s.end = min(s.u + s.per, units);
+        s.request = s.row_tile = s.head = s.tile = 0;
+        if (s.u < s.end) {
+            int lo = 0, hi = p.requests;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if ((uint64_t)prefix[mid] * (uint32_t)p.heads <= s.u) lo = mid; else hi = mid;
+            }
+            const RequestShape q = request_shape<C::kRows, C::kTile>(p, lo);
+            uint64_t in = s.u - (uint64_t)prefix[lo] * (uint32_t)p.heads;
+            s.request = lo;
+            while (true) {
+                const uint32_t n = visible_tiles<C::kRows, C::kTile>(p, q, s.row_tile);
+                const uint64_t all = (uint64_t)n * (uint32_t)p.heads;
+                if (in < all) {
+                    s.head = (int)(in / n);
+                    s.tile = (int)(in - (uint64_t)s.head * n);
+                    break;
+                }
+                in -= all;
+                ++s.row_tile;
+            }
+        }
+        start = s;
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const Waiter wait{&failed, p.error};
+    const uint32_t tmem = tmem_base;
+    Walk<C::kRows, C::kTile> walk;
+    walk.u = start.u;
+    walk.end = start.end;
+    if (walk.u < walk.end) {
+        walk.request = start.request; walk.row_tile = start.row_tile; walk.head = start.head; walk.tile = start.tile;
+        walk.s = request_shape<C::kRows, C::kTile>(p, walk.request);
+        walk.tiles = visible_tiles<C::kRows, C::kTile>(p, walk.s, walk.row_tile);
+    }
+    AttentionSegment w;
+
+    if (warp < kSoftmaxWarps) {
+        // ------------------------------------------------ softmax: one row per thread
+        const int qt = warp / 4, row = tid % 128;
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const uint32_t s_at = tmem + lanes + qt * C::kSColumns, o_at = tmem + lanes + C::kOColumn + qt * D;
+        uint32_t n_tile = 0;          // kv tiles of the block so far (scales)
+        uint32_t s_phase = 0, o_phase = 0;
+        const uint64_t per = start.per;
+        while (walk.next(p, w)) {
+            const int first = w.row_tile * C::kRows + qt * 128;   // of the tile, among the request's rows
+            if (first >= w.rows || qt >= C::kQTiles) {
+                n_tile += w.t1 - w.t0;
+                continue;
+            }
+            // this row of Q: fp16 with a power of two per row, into the swizzled tile
+            const int n = first + row;
+            const bool valid = n < w.rows;
+            const int i = n / p.group;
+            const uint16_t *q = p.q + (int64_t)(w.row0 + i) * p.q_stride_row + ((int64_t)w.head * p.group + n % p.group) * p.q_stride_head;
+            uint32_t m = 0;
+#pragma unroll 4
+            for (int c = 0; c < D / 8; ++c) {
+                if (!valid) break;
+                const uint4 x = __ldg(reinterpret_cast<const uint4 *>(q) + c);
+                m = __vmaxu2(m, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+            }
+            m = max(m & 0xffffu, m >> 16);
+            const int e = max((int)(m >> 7) - 127, -100);
+            // a negative softmax scale turns Q around, so that larger products are larger scores
+            const float up = p.scale_log2 < 0.f ? -pow2f(14 - e) : pow2f(14 - e);
+            const float factor = fabsf(p.scale_log2) * pow2f(e - 14);
+            unsigned char *q_row = q_smem + qt * C::kPanels * C::kQPanel + row * 128;
+#pragma unroll 4
+            for (int c = 0; c < D / 8; ++c) {
+                uint4 x = valid ? __ldg(reinterpret_cast<const uint4 *>(q) + c) : make_uint4(0, 0, 0, 0);
+                x.x = pack_half(__uint_as_float(x.x << 16) * up, __uint_as_float(x.x & 0xffff0000u) * up);
+                x.y = pack_half(__uint_as_float(x.y << 16) * up, __uint_as_float(x.y & 0xffff0000u) * up);
+                x.z = pack_half(__uint_as_float(x.z << 16) * up, __uint_as_float(x.z & 0xffff0000u) * up);
+                x.w = pack_half(__uint_as_float(x.w << 16) * up, __uint_as_float(x.w & 0xffff0000u) * up);
+                *reinterpret_cast<uint4 *>(q_row + c / 8 * C::kQPanel + ((c % 8) ^ (row & 7)) * 16) = x;
+            }
+            fence_async_smem();
+            bar_arrive(&bars.q_full[qt]);
+
+            const int limit = !valid ? 0 : p.causal ? min(w.kv, max(0, w.kv - w.q_len + i + 1)) : w.kv;
+            const int least = __reduce_min_sync(~0u, limit);      // of the warp's rows
+            float top = -INFINITY, sum = 0.f;
+            for (int t = w.t0; t < w.t1; ++t, ++n_tile) {
+                wait.warp(&bars.s_full[qt], s_phase);
+                s_phase ^= 1;
+                wait.warp(&bars.scale_full[n_tile % kScaleStages], n_tile / kScaleStages & 1);
+                fence_after();
+                const float4 *sc = scales[n_tile % kScaleStages];
+                const int left = limit - t * C::kTile;            // columns that this row sees
+                const bool masked = (t + 1) * C::kTile > least;
+                float high = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < C::kTile / 32; ++c) {
+                    uint32_t x[32];
+                    tmem_ld32(x, s_at + 32 * c);
+                    ld_wait();
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        float h = -INFINITY;
+                        if (masked) {
+#pragma unroll
+                            for (int k = 0; k < 16; ++k)
+                                if (32 * c + 16 * b + k < left) h = fmaxf(h, __uint_as_float(x[16 * b + k]));
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) h = fmaxf(h, __uint_as_float(x[16 * b + k]));
+                        }
+                        const float4 z = sc[2 * c + b];
+                        high = fmaxf(high, h == -INFINITY ? h : fmaf(h, factor * z.x, z.y));
+                    }
+                }
+                const bool raise = high > top + kRaise;
+                if (__any_sync(~0u, raise)) {
+                    const float now = raise ? high : top;
+                    const float f = top == now ? 1.f : exp2_fast(top - now);
+                    top = now;
+                    sum *= f;
+                    if (t > w.t0) {
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t x[32];
+                            tmem_ld32(x, o_at + 32 * c);
+                            ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
+                            tmem_st32(o_at + 32 * c, x);
+                        }
+                    }
+                }
+                const float base = (top == -INFINITY ? 0.f : top) - kHeadroom;
+#pragma unroll
+                for (int c = 0; c < C::kTile / 32; ++c) {
+                    uint32_t x[32], y[16];
+                    tmem_ld32(x, s_at + 32 * c);
+                    ld_wait();
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const float4 z = sc[2 * c + b];
+                        const float a = factor * z.x, d = z.y - base;
+                        float part = 0.f;
+#pragma unroll
+                        for (int k = 0; k < 16; k += 2) {
+                            float e0 = exp2_fast(fmaf(__uint_as_float(x[16 * b + k]), a, d));
+                            float e1 = exp2_fast(fmaf(__uint_as_float(x[16 * b + k + 1]), a, d));
+                            if (masked) {
+                                if (32 * c + 16 * b + k >= left) e0 = 0.f;
+                                if (32 * c + 16 * b + k + 1 >= left) e1 = 0.f;
+                            }
+                            part += e0 + e1;
+                            y[8 * b + k / 2] = pack_half(e0, e1);
+                        }
+                        sum = fmaf(part, z.z, sum);
+                    }
+                    tmem_st16(s_at + 16 * c, y);                  // columns whose scores have been read
+                }
+                st_wait();
+                fence_before();
+                bar_arrive(&bars.p_full[qt]);
+            }
+            wait.warp(&bars.o_full[qt], o_phase);
+            o_phase ^= 1;
+            fence_after();
+            const bool whole = w.t0 == 0 && w.t1 == w.tiles;
+            const int rows = min(128, w.rows - first);
+            const int64_t part = ((2 * (int64_t)blockIdx.x + (w.t0 == 0)) * C::kQTiles + qt) * 128;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t x[32];
+                __syncwarp();
+                tmem_ld32(x, o_at + 32 * c);
+                ld_wait();
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                    const float4 y = make_float4(__uint_as_float(x[k]), __uint_as_float(x[k + 1]), __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
+                    if (valid && whole) write_row(p, w, n, 32 * c + k, y, top, sum, kHeadroom);
+                    else if (valid) __stcg(reinterpret_cast<float4 *>(p.part_o + (part + row) * D + 32 * c + k), y);
+                }
+            }
+            if (!whole) {
+                if (valid) __stcg(reinterpret_cast<float2 *>(p.part_ml + (part + row) * 2), make_float2(top, sum));
+                const uint32_t c0 = (uint32_t)(w.unit0 / per), c1 = (uint32_t)((w.unit0 + w.tiles - 1) / per);
+                __threadfence();
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + qt) : "memory");
+                if (row == 0) last_one[qt] = atomicInc(p.arrived + (size_t)qt * gridDim.x + c0, c1 - c0) == c1 - c0;
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + qt) : "memory");
+                if (last_one[qt]) {
+                    __threadfence();
+                    for (int x = row; x < rows * (D / 4); x += 128)
+                        join_parts<D>(p, w, first + x / (D / 4), x % (D / 4) * 4, c0, c1, kHeadroom,
+                                      [&](uint32_t c) { return ((2 * (int64_t)c + (c == c0)) * C::kQTiles + qt) * 128 + x / (D / 4); });
+                }
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + qt) : "memory");
+            }
+        }
+    } else if (warp < kSoftmaxWarps + kLoadWarps) {
+        // ------------------------------------------------ K and V tiles to fp16
+        const int lt = tid - kSoftmaxWarps * 32;
+        constexpr int kPerRow = D / 16;                           // 16-code chunks of a token
+        uint32_t n_tile = 0;
+        const int in_block = (1 << p.log2_block) - 1;
+        while (walk.next(p, w)) {
+            const uint8_t *k_head = p.k + (int64_t)w.head * p.stride_head, *v_head = p.v + (int64_t)w.head * p.stride_head;
+            const int32_t *table = p.block_table + w.request * p.table_width;
+            // a chunk's token may be absent: past the request's tokens, or in a block that is not there
+            auto fetch = [&](const uint8_t *base, int t, uint4 (&x)[C::kChunks]) {
+#pragma unroll
+                for (int c = 0; c < C::kChunks; ++c) {
+                    const int at = lt + c * kLoadThreads, token = t * C::kTile + at / kPerRow;
+                    int block = -1;
+                    if (token < w.kv) block = __ldg(table + (token >> p.log2_block));
+                    x[c] = make_uint4(0, 0, 0, 0);
+                    if (block >= 0 && block < p.num_blocks)
+                        x[c] = __ldg(reinterpret_cast<const uint4 *>(base + (int64_t)block * p.stride_block +
+                                                                     (int64_t)(token & in_block) * p.stride_token + at % kPerRow * 16));
+                }
+            };
+            auto store = [&](unsigned char *tile, const uint4 (&x)[C::kChunks]) {
+#pragma unroll
+                for (int c = 0; c < C::kChunks; ++c) {
+                    const int at = lt + c * kLoadThreads, r = at / kPerRow, d = at % kPerRow * 16;
+                    uint4 lo, hi;
+                    codes_to_half<FORMAT>(x[c].x, lo.x, lo.y);
+                    codes_to_half<FORMAT>(x[c].y, lo.z, lo.w);
+                    codes_to_half<FORMAT>(x[c].z, hi.x, hi.y);
+                    codes_to_half<FORMAT>(x[c].w, hi.z, hi.w);
+                    unsigned char *line = tile + d / 64 * C::kKvPanel + r * 128;
+                    const int at16 = d % 64 / 8;
+                    *reinterpret_cast<uint4 *>(line + (at16 ^ (r & 7)) * 16) = lo;
+                    *reinterpret_cast<uint4 *>(line + ((at16 + 1) ^ (r & 7)) * 16) = hi;
+                }
+            };
+            uint4 kx[C::kChunks], vx[C::kChunks];
+            fetch(k_head, w.t0, kx);
+            for (int t = w.t0; t < w.t1; ++t, ++n_tile) {
+                const int stage = n_tile % kStages;
+                const uint32_t empty = (n_tile / kStages & 1) ^ 1;
+                fetch(v_head, t, vx);
+                if (lt < 32) {
+                    // the tile's scales; an absent block's tokens get weight 2^-inf
+                    if (lt < C::kBlocks) {
+                        const BlockEntry b = block_entry(p, w.request, w.head, (int64_t)t * C::kTile + lt * 16, w.kv);
+                        scales[n_tile % kScaleStages][lt] = b.block < 0 ? make_float4(0.f, -INFINITY, 0.f, 0.f)
+                                                                         : make_float4(b.k_scale, b.v_log2, b.v_inverse, 0.f);
+                    }
+                    __syncwarp();
+                }
+                wait.warp(&bars.k_empty[stage], empty);
+                store(k_smem + stage * C::kKvBytes, kx);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&bars.k_full[stage]);
+                if (lt == 0) bar_arrive(&bars.scale_full[n_tile % kScaleStages]);
+                if (t + 1 < w.t1) fetch(k_head, t + 1, kx);
+                wait.warp(&bars.v_empty[stage], empty);
+                store(v_smem + stage * C::kKvBytes, vx);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&bars.v_full[stage]);
+            }
+        }
+    } else if (lane == 0) {
+        // ------------------------------------------------ the matrix instructions
+        constexpr uint32_t s_instruction = instruction(128, C::kTile, false), o_instruction = instruction(128, D, true);
+        const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
+        uint32_t n_tile = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+        auto scores = [&](int qt, uint32_t stage) {
+            const uint32_t a = q_at + qt * C::kPanels * C::kQPanel, b = k_at + stage * C::kKvBytes;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                mma_ss(tmem + qt * C::kSColumns, operand(a + k / 4 * C::kQPanel + k % 4 * 32, 16, 1024),
+                       operand(b + k / 4 * C::kKvPanel + k % 4 * 32, 16, 1024), s_instruction, k > 0);
+            commit(&bars.s_full[qt]);
+        };
+        while (walk.next(p, w)) {
+            const int tiles = w.t1 - w.t0, n_q = C::kQTiles == 2 && w.rows - w.row_tile * C::kRows > 128 ? 2 : 1;
+            wait(&bars.k_full[n_tile % kStages], n_tile / kStages & 1);
+            for (int qt = 0; qt < n_q; ++qt) {
+                wait(&bars.q_full[qt], q_phase[qt]);
+                q_phase[qt] ^= 1;
+                fence_after();
+                scores(qt, n_tile % kStages);
+            }
+            commit(&bars.k_empty[n_tile % kStages]);
+            for (int t = 0; t < tiles; ++t, ++n_tile) {
+                const uint32_t stage = n_tile % kStages, next = (n_tile + 1) % kStages;
+                wait(&bars.v_full[stage], n_tile / kStages & 1);
+                for (int qt = 0; qt < n_q; ++qt) {
+                    wait(&bars.p_full[qt], p_phase[qt]);
+                    p_phase[qt] ^= 1;
+                    fence_after();
+                    const uint32_t b = v_at + stage * C::kKvBytes;
+#pragma unroll
+                    for (int k = 0; k < C::kTile / 16; ++k)
+                        mma_ts(tmem + C::kOColumn + qt * D, tmem + qt * C::kSColumns + k * 8, operand(b + k * 2048, C::kKvPanel, 1024),
+                               o_instruction, t > 0 || k > 0);
+                    if (t + 1 == tiles) commit(&bars.o_full[qt]);
+                    if (qt == n_q - 1) commit(&bars.v_empty[stage]);
+                    if (t + 1 < tiles) {
+                        if (qt == 0) {
+                            wait(&bars.k_full[next], (n_tile + 1) / kStages & 1);
+                            fence_after();
+                        }
+                        scores(qt, next);
+                        if (qt == n_q - 1) commit(&bars.k_empty[next]);
+                    }
+                }
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    __syncwarp();
+    if (warp == kMmaWarp)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512));
+}
+
+template <int D, int FORMAT>
+cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream) {
+    using C = Shape<D>;
+    // more than half of an SM's shared memory: one block per SM, which holds all of its tensor memory
+    const size_t smem = C::kSmem > 120 * 1024 ? C::kSmem : 120 * 1024;
+    static std::atomic<uint64_t> allowed{0};   // devices on which the shared memory limit is raised
+    if (device >= 64 || !(allowed.load() >> device & 1)) {
+        const cudaError_t e = cudaFuncSetAttribute(prefill_kernel<D, FORMAT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        if (device < 64) allowed.fetch_or(1ull << device);
+    }
+    prefill_kernel<D, FORMAT><<<num_sms, kThreads, smem, stream>>>(p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t qcache_prefill_part_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
+
+cudaError_t launch_qcache_prefill(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream) {
+#define CM_LAUNCH(D) \
+    if (p.head_dim == D) \
+        return p.format == CM_QCACHE_E4M3 ? launch<D, CM_QCACHE_E4M3>(p, num_sms, device, stream) \
+                                          : launch<D, CM_QCACHE_INT8>(p, num_sms, device, stream);
+    CM_LAUNCH(32) CM_LAUNCH(64) CM_LAUNCH(128) CM_LAUNCH(256)
+#undef CM_LAUNCH
+    return cudaErrorInvalidValue;
+}
+
+}  // namespace cm
