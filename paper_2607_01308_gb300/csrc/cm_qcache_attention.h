@@ -144,22 +144,19 @@ __device__ __forceinline__ BlockEntry shuffle(const BlockEntry &e, int lane) {
             __shfl_sync(~0u, e.v_inverse, lane)};
 }
 
-// Adds a part (unnormalised output x, sum l_x, maximum m_x) to one at maximum m >= m_x.
-__device__ __forceinline__ void join(float4 &acc, float &l, const float4 &x, float l_x, float m_x, float m) {
-    const float f = m_x == m ? 1.f : exp2_fast(m_x - m);
-    acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y);
-    acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
-    l = fmaf(l_x, f, l);
-}
-
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t w;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
     return w;
 }
 
+// The natural logarithm of a row's sum at maximum m; -inf if it saw no token.
+__device__ __forceinline__ float log_sum(float m, float l, float headroom) {
+    return l == 0.f ? -INFINITY : (m - headroom + __log2f(l)) * 0.693147180559945309f;
+}
+
 // Elements d .. d + 3 of row n (query token n / group, head n % group) of the segment's request.
-// A row that saw no token is zero, its logarithm -inf.
+// A row that saw no token is zero.
 __device__ __forceinline__ void write_row(const QcacheAttentionParams &p, const AttentionSegment &w, int n, int d, const float4 &acc,
                                           float m, float l, float headroom) {
     const int64_t row = w.row0 + n / p.group, head = (int64_t)w.head * p.group + n % p.group;
@@ -167,26 +164,72 @@ __device__ __forceinline__ void write_row(const QcacheAttentionParams &p, const 
     const uint2 x = make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f));
     *reinterpret_cast<uint2 *>(p.out + row * p.out_stride_row + head * p.out_stride_head + d) = x;
     if (d == 0 && p.lse)
-        p.lse[row * ((int64_t)p.heads * p.group) + head] =
-            l == 0.f ? -INFINITY : (m - headroom + __log2f(l)) * 0.693147180559945309f;
+        p.lse[row * ((int64_t)p.heads * p.group) + head] = log_sum(m, l, headroom);
 }
 
-// The parts of row n of a segment's whole range, held by thread blocks c0 .. c1, in that order;
-// at(c): the workspace row of block c's part.
-template <int D, class At>
-__device__ __forceinline__ void join_parts(const QcacheAttentionParams &p, const AttentionSegment &w, int n, int d, uint32_t c0,
-                                           uint32_t c1, float headroom, At at) {
-    float m = -INFINITY;
-#pragma unroll 8
-    for (uint32_t c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(p.part_ml + at(c) * 2));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-#pragma unroll 8
-    for (uint32_t c = c0; c <= c1; ++c) {
-        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(p.part_ml + at(c) * 2));
-        join(acc, l, __ldcg(reinterpret_cast<const float4 *>(p.part_o + at(c) * D + d)), ml.y, ml.x, m);
+// Joins the parts of rows [0, rows) of a segment's whole range, held by thread blocks c0 .. c1 of the
+// grid, in that order; row_at(c, row): the workspace row of block c's part; first: the rows' place
+// among the request's. WARPS warps share the rows, GROUP at a time to a warp: lanes weigh the parts,
+// then read them along head_dim.
+template <int D, int WARPS, int GROUP, class At>
+__device__ __forceinline__ void join_parts(const QcacheAttentionParams &p, const AttentionSegment &w, int first, int rows,
+                                           uint32_t c0, uint32_t c1, float headroom, int warp, At row_at) {
+    constexpr int kGroup = GROUP, kVecs = D >= 128 ? D / 128 : 1;   // 16-byte vectors of a lane
+    const int lane = threadIdx.x % 32, n = (int)(c1 - c0 + 1);
+    for (int r0 = warp; r0 < rows; r0 += WARPS * kGroup) {
+        float m[kGroup], l[kGroup];
+        float4 acc[kGroup][kVecs];
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) {
+            const int row = min(r0 + k * WARPS, rows - 1);
+            m[k] = -INFINITY;
+            for (int c = lane; c < n; c += 32) m[k] = fmaxf(m[k], __ldcg(p.part_ml + row_at(c0 + c, row) * 2));
+#pragma unroll
+            for (int d = 16; d; d /= 2) m[k] = fmaxf(m[k], __shfl_xor_sync(~0u, m[k], d));
+            l[k] = 0.f;
+#pragma unroll
+            for (int v = 0; v < kVecs; ++v) acc[k][v] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        for (int base = 0; base < n; base += 32) {
+            float f[kGroup];
+#pragma unroll
+            for (int k = 0; k < kGroup; ++k) {
+                const int row = min(r0 + k * WARPS, rows - 1);
+                float2 ml = make_float2(-INFINITY, 0.f);
+                if (base + lane < n) ml = __ldcg(reinterpret_cast<const float2 *>(p.part_ml + row_at(c0 + base + lane, row) * 2));
+                f[k] = ml.x == m[k] ? 1.f : exp2_fast(ml.x - m[k]);
+                float x = ml.y * f[k];
+#pragma unroll
+                for (int d = 16; d; d /= 2) x += __shfl_xor_sync(~0u, x, d);
+                l[k] += x;
+            }
+            const int most = min(32, n - base);
+#pragma unroll(16 / GROUP)
+            for (int c = 0; c < most; ++c)
+#pragma unroll
+                for (int k = 0; k < kGroup; ++k) {
+                    const int row = min(r0 + k * WARPS, rows - 1);
+                    const float g = __shfl_sync(~0u, f[k], c);
+                    const float4 *part = reinterpret_cast<const float4 *>(p.part_o + row_at(c0 + base + c, row) * D);
+#pragma unroll
+                    for (int v = 0; v < kVecs; ++v) {
+                        if (D < 128 && lane >= D / 4) break;
+                        const float4 x = __ldcg(part + lane + 32 * v);
+                        float4 &a = acc[k][v];
+                        a.x = fmaf(x.x, g, a.x); a.y = fmaf(x.y, g, a.y);
+                        a.z = fmaf(x.z, g, a.z); a.w = fmaf(x.w, g, a.w);
+                    }
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) {
+            const int row = r0 + k * WARPS;
+            if (row >= rows) break;
+#pragma unroll
+            for (int v = 0; v < kVecs; ++v)
+                if (D >= 128 || lane < D / 4) write_row(p, w, first + row, (lane + 32 * v) * 4, acc[k][v], m[k], l[k], headroom);
+        }
     }
-    write_row(p, w, n, d, acc, m, l, headroom);
 }
 
 }  // namespace

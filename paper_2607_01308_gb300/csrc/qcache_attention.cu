@@ -287,9 +287,13 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
             float l = 0.f;
 #pragma unroll
-            for (int y = 0; y < kWarps; ++y)
-                join(acc, l, *reinterpret_cast<const float4 *>(merge_o + (y * C::kRows + n) * C::kPitch + d),
-                     merge_ml[(y * C::kRows + n) * 2 + 1], merge_ml[(y * C::kRows + n) * 2], m);
+            for (int y = 0; y < kWarps; ++y) {
+                const float m_y = merge_ml[(y * C::kRows + n) * 2], f = m_y == m ? 1.f : exp2_fast(m_y - m);
+                const float4 x = *reinterpret_cast<const float4 *>(merge_o + (y * C::kRows + n) * C::kPitch + d);
+                acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y);
+                acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
+                l = fmaf(merge_ml[(y * C::kRows + n) * 2 + 1], f, l);
+            }
             if (whole) {
                 write_row(p, w, w.row_tile * C::kRows + n, d, acc, m, l, kHeadroom);
             } else {
@@ -306,11 +310,8 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
             __syncthreads();
             if (last_one) {
                 __threadfence();
-                for (int x = tid; x < rows * (D / 4); x += kThreads) {
-                    const int n = x / (D / 4), d = x % (D / 4) * 4;
-                    join_parts<D>(p, w, w.row_tile * C::kRows + n, d, c0, c1, kHeadroom,
-                                  [&](uint32_t c) { return (2 * (int64_t)c + (c == c0)) * C::kRows + n; });
-                }
+                join_parts<D, kWarps, 1>(p, w, w.row_tile * C::kRows, rows, c0, c1, kHeadroom, warp,
+                                      [&](uint32_t c, int n) { return (2 * (int64_t)c + (c == c0)) * C::kRows + n; });
             }
         }
         __syncthreads();

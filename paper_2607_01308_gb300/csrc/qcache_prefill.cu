@@ -5,14 +5,17 @@
 // One thread block per SM, on the tcgen05 tensor cores, with up to 256 query rows (rows are query
 // tokens x heads of a group) in two tiles of 128, so that each K and V tile that is brought in and
 // taken to fp16 serves both:
-//   warps 0-3, 4-7   softmax of query tile 0 and 1, one row per thread: scores from tensor memory,
-//                    weights back into the same columns as fp16, the output rescaled when the
-//                    running maximum is raised, the row normalised and written at the end
-//   warps 8-11       K and V tiles: 16 codes per load from their blocks, to fp16, into shared
-//                    memory in the 128-byte swizzle (two stages each)
-//   warp 12          one thread issues the matrix instructions: S = Q K^T (both operands from
-//                    shared memory), O += P V (P from tensor memory, V as it lies, tokens x head_dim)
-// While one tile's softmax runs, the tensor cores work on the other tile. Work is cut as in
+//   warps 0-3, 4-7   softmax of query tile 0 and 1, one row per thread: a tile's 128 scores from tensor
+//                    memory into registers, weights back into the same columns as fp16, the output
+//                    rescaled when the running maximum is raised, the row normalised and written
+//   warps 8-11       K and V tiles from codes to fp16, shared memory to shared memory, into the 128-byte
+//                    swizzle (two stages each)
+//   warp 12          issues the matrix instructions: S = Q K^T (both operands from shared memory),
+//                    O += P V (P from tensor memory, V as it lies, tokens x head_dim)
+//   warp 13          looks up blocks and scales of every 16 tokens, several tiles ahead
+//   warp 14          bulk copies of the codes, a tile of K and one of V ahead
+// While one tile's softmax runs, the tensor cores work on the other tile. The softmax warps take
+// registers over from the others (200 and 56 of 128 at launch). Work is cut as in
 // qcache_attention.cu, over kv tiles that the rows of a tile may see at all.
 #include "cm_qcache_kernels.h"
 
@@ -24,11 +27,12 @@
 namespace cm {
 namespace {
 
-constexpr int kSoftmaxWarps = 8, kLoadWarps = 4, kMmaWarp = kSoftmaxWarps + kLoadWarps;
-constexpr int kThreads = (kMmaWarp + 1) * 32;
+constexpr int kSoftmaxWarps = 8, kLoadWarps = 4, kMmaWarp = kSoftmaxWarps + kLoadWarps, kEntryWarp = kMmaWarp + 1, kCopyWarp = kMmaWarp + 2;
+constexpr int kThreads = 16 * 32;           // whole warpgroups: registers change hands by warpgroup
+constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;
+static_assert(256 * kSoftmaxRegs + 256 * kOtherRegs <= kThreads * 128, "registers at launch");
 constexpr int kLoadThreads = kLoadWarps * 32;
 constexpr int kStages = 2;
-constexpr int kScaleStages = 4;             // softmax reads a tile's scales after its K has been given up
 constexpr float kRaise = 8.f, kHeadroom = 7.f;
 
 template <int D>
@@ -41,10 +45,14 @@ struct Shape {
     static constexpr int kQBytes = kQTiles * kPanels * kQPanel;
     static constexpr int kKvBytes = kPanels * kKvPanel;       // one tile of K or V
     static constexpr int kBlocks = kTile / 16;                // scale entries of a tile
-    static constexpr int kChunks = kTile * D / 16 / kLoadThreads;   // 16-code loads of a thread for K (and for V)
+    static constexpr int kEntryTiles = 32 / kBlocks;          // tiles that the entry warp looks up at a time
+    static constexpr int kEntryStages = 2 * kEntryTiles;
+    static constexpr int kChunks = kTile * D / 16 / kLoadThreads;   // 16-code copies of a thread for K (and for V)
+    static constexpr int kRawBytes = kTile * D;               // codes of a tile
+    static constexpr int kSteps = D < 64 ? D / 16 : 4;        // 16 columns each, of a panel
     static constexpr int kSColumns = 128;                     // tensor memory columns between score tiles
     static constexpr int kOColumn = kQTiles * kSColumns;
-    static constexpr size_t kSmem = 1024 + kQBytes + 2 * kStages * kKvBytes;
+    static constexpr size_t kSmem = 1024 + kQBytes + 2 * kStages * kKvBytes + 2 * kRawBytes;
     static_assert(kChunks >= 1, "every load thread has work");
     static_assert(kOColumn + kQTiles * D <= 512, "tensor memory");
 };
@@ -61,6 +69,15 @@ __device__ __forceinline__ void bar_arrive(uint64_t *b) {
     asm volatile("{\n.reg .b64 t;\nmbarrier.arrive.shared::cta.b64 t, [%0];\n}" ::"r"(smem_u32(b)) : "memory");
 }
 
+__device__ __forceinline__ void bar_arrive_expect(uint64_t *b, uint32_t bytes) {
+    asm volatile("{\n.reg .b64 t;\nmbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1;\n}" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_t bytes, uint64_t *b) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(b)) : "memory");
+}
+
 __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity) {
     uint32_t ok;
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000000;\nselp.u32 %0, 1, 0, p;\n}"
@@ -71,7 +88,7 @@ __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity) {
 // Waits for the phase of the given parity. A wait that runs out (about a second) is recorded, and
 // every later one then gives up at once, so that the block runs to its end with a wrong result that
 // the host can learn of.
-__device__ __noinline__ void bar_wait_slow(uint64_t *b, uint32_t parity, volatile int *failed, unsigned int *error) {
+__device__ __forceinline__ void bar_wait_slow(uint64_t *b, uint32_t parity, volatile int *failed, unsigned int *error) {
     const long long t0 = clock64();
     while (!bar_try(b, parity)) {
         if (*failed) return;
@@ -102,8 +119,18 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-__device__ __forceinline__ void commit(uint64_t *b) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+// One lane of a converged warp, the same each time.
+__device__ __forceinline__ uint32_t elect() {
+    uint32_t leader;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(leader));
+    return leader;
+}
+
+// The whole warp runs the code around these, so that addresses and descriptors stay uniform; the
+// leader alone acts.
+__device__ __forceinline__ void commit(uint64_t *b, uint32_t leader) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n"
+                 "@p tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(smem_u32(b)), "r"(leader) : "memory");
 }
 
 #define CM_REGS16(x, i) \
@@ -119,12 +146,11 @@ __device__ __forceinline__ void tmem_ld32(uint32_t (&x)[32], uint32_t at) {
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
                  : CM_REGS16(x, 0), CM_REGS16(x, 16) : "r"(at));
 }
-__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&x)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-                 ::"r"(at), CM_IN16(x, 0), CM_IN16(x, 16) : "memory");
+__device__ __forceinline__ void tmem_ld16(uint32_t (&x)[16], uint32_t at) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : CM_REGS16(x, 0) : "r"(at));
 }
+__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&x)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
                  ::"r"(at), CM_IN16(x, 0) : "memory");
@@ -133,8 +159,12 @@ __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.
 
 // Shared memory operand in 128-byte swizzled atoms of 8 rows x 128 bytes. Rows of K (and Q) are
 // tokens (query rows) and the contraction runs along a row; for V the contraction runs over rows.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading, uint32_t stride) {
-    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+// The descriptor's lower word moves with the address, in units of 16 bytes.
+__device__ __forceinline__ uint32_t operand_lo(uint32_t addr, uint32_t leading) { return (addr & 0x3ffff) >> 4 | (leading >> 4) << 16; }
+__device__ __forceinline__ uint64_t operand(uint32_t lo) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "n"(1024u >> 4 | 1u << 14 | 2u << 29));   // 1024 bytes to the next eight rows
+    return d;
 }
 
 // fp32 accumulator, fp16 operands; b_rows: B's contraction runs over rows.
@@ -142,13 +172,149 @@ __host__ __device__ constexpr uint32_t instruction(int m, int n, bool b_rows) {
     return 1u << 4 | (b_rows ? 1u << 16 : 0u) | (uint32_t)(n / 8) << 17 | (uint32_t)(m / 16) << 24;
 }
 
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t leader) {
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %5, 0;\n"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t leader) {
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %5, 0;\n"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+
+// ---------------------------------------------------------------- softmax
+
+// A pair of fp32 values in one 64-bit register, for the two-wide instructions.
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+    return v;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+
+// One row's scores of a kv tile to weights. left: columns that the row sees (MASKED only).
+template <int D, bool MASKED>
+__device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const float4 *sc, float factor, int left, bool rescale,
+                                             float &top, float &sum) {
+    using C = Shape<D>;
+    uint32_t x[C::kTile / 32][32];
+#pragma unroll
+    for (int c = 0; c < C::kTile / 32; ++c) tmem_ld32(x[c], s_at + 32 * c);
+    ld_wait();
+    float high = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < C::kBlocks; ++b) {
+        float h = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            if (MASKED && 16 * b + k >= left) x[b / 2][b % 2 * 16 + k] = 0xff800000u;
+            h = fmaxf(h, __uint_as_float(x[b / 2][b % 2 * 16 + k]));
+        }
+        const float4 z = sc[b];
+        high = fmaxf(high, MASKED && h == -INFINITY ? h : fmaf(h, factor * z.x, z.y));
+    }
+    const bool raise = high > top + kRaise;
+    if (__any_sync(~0u, raise)) {
+        const float now = raise ? high : top;
+        const float f = top == now ? 1.f : exp2_fast(top - now);
+        top = now;
+        sum *= f;
+        if (rescale) {
+#pragma unroll 1
+            for (int c = 0; c < D / 16; ++c) {
+                uint32_t y[16];
+                tmem_ld16(y, o_at + 16 * c);
+                ld_wait();
+#pragma unroll
+                for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
+                tmem_st16(o_at + 16 * c, y);
+            }
+        }
+    }
+    const float base = (top == -INFINITY ? 0.f : top) - kHeadroom;
+#pragma unroll
+    for (int c = 0; c < C::kTile / 32; ++c) {
+        uint32_t y[16];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const float4 z = sc[2 * c + b];
+            const float a = factor * z.x, d = z.y - base;
+            const uint64_t a2 = pair(a, a), d2 = pair(d, d);
+            uint64_t part = 0;
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) {
+                float e0, e1;
+                unpair(fma2(pair(__uint_as_float(x[c][16 * b + k]), __uint_as_float(x[c][16 * b + k + 1])), a2, d2), e0, e1);
+                e0 = exp2_fast(e0);
+                e1 = exp2_fast(e1);
+                if (MASKED) {   // a score of -inf times a scale of 0 is no number
+                    if (32 * c + 16 * b + k >= left) e0 = 0.f;
+                    if (32 * c + 16 * b + k + 1 >= left) e1 = 0.f;
+                }
+                part = add2(part, pair(e0, e1));
+                y[8 * b + k / 2] = pack_half(e0, e1);
+            }
+            float p0, p1;
+            unpair(part, p0, p1);
+            sum = fmaf(p0 + p1, z.z, sum);
+        }
+        tmem_st16(s_at + 16 * c, y);
+    }
+    st_wait();
+}
+
+// The warp's 32 query rows, rows first .. first + 31 of the request, to fp16 with a power of two per row,
+// into rows at .. at + 31 of the swizzled tile: copied there as they are, each 16 bytes to the place that
+// they will keep, then taken to fp16 in place, a row per lane. `row` points at this lane's row (null: none).
+// Returns the factor that turns a product of this lane's row into a score.
+template <int D>
+__device__ __forceinline__ float load_queries(const QcacheAttentionParams &p, const uint16_t *row, unsigned char *tile, int at) {
+    using C = Shape<D>;
+    constexpr int kLanes = D / 8, kStep = 32 / kLanes;            // lanes to a row, rows of one copy
+    const int lane = threadIdx.x % 32, sub = lane / kLanes, col = lane % kLanes;
+    const uint32_t to = smem_u32(tile) + col / 8 * C::kQPanel + at * 128;
+#pragma unroll 8
+    for (int k = 0; k < 32 / kStep; ++k) {
+        const int r = k * kStep + sub;
+        const uint16_t *from = reinterpret_cast<const uint16_t *>(__shfl_sync(~0u, reinterpret_cast<uint64_t>(row), r));
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + r * 128 + ((col % 8) ^ (r & 7)) * 16),
+                     "l"(from ? from + col * 8 : p.q), "r"(from ? 16 : 0) : "memory");
+    }
+    asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+    __syncwarp();
+    unsigned char *mine = tile + (at + lane) * 128;
+    uint32_t m = 0;
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(mine + c / 8 * C::kQPanel + ((c % 8) ^ (lane & 7)) * 16);
+        m = __vmaxu2(m, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+    }
+    m = max(m & 0xffffu, m >> 16);
+    const int e = max((int)(m >> 7) - 127, -100);
+    // a negative softmax scale turns Q around, so that larger products are larger scores
+    const float up = p.scale_log2 < 0.f ? -pow2f(14 - e) : pow2f(14 - e);
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+        uint4 *place = reinterpret_cast<uint4 *>(mine + c / 8 * C::kQPanel + ((c % 8) ^ (lane & 7)) * 16);
+        uint4 x = *place;
+        x.x = pack_half(__uint_as_float(x.x << 16) * up, __uint_as_float(x.x & 0xffff0000u) * up);
+        x.y = pack_half(__uint_as_float(x.y << 16) * up, __uint_as_float(x.y & 0xffff0000u) * up);
+        x.z = pack_half(__uint_as_float(x.z << 16) * up, __uint_as_float(x.z & 0xffff0000u) * up);
+        x.w = pack_half(__uint_as_float(x.w << 16) * up, __uint_as_float(x.w & 0xffff0000u) * up);
+        *place = x;
+    }
+    return fabsf(p.scale_log2) * pow2f(e - 14);
 }
 
 // ---------------------------------------------------------------- work
@@ -199,7 +365,8 @@ struct Start {
 
 struct Barriers {
     uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-    uint64_t scale_full[kScaleStages];
+    uint64_t entry_full[16], entry_empty[16];
+    uint64_t raw_full[2], raw_empty[2];       // K, V
     uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
 };
 
@@ -208,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     using C = Shape<D>;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Barriers bars;
-    __shared__ float4 scales[kScaleStages][C::kBlocks];   // k_scale, log2 v_scale, 1 / v_scale of 16 tokens each
+    __shared__ float4 entries[C::kEntryStages][C::kBlocks];   // k_scale, log2 v_scale, 1 / v_scale, block of 16 tokens each
     __shared__ uint32_t scan[kThreads / 32];
     __shared__ Start start;
     __shared__ uint32_t tmem_base;
@@ -216,6 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     __shared__ int failed;
     unsigned char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + kStages * C::kKvBytes;
+    unsigned char *raw = v_smem + kStages * C::kKvBytes;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
 
     // the plan: one thread per request, prefix sums in the (still unused) tile memory
@@ -255,8 +423,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             bar_init(&bars.k_empty[i], 1);
             bar_init(&bars.v_empty[i], 1);
         }
-        for (int i = 0; i < kScaleStages; ++i) bar_init(&bars.scale_full[i], 1);
+        for (int i = 0; i < C::kEntryStages; ++i) {
+            bar_init(&bars.entry_full[i], 1);
+            bar_init(&bars.entry_empty[i], 1);
+        }
         for (int i = 0; i < 2; ++i) {
+            bar_init(&bars.raw_full[i], 1);
+            bar_init(&bars.raw_empty[i], kLoadWarps);
             bar_init(&bars.q_full[i], 128);
             bar_init(&bars.p_full[i], 128);
             bar_init(&bars.s_full[i], 1);
@@ -310,10 +483,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
 
     if (warp < kSoftmaxWarps) {
         // ------------------------------------------------ softmax: one row per thread
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int qt = warp / 4, row = tid % 128;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_at = tmem + lanes + qt * C::kSColumns, o_at = tmem + lanes + C::kOColumn + qt * D;
-        uint32_t n_tile = 0;          // kv tiles of the block so far (scales)
+        uint32_t n_tile = 0;          // kv tiles of the block so far
         uint32_t s_phase = 0, o_phase = 0;
         const uint64_t per = start.per;
         while (walk.next(p, w)) {
@@ -322,113 +496,27 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 n_tile += w.t1 - w.t0;
                 continue;
             }
-            // this row of Q: fp16 with a power of two per row, into the swizzled tile
             const int n = first + row;
             const bool valid = n < w.rows;
-            const int i = n / p.group;
-            const uint16_t *q = p.q + (int64_t)(w.row0 + i) * p.q_stride_row + ((int64_t)w.head * p.group + n % p.group) * p.q_stride_head;
-            uint32_t m = 0;
-#pragma unroll 4
-            for (int c = 0; c < D / 8; ++c) {
-                if (!valid) break;
-                const uint4 x = __ldg(reinterpret_cast<const uint4 *>(q) + c);
-                m = __vmaxu2(m, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
-            }
-            m = max(m & 0xffffu, m >> 16);
-            const int e = max((int)(m >> 7) - 127, -100);
-            // a negative softmax scale turns Q around, so that larger products are larger scores
-            const float up = p.scale_log2 < 0.f ? -pow2f(14 - e) : pow2f(14 - e);
-            const float factor = fabsf(p.scale_log2) * pow2f(e - 14);
-            unsigned char *q_row = q_smem + qt * C::kPanels * C::kQPanel + row * 128;
-#pragma unroll 4
-            for (int c = 0; c < D / 8; ++c) {
-                uint4 x = valid ? __ldg(reinterpret_cast<const uint4 *>(q) + c) : make_uint4(0, 0, 0, 0);
-                x.x = pack_half(__uint_as_float(x.x << 16) * up, __uint_as_float(x.x & 0xffff0000u) * up);
-                x.y = pack_half(__uint_as_float(x.y << 16) * up, __uint_as_float(x.y & 0xffff0000u) * up);
-                x.z = pack_half(__uint_as_float(x.z << 16) * up, __uint_as_float(x.z & 0xffff0000u) * up);
-                x.w = pack_half(__uint_as_float(x.w << 16) * up, __uint_as_float(x.w & 0xffff0000u) * up);
-                *reinterpret_cast<uint4 *>(q_row + c / 8 * C::kQPanel + ((c % 8) ^ (row & 7)) * 16) = x;
-            }
+            const int64_t token = w.row0 + n / p.group, head = (int64_t)w.head * p.group + n % p.group;
+            const float factor = load_queries<D>(p, valid ? p.q + token * p.q_stride_row + head * p.q_stride_head : nullptr,
+                                                 q_smem + qt * C::kPanels * C::kQPanel, warp % 4 * 32);
             fence_async_smem();
             bar_arrive(&bars.q_full[qt]);
 
-            const int limit = !valid ? 0 : p.causal ? min(w.kv, max(0, w.kv - w.q_len + i + 1)) : w.kv;
+            const int limit = !valid ? 0 : p.causal ? min(w.kv, max(0, w.kv - w.q_len + (int)(token - w.row0) + 1)) : w.kv;
             const int least = __reduce_min_sync(~0u, limit);      // of the warp's rows
             float top = -INFINITY, sum = 0.f;
             for (int t = w.t0; t < w.t1; ++t, ++n_tile) {
+                wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
                 wait.warp(&bars.s_full[qt], s_phase);
                 s_phase ^= 1;
-                wait.warp(&bars.scale_full[n_tile % kScaleStages], n_tile / kScaleStages & 1);
                 fence_after();
-                const float4 *sc = scales[n_tile % kScaleStages];
-                const int left = limit - t * C::kTile;            // columns that this row sees
-                const bool masked = (t + 1) * C::kTile > least;
-                float high = -INFINITY;
-#pragma unroll
-                for (int c = 0; c < C::kTile / 32; ++c) {
-                    uint32_t x[32];
-                    tmem_ld32(x, s_at + 32 * c);
-                    ld_wait();
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        float h = -INFINITY;
-                        if (masked) {
-#pragma unroll
-                            for (int k = 0; k < 16; ++k)
-                                if (32 * c + 16 * b + k < left) h = fmaxf(h, __uint_as_float(x[16 * b + k]));
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) h = fmaxf(h, __uint_as_float(x[16 * b + k]));
-                        }
-                        const float4 z = sc[2 * c + b];
-                        high = fmaxf(high, h == -INFINITY ? h : fmaf(h, factor * z.x, z.y));
-                    }
-                }
-                const bool raise = high > top + kRaise;
-                if (__any_sync(~0u, raise)) {
-                    const float now = raise ? high : top;
-                    const float f = top == now ? 1.f : exp2_fast(top - now);
-                    top = now;
-                    sum *= f;
-                    if (t > w.t0) {
-#pragma unroll
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t x[32];
-                            tmem_ld32(x, o_at + 32 * c);
-                            ld_wait();
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
-                            tmem_st32(o_at + 32 * c, x);
-                        }
-                    }
-                }
-                const float base = (top == -INFINITY ? 0.f : top) - kHeadroom;
-#pragma unroll
-                for (int c = 0; c < C::kTile / 32; ++c) {
-                    uint32_t x[32], y[16];
-                    tmem_ld32(x, s_at + 32 * c);
-                    ld_wait();
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const float4 z = sc[2 * c + b];
-                        const float a = factor * z.x, d = z.y - base;
-                        float part = 0.f;
-#pragma unroll
-                        for (int k = 0; k < 16; k += 2) {
-                            float e0 = exp2_fast(fmaf(__uint_as_float(x[16 * b + k]), a, d));
-                            float e1 = exp2_fast(fmaf(__uint_as_float(x[16 * b + k + 1]), a, d));
-                            if (masked) {
-                                if (32 * c + 16 * b + k >= left) e0 = 0.f;
-                                if (32 * c + 16 * b + k + 1 >= left) e1 = 0.f;
-                            }
-                            part += e0 + e1;
-                            y[8 * b + k / 2] = pack_half(e0, e1);
-                        }
-                        sum = fmaf(part, z.z, sum);
-                    }
-                    tmem_st16(s_at + 16 * c, y);                  // columns whose scores have been read
-                }
-                st_wait();
+                const float4 *sc = entries[n_tile % C::kEntryStages];
+                if ((t + 1) * C::kTile > least)
+                    softmax_tile<D, true>(s_at, o_at, sc, factor, limit - t * C::kTile, t > w.t0, top, sum);
+                else
+                    softmax_tile<D, false>(s_at, o_at, sc, factor, 0, t > w.t0, top, sum);
                 fence_before();
                 bar_arrive(&bars.p_full[qt]);
             }
@@ -438,19 +526,31 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             const bool whole = w.t0 == 0 && w.t1 == w.tiles;
             const int rows = min(128, w.rows - first);
             const int64_t part = ((2 * (int64_t)blockIdx.x + (w.t0 == 0)) * C::kQTiles + qt) * 128;
+            const float scale = sum == 0.f ? 0.f : 1.f / sum;
+            uint16_t *to = p.out + token * p.out_stride_row + head * p.out_stride_head;
+            float *to_part = p.part_o + (part + row) * D;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t x[32];
                 __syncwarp();
                 tmem_ld32(x, o_at + 32 * c);
                 ld_wait();
+                if (valid && whole) {
 #pragma unroll
-                for (int k = 0; k < 32; k += 4) {
-                    const float4 y = make_float4(__uint_as_float(x[k]), __uint_as_float(x[k + 1]), __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
-                    if (valid && whole) write_row(p, w, n, 32 * c + k, y, top, sum, kHeadroom);
-                    else if (valid) __stcg(reinterpret_cast<float4 *>(p.part_o + (part + row) * D + 32 * c + k), y);
+                    for (int k = 0; k < 32; k += 8) {
+                        uint32_t y[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            y[j] = pack_bf16(__uint_as_float(x[k + 2 * j]) * scale, __uint_as_float(x[k + 2 * j + 1]) * scale);
+                        *reinterpret_cast<uint4 *>(to + 32 * c + k) = make_uint4(y[0], y[1], y[2], y[3]);
+                    }
+                } else if (valid) {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4)
+                        __stcg(reinterpret_cast<uint4 *>(to_part + 32 * c + k), make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]));
                 }
             }
+            if (valid && whole && p.lse) p.lse[token * ((int64_t)p.heads * p.group) + head] = log_sum(top, sum, kHeadroom);
             if (!whole) {
                 if (valid) __stcg(reinterpret_cast<float2 *>(p.part_ml + (part + row) * 2), make_float2(top, sum));
                 const uint32_t c0 = (uint32_t)(w.unit0 / per), c1 = (uint32_t)((w.unit0 + w.tiles - 1) / per);
@@ -460,127 +560,188 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + qt) : "memory");
                 if (last_one[qt]) {
                     __threadfence();
-                    for (int x = row; x < rows * (D / 4); x += 128)
-                        join_parts<D>(p, w, first + x / (D / 4), x % (D / 4) * 4, c0, c1, kHeadroom,
-                                      [&](uint32_t c) { return ((2 * (int64_t)c + (c == c0)) * C::kQTiles + qt) * 128 + x / (D / 4); });
+                    join_parts<D, 4, 4>(p, w, first, rows, c0, c1, kHeadroom, warp % 4,
+                                     [&](uint32_t c, int r) { return ((2 * (int64_t)c + (c == c0)) * C::kQTiles + qt) * 128 + r; });
                 }
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + qt) : "memory");
             }
         }
-    } else if (warp < kSoftmaxWarps + kLoadWarps) {
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+      if (warp < kMmaWarp) {
         // ------------------------------------------------ K and V tiles to fp16
         const int lt = tid - kSoftmaxWarps * 32;
         constexpr int kPerRow = D / 16;                           // 16-code chunks of a token
+        constexpr int kRowStep = kLoadThreads / kPerRow;          // tokens between a thread's chunks: a multiple of 8
+        const int row = lt / kPerRow, d = lt % kPerRow * 16;
+        // the lanes of a store that are in odd panels take their second half first: no bank twice
+        const bool swap = D > 64 && d / 64 % 2;
+        const int place = d / 64 * C::kKvPanel + row * 128, at16 = d % 64 / 8 + swap;
+        const int place0 = place + (at16 ^ (row & 7)) * 16, place1 = place + ((at16 ^ 1) ^ (row & 7)) * 16;
         uint32_t n_tile = 0;
-        const int in_block = (1 << p.log2_block) - 1;
         while (walk.next(p, w)) {
-            const uint8_t *k_head = p.k + (int64_t)w.head * p.stride_head, *v_head = p.v + (int64_t)w.head * p.stride_head;
-            const int32_t *table = p.block_table + w.request * p.table_width;
-            // a chunk's token may be absent: past the request's tokens, or in a block that is not there
-            auto fetch = [&](const uint8_t *base, int t, uint4 (&x)[C::kChunks]) {
+            auto convert = [&](unsigned char *tile, const unsigned char *codes, int t, bool full) {
+                const float4 *entry = entries[n_tile % C::kEntryStages];
 #pragma unroll
                 for (int c = 0; c < C::kChunks; ++c) {
-                    const int at = lt + c * kLoadThreads, token = t * C::kTile + at / kPerRow;
-                    int block = -1;
-                    if (token < w.kv) block = __ldg(table + (token >> p.log2_block));
-                    x[c] = make_uint4(0, 0, 0, 0);
-                    if (block >= 0 && block < p.num_blocks)
-                        x[c] = __ldg(reinterpret_cast<const uint4 *>(base + (int64_t)block * p.stride_block +
-                                                                     (int64_t)(token & in_block) * p.stride_token + at % kPerRow * 16));
+                    uint4 x = *reinterpret_cast<const uint4 *>(codes + (lt + c * kLoadThreads) * 16);
+                    if (!full) {   // a token past the request's, or in a block that is not there, is zero
+                        const int r = row + c * kRowStep;
+                        if (t * C::kTile + r >= w.kv || __float_as_int(entry[r / 16].w) < 0) x = make_uint4(0, 0, 0, 0);
+                    }
+                    if (swap) x = make_uint4(x.z, x.w, x.x, x.y);
+                    uint4 y0, y1;
+                    codes_to_half<FORMAT>(x.x, y0.x, y0.y);
+                    codes_to_half<FORMAT>(x.y, y0.z, y0.w);
+                    codes_to_half<FORMAT>(x.z, y1.x, y1.y);
+                    codes_to_half<FORMAT>(x.w, y1.z, y1.w);
+                    *reinterpret_cast<uint4 *>(tile + place0 + c * kRowStep * 128) = y0;
+                    *reinterpret_cast<uint4 *>(tile + place1 + c * kRowStep * 128) = y1;
                 }
             };
-            auto store = [&](unsigned char *tile, const uint4 (&x)[C::kChunks]) {
-#pragma unroll
-                for (int c = 0; c < C::kChunks; ++c) {
-                    const int at = lt + c * kLoadThreads, r = at / kPerRow, d = at % kPerRow * 16;
-                    uint4 lo, hi;
-                    codes_to_half<FORMAT>(x[c].x, lo.x, lo.y);
-                    codes_to_half<FORMAT>(x[c].y, lo.z, lo.w);
-                    codes_to_half<FORMAT>(x[c].z, hi.x, hi.y);
-                    codes_to_half<FORMAT>(x[c].w, hi.z, hi.w);
-                    unsigned char *line = tile + d / 64 * C::kKvPanel + r * 128;
-                    const int at16 = d % 64 / 8;
-                    *reinterpret_cast<uint4 *>(line + (at16 ^ (r & 7)) * 16) = lo;
-                    *reinterpret_cast<uint4 *>(line + ((at16 + 1) ^ (r & 7)) * 16) = hi;
-                }
-            };
-            uint4 kx[C::kChunks], vx[C::kChunks];
-            fetch(k_head, w.t0, kx);
             for (int t = w.t0; t < w.t1; ++t, ++n_tile) {
                 const int stage = n_tile % kStages;
                 const uint32_t empty = (n_tile / kStages & 1) ^ 1;
-                fetch(v_head, t, vx);
-                if (lt < 32) {
-                    // the tile's scales; an absent block's tokens get weight 2^-inf
-                    if (lt < C::kBlocks) {
-                        const BlockEntry b = block_entry(p, w.request, w.head, (int64_t)t * C::kTile + lt * 16, w.kv);
-                        scales[n_tile % kScaleStages][lt] = b.block < 0 ? make_float4(0.f, -INFINITY, 0.f, 0.f)
-                                                                         : make_float4(b.k_scale, b.v_log2, b.v_inverse, 0.f);
-                    }
-                    __syncwarp();
+                wait.warp(&bars.raw_full[0], n_tile & 1);
+                bool full = (t + 1) * C::kTile <= w.kv;
+                if (full) {
+                    int there = 0;
+                    if (lane < C::kBlocks) there = __float_as_int(entries[n_tile % C::kEntryStages][lane].w);
+                    full = __all_sync(~0u, there >= 0);
                 }
                 wait.warp(&bars.k_empty[stage], empty);
-                store(k_smem + stage * C::kKvBytes, kx);
+                if (full) convert(k_smem + stage * C::kKvBytes, raw, t, true);
+                else convert(k_smem + stage * C::kKvBytes, raw, t, false);
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) bar_arrive(&bars.k_full[stage]);
-                if (lt == 0) bar_arrive(&bars.scale_full[n_tile % kScaleStages]);
-                if (t + 1 < w.t1) fetch(k_head, t + 1, kx);
+                if (lane == 0) {
+                    bar_arrive(&bars.k_full[stage]);
+                    bar_arrive(&bars.raw_empty[0]);
+                }
+                wait.warp(&bars.raw_full[1], n_tile & 1);
                 wait.warp(&bars.v_empty[stage], empty);
-                store(v_smem + stage * C::kKvBytes, vx);
+                if (full) convert(v_smem + stage * C::kKvBytes, raw + C::kRawBytes, t, true);
+                else convert(v_smem + stage * C::kKvBytes, raw + C::kRawBytes, t, false);
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) bar_arrive(&bars.v_full[stage]);
+                if (lane == 0) {
+                    bar_arrive(&bars.v_full[stage]);
+                    bar_arrive(&bars.raw_empty[1]);
+                }
             }
         }
-    } else if (lane == 0) {
+      } else if (warp == kEntryWarp) {
+        // ------------------------------------------------ blocks and scales, kEntryTiles tiles at a time
+        uint32_t n_tile = 0;
+        while (walk.next(p, w)) {
+            for (int t = w.t0; t < w.t1;) {
+                // up to the next multiple of kEntryTiles of the count, so that the stages stay together
+                const int n = min(w.t1 - t, (int)(C::kEntryTiles - n_tile % C::kEntryTiles));
+                const int mine = lane / C::kBlocks, group = lane % C::kBlocks;
+                const uint32_t slot = (n_tile + mine) % C::kEntryStages;
+                if (mine < n) {
+                    wait(&bars.entry_empty[slot], ((n_tile + mine) / C::kEntryStages & 1) ^ 1);
+                    const BlockEntry b = block_entry(p, w.request, w.head, (int64_t)(t + mine) * C::kTile + group * 16, w.kv);
+                    // an absent block's tokens get weight 2^-inf
+                    entries[slot][group] = b.block < 0 ? make_float4(0.f, -INFINITY, 0.f, __int_as_float(-1))
+                                                       : make_float4(b.k_scale, b.v_log2, b.v_inverse, __int_as_float(b.block));
+                }
+                __syncwarp();
+                if (mine < n && group == 0) bar_arrive(&bars.entry_full[slot]);
+                t += n;
+                n_tile += n;
+            }
+        }
+      } else if (warp == kCopyWarp) {
+        // ------------------------------------------------ codes into shared memory, 16 tokens of a block per lane
+        uint32_t n_tile = 0;
+        const int in_block = (1 << p.log2_block) - 1;
+        while (walk.next(p, w)) {
+            for (int t = w.t0; t < w.t1; ++t, ++n_tile) {
+                wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
+                int block = -1;
+                if (lane < C::kBlocks) block = __float_as_int(entries[n_tile % C::kEntryStages][lane].w);
+                const uint32_t bytes = __popc(__ballot_sync(~0u, block >= 0)) * 16 * D;
+                const int64_t from = (int64_t)block * p.stride_block + (int64_t)w.head * p.stride_head +
+                                     (int64_t)((t * C::kTile + lane * 16) & in_block) * p.stride_token;
+#pragma unroll
+                for (int which = 0; which < 2; ++which) {
+                    wait.warp(&bars.raw_empty[which], (n_tile & 1) ^ 1);
+                    // the converting warps have read this tile before the copy engine writes it again
+                    if (lane == 0) bar_arrive_expect(&bars.raw_full[which], bytes);
+                    __syncwarp();
+                    if (block >= 0) {
+                        const uint8_t *src = (which ? p.v : p.k) + from;
+                        const uint32_t dst = smem_u32(raw) + which * C::kRawBytes + lane * 16 * D;
+                        if (p.stride_token == D) {
+                            bulk_copy(dst, src, 16 * D, &bars.raw_full[which]);
+                        } else {
+                            for (int r = 0; r < 16; ++r) bulk_copy(dst + r * D, src + r * p.stride_token, D, &bars.raw_full[which]);
+                        }
+                    }
+                }
+            }
+        }
+      } else if (warp == kMmaWarp) {
         // ------------------------------------------------ the matrix instructions
         constexpr uint32_t s_instruction = instruction(128, C::kTile, false), o_instruction = instruction(128, D, true);
         const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
+        const uint32_t leader = elect();
         uint32_t n_tile = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
         auto scores = [&](int qt, uint32_t stage) {
-            const uint32_t a = q_at + qt * C::kPanels * C::kQPanel, b = k_at + stage * C::kKvBytes;
+            uint32_t a = operand_lo(q_at + qt * C::kPanels * C::kQPanel, 16), b = operand_lo(k_at + stage * C::kKvBytes, 16);
+#pragma unroll 1
+            for (int k = 0; k < D / 16; k += C::kSteps) {         // a panel's 64 columns
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                mma_ss(tmem + qt * C::kSColumns, operand(a + k / 4 * C::kQPanel + k % 4 * 32, 16, 1024),
-                       operand(b + k / 4 * C::kKvPanel + k % 4 * 32, 16, 1024), s_instruction, k > 0);
-            commit(&bars.s_full[qt]);
+                for (int j = 0; j < C::kSteps; ++j)
+                    mma_ss(tmem + qt * C::kSColumns, operand(a + j * 2), operand(b + j * 2), s_instruction, k + j > 0, leader);
+                a += C::kQPanel / 16;
+                b += C::kKvPanel / 16;
+            }
+            commit(&bars.s_full[qt], leader);
         };
         while (walk.next(p, w)) {
             const int tiles = w.t1 - w.t0, n_q = C::kQTiles == 2 && w.rows - w.row_tile * C::kRows > 128 ? 2 : 1;
-            wait(&bars.k_full[n_tile % kStages], n_tile / kStages & 1);
+            wait.warp(&bars.k_full[n_tile % kStages], n_tile / kStages & 1);
             for (int qt = 0; qt < n_q; ++qt) {
-                wait(&bars.q_full[qt], q_phase[qt]);
+                wait.warp(&bars.q_full[qt], q_phase[qt]);
                 q_phase[qt] ^= 1;
                 fence_after();
                 scores(qt, n_tile % kStages);
             }
-            commit(&bars.k_empty[n_tile % kStages]);
+            commit(&bars.k_empty[n_tile % kStages], leader);
             for (int t = 0; t < tiles; ++t, ++n_tile) {
                 const uint32_t stage = n_tile % kStages, next = (n_tile + 1) % kStages;
-                wait(&bars.v_full[stage], n_tile / kStages & 1);
+                wait.warp(&bars.v_full[stage], n_tile / kStages & 1);
                 for (int qt = 0; qt < n_q; ++qt) {
-                    wait(&bars.p_full[qt], p_phase[qt]);
+                    wait.warp(&bars.p_full[qt], p_phase[qt]);
                     p_phase[qt] ^= 1;
                     fence_after();
-                    const uint32_t b = v_at + stage * C::kKvBytes;
+                    // every softmax thread has read the tile's entries, and so have the copies long before
+                    if (qt == n_q - 1 && leader) bar_arrive(&bars.entry_empty[n_tile % C::kEntryStages]);
+                    uint32_t a = tmem + qt * C::kSColumns, b = operand_lo(v_at + stage * C::kKvBytes, C::kKvPanel);
+#pragma unroll 1
+                    for (int k = 0; k < C::kTile / 16; k += 4) {
 #pragma unroll
-                    for (int k = 0; k < C::kTile / 16; ++k)
-                        mma_ts(tmem + C::kOColumn + qt * D, tmem + qt * C::kSColumns + k * 8, operand(b + k * 2048, C::kKvPanel, 1024),
-                               o_instruction, t > 0 || k > 0);
-                    if (t + 1 == tiles) commit(&bars.o_full[qt]);
-                    if (qt == n_q - 1) commit(&bars.v_empty[stage]);
+                        for (int j = 0; j < 4; ++j)
+                            mma_ts(tmem + C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, t > 0 || k + j > 0, leader);
+                        a += 4 * 8;
+                        b += 4 * 128;
+                    }
+                    if (t + 1 == tiles) commit(&bars.o_full[qt], leader);
+                    if (qt == n_q - 1) commit(&bars.v_empty[stage], leader);
                     if (t + 1 < tiles) {
                         if (qt == 0) {
-                            wait(&bars.k_full[next], (n_tile + 1) / kStages & 1);
+                            wait.warp(&bars.k_full[next], (n_tile + 1) / kStages & 1);
                             fence_after();
                         }
                         scores(qt, next);
-                        if (qt == n_q - 1) commit(&bars.k_empty[next]);
+                        if (qt == n_q - 1) commit(&bars.k_empty[next], leader);
                     }
                 }
             }
         }
+      }
     }
     fence_before();
     __syncthreads();
