@@ -45,6 +45,12 @@ struct QcacheAppendParams {
 cudaError_t launch_qcache_append(QcacheAppendParams p, int num_sms, cudaStream_t stream);
 
 // ---------------------------------------------------------------- attention
+// A range of kv tiles that is cut: the row tile and kv head that it belongs to, and the last thread
+// block that has a part of it.
+struct QcacheSplit {
+    int32_t request, head, row_tile, row0, rows, last_block;
+};
+
 struct QcacheAttentionParams {
     const uint8_t *k, *v;         // codes of the layer
     const float *k_scale, *v_scale;
@@ -60,7 +66,8 @@ struct QcacheAttentionParams {
     int64_t q_stride_row, q_stride_head, out_stride_row, out_stride_head;
     float *part_o;                // workspace: partial outputs, then their (maximum, sum) pairs
     float *part_ml;
-    unsigned int *arrived;
+    unsigned int *arrived;        // decode: parts of a range that have come
+    QcacheSplit *splits;          // prefill: the range that each thread block begins and does not end
     unsigned int *error;          // the context's word: bit 0 set when a bounded wait ran out
     float scale_log2;             // softmax scale * log2(e)
     int32_t requests, heads, group, head_dim, log2_block;
@@ -68,7 +75,7 @@ struct QcacheAttentionParams {
 };
 
 // The workspace holds, for every thread block of a launch, two partial results and an arrival
-// counter (for each of a block's row tiles).
+// counter or a QcacheSplit.
 constexpr int kQcacheDecodeBlocksPerSm = 4;
 constexpr int kQcacheMaxAttentionRequests = 4096;   // a word of shared memory each
 size_t qcache_workspace_bytes(int head_dim, int num_sms);

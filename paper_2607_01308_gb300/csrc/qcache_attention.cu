@@ -342,13 +342,15 @@ static size_t part_rows(int head_dim, int num_sms) {
 }
 
 size_t qcache_workspace_bytes(int head_dim, int num_sms) {
-    return part_rows(head_dim, num_sms) * ((size_t)head_dim + 2) * 4 + (size_t)num_sms * kQcacheDecodeBlocksPerSm * 4;
+    return part_rows(head_dim, num_sms) * ((size_t)head_dim + 2) * 4 + (size_t)num_sms * kQcacheDecodeBlocksPerSm * 4 +
+           (size_t)num_sms * sizeof(QcacheSplit);
 }
 
 void qcache_workspace_split(QcacheAttentionParams &p, void *workspace, int num_sms) {
     p.part_o = static_cast<float *>(workspace);
     p.part_ml = p.part_o + part_rows(p.head_dim, num_sms) * p.head_dim;
     p.arrived = reinterpret_cast<unsigned int *>(p.part_ml + part_rows(p.head_dim, num_sms) * 2);
+    p.splits = reinterpret_cast<QcacheSplit *>(p.arrived + (size_t)num_sms * kQcacheDecodeBlocksPerSm);
 }
 
 #define CM_EACH_DECODE(X) \

@@ -14,7 +14,9 @@
 //                    O += P V (P from tensor memory, V as it lies, tokens x head_dim)
 //   warp 13          looks up blocks and scales of every 16 tokens, several tiles ahead
 //   warp 14          bulk copies of the codes, a tile of K and one of V ahead
-// While one tile's softmax runs, the tensor cores work on the other tile. The softmax warps take
+// While one tile's softmax runs, the tensor cores work on the other tile. A second, small kernel joins
+// the ranges that were cut between thread blocks, over the whole GPU (one thread block alone took 95 us
+// for 256 rows in 19 parts). The softmax warps take
 // registers over from the others (200 and 56 of 128 at launch). Work is cut as in
 // qcache_attention.cu, over kv tiles that the rows of a tile may see at all.
 #include "cm_qcache_kernels.h"
@@ -203,59 +205,34 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return v;
 }
 
-// One row's scores of a kv tile to weights. left: columns that the row sees (MASKED only).
-template <int D, bool MASKED>
-__device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const float4 *sc, float factor, int left, bool rescale,
-                                             float &top, float &sum) {
-    using C = Shape<D>;
-    uint32_t x[C::kTile / 32][32];
-#pragma unroll
-    for (int c = 0; c < C::kTile / 32; ++c) tmem_ld32(x[c], s_at + 32 * c);
-    ld_wait();
-    float high = -INFINITY;
-#pragma unroll
-    for (int b = 0; b < C::kBlocks; ++b) {
-        float h = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            if (MASKED && 16 * b + k >= left) x[b / 2][b % 2 * 16 + k] = 0xff800000u;
-            h = fmaxf(h, __uint_as_float(x[b / 2][b % 2 * 16 + k]));
-        }
-        const float4 z = sc[b];
-        high = fmaxf(high, MASKED && h == -INFINITY ? h : fmaf(h, factor * z.x, z.y));
-    }
-    const bool raise = high > top + kRaise;
-    if (__any_sync(~0u, raise)) {
-        const float now = raise ? high : top;
-        const float f = top == now ? 1.f : exp2_fast(top - now);
-        top = now;
-        sum *= f;
-        if (rescale) {
-#pragma unroll 1
-            for (int c = 0; c < D / 16; ++c) {
-                uint32_t y[16];
-                tmem_ld16(y, o_at + 16 * c);
-                ld_wait();
-#pragma unroll
-                for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
-                tmem_st16(o_at + 16 * c, y);
-            }
-        }
-    }
+// One row's scores x of a kv tile to weights against the maximum `top`, into the tile's columns as fp16.
+// left: columns that the row sees (MASKED only). Returns the sum of the weights without the V scales;
+// high: the largest exponent. EXACT rounds a score before the maximum is taken off it, as the maximum
+// itself was rounded, which keeps the exponents at or below the headroom however large the scores are.
+template <int D, bool MASKED, bool EXACT>
+__device__ __forceinline__ float weights(const uint32_t (&x)[Shape<D>::kTile / 32][32], uint32_t s_at, const float4 *sc, float factor,
+                                         int left, float top, float &high) {
     const float base = (top == -INFINITY ? 0.f : top) - kHeadroom;
+    const uint64_t base2 = pair(-base, -base);
+    float sum = 0.f;
+    high = -INFINITY;
 #pragma unroll
-    for (int c = 0; c < C::kTile / 32; ++c) {
+    for (int c = 0; c < Shape<D>::kTile / 32; ++c) {
         uint32_t y[16];
+        float high_c = -INFINITY;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const float4 z = sc[2 * c + b];
-            const float a = factor * z.x, d = z.y - base;
+            const float a = factor * z.x, d = EXACT ? z.y : z.y - base;
             const uint64_t a2 = pair(a, a), d2 = pair(d, d);
             uint64_t part = 0;
 #pragma unroll
             for (int k = 0; k < 16; k += 2) {
                 float e0, e1;
-                unpair(fma2(pair(__uint_as_float(x[c][16 * b + k]), __uint_as_float(x[c][16 * b + k + 1])), a2, d2), e0, e1);
+                uint64_t e = fma2(pair(__uint_as_float(x[c][16 * b + k]), __uint_as_float(x[c][16 * b + k + 1])), a2, d2);
+                if (EXACT) e = add2(e, base2);
+                unpair(e, e0, e1);
+                high_c = fmaxf(fmaxf(high_c, e0), e1);
                 e0 = exp2_fast(e0);
                 e1 = exp2_fast(e1);
                 if (MASKED) {   // a score of -inf times a scale of 0 is no number
@@ -269,8 +246,60 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const
             unpair(part, p0, p1);
             sum = fmaf(p0 + p1, z.z, sum);
         }
+        high = fmaxf(high, high_c);
         tmem_st16(s_at + 16 * c, y);
     }
+    return sum;
+}
+
+// A kv tile of one row. The weights are computed against the maximum as it stands; only if that leaves
+// fp16's range for some row of the warp is the maximum raised, the output rescaled and the tile done again
+// from the registers. The first tile of a segment looks for its maximum first.
+template <int D, bool MASKED>
+__device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const float4 *sc, float factor, int left, bool first,
+                                             float &top, float &sum) {
+    using C = Shape<D>;
+    uint32_t x[C::kTile / 32][32];
+#pragma unroll
+    for (int c = 0; c < C::kTile / 32; ++c) tmem_ld32(x[c], s_at + 32 * c);
+    ld_wait();
+    if (MASKED) {
+#pragma unroll
+        for (int k = 0; k < C::kTile; ++k)
+            if (k >= left) x[k / 32][k % 32] = 0xff800000u;
+    }
+    float high;
+    if (!first) {
+        const float tile = weights<D, MASKED, false>(x, s_at, sc, factor, left, top, high);
+        if (!__any_sync(~0u, high > kRaise + kHeadroom)) {
+            sum += tile;
+            st_wait();
+            return;
+        }
+    }
+    high = top;
+#pragma unroll
+    for (int b = 0; b < C::kBlocks; ++b) {
+        float h = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) h = fmaxf(h, __uint_as_float(x[b / 2][b % 2 * 16 + k]));
+        const float4 z = sc[b];
+        high = fmaxf(high, MASKED && h == -INFINITY ? h : fmaf(h, factor * z.x, z.y));
+    }
+    const float f = top == high ? 1.f : exp2_fast(top - high);
+    top = high;
+    if (!first) {
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+            uint32_t y[16];
+            tmem_ld16(y, o_at + 16 * c);
+            ld_wait();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
+            tmem_st16(o_at + 16 * c, y);
+        }
+    }
+    sum = fmaf(sum, f, weights<D, MASKED, true>(x, s_at, sc, factor, left, top, high));
     st_wait();
 }
 
@@ -379,7 +408,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     __shared__ uint32_t scan[kThreads / 32];
     __shared__ Start start;
     __shared__ uint32_t tmem_base;
-    __shared__ uint32_t last_one[2];
     __shared__ int failed;
     unsigned char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + kStages * C::kKvBytes;
@@ -489,7 +517,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         const uint32_t s_at = tmem + lanes + qt * C::kSColumns, o_at = tmem + lanes + C::kOColumn + qt * D;
         uint32_t n_tile = 0;          // kv tiles of the block so far
         uint32_t s_phase = 0, o_phase = 0;
-        const uint64_t per = start.per;
         while (walk.next(p, w)) {
             const int first = w.row_tile * C::kRows + qt * 128;   // of the tile, among the request's rows
             if (first >= w.rows || qt >= C::kQTiles) {
@@ -504,7 +531,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             fence_async_smem();
             bar_arrive(&bars.q_full[qt]);
 
-            const int limit = !valid ? 0 : p.causal ? min(w.kv, max(0, w.kv - w.q_len + (int)(token - w.row0) + 1)) : w.kv;
+            // a row that is not there sees everything, so that no tile is masked for its sake
+            const int limit = !valid ? INT32_MAX : p.causal ? min(w.kv, max(0, w.kv - w.q_len + (int)(token - w.row0) + 1)) : w.kv;
             const int least = __reduce_min_sync(~0u, limit);      // of the warp's rows
             float top = -INFINITY, sum = 0.f;
             for (int t = w.t0; t < w.t1; ++t, ++n_tile) {
@@ -514,9 +542,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 fence_after();
                 const float4 *sc = entries[n_tile % C::kEntryStages];
                 if ((t + 1) * C::kTile > least)
-                    softmax_tile<D, true>(s_at, o_at, sc, factor, limit - t * C::kTile, t > w.t0, top, sum);
+                    softmax_tile<D, true>(s_at, o_at, sc, factor, limit - t * C::kTile, t == w.t0, top, sum);
                 else
-                    softmax_tile<D, false>(s_at, o_at, sc, factor, 0, t > w.t0, top, sum);
+                    softmax_tile<D, false>(s_at, o_at, sc, factor, 0, t == w.t0, top, sum);
                 fence_before();
                 bar_arrive(&bars.p_full[qt]);
             }
@@ -525,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             fence_after();
             const bool whole = w.t0 == 0 && w.t1 == w.tiles;
             const int rows = min(128, w.rows - first);
-            const int64_t part = ((2 * (int64_t)blockIdx.x + (w.t0 == 0)) * C::kQTiles + qt) * 128;
+            const int64_t part = (2 * (int64_t)blockIdx.x + (w.t0 == 0)) * C::kRows + qt * 128;
             const float scale = sum == 0.f ? 0.f : 1.f / sum;
             uint16_t *to = p.out + token * p.out_stride_row + head * p.out_stride_head;
             float *to_part = p.part_o + (part + row) * D;
@@ -551,20 +579,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 }
             }
             if (valid && whole && p.lse) p.lse[token * ((int64_t)p.heads * p.group) + head] = log_sum(top, sum, kHeadroom);
-            if (!whole) {
-                if (valid) __stcg(reinterpret_cast<float2 *>(p.part_ml + (part + row) * 2), make_float2(top, sum));
-                const uint32_t c0 = (uint32_t)(w.unit0 / per), c1 = (uint32_t)((w.unit0 + w.tiles - 1) / per);
-                __threadfence();
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + qt) : "memory");
-                if (row == 0) last_one[qt] = atomicInc(p.arrived + (size_t)qt * gridDim.x + c0, c1 - c0) == c1 - c0;
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + qt) : "memory");
-                if (last_one[qt]) {
-                    __threadfence();
-                    join_parts<D, 4, 4>(p, w, first, rows, c0, c1, kHeadroom, warp % 4,
-                                     [&](uint32_t c, int r) { return ((2 * (int64_t)c + (c == c0)) * C::kQTiles + qt) * 128 + r; });
-                }
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + qt) : "memory");
-            }
+            if (valid && !whole) __stcg(reinterpret_cast<float2 *>(p.part_ml + (part + row) * 2), make_float2(top, sum));
         }
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
@@ -700,7 +715,15 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             }
             commit(&bars.s_full[qt], leader);
         };
+        bool split = false;
         while (walk.next(p, w)) {
+            if (w.t0 == 0 && w.t1 < w.tiles) {
+                // the part that begins a range which the next blocks go on with: for the joining kernel
+                split = true;
+                if (leader) {
+                    p.splits[blockIdx.x] = {w.request, w.head, w.row_tile, w.row0, w.rows, (int)((w.unit0 + w.tiles - 1) / start.per)};
+                }
+            }
             const int tiles = w.t1 - w.t0, n_q = C::kQTiles == 2 && w.rows - w.row_tile * C::kRows > 128 ? 2 : 1;
             wait.warp(&bars.k_full[n_tile % kStages], n_tile / kStages & 1);
             for (int qt = 0; qt < n_q; ++qt) {
@@ -741,6 +764,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 }
             }
         }
+        if (!split && leader) p.splits[blockIdx.x].rows = 0;
       }
     }
     fence_before();
@@ -749,6 +773,25 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     __syncwarp();
     if (warp == kMmaWarp)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512));
+}
+
+// The parts of ranges that were cut: a thread block for 16 rows of a range, which begins in block
+// blockIdx.x of the kernel before.
+constexpr int kJoinRows = 16, kJoinWarps = 4;
+
+template <int D>
+__global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const __grid_constant__ QcacheAttentionParams p) {
+    using C = Shape<D>;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const QcacheSplit z = p.splits[blockIdx.x];
+    const int in_tile = blockIdx.y * kJoinRows, first = z.row_tile * C::kRows + in_tile;
+    if (first >= z.rows) return;
+    AttentionSegment w{};
+    w.head = z.head;
+    w.row0 = z.row0;
+    const uint32_t c0 = blockIdx.x;
+    join_parts<D, kJoinWarps, 4>(p, w, first, min(kJoinRows, z.rows - first), c0, (uint32_t)z.last_block, kHeadroom, threadIdx.x / 32,
+                                 [&](uint32_t c, int r) { return (2 * (int64_t)c + (c == c0)) * C::kRows + in_tile + r; });
 }
 
 template <int D, int FORMAT>
@@ -763,7 +806,18 @@ cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cuda
         if (device < 64) allowed.fetch_or(1ull << device);
     }
     prefill_kernel<D, FORMAT><<<num_sms, kThreads, smem, stream>>>(p);
-    return cudaGetLastError();
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute early;                  // it may be set up while the kernel before it ends
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(num_sms, C::kRows / kJoinRows);
+    config.blockDim = dim3(kJoinWarps * 32);
+    config.stream = stream;
+    config.attrs = &early;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, join_kernel<D>, p);
 }
 
 }  // namespace
