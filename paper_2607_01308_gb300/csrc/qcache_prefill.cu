@@ -5,19 +5,22 @@
 // One thread block per SM, on the tcgen05 tensor cores, with up to 256 query rows (rows are query
 // tokens x heads of a group) in two tiles of 128, so that each K and V tile that is brought in and
 // taken to fp16 serves both:
-//   warps 0-3, 4-7   softmax of query tile 0 and 1, one row per thread: a tile's 128 scores from tensor
-//                    memory into registers, weights back into the same columns as fp16, the output
+//   warps 0-3, 4-7   softmax of query tile 0 and 1, one row per thread: half a kv tile (64 scores) from
+//                    tensor memory into registers, weights back into the same columns as fp16, the output
 //                    rescaled when the running maximum is raised, the row normalised and written
-//   warps 8-11       K and V tiles from codes to fp16, shared memory to shared memory, into the 128-byte
-//                    swizzle (two stages each)
-//   warp 12          issues the matrix instructions: S = Q K^T (both operands from shared memory),
+//   warps 8-11       K tiles from codes to fp16, shared memory to shared memory, into the 128-byte swizzle
+//   warps 12-15      V tiles
+//   warp 16          issues the matrix instructions: S = Q K^T (both operands from shared memory),
 //                    O += P V (P from tensor memory, V as it lies, tokens x head_dim)
-//   warp 13          looks up blocks and scales of every 16 tokens, several tiles ahead
-//   warp 14          bulk copies of the codes, a tile of K and one of V ahead
-// While one tile's softmax runs, the tensor cores work on the other tile. A second, small kernel joins
+//   warp 17          looks up blocks and scales of every 16 tokens, several tiles ahead
+//   warps 18, 19     bulk copies of the codes of K, of V, half a tile or two ahead
+// Scores are products of 128 x 128 (64 columns at a time cost the tensor cores as much as 128); weights
+// go in by halves, so that the second half's softmax runs beside the first half's product, and one query
+// tile's softmax beside the other's products. At head_dim 256 the output of one query tile is all that
+// fits beside the scores: kv tiles are 64 tokens, with scores two tiles ahead in two buffers. A second, small kernel joins
 // the ranges that were cut between thread blocks, over the whole GPU (one thread block alone took 95 us
 // for 256 rows in 19 parts). The softmax warps take
-// registers over from the others (200 and 56 of 128 at launch). Work is cut as in
+// registers over from the others (144 and 64 of 96 at launch). Work is cut as in
 // qcache_attention.cu, over kv tiles that the rows of a tile may see at all.
 #include "cm_qcache_kernels.h"
 
@@ -29,32 +32,38 @@
 namespace cm {
 namespace {
 
-constexpr int kSoftmaxWarps = 8, kLoadWarps = 4, kMmaWarp = kSoftmaxWarps + kLoadWarps, kEntryWarp = kMmaWarp + 1, kCopyWarp = kMmaWarp + 2;
-constexpr int kThreads = 16 * 32;           // whole warpgroups: registers change hands by warpgroup
-constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;
-static_assert(256 * kSoftmaxRegs + 256 * kOtherRegs <= kThreads * 128, "registers at launch");
+constexpr int kSoftmaxWarps = 8, kLoadWarps = 4;              // load warps: for K, and as many for V
+constexpr int kMmaWarp = kSoftmaxWarps + 2 * kLoadWarps, kEntryWarp = kMmaWarp + 1, kCopyWarp = kMmaWarp + 2;
+constexpr int kThreads = 20 * 32;           // whole warpgroups: registers change hands by warpgroup
+constexpr int kLaunchRegs = 96, kSoftmaxRegs = 144, kOtherRegs = 64;
+static_assert(256 * kSoftmaxRegs + (kThreads - 256) * kOtherRegs <= kThreads * kLaunchRegs, "registers at launch");
 constexpr int kLoadThreads = kLoadWarps * 32;
-constexpr int kStages = 2;
 constexpr float kRaise = 8.f, kHeadroom = 7.f;
+
+constexpr int kHalf = 64;                   // tokens that go through the softmax at a time
+constexpr int kHalfBlocks = kHalf / 16;     // their scale entries
 
 template <int D>
 struct Shape {
-    static constexpr int kQTiles = D == 256 ? 1 : 2;          // tensor memory: scores and outputs, 512 columns
-    static constexpr int kRows = 128 * kQTiles;
-    static constexpr int kTile = D == 256 ? 64 : 128;         // tokens of a kv tile
-    static constexpr int kPanels = D < 64 ? 1 : D / 64;       // 64 columns (128 bytes) of fp16 each
-    static constexpr int kQPanel = 128 * 128, kKvPanel = kTile * 128;   // bytes
-    static constexpr int kQBytes = kQTiles * kPanels * kQPanel;
-    static constexpr int kKvBytes = kPanels * kKvPanel;       // one tile of K or V
+    // tensor memory, 512 columns: two tiles of scores, and the outputs
+    static constexpr int kQTiles = D == 256 ? 1 : 2;
+    static constexpr int kTile = D == 256 ? 64 : 128, kHalves = kTile / kHalf;   // tokens of a kv tile
     static constexpr int kBlocks = kTile / 16;                // scale entries of a tile
-    static constexpr int kEntryTiles = 32 / kBlocks;          // tiles that the entry warp looks up at a time
-    static constexpr int kEntryStages = 2 * kEntryTiles;
-    static constexpr int kChunks = kTile * D / 16 / kLoadThreads;   // 16-code copies of a thread for K (and for V)
-    static constexpr int kRawBytes = kTile * D;               // codes of a tile
+    static constexpr int kEntryTiles = 32 / kBlocks, kEntryStages = 2 * kEntryTiles;   // looked up at a time; held
+    static constexpr int kScoreBuffers = 2 / kQTiles;         // for each query tile
+    static constexpr int kRows = 128 * kQTiles;
+    static constexpr int kOColumn = 2 * kTile;
+    static constexpr int kPanels = D < 64 ? 1 : D / 64;       // 64 columns (128 bytes) of fp16 each
     static constexpr int kSteps = D < 64 ? D / 16 : 4;        // 16 columns each, of a panel
-    static constexpr int kSColumns = 128;                     // tensor memory columns between score tiles
-    static constexpr int kOColumn = kQTiles * kSColumns;
-    static constexpr size_t kSmem = 1024 + kQBytes + 2 * kStages * kKvBytes + 2 * kRawBytes;
+    static constexpr int kKStages = 2;                        // tiles of K
+    static constexpr int kVStages = 2 * kHalves;              // half tiles of V
+    static constexpr int kRawStages = D == 256 ? 1 : 2;       // half tiles of codes, of K and of V
+    static constexpr int kQPanel = 128 * 128, kKPanel = kTile * 128, kVPanel = kHalf * 128;   // bytes
+    static constexpr int kQBytes = kQTiles * kPanels * kQPanel;
+    static constexpr int kKBytes = kPanels * kKPanel, kVBytes = kPanels * kVPanel;   // a tile of K, half a tile of V
+    static constexpr int kChunks = kHalf * D / 16 / kLoadThreads;   // 16-code chunks of a thread in half a tile
+    static constexpr int kRawBytes = kHalf * D;
+    static constexpr size_t kSmem = 1024 + kQBytes + kKStages * kKBytes + kVStages * kVBytes + 2 * kRawStages * kRawBytes;
     static_assert(kChunks >= 1, "every load thread has work");
     static_assert(kOColumn + kQTiles * D <= 512, "tensor memory");
 };
@@ -157,6 +166,11 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&x)[16]) 
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
                  ::"r"(at), CM_IN16(x, 0) : "memory");
 }
+__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&x)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(at), CM_IN16(x, 0), CM_IN16(x, 16) : "memory");
+}
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Shared memory operand in 128-byte swizzled atoms of 8 rows x 128 bytes. Rows of K (and Q) are
@@ -205,101 +219,93 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return v;
 }
 
-// One row's scores x of a kv tile to weights against the maximum `top`, into the tile's columns as fp16.
-// left: columns that the row sees (MASKED only). Returns the sum of the weights without the V scales;
-// high: the largest exponent. EXACT rounds a score before the maximum is taken off it, as the maximum
-// itself was rounded, which keeps the exponents at or below the headroom however large the scores are.
-template <int D, bool MASKED, bool EXACT>
-__device__ __forceinline__ float weights(const uint32_t (&x)[Shape<D>::kTile / 32][32], uint32_t s_at, const float4 *sc, float factor,
-                                         int left, float top, float &high) {
-    const float base = (top == -INFINITY ? 0.f : top) - kHeadroom;
-    const uint64_t base2 = pair(-base, -base);
-    float sum = 0.f;
-    high = -INFINITY;
-#pragma unroll
-    for (int c = 0; c < Shape<D>::kTile / 32; ++c) {
-        uint32_t y[16];
-        float high_c = -INFINITY;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const float4 z = sc[2 * c + b];
-            const float a = factor * z.x, d = EXACT ? z.y : z.y - base;
-            const uint64_t a2 = pair(a, a), d2 = pair(d, d);
-            uint64_t part = 0;
-#pragma unroll
-            for (int k = 0; k < 16; k += 2) {
-                float e0, e1;
-                uint64_t e = fma2(pair(__uint_as_float(x[c][16 * b + k]), __uint_as_float(x[c][16 * b + k + 1])), a2, d2);
-                if (EXACT) e = add2(e, base2);
-                unpair(e, e0, e1);
-                high_c = fmaxf(fmaxf(high_c, e0), e1);
-                e0 = exp2_fast(e0);
-                e1 = exp2_fast(e1);
-                if (MASKED) {   // a score of -inf times a scale of 0 is no number
-                    if (32 * c + 16 * b + k >= left) e0 = 0.f;
-                    if (32 * c + 16 * b + k + 1 >= left) e1 = 0.f;
-                }
-                part = add2(part, pair(e0, e1));
-                y[8 * b + k / 2] = pack_half(e0, e1);
-            }
-            float p0, p1;
-            unpair(part, p0, p1);
-            sum = fmaf(p0 + p1, z.z, sum);
-        }
-        high = fmaxf(high, high_c);
-        tmem_st16(s_at + 16 * c, y);
-    }
-    return sum;
-}
+// What a softmax thread keeps of its row. The weights of a tile are 2^(t - top + headroom); `limit` is the
+// largest exponent that is let pass: without bound until the row has seen a token, which then sets `top`.
+struct RowState {
+    float top, sum, limit;
+};
 
-// A kv tile of one row. The weights are computed against the maximum as it stands; only if that leaves
-// fp16's range for some row of the warp is the maximum raised, the output rescaled and the tile done again
-// from the registers. The first tile of a segment looks for its maximum first.
-template <int D, bool MASKED>
-__device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const float4 *sc, float factor, int left, bool first,
-                                             float &top, float &sum) {
-    using C = Shape<D>;
-    uint32_t x[C::kTile / 32][32];
+// Half a kv tile of one row: scores to weights, into its own columns as fp16. left: columns that the row sees
+// (only if `masked`, which is the warp's). Where the largest exponent of some row passes its limit, that row's
+// maximum is raised by as much, its sum and (behind `wait_output`) its output rescaled.
+template <int D, class Wait>
+__device__ __forceinline__ void softmax_half(uint32_t s_at, uint32_t o_at, const float4 *sc, float factor, bool masked, int left,
+                                             bool first, RowState &r, Wait wait_output) {
+    uint32_t x[kHalf / 32][32];
 #pragma unroll
-    for (int c = 0; c < C::kTile / 32; ++c) tmem_ld32(x[c], s_at + 32 * c);
+    for (int c = 0; c < kHalf / 32; ++c) tmem_ld32(x[c], s_at + 32 * c);
     ld_wait();
-    if (MASKED) {
+    const float base = kHeadroom - r.top;
+    float z_inverse[kHalfBlocks], high[kHalfBlocks];
 #pragma unroll
-        for (int k = 0; k < C::kTile; ++k)
+    for (int b = 0; b < kHalfBlocks; ++b) {
+        const float4 z = sc[b];
+        z_inverse[b] = z.z;
+        const float a = factor * z.x, d = z.y + base;
+        const uint64_t a2 = pair(a, a), d2 = pair(d, d);
+        uint32_t *y = &x[b / 2][b % 2 * 16];
+#pragma unroll
+        for (int k = 0; k < 16; k += 2) {
+            float e0, e1;
+            unpair(fma2(pair(__uint_as_float(y[k]), __uint_as_float(y[k + 1])), a2, d2), e0, e1);
+            y[k] = __float_as_uint(e0);
+            y[k + 1] = __float_as_uint(e1);
+        }
+    }
+    if (masked) {
+#pragma unroll
+        for (int k = 0; k < kHalf; ++k)
             if (k >= left) x[k / 32][k % 32] = 0xff800000u;
     }
-    float high;
-    if (!first) {
-        const float tile = weights<D, MASKED, false>(x, s_at, sc, factor, left, top, high);
-        if (!__any_sync(~0u, high > kRaise + kHeadroom)) {
-            sum += tile;
-            st_wait();
-            return;
-        }
-    }
-    high = top;
 #pragma unroll
-    for (int b = 0; b < C::kBlocks; ++b) {
-        float h = -INFINITY;
+    for (int b = 0; b < kHalfBlocks; ++b) {
+        const uint32_t *y = &x[b / 2][b % 2 * 16];
+        high[b] = __uint_as_float(y[0]);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) h = fmaxf(h, __uint_as_float(x[b / 2][b % 2 * 16 + k]));
-        const float4 z = sc[b];
-        high = fmaxf(high, MASKED && h == -INFINITY ? h : fmaf(h, factor * z.x, z.y));
+        for (int k = 1; k < 16; ++k) high[b] = fmaxf(high[b], __uint_as_float(y[k]));
     }
-    const float f = top == high ? 1.f : exp2_fast(top - high);
-    top = high;
-    if (!first) {
+    float most = high[0];
+#pragma unroll
+    for (int b = 1; b < kHalfBlocks; ++b) most = fmaxf(most, high[b]);
+    if (__any_sync(~0u, most > r.limit)) {
+        const bool raise = most > r.limit;
+        const float by = raise ? most - kHeadroom : 0.f;
+        const float f = !raise ? 1.f : r.limit == -INFINITY ? 0.f : exp2_fast(-by);
+        r.top += by;
+        r.sum *= f;
+        if (raise) r.limit = kRaise + kHeadroom;
+#pragma unroll
+        for (int k = 0; k < kHalf; ++k) x[k / 32][k % 32] = __float_as_uint(__uint_as_float(x[k / 32][k % 32]) - by);
+        if (!first) {
+            wait_output();
+            fence_after();
 #pragma unroll 1
-        for (int c = 0; c < D / 16; ++c) {
-            uint32_t y[16];
-            tmem_ld16(y, o_at + 16 * c);
-            ld_wait();
+            for (int c = 0; c < D / 16; ++c) {
+                uint32_t y[16];
+                tmem_ld16(y, o_at + 16 * c);
+                ld_wait();
 #pragma unroll
-            for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
-            tmem_st16(o_at + 16 * c, y);
+                for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
+                tmem_st16(o_at + 16 * c, y);
+            }
         }
     }
-    sum = fmaf(sum, f, weights<D, MASKED, true>(x, s_at, sc, factor, left, top, high));
+    uint32_t w[kHalf / 2];
+#pragma unroll
+    for (int b = 0; b < kHalfBlocks; ++b) {
+        const uint32_t *y = &x[b / 2][b % 2 * 16];
+        uint64_t part = 0;
+#pragma unroll
+        for (int k = 0; k < 16; k += 2) {
+            const float e0 = exp2_fast(__uint_as_float(y[k])), e1 = exp2_fast(__uint_as_float(y[k + 1]));
+            part = add2(part, pair(e0, e1));
+            w[8 * b + k / 2] = pack_half(e0, e1);
+        }
+        float p0, p1;
+        unpair(part, p0, p1);
+        r.sum = fmaf(p0 + p1, z_inverse[b], r.sum);
+    }
+    tmem_st32(s_at, w);
     st_wait();
 }
 
@@ -393,10 +399,13 @@ struct Start {
 };
 
 struct Barriers {
-    uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+    uint64_t k_full[2], k_empty[2], v_full[4], v_empty[4];
     uint64_t entry_full[16], entry_empty[16];
-    uint64_t raw_full[2], raw_empty[2];       // K, V
-    uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
+    uint64_t raw_full[2][2], raw_empty[2][2];       // K, V
+    uint64_t q_full[2], o_full[2];
+    uint64_t s_full[2];                       // score buffer
+    uint64_t p_full[2][2];                    // query tile; half, or score buffer where there are two
+    uint64_t o_done[2];                       // another half tile is in the output
 };
 
 template <int D, int FORMAT>
@@ -410,8 +419,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     __shared__ uint32_t tmem_base;
     __shared__ int failed;
     unsigned char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-    unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + kStages * C::kKvBytes;
-    unsigned char *raw = v_smem + kStages * C::kKvBytes;
+    unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + C::kKStages * C::kKBytes;
+    unsigned char *raw = v_smem + C::kVStages * C::kVBytes;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
 
     // the plan: one thread per request, prefix sums in the (still unused) tile memory
@@ -445,10 +454,12 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (tid == 0) {
-        for (int i = 0; i < kStages; ++i) {
-            bar_init(&bars.k_full[i], kLoadWarps);
-            bar_init(&bars.v_full[i], kLoadWarps);
+        for (int i = 0; i < C::kKStages; ++i) {
+            bar_init(&bars.k_full[i], C::kHalves * kLoadWarps);
             bar_init(&bars.k_empty[i], 1);
+        }
+        for (int i = 0; i < C::kVStages; ++i) {
+            bar_init(&bars.v_full[i], kLoadWarps);
             bar_init(&bars.v_empty[i], 1);
         }
         for (int i = 0; i < C::kEntryStages; ++i) {
@@ -456,12 +467,15 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             bar_init(&bars.entry_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
-            bar_init(&bars.raw_full[i], 1);
-            bar_init(&bars.raw_empty[i], kLoadWarps);
-            bar_init(&bars.q_full[i], 128);
-            bar_init(&bars.p_full[i], 128);
+            for (int j = 0; j < C::kRawStages; ++j) {
+                bar_init(&bars.raw_full[i][j], 1);
+                bar_init(&bars.raw_empty[i][j], kLoadWarps);
+            }
+            for (int j = 0; j < 2; ++j) bar_init(&bars.p_full[i][j], 128);
             bar_init(&bars.s_full[i], 1);
+            bar_init(&bars.q_full[i], 128);
             bar_init(&bars.o_full[i], 1);
+            bar_init(&bars.o_done[i], 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
@@ -514,9 +528,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const int qt = warp / 4, row = tid % 128;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
-        const uint32_t s_at = tmem + lanes + qt * C::kSColumns, o_at = tmem + lanes + C::kOColumn + qt * D;
+        const uint32_t s_at = tmem + lanes, o_at = tmem + lanes + C::kOColumn + qt * D;
         uint32_t n_tile = 0;          // kv tiles of the block so far
-        uint32_t s_phase = 0, o_phase = 0;
+        uint32_t n_mine = 0, o_phase = 0;       // those with rows in this query tile
         while (walk.next(p, w)) {
             const int first = w.row_tile * C::kRows + qt * 128;   // of the tile, among the request's rows
             if (first >= w.rows || qt >= C::kQTiles) {
@@ -534,20 +548,26 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             // a row that is not there sees everything, so that no tile is masked for its sake
             const int limit = !valid ? INT32_MAX : p.causal ? min(w.kv, max(0, w.kv - w.q_len + (int)(token - w.row0) + 1)) : w.kv;
             const int least = __reduce_min_sync(~0u, limit);      // of the warp's rows
-            float top = -INFINITY, sum = 0.f;
-            for (int t = w.t0; t < w.t1; ++t, ++n_tile) {
+            RowState r{0.f, 0.f, -INFINITY};
+            for (int t = w.t0; t < w.t1; ++t, ++n_tile, ++n_mine) {
+                // one buffer for each query tile, or two that take turns
+                const uint32_t buffer = C::kQTiles == 2 ? qt : n_mine & 1, phase = n_mine / C::kScoreBuffers & 1;
                 wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
-                wait.warp(&bars.s_full[qt], s_phase);
-                s_phase ^= 1;
+                wait.warp(&bars.s_full[buffer], phase);
                 fence_after();
-                const float4 *sc = entries[n_tile % C::kEntryStages];
-                if ((t + 1) * C::kTile > least)
-                    softmax_tile<D, true>(s_at, o_at, sc, factor, limit - t * C::kTile, t == w.t0, top, sum);
-                else
-                    softmax_tile<D, false>(s_at, o_at, sc, factor, 0, t == w.t0, top, sum);
-                fence_before();
-                bar_arrive(&bars.p_full[qt]);
+#pragma unroll 1
+                for (int h = 0; h < C::kHalves; ++h) {
+                    const int token = t * C::kTile + h * kHalf;
+                    // the product before: half h ^ 1 of this tile or the one before; or the tile before
+                    const uint32_t before = C::kHalves == 2 ? h ^ 1 : (n_mine & 1) ^ 1;
+                    softmax_half<D>(s_at + buffer * C::kTile + h * kHalf, o_at, entries[n_tile % C::kEntryStages] + h * kHalfBlocks, factor,
+                                    token + kHalf > least, limit - token, t == w.t0 && h == 0, r,
+                                    [&] { wait.warp(&bars.o_done[qt], before); });
+                    fence_before();
+                    bar_arrive(&bars.p_full[qt][C::kHalves == 2 ? h : buffer]);
+                }
             }
+            const float top = r.top, sum = r.sum;
             wait.warp(&bars.o_full[qt], o_phase);
             o_phase ^= 1;
             fence_after();
@@ -579,78 +599,82 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 }
             }
             if (valid && whole && p.lse) p.lse[token * ((int64_t)p.heads * p.group) + head] = log_sum(top, sum, kHeadroom);
-            if (valid && !whole) __stcg(reinterpret_cast<float2 *>(p.part_ml + (part + row) * 2), make_float2(top, sum));
+            if (valid && !whole) __stcg(reinterpret_cast<float2 *>(p.part_ml + (part + row) * 2), make_float2(sum == 0.f ? -INFINITY : top, sum));
         }
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
       if (warp < kMmaWarp) {
-        // ------------------------------------------------ K and V tiles to fp16
-        const int lt = tid - kSoftmaxWarps * 32;
+        // ------------------------------------------------ K (the first four warps) and V tiles to fp16
+        const bool is_v = warp >= kSoftmaxWarps + kLoadWarps;
+        const int lt = tid % kLoadThreads;
         constexpr int kPerRow = D / 16;                           // 16-code chunks of a token
         constexpr int kRowStep = kLoadThreads / kPerRow;          // tokens between a thread's chunks: a multiple of 8
         const int row = lt / kPerRow, d = lt % kPerRow * 16;
         // the lanes of a store that are in odd panels take their second half first: no bank twice
         const bool swap = D > 64 && d / 64 % 2;
-        const int place = d / 64 * C::kKvPanel + row * 128, at16 = d % 64 / 8 + swap;
-        const int place0 = place + (at16 ^ (row & 7)) * 16, place1 = place + ((at16 ^ 1) ^ (row & 7)) * 16;
-        uint32_t n_tile = 0;
+        const int at16 = d % 64 / 8 + swap, panel = is_v ? C::kVPanel : C::kKPanel;
+        unsigned char *to0 = (is_v ? v_smem : k_smem) + d / 64 * panel + row * 128;
+        unsigned char *to1 = to0 + ((at16 ^ 1) ^ (row & 7)) * 16;
+        to0 += (at16 ^ (row & 7)) * 16;
+        const unsigned char *from = raw + is_v * C::kRawStages * C::kRawBytes + lt * 16;
+        uint64_t *raw_full = bars.raw_full[is_v], *raw_empty = bars.raw_empty[is_v];
+        uint32_t n_half = 0;                                      // half tiles so far
         while (walk.next(p, w)) {
-            auto convert = [&](unsigned char *tile, const unsigned char *codes, int t, bool full) {
-                const float4 *entry = entries[n_tile % C::kEntryStages];
-#pragma unroll
-                for (int c = 0; c < C::kChunks; ++c) {
-                    uint4 x = *reinterpret_cast<const uint4 *>(codes + (lt + c * kLoadThreads) * 16);
-                    if (!full) {   // a token past the request's, or in a block that is not there, is zero
-                        const int r = row + c * kRowStep;
-                        if (t * C::kTile + r >= w.kv || __float_as_int(entry[r / 16].w) < 0) x = make_uint4(0, 0, 0, 0);
-                    }
-                    if (swap) x = make_uint4(x.z, x.w, x.x, x.y);
-                    uint4 y0, y1;
-                    codes_to_half<FORMAT>(x.x, y0.x, y0.y);
-                    codes_to_half<FORMAT>(x.y, y0.z, y0.w);
-                    codes_to_half<FORMAT>(x.z, y1.x, y1.y);
-                    codes_to_half<FORMAT>(x.w, y1.z, y1.w);
-                    *reinterpret_cast<uint4 *>(tile + place0 + c * kRowStep * 128) = y0;
-                    *reinterpret_cast<uint4 *>(tile + place1 + c * kRowStep * 128) = y1;
-                }
-            };
-            for (int t = w.t0; t < w.t1; ++t, ++n_tile) {
-                const int stage = n_tile % kStages;
-                const uint32_t empty = (n_tile / kStages & 1) ^ 1;
-                wait.warp(&bars.raw_full[0], n_tile & 1);
+            for (int t = w.t0; t < w.t1; ++t) {
+                const uint32_t n_tile = n_half / C::kHalves;
                 bool full = (t + 1) * C::kTile <= w.kv;
-                if (full) {
-                    int there = 0;
-                    if (lane < C::kBlocks) there = __float_as_int(entries[n_tile % C::kEntryStages][lane].w);
-                    full = __all_sync(~0u, there >= 0);
-                }
-                wait.warp(&bars.k_empty[stage], empty);
-                if (full) convert(k_smem + stage * C::kKvBytes, raw, t, true);
-                else convert(k_smem + stage * C::kKvBytes, raw, t, false);
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    bar_arrive(&bars.k_full[stage]);
-                    bar_arrive(&bars.raw_empty[0]);
-                }
-                wait.warp(&bars.raw_full[1], n_tile & 1);
-                wait.warp(&bars.v_empty[stage], empty);
-                if (full) convert(v_smem + stage * C::kKvBytes, raw + C::kRawBytes, t, true);
-                else convert(v_smem + stage * C::kKvBytes, raw + C::kRawBytes, t, false);
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    bar_arrive(&bars.v_full[stage]);
-                    bar_arrive(&bars.raw_empty[1]);
+#pragma unroll 1
+                for (int h = 0; h < C::kHalves; ++h, ++n_half) {
+                    const uint32_t raw_stage = n_half % C::kRawStages;
+                    wait.warp(&raw_full[raw_stage], n_half / C::kRawStages & 1);
+                    const float4 *entry = entries[n_tile % C::kEntryStages];
+                    if (h == 0 && full) full = __all_sync(~0u, __float_as_int(entry[lane % C::kBlocks].w) >= 0);
+                    int to;                                       // of the half tile, in bytes
+                    if (is_v) {
+                        wait.warp(&bars.v_empty[n_half % C::kVStages], (n_half / C::kVStages & 1) ^ 1);
+                        to = n_half % C::kVStages * C::kVBytes;
+                    } else {
+                        if (h == 0) wait.warp(&bars.k_empty[n_tile % C::kKStages], (n_tile / C::kKStages & 1) ^ 1);
+                        to = n_tile % C::kKStages * C::kKBytes + h * kHalf * 128;
+                    }
+                    uint4 x[C::kChunks];
+#pragma unroll
+                    for (int c = 0; c < C::kChunks; ++c)
+                        x[c] = *reinterpret_cast<const uint4 *>(from + raw_stage * C::kRawBytes + c * kLoadThreads * 16);
+                    if (!full) {   // a token past the request's, or in a block that is not there, is zero
+                        const int left = w.kv - t * C::kTile - h * kHalf;
+#pragma unroll
+                        for (int c = 0; c < C::kChunks; ++c) {
+                            const int r = row + c * kRowStep;
+                            if (r >= left || __float_as_int(entry[h * kHalfBlocks + r / 16].w) < 0) x[c] = make_uint4(0, 0, 0, 0);
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < C::kChunks; ++c) {
+                        if (swap) x[c] = make_uint4(x[c].z, x[c].w, x[c].x, x[c].y);
+                        uint4 y0, y1;
+                        codes_to_half<FORMAT>(x[c].x, y0.x, y0.y);
+                        codes_to_half<FORMAT>(x[c].y, y0.z, y0.w);
+                        codes_to_half<FORMAT>(x[c].z, y1.x, y1.y);
+                        codes_to_half<FORMAT>(x[c].w, y1.z, y1.w);
+                        *reinterpret_cast<uint4 *>(to0 + to + c * kRowStep * 128) = y0;
+                        *reinterpret_cast<uint4 *>(to1 + to + c * kRowStep * 128) = y1;
+                    }
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        bar_arrive(is_v ? &bars.v_full[n_half % C::kVStages] : &bars.k_full[n_tile % C::kKStages]);
+                        bar_arrive(&raw_empty[raw_stage]);
+                    }
                 }
             }
         }
       } else if (warp == kEntryWarp) {
-        // ------------------------------------------------ blocks and scales, kEntryTiles tiles at a time
+        // ------------------------------------------------ blocks and scales, C::kEntryTiles tiles at a time
         uint32_t n_tile = 0;
         while (walk.next(p, w)) {
             for (int t = w.t0; t < w.t1;) {
-                // up to the next multiple of kEntryTiles of the count, so that the stages stay together
+                // up to the next multiple of C::kEntryTiles of the count, so that the stages stay together
                 const int n = min(w.t1 - t, (int)(C::kEntryTiles - n_tile % C::kEntryTiles));
                 const int mine = lane / C::kBlocks, group = lane % C::kBlocks;
                 const uint32_t slot = (n_tile + mine) % C::kEntryStages;
@@ -667,8 +691,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 n_tile += n;
             }
         }
-      } else if (warp == kCopyWarp) {
-        // ------------------------------------------------ codes into shared memory, 16 tokens of a block per lane
+      } else if (warp >= kCopyWarp) {
+        // ------------------------------------------------ codes of K, of V into shared memory, 16 tokens of a block per lane
+        const bool is_v = warp > kCopyWarp;
+        const uint8_t *codes = is_v ? p.v : p.k;
         uint32_t n_tile = 0;
         const int in_block = (1 << p.log2_block) - 1;
         while (walk.next(p, w)) {
@@ -676,22 +702,24 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
                 int block = -1;
                 if (lane < C::kBlocks) block = __float_as_int(entries[n_tile % C::kEntryStages][lane].w);
-                const uint32_t bytes = __popc(__ballot_sync(~0u, block >= 0)) * 16 * D;
+                const unsigned there = __ballot_sync(~0u, block >= 0);
                 const int64_t from = (int64_t)block * p.stride_block + (int64_t)w.head * p.stride_head +
                                      (int64_t)((t * C::kTile + lane * 16) & in_block) * p.stride_token;
-#pragma unroll
-                for (int which = 0; which < 2; ++which) {
-                    wait.warp(&bars.raw_empty[which], (n_tile & 1) ^ 1);
-                    // the converting warps have read this tile before the copy engine writes it again
-                    if (lane == 0) bar_arrive_expect(&bars.raw_full[which], bytes);
+#pragma unroll 1
+                for (int h = 0; h < C::kHalves; ++h) {
+                    const uint32_t n = C::kHalves * n_tile + h, stage = n % C::kRawStages;
+                    uint64_t *full = &bars.raw_full[is_v][stage];
+                    wait.warp(&bars.raw_empty[is_v][stage], (n / C::kRawStages & 1) ^ 1);
+                    const unsigned mine = there >> h * kHalfBlocks & ((1u << kHalfBlocks) - 1);
+                    if (lane == 0) bar_arrive_expect(full, __popc(mine) * 16 * D);
                     __syncwarp();
-                    if (block >= 0) {
-                        const uint8_t *src = (which ? p.v : p.k) + from;
-                        const uint32_t dst = smem_u32(raw) + which * C::kRawBytes + lane * 16 * D;
+                    if (block >= 0 && lane / kHalfBlocks == h) {
+                        const uint8_t *src = codes + from;
+                        const uint32_t dst = smem_u32(raw) + (is_v * C::kRawStages + stage) * C::kRawBytes + lane % kHalfBlocks * 16 * D;
                         if (p.stride_token == D) {
-                            bulk_copy(dst, src, 16 * D, &bars.raw_full[which]);
+                            bulk_copy(dst, src, 16 * D, full);
                         } else {
-                            for (int r = 0; r < 16; ++r) bulk_copy(dst + r * D, src + r * p.stride_token, D, &bars.raw_full[which]);
+                            for (int r = 0; r < 16; ++r) bulk_copy(dst + r * D, src + r * p.stride_token, D, full);
                         }
                     }
                 }
@@ -702,67 +730,75 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         constexpr uint32_t s_instruction = instruction(128, C::kTile, false), o_instruction = instruction(128, D, true);
         const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
         const uint32_t leader = elect();
-        uint32_t n_tile = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-        auto scores = [&](int qt, uint32_t stage) {
-            uint32_t a = operand_lo(q_at + qt * C::kPanels * C::kQPanel, 16), b = operand_lo(k_at + stage * C::kKvBytes, 16);
+        uint32_t n_tile = 0, n_of[2] = {0, 0}, q_phase[2] = {0, 0};     // kv tiles: all, by query tile
+        bool split = false;
+        // scores of a query tile with the n-th kv tile of all
+        auto scores = [&](int qt, uint32_t buffer, uint32_t n) {
+            uint32_t a = operand_lo(q_at + qt * C::kPanels * C::kQPanel, 16), b = operand_lo(k_at + n % C::kKStages * C::kKBytes, 16);
 #pragma unroll 1
             for (int k = 0; k < D / 16; k += C::kSteps) {         // a panel's 64 columns
 #pragma unroll
                 for (int j = 0; j < C::kSteps; ++j)
-                    mma_ss(tmem + qt * C::kSColumns, operand(a + j * 2), operand(b + j * 2), s_instruction, k + j > 0, leader);
+                    mma_ss(tmem + buffer * C::kTile, operand(a + j * 2), operand(b + j * 2), s_instruction, k + j > 0, leader);
                 a += C::kQPanel / 16;
-                b += C::kKvPanel / 16;
+                b += C::kKPanel / 16;
             }
-            commit(&bars.s_full[qt], leader);
+            commit(&bars.s_full[buffer], leader);
         };
-        bool split = false;
         while (walk.next(p, w)) {
             if (w.t0 == 0 && w.t1 < w.tiles) {
                 // the part that begins a range which the next blocks go on with: for the joining kernel
                 split = true;
-                if (leader) {
+                if (leader)
                     p.splits[blockIdx.x] = {w.request, w.head, w.row_tile, w.row0, w.rows, (int)((w.unit0 + w.tiles - 1) / start.per)};
-                }
             }
             const int tiles = w.t1 - w.t0, n_q = C::kQTiles == 2 && w.rows - w.row_tile * C::kRows > 128 ? 2 : 1;
-            wait.warp(&bars.k_full[n_tile % kStages], n_tile / kStages & 1);
             for (int qt = 0; qt < n_q; ++qt) {
                 wait.warp(&bars.q_full[qt], q_phase[qt]);
                 q_phase[qt] ^= 1;
-                fence_after();
-                scores(qt, n_tile % kStages);
             }
-            commit(&bars.k_empty[n_tile % kStages], leader);
-            for (int t = 0; t < tiles; ++t, ++n_tile) {
-                const uint32_t stage = n_tile % kStages, next = (n_tile + 1) % kStages;
-                wait.warp(&bars.v_full[stage], n_tile / kStages & 1);
-                for (int qt = 0; qt < n_q; ++qt) {
-                    wait.warp(&bars.p_full[qt], p_phase[qt]);
-                    p_phase[qt] ^= 1;
-                    fence_after();
-                    // every softmax thread has read the tile's entries, and so have the copies long before
-                    if (qt == n_q - 1 && leader) bar_arrive(&bars.entry_empty[n_tile % C::kEntryStages]);
-                    uint32_t a = tmem + qt * C::kSColumns, b = operand_lo(v_at + stage * C::kKvBytes, C::kKvPanel);
+            constexpr int kAhead = C::kScoreBuffers;              // kv tiles that the scores are ahead
+            auto buffer_of = [&](int qt, int t) { return C::kQTiles == 2 ? qt : (n_of[0] + t) & 1; };
+            for (int t = 0; t < kAhead && t < tiles; ++t) {
+                wait.warp(&bars.k_full[(n_tile + t) % C::kKStages], (n_tile + t) / C::kKStages & 1);
+                fence_after();
+                for (int qt = 0; qt < n_q; ++qt) scores(qt, buffer_of(qt, t), n_tile + t);
+                commit(&bars.k_empty[(n_tile + t) % C::kKStages], leader);
+            }
+            // One query tile's products after the other's: while they run, the other is in its softmax.
+            for (int t = 0; t < tiles; ++t) {
 #pragma unroll 1
-                    for (int k = 0; k < C::kTile / 16; k += 4) {
+                for (int qt = 0; qt < n_q; ++qt) {
+                    const uint32_t buffer = buffer_of(qt, t), n = n_of[qt] + t;
+#pragma unroll 1
+                    for (int h = 0; h < C::kHalves; ++h) {
+                        const uint32_t v = C::kHalves * (n_tile + t) + h;   // half tile of V
+                        if (qt == 0) wait.warp(&bars.v_full[v % C::kVStages], v / C::kVStages & 1);
+                        wait.warp(&bars.p_full[qt][C::kHalves == 2 ? h : buffer], n / C::kScoreBuffers & 1);
+                        fence_after();
+                        const uint32_t a = tmem + buffer * C::kTile + h * kHalf, b = operand_lo(v_at + v % C::kVStages * C::kVBytes, C::kVPanel);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            mma_ts(tmem + C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, t > 0 || k + j > 0, leader);
-                        a += 4 * 8;
-                        b += 4 * 128;
+                        for (int j = 0; j < kHalf / 16; ++j)
+                            mma_ts(tmem + C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, t + h > 0 || j > 0, leader);
+                        commit(&bars.o_done[qt], leader);
+                        if (qt == n_q - 1) commit(&bars.v_empty[v % C::kVStages], leader);
                     }
                     if (t + 1 == tiles) commit(&bars.o_full[qt], leader);
-                    if (qt == n_q - 1) commit(&bars.v_empty[stage], leader);
-                    if (t + 1 < tiles) {
+                    // every softmax thread has read the tile's entries, and so have the copies long before
+                    if (qt == n_q - 1 && leader) bar_arrive(&bars.entry_empty[(n_tile + t) % C::kEntryStages]);
+                    if (t + kAhead < tiles) {
+                        const uint32_t ahead = n_tile + t + kAhead;
                         if (qt == 0) {
-                            wait.warp(&bars.k_full[next], (n_tile + 1) / kStages & 1);
+                            wait.warp(&bars.k_full[ahead % C::kKStages], ahead / C::kKStages & 1);
                             fence_after();
                         }
-                        scores(qt, next);
-                        if (qt == n_q - 1) commit(&bars.k_empty[next], leader);
+                        scores(qt, buffer, ahead);
+                        if (qt == n_q - 1) commit(&bars.k_empty[ahead % C::kKStages], leader);
                     }
                 }
             }
+            n_tile += tiles;
+            for (int qt = 0; qt < n_q; ++qt) n_of[qt] += tiles;
         }
         if (!split && leader) p.splits[blockIdx.x].rows = 0;
       }
