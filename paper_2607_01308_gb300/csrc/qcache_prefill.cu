@@ -20,7 +20,7 @@
 // fits beside the scores: kv tiles are 64 tokens, with scores two tiles ahead in two buffers. A second, small kernel joins
 // the ranges that were cut between thread blocks, over the whole GPU (one thread block alone took 95 us
 // for 256 rows in 19 parts). The softmax warps take
-// registers over from the others (144 and 64 of 96 at launch). Work is cut as in
+// registers over from the others (168 and 48 of 96 at launch). Work is cut as in
 // qcache_attention.cu, over kv tiles that the rows of a tile may see at all.
 #include "cm_qcache_kernels.h"
 
@@ -35,7 +35,7 @@ namespace {
 constexpr int kSoftmaxWarps = 8, kLoadWarps = 4;              // load warps: for K, and as many for V
 constexpr int kMmaWarp = kSoftmaxWarps + 2 * kLoadWarps, kEntryWarp = kMmaWarp + 1, kCopyWarp = kMmaWarp + 2;
 constexpr int kThreads = 20 * 32;           // whole warpgroups: registers change hands by warpgroup
-constexpr int kLaunchRegs = 96, kSoftmaxRegs = 144, kOtherRegs = 64;
+constexpr int kLaunchRegs = 96, kSoftmaxRegs = 168, kOtherRegs = 48;
 static_assert(256 * kSoftmaxRegs + (kThreads - 256) * kOtherRegs <= kThreads * kLaunchRegs, "registers at launch");
 constexpr int kLoadThreads = kLoadWarps * 32;
 constexpr float kRaise = 8.f, kHeadroom = 7.f;
@@ -151,25 +151,34 @@ __device__ __forceinline__ void commit(uint64_t *b, uint32_t leader) {
     "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7]), \
     "r"(x[i + 8]), "r"(x[i + 9]), "r"(x[i + 10]), "r"(x[i + 11]), "r"(x[i + 12]), "r"(x[i + 13]), "r"(x[i + 14]), "r"(x[i + 15])
 
-// 32 columns of the warp's 32 lanes, one row per thread; the values are there after ld_wait.
-__device__ __forceinline__ void tmem_ld32(uint32_t (&x)[32], uint32_t at) {
+#define CM_INOUT16(x, i) \
+    "+r"(x[i]), "+r"(x[i + 1]), "+r"(x[i + 2]), "+r"(x[i + 3]), "+r"(x[i + 4]), "+r"(x[i + 5]), "+r"(x[i + 6]), "+r"(x[i + 7]), \
+    "+r"(x[i + 8]), "+r"(x[i + 9]), "+r"(x[i + 10]), "+r"(x[i + 11]), "+r"(x[i + 12]), "+r"(x[i + 13]), "+r"(x[i + 14]), "+r"(x[i + 15])
+
+// Columns of the warp's 32 lanes, one row per thread; the values are there after ld_wait.
+__device__ __forceinline__ void tmem_ld(uint32_t (&x)[32], uint32_t at) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
                  : CM_REGS16(x, 0), CM_REGS16(x, 16) : "r"(at));
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t (&x)[16], uint32_t at) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                 : CM_REGS16(x, 0) : "r"(at));
+__device__ __forceinline__ void tmem_ld(uint32_t (&x)[8], uint32_t at) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]) : "r"(at));
 }
-__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void ld_wait(uint32_t (&x)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : CM_INOUT16(x, 0), CM_INOUT16(x, 16) :: "memory");
+}
+__device__ __forceinline__ void ld_wait(uint32_t (&x)[8]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]) :: "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&x)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
+}
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&x)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
                  ::"r"(at), CM_IN16(x, 0) : "memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&x)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-                 ::"r"(at), CM_IN16(x, 0), CM_IN16(x, 16) : "memory");
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -225,22 +234,29 @@ struct RowState {
     float top, sum, limit;
 };
 
-// Half a kv tile of one row: scores to weights, into its own columns as fp16. left: columns that the row sees
-// (only if `masked`, which is the warp's). Where the largest exponent of some row passes its limit, that row's
-// maximum is raised by as much, its sum and (behind `wait_output`) its output rescaled.
-template <int D, class Wait>
-__device__ __forceinline__ void softmax_half(uint32_t s_at, uint32_t o_at, const float4 *sc, float factor, bool masked, int left,
-                                             bool first, RowState &r, Wait wait_output) {
-    uint32_t x[kHalf / 32][32];
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float m;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+    return m;
+}
+
+// A kv tile of one row: scores to weights, as fp16 into the first 32 columns of each half, which `arrive` hands
+// over. left: columns that the row sees (only if `masked`, which is the warp's). Where the largest exponent of
+// some row passes its limit, that row's maximum is raised by as much, its sum and, unless this is the first tile
+// (behind `wait_output`), its output rescaled.
+template <int D, class Wait, class Arrive>
+__device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const float4 *sc, float factor, bool masked, int left,
+                                             bool first, RowState &r, Wait wait_output, Arrive arrive) {
+    using C = Shape<D>;
+    uint32_t x[C::kTile / 32][32];
 #pragma unroll
-    for (int c = 0; c < kHalf / 32; ++c) tmem_ld32(x[c], s_at + 32 * c);
-    ld_wait();
+    for (int c = 0; c < C::kTile / 32; ++c) tmem_ld(x[c], s_at + 32 * c);
+#pragma unroll
+    for (int c = 0; c < C::kTile / 32; ++c) ld_wait(x[c]);        // all of them; the others order their own registers
     const float base = kHeadroom - r.top;
-    float z_inverse[kHalfBlocks], high[kHalfBlocks];
 #pragma unroll
-    for (int b = 0; b < kHalfBlocks; ++b) {
+    for (int b = 0; b < C::kBlocks; ++b) {
         const float4 z = sc[b];
-        z_inverse[b] = z.z;
         const float a = factor * z.x, d = z.y + base;
         const uint64_t a2 = pair(a, a), d2 = pair(d, d);
         uint32_t *y = &x[b / 2][b % 2 * 16];
@@ -254,19 +270,17 @@ __device__ __forceinline__ void softmax_half(uint32_t s_at, uint32_t o_at, const
     }
     if (masked) {
 #pragma unroll
-        for (int k = 0; k < kHalf; ++k)
+        for (int k = 0; k < C::kTile; ++k)
             if (k >= left) x[k / 32][k % 32] = 0xff800000u;
     }
+    float most = -INFINITY;
 #pragma unroll
-    for (int b = 0; b < kHalfBlocks; ++b) {
-        const uint32_t *y = &x[b / 2][b % 2 * 16];
-        high[b] = __uint_as_float(y[0]);
+    for (int c = 0; c < C::kTile / 32; ++c) {
+        float high[2] = {__uint_as_float(x[c][0]), __uint_as_float(x[c][1])};
 #pragma unroll
-        for (int k = 1; k < 16; ++k) high[b] = fmaxf(high[b], __uint_as_float(y[k]));
+        for (int k = 2; k < 32; k += 2) high[k / 2 & 1] = max3(high[k / 2 & 1], __uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1]));
+        most = max3(most, high[0], high[1]);
     }
-    float most = high[0];
-#pragma unroll
-    for (int b = 1; b < kHalfBlocks; ++b) most = fmaxf(most, high[b]);
     if (__any_sync(~0u, most > r.limit)) {
         const bool raise = most > r.limit;
         const float by = raise ? most - kHeadroom : 0.f;
@@ -275,38 +289,44 @@ __device__ __forceinline__ void softmax_half(uint32_t s_at, uint32_t o_at, const
         r.sum *= f;
         if (raise) r.limit = kRaise + kHeadroom;
 #pragma unroll
-        for (int k = 0; k < kHalf; ++k) x[k / 32][k % 32] = __float_as_uint(__uint_as_float(x[k / 32][k % 32]) - by);
+        for (int k = 0; k < C::kTile; ++k) x[k / 32][k % 32] = __float_as_uint(__uint_as_float(x[k / 32][k % 32]) - by);
         if (!first) {
             wait_output();
             fence_after();
 #pragma unroll 1
-            for (int c = 0; c < D / 16; ++c) {
-                uint32_t y[16];
-                tmem_ld16(y, o_at + 16 * c);
-                ld_wait();
+            for (int c = 0; c < D / 8; ++c) {
+                uint32_t y[8];
+                tmem_ld(y, o_at + 8 * c);
+                ld_wait(y);
 #pragma unroll
-                for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
-                tmem_st16(o_at + 16 * c, y);
+                for (int k = 0; k < 8; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
+                tmem_st8(o_at + 8 * c, y);
             }
         }
     }
-    uint32_t w[kHalf / 2];
 #pragma unroll
-    for (int b = 0; b < kHalfBlocks; ++b) {
-        const uint32_t *y = &x[b / 2][b % 2 * 16];
-        uint64_t part = 0;
+    for (int h = 0; h < C::kHalves; ++h) {
 #pragma unroll
-        for (int k = 0; k < 16; k += 2) {
-            const float e0 = exp2_fast(__uint_as_float(y[k])), e1 = exp2_fast(__uint_as_float(y[k + 1]));
-            part = add2(part, pair(e0, e1));
-            w[8 * b + k / 2] = pack_half(e0, e1);
+        for (int c = 2 * h; c < 2 * h + 2; ++c) {
+            uint32_t w[16];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                uint64_t part = 0;
+#pragma unroll
+                for (int k = 16 * b; k < 16 * b + 16; k += 2) {
+                    const float e0 = exp2_fast(__uint_as_float(x[c][k])), e1 = exp2_fast(__uint_as_float(x[c][k + 1]));
+                    part = add2(part, pair(e0, e1));
+                    w[k / 2] = pack_half(e0, e1);
+                }
+                float p0, p1;
+                unpair(part, p0, p1);
+                r.sum = fmaf(p0 + p1, sc[2 * c + b].z, r.sum);
+            }
+            tmem_st16(s_at + h * kHalf + c % 2 * 16, w);
         }
-        float p0, p1;
-        unpair(part, p0, p1);
-        r.sum = fmaf(p0 + p1, z_inverse[b], r.sum);
+        st_wait();
+        arrive(h);
     }
-    tmem_st32(s_at, w);
-    st_wait();
 }
 
 // The warp's 32 query rows, rows first .. first + 31 of the request, to fp16 with a power of two per row,
@@ -555,17 +575,14 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
                 wait.warp(&bars.s_full[buffer], phase);
                 fence_after();
-#pragma unroll 1
-                for (int h = 0; h < C::kHalves; ++h) {
-                    const int token = t * C::kTile + h * kHalf;
-                    // the product before: half h ^ 1 of this tile or the one before; or the tile before
-                    const uint32_t before = C::kHalves == 2 ? h ^ 1 : (n_mine & 1) ^ 1;
-                    softmax_half<D>(s_at + buffer * C::kTile + h * kHalf, o_at, entries[n_tile % C::kEntryStages] + h * kHalfBlocks, factor,
-                                    token + kHalf > least, limit - token, t == w.t0 && h == 0, r,
-                                    [&] { wait.warp(&bars.o_done[qt], before); });
-                    fence_before();
-                    bar_arrive(&bars.p_full[qt][C::kHalves == 2 ? h : buffer]);
-                }
+                // the product before: the second half of the tile before, which the scores came after; or that tile
+                const uint32_t before = C::kHalves == 2 ? 1 : (n_mine & 1) ^ 1;
+                softmax_tile<D>(s_at + buffer * C::kTile, o_at, entries[n_tile % C::kEntryStages], factor, (t + 1) * C::kTile > least,
+                                limit - t * C::kTile, t == w.t0, r, [&] { wait.warp(&bars.o_done[qt], before); },
+                                [&](int h) {
+                                    fence_before();
+                                    bar_arrive(&bars.p_full[qt][C::kHalves == 2 ? h : buffer]);
+                                });
             }
             const float top = r.top, sum = r.sum;
             wait.warp(&bars.o_full[qt], o_phase);
@@ -581,8 +598,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t x[32];
                 __syncwarp();
-                tmem_ld32(x, o_at + 32 * c);
-                ld_wait();
+                tmem_ld(x, o_at + 32 * c);
+                ld_wait(x);
                 if (valid && whole) {
 #pragma unroll
                     for (int k = 0; k < 32; k += 8) {
