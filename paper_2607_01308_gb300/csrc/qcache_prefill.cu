@@ -20,7 +20,7 @@
 // fits beside the scores: kv tiles are 64 tokens, with scores two tiles ahead in two buffers. A second, small kernel joins
 // the ranges that were cut between thread blocks, over the whole GPU (one thread block alone took 95 us
 // for 256 rows in 19 parts). The softmax warps take
-// registers over from the others (168 and 48 of 96 at launch). Work is cut as in
+// registers over from the others (168 of 96 at launch). Work is cut as in
 // qcache_attention.cu, over kv tiles that the rows of a tile may see at all.
 #include "cm_qcache_kernels.h"
 
@@ -35,8 +35,8 @@ namespace {
 constexpr int kSoftmaxWarps = 8, kLoadWarps = 4;              // load warps: for K, and as many for V
 constexpr int kMmaWarp = kSoftmaxWarps + 2 * kLoadWarps, kEntryWarp = kMmaWarp + 1, kCopyWarp = kMmaWarp + 2;
 constexpr int kThreads = 20 * 32;           // whole warpgroups: registers change hands by warpgroup
-constexpr int kLaunchRegs = 96, kSoftmaxRegs = 168, kOtherRegs = 48;
-static_assert(256 * kSoftmaxRegs + (kThreads - 256) * kOtherRegs <= kThreads * kLaunchRegs, "registers at launch");
+constexpr int kLaunchRegs = 96, kSoftmaxRegs = 168, kLoadRegs = 48, kIssueRegs = 48;
+static_assert(256 * kSoftmaxRegs + 256 * kLoadRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs, "registers at launch");
 constexpr int kLoadThreads = kLoadWarps * 32;
 constexpr float kRaise = 8.f, kHeadroom = 7.f;
 
@@ -54,7 +54,6 @@ struct Shape {
     static constexpr int kRows = 128 * kQTiles;
     static constexpr int kOColumn = 2 * kTile;
     static constexpr int kPanels = D < 64 ? 1 : D / 64;       // 64 columns (128 bytes) of fp16 each
-    static constexpr int kSteps = D < 64 ? D / 16 : 4;        // 16 columns each, of a panel
     static constexpr int kKStages = 2;                        // tiles of K
     static constexpr int kVStages = 2 * kHalves;              // half tiles of V
     static constexpr int kRawStages = D == 256 ? 1 : 2;       // half tiles of codes, of K and of V
@@ -63,7 +62,7 @@ struct Shape {
     static constexpr int kKBytes = kPanels * kKPanel, kVBytes = kPanels * kVPanel;   // a tile of K, half a tile of V
     static constexpr int kChunks = kHalf * D / 16 / kLoadThreads;   // 16-code chunks of a thread in half a tile
     static constexpr int kRawBytes = kHalf * D;
-    static constexpr size_t kSmem = 1024 + kQBytes + kKStages * kKBytes + kVStages * kVBytes + 2 * kRawStages * kRawBytes;
+    static constexpr size_t kSmem = kQBytes + kKStages * kKBytes + kVStages * kVBytes + 2 * kRawStages * kRawBytes;
     static_assert(kChunks >= 1, "every load thread has work");
     static_assert(kOColumn + kQTiles * D <= 512, "tensor memory");
 };
@@ -382,40 +381,73 @@ __device__ __forceinline__ int visible_tiles(const QcacheAttentionParams &p, con
     return max(1, (limit + TILE - 1) / TILE);
 }
 
-// Where a block's share begins, and the walk through it that every role makes for itself.
-template <int ROWS, int TILE>
-struct Walk {
-    RequestShape s;
-    int request, row_tile, head, tile, tiles;
-    uint64_t u, end;              // units: the next one, and the share's end
-
-    __device__ __forceinline__ bool next(const QcacheAttentionParams &p, AttentionSegment &w) {
-        if (u >= end) return false;
-        if (tile == tiles) {
-            tile = 0;
-            if (++head == p.heads) {
-                head = 0;
-                if (++row_tile == s.row_tiles) {
-                    row_tile = 0;
-                    do s = request_shape<ROWS, TILE>(p, ++request); while (s.row_tiles == 0);
-                }
-                tiles = visible_tiles<ROWS, TILE>(p, s, row_tile);
-            }
-        }
-        const int n = (int)min((uint64_t)(tiles - tile), end - u);
-        w.request = request; w.head = head; w.row_tile = row_tile;
-        w.t0 = tile; w.t1 = tile + n;
-        w.row0 = s.row0; w.q_len = s.q_len; w.kv = s.kv; w.rows = s.rows; w.tiles = tiles;
-        w.unit0 = u - tile;
-        tile += n;
-        u += n;
-        return true;
-    }
-};
-
 struct Start {
     uint64_t u, end, per;
     int request, row_tile, head, tile;
+};
+
+// The walk through a block's share, and the segment that it is at: each warp makes it for itself, in
+// shared memory, so that neither takes registers from the loops.
+template <int ROWS, int TILE>
+struct Walk {
+    AttentionSegment w;
+    int left;                     // units of the share behind w
+    bool more;
+
+    __device__ void begin(const QcacheAttentionParams &p, const Start &start) {
+        left = (int)(start.end > start.u ? start.end - start.u : 0);
+        if (left == 0) return;
+        w.request = start.request; w.head = start.head; w.row_tile = start.row_tile;
+        w.t1 = start.tile;        // an empty segment in front of the first
+        w.unit0 = start.u - start.tile;
+        request(p);
+    }
+
+    __device__ __forceinline__ void request(const QcacheAttentionParams &p) {
+        const RequestShape s = request_shape<ROWS, TILE>(p, w.request);
+        w.row0 = s.row0; w.q_len = s.q_len; w.kv = s.kv; w.rows = s.rows;
+        w.tiles = visible_tiles<ROWS, TILE>(p, s, w.row_tile);
+    }
+
+    // The next segment into w, for the whole warp; false at the end.
+    __device__ __forceinline__ bool next(const QcacheAttentionParams &p) {
+        __syncwarp();
+        if (threadIdx.x % 32 == 0) {
+            more = left > 0;
+            if (more) {
+                if (w.t1 == w.tiles) {
+                    w.unit0 += w.tiles;
+                    w.t1 = 0;
+                    if (++w.head == p.heads) {
+                        w.head = 0;
+                        if (++w.row_tile * ROWS >= w.rows) {
+                            w.row_tile = 0;
+                            do ++w.request, request(p); while (w.rows == 0);
+                        } else {
+                            request(p);
+                        }
+                    }
+                }
+                w.t0 = w.t1;
+                w.t1 = min(w.tiles, w.t0 + left);
+                left -= w.t1 - w.t0;
+            }
+        }
+        __syncwarp();
+        return more;
+    }
+};
+
+// The parity of each of a few stages' barriers, flipped at every use. Stages are counted from the first tile
+// of a segment: a loop whose counter starts at a constant keeps its addresses in uniform registers, which the
+// tensor instructions want.
+struct Parity {
+    uint32_t bits = 0;
+    __device__ __forceinline__ uint32_t use(uint32_t stage) {
+        const uint32_t p = bits >> stage & 1;
+        bits ^= 1u << stage;
+        return p;
+    }
 };
 
 struct Barriers {
@@ -431,14 +463,14 @@ struct Barriers {
 template <int D, int FORMAT>
 __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_constant__ QcacheAttentionParams p) {
     using C = Shape<D>;
-    extern __shared__ unsigned char smem_raw[];
+    extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ Barriers bars;
     __shared__ float4 entries[C::kEntryStages][C::kBlocks];   // k_scale, log2 v_scale, 1 / v_scale, block of 16 tokens each
     __shared__ uint32_t scan[kThreads / 32];
     __shared__ Start start;
+    __shared__ Walk<C::kRows, C::kTile> walks[kThreads / 32];
     __shared__ uint32_t tmem_base;
     __shared__ int failed;
-    unsigned char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + C::kKStages * C::kKBytes;
     unsigned char *raw = v_smem + C::kVStages * C::kVBytes;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -532,16 +564,12 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     __syncthreads();
     fence_after();
     const Waiter wait{&failed, p.error};
-    const uint32_t tmem = tmem_base;
-    Walk<C::kRows, C::kTile> walk;
-    walk.u = start.u;
-    walk.end = start.end;
-    if (walk.u < walk.end) {
-        walk.request = start.request; walk.row_tile = start.row_tile; walk.head = start.head; walk.tile = start.tile;
-        walk.s = request_shape<C::kRows, C::kTile>(p, walk.request);
-        walk.tiles = visible_tiles<C::kRows, C::kTile>(p, walk.s, walk.row_tile);
-    }
-    AttentionSegment w;
+    // all 512 columns: they begin at 0, which is what the addresses below take them to do
+    if (tmem_base != 0 && tid == 0) atomicOr(p.error, 1u);
+    constexpr uint32_t tmem = 0;
+    Walk<C::kRows, C::kTile> &walk = walks[warp];
+    const AttentionSegment &w = walk.w;
+    if (lane == 0) walk.begin(p, start);
 
     if (warp < kSoftmaxWarps) {
         // ------------------------------------------------ softmax: one row per thread
@@ -551,7 +579,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         const uint32_t s_at = tmem + lanes, o_at = tmem + lanes + C::kOColumn + qt * D;
         uint32_t n_tile = 0;          // kv tiles of the block so far
         uint32_t n_mine = 0, o_phase = 0;       // those with rows in this query tile
-        while (walk.next(p, w)) {
+        Parity scored;
+        while (walk.next(p)) {
             const int first = w.row_tile * C::kRows + qt * 128;   // of the tile, among the request's rows
             if (first >= w.rows || qt >= C::kQTiles) {
                 n_tile += w.t1 - w.t0;
@@ -569,16 +598,17 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             const int limit = !valid ? INT32_MAX : p.causal ? min(w.kv, max(0, w.kv - w.q_len + (int)(token - w.row0) + 1)) : w.kv;
             const int least = __reduce_min_sync(~0u, limit);      // of the warp's rows
             RowState r{0.f, 0.f, -INFINITY};
-            for (int t = w.t0; t < w.t1; ++t, ++n_tile, ++n_mine) {
+            const int t0 = w.t0, t1 = w.t1;
+            for (int t = t0; t < t1; ++t, ++n_tile, ++n_mine) {
                 // one buffer for each query tile, or two that take turns
-                const uint32_t buffer = C::kQTiles == 2 ? qt : n_mine & 1, phase = n_mine / C::kScoreBuffers & 1;
+                const uint32_t buffer = C::kQTiles == 2 ? qt : (t - t0) & 1;
                 wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
-                wait.warp(&bars.s_full[buffer], phase);
+                wait.warp(&bars.s_full[buffer], scored.use(buffer));
                 fence_after();
                 // the product before: the second half of the tile before, which the scores came after; or that tile
                 const uint32_t before = C::kHalves == 2 ? 1 : (n_mine & 1) ^ 1;
                 softmax_tile<D>(s_at + buffer * C::kTile, o_at, entries[n_tile % C::kEntryStages], factor, (t + 1) * C::kTile > least,
-                                limit - t * C::kTile, t == w.t0, r, [&] { wait.warp(&bars.o_done[qt], before); },
+                                limit - t * C::kTile, t == t0, r, [&] { wait.warp(&bars.o_done[qt], before); },
                                 [&](int h) {
                                     fence_before();
                                     bar_arrive(&bars.p_full[qt][C::kHalves == 2 ? h : buffer]);
@@ -618,9 +648,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             if (valid && whole && p.lse) p.lse[token * ((int64_t)p.heads * p.group) + head] = log_sum(top, sum, kHeadroom);
             if (valid && !whole) __stcg(reinterpret_cast<float2 *>(p.part_ml + (part + row) * 2), make_float2(sum == 0.f ? -INFINITY : top, sum));
         }
-    } else {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-      if (warp < kMmaWarp) {
+    } else if (warp < kMmaWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
         // ------------------------------------------------ K (the first four warps) and V tiles to fp16
         const bool is_v = warp >= kSoftmaxWarps + kLoadWarps;
         const int lt = tid % kLoadThreads;
@@ -635,25 +664,26 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         to0 += (at16 ^ (row & 7)) * 16;
         const unsigned char *from = raw + is_v * C::kRawStages * C::kRawBytes + lt * 16;
         uint64_t *raw_full = bars.raw_full[is_v], *raw_empty = bars.raw_empty[is_v];
-        uint32_t n_half = 0;                                      // half tiles so far
-        while (walk.next(p, w)) {
-            for (int t = w.t0; t < w.t1; ++t) {
-                const uint32_t n_tile = n_half / C::kHalves;
+        uint32_t n_tile = 0;
+        Parity filled, freed;
+        while (walk.next(p)) {
+            const int tiles = w.t1 - w.t0;
+            for (int i = 0; i < tiles; ++i, ++n_tile) {
+                const int t = w.t0 + i;
                 bool full = (t + 1) * C::kTile <= w.kv;
+                const float4 *entry = entries[n_tile % C::kEntryStages];
 #pragma unroll 1
-                for (int h = 0; h < C::kHalves; ++h, ++n_half) {
-                    const uint32_t raw_stage = n_half % C::kRawStages;
-                    wait.warp(&raw_full[raw_stage], n_half / C::kRawStages & 1);
-                    const float4 *entry = entries[n_tile % C::kEntryStages];
+                for (int h = 0; h < C::kHalves; ++h) {
+                    const uint32_t raw_stage = h % C::kRawStages;
+                    wait.warp(&raw_full[raw_stage], filled.use(raw_stage));
                     if (h == 0 && full) full = __all_sync(~0u, __float_as_int(entry[lane % C::kBlocks].w) >= 0);
-                    int to;                                       // of the half tile, in bytes
+                    uint32_t stage = i % C::kKStages;             // of K: a tile; of V: a half
+                    int to = stage * C::kKBytes + h * kHalf * 128;
                     if (is_v) {
-                        wait.warp(&bars.v_empty[n_half % C::kVStages], (n_half / C::kVStages & 1) ^ 1);
-                        to = n_half % C::kVStages * C::kVBytes;
-                    } else {
-                        if (h == 0) wait.warp(&bars.k_empty[n_tile % C::kKStages], (n_tile / C::kKStages & 1) ^ 1);
-                        to = n_tile % C::kKStages * C::kKBytes + h * kHalf * 128;
+                        stage = (i * C::kHalves + h) % C::kVStages;
+                        to = stage * C::kVBytes;
                     }
+                    if (is_v || h == 0) wait.warp(is_v ? &bars.v_empty[stage] : &bars.k_empty[stage], freed.use(stage) ^ 1);
                     uint4 x[C::kChunks];
 #pragma unroll
                     for (int c = 0; c < C::kChunks; ++c)
@@ -680,16 +710,18 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        bar_arrive(is_v ? &bars.v_full[n_half % C::kVStages] : &bars.k_full[n_tile % C::kKStages]);
+                        bar_arrive(is_v ? &bars.v_full[stage] : &bars.k_full[stage]);
                         bar_arrive(&raw_empty[raw_stage]);
                     }
                 }
             }
         }
-      } else if (warp == kEntryWarp) {
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
+      if (warp == kEntryWarp) {
         // ------------------------------------------------ blocks and scales, C::kEntryTiles tiles at a time
         uint32_t n_tile = 0;
-        while (walk.next(p, w)) {
+        while (walk.next(p)) {
             for (int t = w.t0; t < w.t1;) {
                 // up to the next multiple of C::kEntryTiles of the count, so that the stages stay together
                 const int n = min(w.t1 - t, (int)(C::kEntryTiles - n_tile % C::kEntryTiles));
@@ -713,8 +745,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         const bool is_v = warp > kCopyWarp;
         const uint8_t *codes = is_v ? p.v : p.k;
         uint32_t n_tile = 0;
+        Parity emptied;
         const int in_block = (1 << p.log2_block) - 1;
-        while (walk.next(p, w)) {
+        while (walk.next(p)) {
             for (int t = w.t0; t < w.t1; ++t, ++n_tile) {
                 wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
                 int block = -1;
@@ -724,9 +757,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                                      (int64_t)((t * C::kTile + lane * 16) & in_block) * p.stride_token;
 #pragma unroll 1
                 for (int h = 0; h < C::kHalves; ++h) {
-                    const uint32_t n = C::kHalves * n_tile + h, stage = n % C::kRawStages;
+                    const uint32_t stage = h % C::kRawStages;
                     uint64_t *full = &bars.raw_full[is_v][stage];
-                    wait.warp(&bars.raw_empty[is_v][stage], (n / C::kRawStages & 1) ^ 1);
+                    wait.warp(&bars.raw_empty[is_v][stage], emptied.use(stage) ^ 1);
                     const unsigned mine = there >> h * kHalfBlocks & ((1u << kHalfBlocks) - 1);
                     if (lane == 0) bar_arrive_expect(full, __popc(mine) * 16 * D);
                     __syncwarp();
@@ -747,75 +780,70 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         constexpr uint32_t s_instruction = instruction(128, C::kTile, false), o_instruction = instruction(128, D, true);
         const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
         const uint32_t leader = elect();
-        uint32_t n_tile = 0, n_of[2] = {0, 0}, q_phase[2] = {0, 0};     // kv tiles: all, by query tile
+        uint32_t n_tile = 0, segment = 0, second = 0;            // second: segments with rows in the second query tile
+        Parity k_full, v_full, weighted[2];
         bool split = false;
-        // scores of a query tile with the n-th kv tile of all
-        auto scores = [&](int qt, uint32_t buffer, uint32_t n) {
-            uint32_t a = operand_lo(q_at + qt * C::kPanels * C::kQPanel, 16), b = operand_lo(k_at + n % C::kKStages * C::kKBytes, 16);
-#pragma unroll 1
-            for (int k = 0; k < D / 16; k += C::kSteps) {         // a panel's 64 columns
+        // scores of a query tile with the K tile in `stage`
+        auto scores = [&](int qt, uint32_t buffer, uint32_t stage) {
+            const uint32_t a = operand_lo(q_at + qt * C::kPanels * C::kQPanel, 16), b = operand_lo(k_at + stage * C::kKBytes, 16);
 #pragma unroll
-                for (int j = 0; j < C::kSteps; ++j)
-                    mma_ss(tmem + buffer * C::kTile, operand(a + j * 2), operand(b + j * 2), s_instruction, k + j > 0, leader);
-                a += C::kQPanel / 16;
-                b += C::kKPanel / 16;
-            }
+            for (int k = 0; k < D / 16; ++k)
+                mma_ss(buffer * C::kTile, operand(a + k / 4 * (C::kQPanel / 16) + k % 4 * 2), operand(b + k / 4 * (C::kKPanel / 16) + k % 4 * 2),
+                       s_instruction, k > 0, leader);
             commit(&bars.s_full[buffer], leader);
         };
-        while (walk.next(p, w)) {
+        while (__any_sync(~0u, walk.next(p))) {
             if (w.t0 == 0 && w.t1 < w.tiles) {
                 // the part that begins a range which the next blocks go on with: for the joining kernel
                 split = true;
                 if (leader)
                     p.splits[blockIdx.x] = {w.request, w.head, w.row_tile, w.row0, w.rows, (int)((w.unit0 + w.tiles - 1) / start.per)};
             }
-            const int tiles = w.t1 - w.t0, n_q = C::kQTiles == 2 && w.rows - w.row_tile * C::kRows > 128 ? 2 : 1;
-            for (int qt = 0; qt < n_q; ++qt) {
-                wait.warp(&bars.q_full[qt], q_phase[qt]);
-                q_phase[qt] ^= 1;
-            }
+            // votes, so that the branches are uniform
+            const int tiles = w.t1 - w.t0;
+            const bool both = C::kQTiles == 2 && __any_sync(~0u, w.rows - w.row_tile * C::kRows > 128);
+            wait.warp(&bars.q_full[0], segment++ & 1);
+            if (both) wait.warp(&bars.q_full[1], second++ & 1);
             constexpr int kAhead = C::kScoreBuffers;              // kv tiles that the scores are ahead
-            auto buffer_of = [&](int qt, int t) { return C::kQTiles == 2 ? qt : (n_of[0] + t) & 1; };
-            for (int t = 0; t < kAhead && t < tiles; ++t) {
-                wait.warp(&bars.k_full[(n_tile + t) % C::kKStages], (n_tile + t) / C::kKStages & 1);
-                fence_after();
-                for (int qt = 0; qt < n_q; ++qt) scores(qt, buffer_of(qt, t), n_tile + t);
-                commit(&bars.k_empty[(n_tile + t) % C::kKStages], leader);
-            }
             // One query tile's products after the other's: while they run, the other is in its softmax.
-            for (int t = 0; t < tiles; ++t) {
-#pragma unroll 1
-                for (int qt = 0; qt < n_q; ++qt) {
-                    const uint32_t buffer = buffer_of(qt, t), n = n_of[qt] + t;
-#pragma unroll 1
-                    for (int h = 0; h < C::kHalves; ++h) {
-                        const uint32_t v = C::kHalves * (n_tile + t) + h;   // half tile of V
-                        if (qt == 0) wait.warp(&bars.v_full[v % C::kVStages], v / C::kVStages & 1);
-                        wait.warp(&bars.p_full[qt][C::kHalves == 2 ? h : buffer], n / C::kScoreBuffers & 1);
-                        fence_after();
-                        const uint32_t a = tmem + buffer * C::kTile + h * kHalf, b = operand_lo(v_at + v % C::kVStages * C::kVBytes, C::kVPanel);
+            for (int i = -kAhead; __any_sync(~0u, i < tiles); ++i) {
 #pragma unroll
-                        for (int j = 0; j < kHalf / 16; ++j)
-                            mma_ts(tmem + C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, t + h > 0 || j > 0, leader);
-                        commit(&bars.o_done[qt], leader);
-                        if (qt == n_q - 1) commit(&bars.v_empty[v % C::kVStages], leader);
+                for (int qt = 0; qt < C::kQTiles; ++qt) {
+                    if (qt == 1 && !both) break;
+                    const bool last = qt == 1 || !both;           // that reads this K and V
+                    const uint32_t buffer = C::kQTiles == 2 ? qt : i & 1;
+                    if (i >= 0) {
+#pragma unroll
+                        for (int h = 0; h < C::kHalves; ++h) {
+                            const uint32_t v = (i * C::kHalves + h) % C::kVStages, q = C::kHalves == 2 ? h : buffer;
+                            if (qt == 0) wait.warp(&bars.v_full[v], v_full.use(v));
+                            wait.warp(&bars.p_full[qt][q], weighted[qt].use(q));
+                            fence_after();
+                            const uint32_t a = buffer * C::kTile + h * kHalf, b = operand_lo(v_at + v * C::kVBytes, C::kVPanel);
+#pragma unroll
+                            for (int j = 0; j < kHalf / 16; ++j)
+                                mma_ts(C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, j + h > 0 || i > 0, leader);
+                            commit(&bars.o_done[qt], leader);
+                            if (last) commit(&bars.v_empty[v], leader);
+                        }
+                        if (__any_sync(~0u, i + 1 == tiles)) commit(&bars.o_full[qt], leader);
+                        // every softmax thread has read the tile's entries, and so have the copies long before
+                        if (last) {
+                            if (leader) bar_arrive(&bars.entry_empty[n_tile % C::kEntryStages]);
+                            ++n_tile;
+                        }
                     }
-                    if (t + 1 == tiles) commit(&bars.o_full[qt], leader);
-                    // every softmax thread has read the tile's entries, and so have the copies long before
-                    if (qt == n_q - 1 && leader) bar_arrive(&bars.entry_empty[(n_tile + t) % C::kEntryStages]);
-                    if (t + kAhead < tiles) {
-                        const uint32_t ahead = n_tile + t + kAhead;
+                    if (__any_sync(~0u, i + kAhead < tiles)) {
+                        const uint32_t k = (i + kAhead) % C::kKStages;
                         if (qt == 0) {
-                            wait.warp(&bars.k_full[ahead % C::kKStages], ahead / C::kKStages & 1);
+                            wait.warp(&bars.k_full[k], k_full.use(k));
                             fence_after();
                         }
-                        scores(qt, buffer, ahead);
-                        if (qt == n_q - 1) commit(&bars.k_empty[ahead % C::kKStages], leader);
+                        scores(qt, C::kQTiles == 2 ? qt : k, k);
+                        if (last) commit(&bars.k_empty[k], leader);
                     }
                 }
             }
-            n_tile += tiles;
-            for (int qt = 0; qt < n_q; ++qt) n_of[qt] += tiles;
         }
         if (!split && leader) p.splits[blockIdx.x].rows = 0;
       }
