@@ -8,19 +8,19 @@
 //   warps 0-3, 4-7   softmax of query tile 0 and 1, one row per thread: half a kv tile (64 scores) from
 //                    tensor memory into registers, weights back into the same columns as fp16, the output
 //                    rescaled when the running maximum is raised, the row normalised and written
-//   warps 8-11       K tiles from codes to fp16, shared memory to shared memory, into the 128-byte swizzle
+//   warps 8-11       K tiles, from global memory through registers to fp16 in shared memory, in the 128-byte
+//                    swizzle, the next half tile's codes on their way meanwhile
 //   warps 12-15      V tiles
 //   warp 16          issues the matrix instructions: S = Q K^T (both operands from shared memory),
 //                    O += P V (P from tensor memory, V as it lies, tokens x head_dim)
 //   warp 17          looks up blocks and scales of every 16 tokens, several tiles ahead
-//   warps 18, 19     bulk copies of the codes of K, of V, half a tile or two ahead
 // Scores are products of 128 x 128 (64 columns at a time cost the tensor cores as much as 128); weights
 // go in by halves, so that the second half's softmax runs beside the first half's product, and one query
 // tile's softmax beside the other's products. At head_dim 256 the output of one query tile is all that
 // fits beside the scores: kv tiles are 64 tokens, with scores two tiles ahead in two buffers. A second, small kernel joins
 // the ranges that were cut between thread blocks, over the whole GPU (one thread block alone took 95 us
 // for 256 rows in 19 parts). The softmax warps take
-// registers over from the others (168 of 96 at launch). Work is cut as in
+// registers over from the others. Work is cut as in
 // qcache_attention.cu, over kv tiles that the rows of a tile may see at all.
 #include "cm_qcache_kernels.h"
 
@@ -33,10 +33,9 @@ namespace cm {
 namespace {
 
 constexpr int kSoftmaxWarps = 8, kLoadWarps = 4;              // load warps: for K, and as many for V
-constexpr int kMmaWarp = kSoftmaxWarps + 2 * kLoadWarps, kEntryWarp = kMmaWarp + 1, kCopyWarp = kMmaWarp + 2;
+constexpr int kMmaWarp = kSoftmaxWarps + 2 * kLoadWarps, kEntryWarp = kMmaWarp + 1;
 constexpr int kThreads = 20 * 32;           // whole warpgroups: registers change hands by warpgroup
-constexpr int kLaunchRegs = 96, kSoftmaxRegs = 168, kLoadRegs = 48, kIssueRegs = 48;
-static_assert(256 * kSoftmaxRegs + 256 * kLoadRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs, "registers at launch");
+constexpr int kLaunchRegs = 96;
 constexpr int kLoadThreads = kLoadWarps * 32;
 constexpr float kRaise = 8.f, kHeadroom = 7.f;
 
@@ -54,15 +53,15 @@ struct Shape {
     static constexpr int kRows = 128 * kQTiles;
     static constexpr int kOColumn = 2 * kTile;
     static constexpr int kPanels = D < 64 ? 1 : D / 64;       // 64 columns (128 bytes) of fp16 each
-    static constexpr int kKStages = 2;                        // tiles of K
-    static constexpr int kVStages = 2 * kHalves;              // half tiles of V
-    static constexpr int kRawStages = D == 256 ? 1 : 2;       // half tiles of codes, of K and of V
-    static constexpr int kQPanel = 128 * 128, kKPanel = kTile * 128, kVPanel = kHalf * 128;   // bytes
+    static constexpr int kStages = 2;                         // tiles of K, of V
+    static constexpr int kQPanel = 128 * 128, kKvPanel = kTile * 128;   // bytes
     static constexpr int kQBytes = kQTiles * kPanels * kQPanel;
-    static constexpr int kKBytes = kPanels * kKPanel, kVBytes = kPanels * kVPanel;   // a tile of K, half a tile of V
-    static constexpr int kChunks = kHalf * D / 16 / kLoadThreads;   // 16-code chunks of a thread in half a tile
-    static constexpr int kRawBytes = kHalf * D;
-    static constexpr size_t kSmem = kQBytes + kKStages * kKBytes + kVStages * kVBytes + 2 * kRawStages * kRawBytes;
+    static constexpr int kKvBytes = kPanels * kKvPanel;       // a tile of K, of V
+    static constexpr int kChunks = kHalf * D / 16 / kLoadThreads;   // 16-code loads of a thread for half a tile
+    static constexpr size_t kSmem = kQBytes + 2 * kStages * kKvBytes;
+    // registers of the softmax, the converting and the issuing warps
+    static constexpr int kSoftmaxRegs = D == 256 ? 120 : 168, kLoadRegs = D == 256 ? 88 : 48, kIssueRegs = D == 256 ? 64 : 48;
+    static_assert(256 * kSoftmaxRegs + 256 * kLoadRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs, "registers at launch");
     static_assert(kChunks >= 1, "every load thread has work");
     static_assert(kOColumn + kQTiles * D <= 512, "tensor memory");
 };
@@ -77,15 +76,6 @@ __device__ __forceinline__ void bar_init(uint64_t *b, int n) {
 
 __device__ __forceinline__ void bar_arrive(uint64_t *b) {
     asm volatile("{\n.reg .b64 t;\nmbarrier.arrive.shared::cta.b64 t, [%0];\n}" ::"r"(smem_u32(b)) : "memory");
-}
-
-__device__ __forceinline__ void bar_arrive_expect(uint64_t *b, uint32_t bytes) {
-    asm volatile("{\n.reg .b64 t;\nmbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1;\n}" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
-}
-
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_t bytes, uint64_t *b) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(b)) : "memory");
 }
 
 __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity) {
@@ -207,6 +197,13 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
                  ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
 }
 
+// 16 codes, read once by this block.
+__device__ __forceinline__ uint4 load_codes(const uint8_t *p) {
+    uint4 x;
+    asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
+    return x;
+}
+
 // ---------------------------------------------------------------- softmax
 
 // A pair of fp32 values in one 64-bit register, for the two-wide instructions.
@@ -227,6 +224,16 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return v;
 }
 
+// What a tile needs to know of each 16 tokens: the scales, and where their codes begin in a head's plane, in
+// bytes (negative: in a block that is not there, or past the request's tokens).
+template <int BLOCKS>
+struct alignas(16) Entries {      // read 16 bytes at a time
+    float2 scale[BLOCKS];         // k_scale, log2 v_scale
+    float v_inverse[BLOCKS];
+    int64_t offset[BLOCKS];
+};
+static_assert(sizeof(Entries<8>) % 16 == 0 && sizeof(Entries<4>) % 16 == 0, "every tile's entries are aligned alike");
+
 // What a softmax thread keeps of its row. The weights of a tile are 2^(t - top + headroom); `limit` is the
 // largest exponent that is let pass: without bound until the row has seen a token, which then sets `top`.
 struct RowState {
@@ -244,7 +251,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // some row passes its limit, that row's maximum is raised by as much, its sum and, unless this is the first tile
 // (behind `wait_output`), its output rescaled.
 template <int D, class Wait, class Arrive>
-__device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const float4 *sc, float factor, bool masked, int left,
+__device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const Entries<Shape<D>::kBlocks> &entry, float factor, bool masked, int left,
                                              bool first, RowState &r, Wait wait_output, Arrive arrive) {
     using C = Shape<D>;
     uint32_t x[C::kTile / 32][32];
@@ -253,10 +260,11 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const
 #pragma unroll
     for (int c = 0; c < C::kTile / 32; ++c) ld_wait(x[c]);        // all of them; the others order their own registers
     const float base = kHeadroom - r.top;
+    float4 z;
 #pragma unroll
     for (int b = 0; b < C::kBlocks; ++b) {
-        const float4 z = sc[b];
-        const float a = factor * z.x, d = z.y + base;
+        if (b % 2 == 0) z = *reinterpret_cast<const float4 *>(&entry.scale[b]);   // of two blocks
+        const float a = factor * (b % 2 ? z.z : z.x), d = (b % 2 ? z.w : z.y) + base;
         const uint64_t a2 = pair(a, a), d2 = pair(d, d);
         uint32_t *y = &x[b / 2][b % 2 * 16];
 #pragma unroll
@@ -307,6 +315,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const
     for (int h = 0; h < C::kHalves; ++h) {
 #pragma unroll
         for (int c = 2 * h; c < 2 * h + 2; ++c) {
+            const float2 inverse = *reinterpret_cast<const float2 *>(&entry.v_inverse[2 * c]);
             uint32_t w[16];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
@@ -319,7 +328,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const
                 }
                 float p0, p1;
                 unpair(part, p0, p1);
-                r.sum = fmaf(p0 + p1, sc[2 * c + b].z, r.sum);
+                r.sum = fmaf(p0 + p1, b ? inverse.y : inverse.x, r.sum);
             }
             tmem_st16(s_at + h * kHalf + c % 2 * 16, w);
         }
@@ -451,13 +460,12 @@ struct Parity {
 };
 
 struct Barriers {
-    uint64_t k_full[2], k_empty[2], v_full[4], v_empty[4];
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
     uint64_t entry_full[16], entry_empty[16];
-    uint64_t raw_full[2][2], raw_empty[2][2];       // K, V
     uint64_t q_full[2], o_full[2];
     uint64_t s_full[2];                       // score buffer
     uint64_t p_full[2][2];                    // query tile; half, or score buffer where there are two
-    uint64_t o_done[2];                       // another half tile is in the output
+    uint64_t o_done;                          // another tile is in the output (two score buffers only)
 };
 
 template <int D, int FORMAT>
@@ -465,14 +473,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     using C = Shape<D>;
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ Barriers bars;
-    __shared__ float4 entries[C::kEntryStages][C::kBlocks];   // k_scale, log2 v_scale, 1 / v_scale, block of 16 tokens each
+    __shared__ Entries<C::kBlocks> entries[C::kEntryStages];
     __shared__ uint32_t scan[kThreads / 32];
     __shared__ Start start;
     __shared__ Walk<C::kRows, C::kTile> walks[kThreads / 32];
     __shared__ uint32_t tmem_base;
     __shared__ int failed;
-    unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + C::kKStages * C::kKBytes;
-    unsigned char *raw = v_smem + C::kVStages * C::kVBytes;
+    unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + C::kStages * C::kKvBytes;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
 
     // the plan: one thread per request, prefix sums in the (still unused) tile memory
@@ -506,12 +513,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (tid == 0) {
-        for (int i = 0; i < C::kKStages; ++i) {
-            bar_init(&bars.k_full[i], C::kHalves * kLoadWarps);
-            bar_init(&bars.k_empty[i], 1);
-        }
-        for (int i = 0; i < C::kVStages; ++i) {
+        for (int i = 0; i < C::kStages; ++i) {
+            bar_init(&bars.k_full[i], kLoadWarps);
             bar_init(&bars.v_full[i], kLoadWarps);
+            bar_init(&bars.k_empty[i], 1);
             bar_init(&bars.v_empty[i], 1);
         }
         for (int i = 0; i < C::kEntryStages; ++i) {
@@ -519,16 +524,12 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             bar_init(&bars.entry_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
-            for (int j = 0; j < C::kRawStages; ++j) {
-                bar_init(&bars.raw_full[i][j], 1);
-                bar_init(&bars.raw_empty[i][j], kLoadWarps);
-            }
             for (int j = 0; j < 2; ++j) bar_init(&bars.p_full[i][j], 128);
             bar_init(&bars.s_full[i], 1);
             bar_init(&bars.q_full[i], 128);
             bar_init(&bars.o_full[i], 1);
-            bar_init(&bars.o_done[i], 1);
         }
+        bar_init(&bars.o_done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
         const uint64_t units = (uint64_t)total * (uint32_t)p.heads;
@@ -573,7 +574,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
 
     if (warp < kSoftmaxWarps) {
         // ------------------------------------------------ softmax: one row per thread
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftmaxRegs));
         const int qt = warp / 4, row = tid % 128;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_at = tmem + lanes, o_at = tmem + lanes + C::kOColumn + qt * D;
@@ -605,10 +606,12 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
                 wait.warp(&bars.s_full[buffer], scored.use(buffer));
                 fence_after();
-                // the product before: the second half of the tile before, which the scores came after; or that tile
-                const uint32_t before = C::kHalves == 2 ? 1 : (n_mine & 1) ^ 1;
+                // the output holds the tile before: these scores came after it, unless they run two tiles ahead
+                auto output = [&] {
+                    if (C::kScoreBuffers == 2) wait.warp(&bars.o_done, (n_mine & 1) ^ 1);
+                };
                 softmax_tile<D>(s_at + buffer * C::kTile, o_at, entries[n_tile % C::kEntryStages], factor, (t + 1) * C::kTile > least,
-                                limit - t * C::kTile, t == t0, r, [&] { wait.warp(&bars.o_done[qt], before); },
+                                limit - t * C::kTile, t == t0, r, output,
                                 [&](int h) {
                                     fence_before();
                                     bar_arrive(&bars.p_full[qt][C::kHalves == 2 ? h : buffer]);
@@ -649,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             if (valid && !whole) __stcg(reinterpret_cast<float2 *>(p.part_ml + (part + row) * 2), make_float2(sum == 0.f ? -INFINITY : top, sum));
         }
     } else if (warp < kMmaWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
+        if constexpr (C::kLoadRegs < kLaunchRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kLoadRegs));
         // ------------------------------------------------ K (the first four warps) and V tiles to fp16
         const bool is_v = warp >= kSoftmaxWarps + kLoadWarps;
         const int lt = tid % kLoadThreads;
@@ -658,44 +661,37 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         const int row = lt / kPerRow, d = lt % kPerRow * 16;
         // the lanes of a store that are in odd panels take their second half first: no bank twice
         const bool swap = D > 64 && d / 64 % 2;
-        const int at16 = d % 64 / 8 + swap, panel = is_v ? C::kVPanel : C::kKPanel;
-        unsigned char *to0 = (is_v ? v_smem : k_smem) + d / 64 * panel + row * 128;
+        const int at16 = d % 64 / 8 + swap;
+        unsigned char *to0 = (is_v ? v_smem : k_smem) + d / 64 * C::kKvPanel + row * 128;
         unsigned char *to1 = to0 + ((at16 ^ 1) ^ (row & 7)) * 16;
         to0 += (at16 ^ (row & 7)) * 16;
-        const unsigned char *from = raw + is_v * C::kRawStages * C::kRawBytes + lt * 16;
-        uint64_t *raw_full = bars.raw_full[is_v], *raw_empty = bars.raw_empty[is_v];
+        const uint8_t *codes = (is_v ? p.v : p.k) + (row % 16) * p.stride_token + d;
         uint32_t n_tile = 0;
-        Parity filled, freed;
+        Parity freed;
         while (walk.next(p)) {
             const int tiles = w.t1 - w.t0;
-            for (int i = 0; i < tiles; ++i, ++n_tile) {
-                const int t = w.t0 + i;
-                bool full = (t + 1) * C::kTile <= w.kv;
-                const float4 *entry = entries[n_tile % C::kEntryStages];
+            const uint8_t *head = codes + (int64_t)w.head * p.stride_head;
+            uint4 x[C::kChunks];
+            // half h of the segment's tile i; a token past the request's, or in a block that is not there, is zero
+            auto fetch = [&](int i, int h) {
+                if (h == 0) wait.warp(&bars.entry_full[(n_tile + i) % C::kEntryStages], (n_tile + i) / C::kEntryStages & 1);
+                const int64_t *offset = entries[(n_tile + i) % C::kEntryStages].offset + h * kHalfBlocks;
+                const int left = w.kv - (w.t0 + i) * C::kTile - h * kHalf;
+#pragma unroll
+                for (int c = 0; c < C::kChunks; ++c) {
+                    const int r = row + c * kRowStep;
+                    const int64_t at = offset[r / 16];
+                    x[c] = make_uint4(0, 0, 0, 0);
+                    if (at >= 0 && r < left) x[c] = load_codes(head + at + (kRowStep % 16 ? c % 2 * 8 * p.stride_token : 0));
+                }
+            };
+            fetch(0, 0);
+            for (int i = 0; i < tiles; ++i) {
 #pragma unroll 1
                 for (int h = 0; h < C::kHalves; ++h) {
-                    const uint32_t raw_stage = h % C::kRawStages;
-                    wait.warp(&raw_full[raw_stage], filled.use(raw_stage));
-                    if (h == 0 && full) full = __all_sync(~0u, __float_as_int(entry[lane % C::kBlocks].w) >= 0);
-                    uint32_t stage = i % C::kKStages;             // of K: a tile; of V: a half
-                    int to = stage * C::kKBytes + h * kHalf * 128;
-                    if (is_v) {
-                        stage = (i * C::kHalves + h) % C::kVStages;
-                        to = stage * C::kVBytes;
-                    }
-                    if (is_v || h == 0) wait.warp(is_v ? &bars.v_empty[stage] : &bars.k_empty[stage], freed.use(stage) ^ 1);
-                    uint4 x[C::kChunks];
-#pragma unroll
-                    for (int c = 0; c < C::kChunks; ++c)
-                        x[c] = *reinterpret_cast<const uint4 *>(from + raw_stage * C::kRawBytes + c * kLoadThreads * 16);
-                    if (!full) {   // a token past the request's, or in a block that is not there, is zero
-                        const int left = w.kv - t * C::kTile - h * kHalf;
-#pragma unroll
-                        for (int c = 0; c < C::kChunks; ++c) {
-                            const int r = row + c * kRowStep;
-                            if (r >= left || __float_as_int(entry[h * kHalfBlocks + r / 16].w) < 0) x[c] = make_uint4(0, 0, 0, 0);
-                        }
-                    }
+                    const uint32_t stage = i % C::kStages;
+                    const int to = stage * C::kKvBytes + h * kHalf * 128;
+                    if (h == 0) wait.warp(is_v ? &bars.v_empty[stage] : &bars.k_empty[stage], freed.use(stage) ^ 1);
 #pragma unroll
                     for (int c = 0; c < C::kChunks; ++c) {
                         if (swap) x[c] = make_uint4(x[c].z, x[c].w, x[c].x, x[c].y);
@@ -707,17 +703,20 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                         *reinterpret_cast<uint4 *>(to0 + to + c * kRowStep * 128) = y0;
                         *reinterpret_cast<uint4 *>(to1 + to + c * kRowStep * 128) = y1;
                     }
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        bar_arrive(is_v ? &bars.v_full[stage] : &bars.k_full[stage]);
-                        bar_arrive(&raw_empty[raw_stage]);
+                    if (h + 1 < C::kHalves) {
+                        fetch(i, h + 1);
+                    } else {
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(is_v ? &bars.v_full[stage] : &bars.k_full[stage]);
+                        if (i + 1 < tiles) fetch(i + 1, 0);
                     }
                 }
             }
+            n_tile += tiles;
         }
     } else {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kIssueRegs));
       if (warp == kEntryWarp) {
         // ------------------------------------------------ blocks and scales, C::kEntryTiles tiles at a time
         uint32_t n_tile = 0;
@@ -729,50 +728,18 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 const uint32_t slot = (n_tile + mine) % C::kEntryStages;
                 if (mine < n) {
                     wait(&bars.entry_empty[slot], ((n_tile + mine) / C::kEntryStages & 1) ^ 1);
-                    const BlockEntry b = block_entry(p, w.request, w.head, (int64_t)(t + mine) * C::kTile + group * 16, w.kv);
+                    const int64_t token = (int64_t)(t + mine) * C::kTile + group * 16;
+                    const BlockEntry b = block_entry(p, w.request, w.head, token, w.kv);
                     // an absent block's tokens get weight 2^-inf
-                    entries[slot][group] = b.block < 0 ? make_float4(0.f, -INFINITY, 0.f, __int_as_float(-1))
-                                                       : make_float4(b.k_scale, b.v_log2, b.v_inverse, __int_as_float(b.block));
+                    entries[slot].scale[group] = make_float2(b.k_scale, b.block < 0 ? -INFINITY : b.v_log2);
+                    entries[slot].v_inverse[group] = b.v_inverse;
+                    entries[slot].offset[group] = b.block < 0 ? -1 : (int64_t)b.block * p.stride_block +
+                                                                         (token & ((1 << p.log2_block) - 1)) * p.stride_token;
                 }
                 __syncwarp();
                 if (mine < n && group == 0) bar_arrive(&bars.entry_full[slot]);
                 t += n;
                 n_tile += n;
-            }
-        }
-      } else if (warp >= kCopyWarp) {
-        // ------------------------------------------------ codes of K, of V into shared memory, 16 tokens of a block per lane
-        const bool is_v = warp > kCopyWarp;
-        const uint8_t *codes = is_v ? p.v : p.k;
-        uint32_t n_tile = 0;
-        Parity emptied;
-        const int in_block = (1 << p.log2_block) - 1;
-        while (walk.next(p)) {
-            for (int t = w.t0; t < w.t1; ++t, ++n_tile) {
-                wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
-                int block = -1;
-                if (lane < C::kBlocks) block = __float_as_int(entries[n_tile % C::kEntryStages][lane].w);
-                const unsigned there = __ballot_sync(~0u, block >= 0);
-                const int64_t from = (int64_t)block * p.stride_block + (int64_t)w.head * p.stride_head +
-                                     (int64_t)((t * C::kTile + lane * 16) & in_block) * p.stride_token;
-#pragma unroll 1
-                for (int h = 0; h < C::kHalves; ++h) {
-                    const uint32_t stage = h % C::kRawStages;
-                    uint64_t *full = &bars.raw_full[is_v][stage];
-                    wait.warp(&bars.raw_empty[is_v][stage], emptied.use(stage) ^ 1);
-                    const unsigned mine = there >> h * kHalfBlocks & ((1u << kHalfBlocks) - 1);
-                    if (lane == 0) bar_arrive_expect(full, __popc(mine) * 16 * D);
-                    __syncwarp();
-                    if (block >= 0 && lane / kHalfBlocks == h) {
-                        const uint8_t *src = codes + from;
-                        const uint32_t dst = smem_u32(raw) + (is_v * C::kRawStages + stage) * C::kRawBytes + lane % kHalfBlocks * 16 * D;
-                        if (p.stride_token == D) {
-                            bulk_copy(dst, src, 16 * D, full);
-                        } else {
-                            for (int r = 0; r < 16; ++r) bulk_copy(dst + r * D, src + r * p.stride_token, D, full);
-                        }
-                    }
-                }
             }
         }
       } else if (warp == kMmaWarp) {
@@ -785,10 +752,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         bool split = false;
         // scores of a query tile with the K tile in `stage`
         auto scores = [&](int qt, uint32_t buffer, uint32_t stage) {
-            const uint32_t a = operand_lo(q_at + qt * C::kPanels * C::kQPanel, 16), b = operand_lo(k_at + stage * C::kKBytes, 16);
+            const uint32_t a = operand_lo(q_at + qt * C::kPanels * C::kQPanel, 16), b = operand_lo(k_at + stage * C::kKvBytes, 16);
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
-                mma_ss(buffer * C::kTile, operand(a + k / 4 * (C::kQPanel / 16) + k % 4 * 2), operand(b + k / 4 * (C::kKPanel / 16) + k % 4 * 2),
+                mma_ss(buffer * C::kTile, operand(a + k / 4 * (C::kQPanel / 16) + k % 4 * 2), operand(b + k / 4 * (C::kKvPanel / 16) + k % 4 * 2),
                        s_instruction, k > 0, leader);
             commit(&bars.s_full[buffer], leader);
         };
@@ -813,19 +780,20 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                     const bool last = qt == 1 || !both;           // that reads this K and V
                     const uint32_t buffer = C::kQTiles == 2 ? qt : i & 1;
                     if (i >= 0) {
+                        const uint32_t v = i % C::kStages;
+                        if (qt == 0) wait.warp(&bars.v_full[v], v_full.use(v));
 #pragma unroll
                         for (int h = 0; h < C::kHalves; ++h) {
-                            const uint32_t v = (i * C::kHalves + h) % C::kVStages, q = C::kHalves == 2 ? h : buffer;
-                            if (qt == 0) wait.warp(&bars.v_full[v], v_full.use(v));
+                            const uint32_t q = C::kHalves == 2 ? h : buffer;
                             wait.warp(&bars.p_full[qt][q], weighted[qt].use(q));
                             fence_after();
-                            const uint32_t a = buffer * C::kTile + h * kHalf, b = operand_lo(v_at + v * C::kVBytes, C::kVPanel);
+                            const uint32_t a = buffer * C::kTile + h * kHalf, b = operand_lo(v_at + v * C::kKvBytes + h * kHalf * 128, C::kKvPanel);
 #pragma unroll
                             for (int j = 0; j < kHalf / 16; ++j)
                                 mma_ts(C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, j + h > 0 || i > 0, leader);
-                            commit(&bars.o_done[qt], leader);
-                            if (last) commit(&bars.v_empty[v], leader);
                         }
+                        if (C::kScoreBuffers == 2) commit(&bars.o_done, leader);
+                        if (last) commit(&bars.v_empty[v], leader);
                         if (__any_sync(~0u, i + 1 == tiles)) commit(&bars.o_full[qt], leader);
                         // every softmax thread has read the tile's entries, and so have the copies long before
                         if (last) {
@@ -834,7 +802,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                         }
                     }
                     if (__any_sync(~0u, i + kAhead < tiles)) {
-                        const uint32_t k = (i + kAhead) % C::kKStages;
+                        const uint32_t k = (i + kAhead) % C::kStages;
                         if (qt == 0) {
                             wait.warp(&bars.k_full[k], k_full.use(k));
                             fence_after();
