@@ -156,28 +156,53 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
 
         const uint8_t *k_head = p.k + kv_head * p.stride_head, *v_head = p.v + kv_head * p.stride_head;
         const int in_block = (1 << p.log2_block) - 1;
-        BlockEntry mine;
-        for (int ti = w.t0; ti < w.t1; ++ti) {
+        // a lane looks up the block of the warp's 16 tokens of one tile, for 32 tiles at a time
+        BlockEntry mine, b;
+        auto look_up = [&](int ti) {
             const int at = (ti - w.t0) % 32;
-            if (at == 0)   // lane l looks up the block of the warp's tokens of tile ti + l
+            if (at == 0)
                 mine = block_entry(p, w.request, kv_head, (int64_t)(ti + lane) * kTile + warp * 16, ti + lane < w.t1 ? w.kv : 0);
-            const int token = ti * kTile + warp * 16;
-            const BlockEntry b = shuffle(mine, at);
-            if (b.block < 0) continue;
-            const int64_t base = (int64_t)b.block * p.stride_block + (int64_t)(token & in_block) * p.stride_token;
-            uint32_t kw[2][C::kWordsK], vw[4][C::kWordsV];
+            return shuffle(mine, at);
+        };
+        // codes of the 16 tokens; each register's next load follows its last use
+        uint32_t kw[2][C::kWordsK], vw[4][C::kWordsV];
+        auto offset = [&](int ti, const BlockEntry &e) {
+            return (int64_t)e.block * p.stride_block + (int64_t)((ti * kTile + warp * 16) & in_block) * p.stride_token;
+        };
+        auto load_k = [&](int64_t base) {
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int c = 0; c < C::kWordsK * 4 / C::kVecK; ++c)
                     load_words<C::kVecK>(&kw[x][c * C::kVecK / 4],
                                          k_head + base + (g + 8 * x) * p.stride_token + c * 4 * C::kVecK + t * C::kVecK);
+        };
+        auto load_v = [&](int64_t base) {
 #pragma unroll
             for (int x = 0; x < 4; ++x)
 #pragma unroll
                 for (int c = 0; c < C::kWordsV * 4 / C::kVecV; ++c)
                     load_words<C::kVecV>(&vw[x][c * C::kVecV / 4],
                                          v_head + base + (2 * t + (x & 1) + 8 * (x >> 1)) * p.stride_token + c * 8 * C::kVecV + g * C::kVecV);
+        };
+        BlockEntry next = look_up(w.t0);
+        if (next.block >= 0) {
+            load_k(offset(w.t0, next));
+            load_v(offset(w.t0, next));
+        }
+        for (int ti = w.t0; ti < w.t1; ++ti) {
+            const int token = ti * kTile + warp * 16;
+            b = next;
+            next.block = -1;
+            if (ti + 1 < w.t1) next = look_up(ti + 1);
+            const int64_t ahead = offset(ti + 1, next);
+            if (b.block < 0) {
+                if (next.block >= 0) {
+                    load_k(ahead);
+                    load_v(ahead);
+                }
+                continue;
+            }
 
             float s[NT][4];
 #pragma unroll
@@ -190,6 +215,7 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt], a0, a1, a2, a3, qf[nt][2 * j], qf[nt][2 * j + 1]);
             }
+            if (next.block >= 0) load_k(ahead);
             bool raise = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -253,6 +279,7 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) mma_f16(o[2 * i + 1][nt], a0, a1, a2, a3, w0[nt], w1[nt]);
             }
+            if (next.block >= 0) load_v(ahead);
         }
 
         // the four warps' parts through shared memory
