@@ -13,11 +13,11 @@
 // down to 2^-28 of it), w to fp16 with M set so that w <= 2^15 (11 bits; w below 2^-40 of the
 // largest are lost), the result to bf16.
 //
-// Layout. A warp takes 16 tokens at a time straight from global memory into the fragments of
-// mma.m16n8k16: scores as K (16 tokens) x Q^T (8 rows), outputs as V^T (16 of head_dim) x w^T.
-// Which element of head_dim a fragment position stands for is free as long as K and Q (V and the
-// output) agree, so every lane reads whole 16-byte vectors and no shared memory is touched until
-// the end. The work, every (request, kv head, tile of 64 tokens), is laid out on one line and cut
+// Layout. A warp takes 16 tokens at a time through a ring of its own in shared memory, copied two or
+// more stages ahead (about 130 KB on their way per SM), into the fragments of mma.m16n8k16: scores as
+// K (16 tokens) x Q^T (8 rows), outputs as V^T (16 of head_dim) x w^T. Which element of head_dim a
+// fragment position stands for is free as long as K and Q (V and the output) agree, so every lane
+// reads whole vectors and no code is transposed. The work, every (request, kv head, tile of 64 tokens), is laid out on one line and cut
 // evenly over a grid that just fills the GPU; where a cut falls inside a (request, head), the
 // parts meet in the workspace and whoever comes last joins them in their order, so that the
 // result does not depend on timing.
@@ -51,29 +51,45 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     return y;
 }
 
-// N bytes as words; the cache is read once, so it does not need to stay.
 template <int N>
-__device__ __forceinline__ void load_words(uint32_t *w, const uint8_t *p) {
+__device__ __forceinline__ void load_words(uint32_t *w, const unsigned char *p) {
     if constexpr (N == 16) {
-        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
+        const uint4 v = *reinterpret_cast<const uint4 *>(p);
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
     } else if constexpr (N == 8) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
+        const uint2 v = *reinterpret_cast<const uint2 *>(p);
         w[0] = v.x; w[1] = v.y;
     } else {
-        w[0] = __ldg(reinterpret_cast<const uint32_t *>(p));
+        w[0] = *reinterpret_cast<const uint32_t *>(p);
     }
 }
+
+__device__ __forceinline__ void copy16(unsigned char *to, const uint8_t *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 template <int D, int FORMAT, int NT>
 struct Decode {
     static constexpr int kRows = 8 * NT;                      // query rows of a tile
-    static constexpr int kVecK = D / 4 < 16 ? D / 4 : 16;     // bytes of a K load: a lane has D / 4 of a row
-    static constexpr int kVecV = D / 8 < 16 ? D / 8 : 16;     // bytes of a V load: D / 8 of a row
+    static constexpr int kVecK = D / 4 < 16 ? D / 4 : 16;     // bytes of a K read: a lane has D / 4 of a row
+    static constexpr int kVecV = D / 8 < 16 ? D / 8 : 16;     // bytes of a V read: D / 8 of a row
     static constexpr int kWordsK = D / 16, kWordsV = D / 32;
     static constexpr int kPitch = D + 4;                      // floats of a row in shared memory
     static constexpr int kBlocksPerSm = D == 256 ? 2 : NT == 2 ? 3 : 4;
-    static constexpr size_t kMergeBytes = (size_t)kWarps * kRows * (kPitch + 2) * 4;
+    static constexpr int kStageBytes = 32 * D;                // 16 tokens of K, then of V
+    static constexpr int kStages = D == 256 ? 3 : D == 128 ? 3 : D == 64 ? 6 : 8;
+    static constexpr int kRing = kWarps * kStages * kStageBytes;
+    static constexpr int kMerge = kWarps * kRows * (kPitch + 2) * 4;   // over the ring, once it has been read
+    static constexpr size_t kShared = kRing > kMerge ? kRing : kMerge;
+    // Places of a row's 16-byte chunks, so that the lanes that read together (K: two rows and four chunks; V: four
+    // rows two apart and two chunks) meet no bank twice.
+    static __device__ __forceinline__ int place_k(int row, int chunk) { return D >= 128 ? chunk ^ (row & 1) << 2 : chunk; }
+    static __device__ __forceinline__ int place_v(int row, int chunk) {
+        return D >= 128 ? chunk ^ (row >> 1 & 3) << 1 : D == 64 ? chunk ^ (row >> 1 & 3) : chunk;
+    }
 };
 
 template <int D, int FORMAT, int NT>
@@ -83,7 +99,8 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
     extern __shared__ __align__(16) unsigned char smem[];
     float *merge_o = reinterpret_cast<float *>(smem);                        // [warps][rows][pitch]
     float *merge_ml = merge_o + kWarps * C::kRows * C::kPitch;               // [warps][rows][2]
-    uint32_t *prefix = reinterpret_cast<uint32_t *>(merge_ml + kWarps * C::kRows * 2);
+    uint32_t *prefix = reinterpret_cast<uint32_t *>(smem + C::kShared);
+    __shared__ float4 ring_scales[kWarps][C::kStages];                       // k_scale, log2 v_scale, 1 / v_scale, block
     __shared__ uint32_t scan[kWarps];
     __shared__ uint32_t last_one;
     const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, g = lane / 4, t = lane % 4;
@@ -98,6 +115,38 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
         const AttentionSegment w = locate<C::kRows, kTile>(p, prefix, u, u_end);
         u += w.t1 - w.t0;
         const int64_t kv_head = w.head;
+
+        // The warp's own ring: 16 tokens of K and V a stage, copied some stages ahead. A lane looks up the block of
+        // one tile, for 32 tiles at a time; a tile without a block is passed over.
+        const uint8_t *k_head = p.k + kv_head * p.stride_head, *v_head = p.v + kv_head * p.stride_head;
+        const int in_block = (1 << p.log2_block) - 1;
+        unsigned char *ring = smem + warp * (C::kStages * C::kStageBytes);
+        BlockEntry mine;
+        auto issue = [&](int ti) {
+            if (ti < w.t1) {
+                const int at = (ti - w.t0) % 32;
+                if (at == 0)
+                    mine = block_entry(p, w.request, kv_head, (int64_t)(ti + lane) * kTile + warp * 16, ti + lane < w.t1 ? w.kv : 0);
+                const BlockEntry e = shuffle(mine, at);
+                const int stage = (ti - w.t0) % C::kStages;
+                if (lane == 0) ring_scales[warp][stage] = make_float4(e.k_scale, e.v_log2, e.v_inverse, __int_as_float(e.block));
+                if (e.block >= 0) {
+                    constexpr int kPerRow = D / 16, kStep = 32 / kPerRow;   // chunks of a row, rows of one copy
+                    const int row = lane / kPerRow, chunk = lane % kPerRow;
+                    const int64_t from = (int64_t)e.block * p.stride_block +
+                                         (int64_t)(((ti * kTile + warp * 16) & in_block) + row) * p.stride_token + chunk * 16;
+                    unsigned char *to = ring + stage * C::kStageBytes + row * D;
+#pragma unroll
+                    for (int r = 0; r < 16; r += kStep) {
+                        copy16(to + r * D + C::place_k(row + r, chunk) * 16, k_head + from + r * p.stride_token);
+                        copy16(to + (16 + r) * D + C::place_v(row + r, chunk) * 16, v_head + from + r * p.stride_token);
+                    }
+                }
+            }
+            copies_end_group();
+        };
+#pragma unroll
+        for (int i = 0; i < C::kStages - 1; ++i) issue(w.t0 + i);
 
         // the query rows of this lane's fragments, as fp16 with a power of two per row
         uint32_t qf[NT][D / 8];
@@ -154,68 +203,36 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = -INFINITY, sum[nt][0] = sum[nt][1] = 0.f;
 
-        const uint8_t *k_head = p.k + kv_head * p.stride_head, *v_head = p.v + kv_head * p.stride_head;
-        const int in_block = (1 << p.log2_block) - 1;
-        // a lane looks up the block of the warp's 16 tokens of one tile, for 32 tiles at a time
-        BlockEntry mine, b;
-        auto look_up = [&](int ti) {
-            const int at = (ti - w.t0) % 32;
-            if (at == 0)
-                mine = block_entry(p, w.request, kv_head, (int64_t)(ti + lane) * kTile + warp * 16, ti + lane < w.t1 ? w.kv : 0);
-            return shuffle(mine, at);
-        };
-        // codes of the 16 tokens; each register's next load follows its last use
-        uint32_t kw[2][C::kWordsK], vw[4][C::kWordsV];
-        auto offset = [&](int ti, const BlockEntry &e) {
-            return (int64_t)e.block * p.stride_block + (int64_t)((ti * kTile + warp * 16) & in_block) * p.stride_token;
-        };
-        auto load_k = [&](int64_t base) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int c = 0; c < C::kWordsK * 4 / C::kVecK; ++c)
-                    load_words<C::kVecK>(&kw[x][c * C::kVecK / 4],
-                                         k_head + base + (g + 8 * x) * p.stride_token + c * 4 * C::kVecK + t * C::kVecK);
-        };
-        auto load_v = [&](int64_t base) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-#pragma unroll
-                for (int c = 0; c < C::kWordsV * 4 / C::kVecV; ++c)
-                    load_words<C::kVecV>(&vw[x][c * C::kVecV / 4],
-                                         v_head + base + (2 * t + (x & 1) + 8 * (x >> 1)) * p.stride_token + c * 8 * C::kVecV + g * C::kVecV);
-        };
-        BlockEntry next = look_up(w.t0);
-        if (next.block >= 0) {
-            load_k(offset(w.t0, next));
-            load_v(offset(w.t0, next));
-        }
         for (int ti = w.t0; ti < w.t1; ++ti) {
-            const int token = ti * kTile + warp * 16;
-            b = next;
-            next.block = -1;
-            if (ti + 1 < w.t1) next = look_up(ti + 1);
-            const int64_t ahead = offset(ti + 1, next);
-            if (b.block < 0) {
-                if (next.block >= 0) {
-                    load_k(ahead);
-                    load_v(ahead);
-                }
-                continue;
-            }
+            const int token = ti * kTile + warp * 16, stage = (ti - w.t0) % C::kStages;
+            copies_wait<C::kStages - 2>();
+            __syncwarp();                         // the warp's copies are there, and the stage before has been read
+            issue(ti + C::kStages - 1);
+            const float4 z = ring_scales[warp][stage];
+            const BlockEntry b{__float_as_int(z.w), z.x, z.y, z.z};
+            if (b.block < 0) continue;
+            const unsigned char *k_at = ring + stage * C::kStageBytes, *v_at = k_at + 16 * D;
 
             float s[NT][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
-            for (int j = 0; j < C::kWordsK; ++j) {
-                uint32_t a0, a1, a2, a3;
-                codes_to_half<FORMAT>(kw[0][j], a0, a2);
-                codes_to_half<FORMAT>(kw[1][j], a1, a3);
+            for (int c = 0; c < C::kWordsK * 4 / C::kVecK; ++c) {
+                uint32_t kw[2][C::kVecK / 4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt], a0, a1, a2, a3, qf[nt][2 * j], qf[nt][2 * j + 1]);
+                for (int x = 0; x < 2; ++x)
+                    load_words<C::kVecK>(kw[x], C::kVecK == 16 ? k_at + (g + 8 * x) * D + C::place_k(g, c * 4 + t) * 16
+                                                               : k_at + (g + 8 * x) * D + t * C::kVecK);
+#pragma unroll
+                for (int i = 0; i < C::kVecK / 4; ++i) {
+                    const int j = c * (C::kVecK / 4) + i;
+                    uint32_t a0, a1, a2, a3;
+                    codes_to_half<FORMAT>(kw[0][i], a0, a2);
+                    codes_to_half<FORMAT>(kw[1][i], a1, a3);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt], a0, a1, a2, a3, qf[nt][2 * j], qf[nt][2 * j + 1]);
+                }
             }
-            if (next.block >= 0) load_k(ahead);
             bool raise = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -260,27 +277,34 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
                 w0[nt] = transpose8x8(pack_half(e0, e1));
                 w1[nt] = transpose8x8(pack_half(e2, e3));
             }
-            if (token + 16 > w.kv) {            // what lies behind the last token may be anything
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    if (token + 2 * t + (x & 1) + 8 * (x >> 1) >= w.kv)
+            for (int c = 0; c < C::kWordsV * 4 / C::kVecV; ++c) {
+                uint32_t vw[4][C::kVecV / 4];
 #pragma unroll
-                        for (int i = 0; i < C::kWordsV; ++i) vw[x][i] = 0;
+                for (int x = 0; x < 4; ++x) {
+                    const int row = 2 * t + (x & 1) + 8 * (x >> 1), byte = c * 8 * C::kVecV + g * C::kVecV;
+                    load_words<C::kVecV>(vw[x], v_at + row * D + C::place_v(row, byte / 16) * 16 + byte % 16);
+                    if (token + 16 > w.kv && token + row >= w.kv)   // what lies behind the last token may be anything
+#pragma unroll
+                        for (int i = 0; i < C::kVecV / 4; ++i) vw[x][i] = 0;
+                }
+#pragma unroll
+                for (int j = 0; j < C::kVecV / 4; ++j) {
+                    const int i = c * (C::kVecV / 4) + j;
+                    uint32_t a0, a1, a2, a3;    // bytes 4i, 4i + 1: fragment rows g and g + 8
+                    codes_to_half<FORMAT>(prmt(vw[0][j], vw[1][j], 0x5140), a0, a1);
+                    codes_to_half<FORMAT>(prmt(vw[2][j], vw[3][j], 0x5140), a2, a3);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[2 * i][nt], a0, a1, a2, a3, w0[nt], w1[nt]);
+                    codes_to_half<FORMAT>(prmt(vw[0][j], vw[1][j], 0x7362), a0, a1);
+                    codes_to_half<FORMAT>(prmt(vw[2][j], vw[3][j], 0x7362), a2, a3);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[2 * i + 1][nt], a0, a1, a2, a3, w0[nt], w1[nt]);
+                }
             }
-#pragma unroll
-            for (int i = 0; i < C::kWordsV; ++i) {
-                uint32_t a0, a1, a2, a3;        // bytes 4i, 4i + 1: fragment rows g and g + 8
-                codes_to_half<FORMAT>(prmt(vw[0][i], vw[1][i], 0x5140), a0, a1);
-                codes_to_half<FORMAT>(prmt(vw[2][i], vw[3][i], 0x5140), a2, a3);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma_f16(o[2 * i][nt], a0, a1, a2, a3, w0[nt], w1[nt]);
-                codes_to_half<FORMAT>(prmt(vw[0][i], vw[1][i], 0x7362), a0, a1);
-                codes_to_half<FORMAT>(prmt(vw[2][i], vw[3][i], 0x7362), a2, a3);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma_f16(o[2 * i + 1][nt], a0, a1, a2, a3, w0[nt], w1[nt]);
-            }
-            if (next.block >= 0) load_v(ahead);
         }
+        copies_wait<0>();
+        __syncthreads();                          // every warp has read its ring: the parts go over it
 
         // the four warps' parts through shared memory
 #pragma unroll
@@ -349,10 +373,10 @@ template <int D, int FORMAT, int NT>
 cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream) {
     using C = Decode<D, FORMAT, NT>;
     static std::atomic<uint64_t> allowed{0};   // devices on which the shared memory limit is raised
-    const size_t smem = C::kMergeBytes + ((size_t)p.requests + 1) * 4;
+    const size_t smem = C::kShared + ((size_t)p.requests + 1) * 4;
     if (smem > 48 * 1024 && (device >= 64 || !(allowed.load() >> device & 1))) {
         const cudaError_t e = cudaFuncSetAttribute(decode_kernel<D, FORMAT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)(C::kMergeBytes + (kQcacheMaxAttentionRequests + 1) * 4));
+                                                   (int)(C::kShared + (kQcacheMaxAttentionRequests + 1) * 4));
         if (e != cudaSuccess) return e;
         if (device < 64) allowed.fetch_or(1ull << device);
     }
