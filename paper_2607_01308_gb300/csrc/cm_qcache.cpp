@@ -240,7 +240,7 @@ cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t laye
         const int num_sms = cm::context_num_sms(ctx);
         if (workspace_bytes < 0 || (uint64_t)workspace_bytes < cm::qcache_workspace_bytes(cache->head_dim, num_sms))
             return fail(CM_ERR_CAPACITY, "workspace is smaller than cm_qcache_workspace says");
-        const double tiles = (double)batch->table_width * batch->block_size / 64 + 1;
+        const double tiles = (double)batch->table_width * batch->block_size / 64 + 9;   // and their setup
         const double row_tiles = (double)query->total_rows * group / 8 + batch->num_requests;
         if (tiles * row_tiles >= 2147483648.0)
             return fail(CM_ERR_UNSUPPORTED, "too much work for one call: split the rows");

@@ -44,9 +44,13 @@ __device__ __forceinline__ RequestShape request_shape(const QcacheAttentionParam
     return s;
 }
 
-// The requests' units (row tiles x kv tiles) for one kv head as exclusive prefix sums in
-// prefix[0 .. requests]; returns their total. Every thread of the block takes part.
-template <int THREADS, int ROWS, int TILE>
+// A unit of work is a kv tile of one row tile and kv head. What beginning and ending a (row tile, head)
+// costs besides its tiles (the query rows, the first copies, the parts' meeting) counts as SETUP units in
+// front of them, or short requests would come to the same few thread blocks.
+
+// The requests' units for one kv head as exclusive prefix sums in prefix[0 .. requests]; returns their
+// total. Every thread of the block takes part.
+template <int THREADS, int ROWS, int TILE, int SETUP>
 __device__ __forceinline__ uint32_t plan_units(const QcacheAttentionParams &p, uint32_t *prefix, uint32_t *scan) {
     const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     uint32_t total = 0;
@@ -55,7 +59,7 @@ __device__ __forceinline__ uint32_t plan_units(const QcacheAttentionParams &p, u
         uint32_t n = 0;
         if (r < p.requests) {
             const RequestShape s = request_shape<ROWS, TILE>(p, r);
-            n = (uint32_t)s.row_tiles * (uint32_t)s.tiles;
+            n = (uint32_t)s.row_tiles * (uint32_t)(s.tiles + SETUP);
         }
         uint32_t a = n;
 #pragma unroll
@@ -79,10 +83,11 @@ __device__ __forceinline__ uint32_t plan_units(const QcacheAttentionParams &p, u
     return total;
 }
 
-// Units of one thread block: an even share, but no less than a few, below which joining the
+// Units of one thread block: an even share, but no less than a few tiles, below which joining the
 // parts costs more than reading alone.
+template <int SETUP>
 __device__ __forceinline__ uint64_t units_per_block(uint64_t units, uint32_t blocks) {
-    return max((units + blocks - 1) / blocks, (uint64_t)2);
+    return max((units + blocks - 1) / blocks, (uint64_t)(SETUP + 2));
 }
 
 // A run of kv tiles [t0, t1) of one row tile of one kv head of one request.
@@ -92,9 +97,10 @@ struct AttentionSegment {
     uint64_t unit0;               // the unit of tile 0
 };
 
-// Units lie by request, row tile, kv head, kv tile.
-template <int ROWS, int TILE>
-__device__ __forceinline__ AttentionSegment locate(const QcacheAttentionParams &p, const uint32_t *prefix, uint64_t u,
+// The segment at unit u, up to u_end; moves u behind it. Units lie by request, row tile, kv head, kv tile;
+// a segment without tiles (t0 == t1) is the share of a setup whose tiles come later.
+template <int ROWS, int TILE, int SETUP>
+__device__ __forceinline__ AttentionSegment locate(const QcacheAttentionParams &p, const uint32_t *prefix, uint64_t &u,
                                                    uint64_t u_end) {
     int lo = 0, hi = p.requests;
     while (hi - lo > 1) {
@@ -106,12 +112,15 @@ __device__ __forceinline__ AttentionSegment locate(const QcacheAttentionParams &
     w.request = lo;
     w.row0 = s.row0; w.q_len = s.q_len; w.kv = s.kv; w.rows = s.rows; w.tiles = s.tiles;
     const uint64_t in = u - (uint64_t)prefix[lo] * (uint32_t)p.heads;
-    const uint64_t pair = in / (uint32_t)s.tiles;
-    w.t0 = (int)(in - pair * (uint32_t)s.tiles);
-    w.t1 = (int)min((uint64_t)s.tiles, w.t0 + (u_end - u));
+    const uint64_t pair = in / (uint32_t)(s.tiles + SETUP);
+    const int at = (int)(in - pair * (uint32_t)(s.tiles + SETUP));
+    const int to = (int)min((uint64_t)(s.tiles + SETUP), at + (u_end - u));
+    w.t0 = max(0, at - SETUP);
+    w.t1 = max(0, to - SETUP);
     w.row_tile = (int)(pair / (uint32_t)p.heads);
     w.head = (int)(pair - (uint64_t)w.row_tile * (uint32_t)p.heads);
-    w.unit0 = u - w.t0;
+    w.unit0 = u - at + SETUP;
+    u += to - at;
     return w;
 }
 
@@ -175,50 +184,76 @@ template <int D, int WARPS, int GROUP, class At>
 __device__ __forceinline__ void join_parts(const QcacheAttentionParams &p, const AttentionSegment &w, int first, int rows,
                                            uint32_t c0, uint32_t c1, float headroom, int warp, At row_at) {
     constexpr int kGroup = GROUP, kVecs = D >= 128 ? D / 128 : 1;   // 16-byte vectors of a lane
+    constexpr int kAhead = 8 / kGroup;                          // parts that are read before they can be weighed
     const int lane = threadIdx.x % 32, n = (int)(c1 - c0 + 1);
     for (int r0 = warp; r0 < rows; r0 += WARPS * kGroup) {
         float m[kGroup], l[kGroup];
         float4 acc[kGroup][kVecs];
+        auto read = [&](int c, int k, int v) {
+            if ((D < 128 && lane >= D / 4) || c >= n) return make_float4(0.f, 0.f, 0.f, 0.f);
+            return __ldcg(reinterpret_cast<const float4 *>(p.part_o + row_at(c0 + c, min(r0 + k * WARPS, rows - 1)) * D) + lane + 32 * v);
+        };
+        float2 ml[kGroup];
+        float4 early[kAhead][kGroup][kVecs];
 #pragma unroll
         for (int k = 0; k < kGroup; ++k) {
-            const int row = min(r0 + k * WARPS, rows - 1);
-            m[k] = -INFINITY;
-            for (int c = lane; c < n; c += 32) m[k] = fmaxf(m[k], __ldcg(p.part_ml + row_at(c0 + c, row) * 2));
+            ml[k] = make_float2(-INFINITY, 0.f);
+            if (lane < n) ml[k] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml + row_at(c0 + lane, min(r0 + k * WARPS, rows - 1)) * 2));
+        }
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c)
+#pragma unroll
+            for (int k = 0; k < kGroup; ++k)
+#pragma unroll
+                for (int v = 0; v < kVecs; ++v) early[c][k][v] = read(c, k, v);
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) {
+            m[k] = ml[k].x;
+            for (int c = 32 + lane; c < n; c += 32) m[k] = fmaxf(m[k], __ldcg(p.part_ml + row_at(c0 + c, min(r0 + k * WARPS, rows - 1)) * 2));
 #pragma unroll
             for (int d = 16; d; d /= 2) m[k] = fmaxf(m[k], __shfl_xor_sync(~0u, m[k], d));
             l[k] = 0.f;
 #pragma unroll
             for (int v = 0; v < kVecs; ++v) acc[k][v] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
+        auto add = [&](int k, int v, const float4 &x, float g) {
+            float4 &a = acc[k][v];
+            a.x = fmaf(x.x, g, a.x); a.y = fmaf(x.y, g, a.y);
+            a.z = fmaf(x.z, g, a.z); a.w = fmaf(x.w, g, a.w);
+        };
         for (int base = 0; base < n; base += 32) {
             float f[kGroup];
 #pragma unroll
             for (int k = 0; k < kGroup; ++k) {
-                const int row = min(r0 + k * WARPS, rows - 1);
-                float2 ml = make_float2(-INFINITY, 0.f);
-                if (base + lane < n) ml = __ldcg(reinterpret_cast<const float2 *>(p.part_ml + row_at(c0 + base + lane, row) * 2));
-                f[k] = ml.x == m[k] ? 1.f : exp2_fast(ml.x - m[k]);
-                float x = ml.y * f[k];
+                if (base > 0) {
+                    ml[k] = make_float2(-INFINITY, 0.f);
+                    if (base + lane < n)
+                        ml[k] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml + row_at(c0 + base + lane, min(r0 + k * WARPS, rows - 1)) * 2));
+                }
+                f[k] = ml[k].x == m[k] ? 1.f : exp2_fast(ml[k].x - m[k]);
+                float x = ml[k].y * f[k];
 #pragma unroll
                 for (int d = 16; d; d /= 2) x += __shfl_xor_sync(~0u, x, d);
                 l[k] += x;
             }
+            if (base == 0) {
+#pragma unroll
+                for (int c = 0; c < kAhead; ++c)
+#pragma unroll
+                    for (int k = 0; k < kGroup; ++k) {
+                        const float g = __shfl_sync(~0u, f[k], c);
+#pragma unroll
+                        for (int v = 0; v < kVecs; ++v) add(k, v, early[c][k][v], c < n ? g : 0.f);
+                    }
+            }
             const int most = min(32, n - base);
-#pragma unroll(16 / GROUP)
-            for (int c = 0; c < most; ++c)
+#pragma unroll kAhead
+            for (int c = base == 0 ? kAhead : 0; c < most; ++c)
 #pragma unroll
                 for (int k = 0; k < kGroup; ++k) {
-                    const int row = min(r0 + k * WARPS, rows - 1);
                     const float g = __shfl_sync(~0u, f[k], c);
-                    const float4 *part = reinterpret_cast<const float4 *>(p.part_o + row_at(c0 + base + c, row) * D);
 #pragma unroll
-                    for (int v = 0; v < kVecs; ++v) {
-                        if (D < 128 && lane >= D / 4) break;
-                        const float4 x = __ldcg(part + lane + 32 * v);
-                        float4 &a = acc[k][v];
-                        a.x = fmaf(x.x, g, a.x); a.y = fmaf(x.y, g, a.y);
-                        a.z = fmaf(x.z, g, a.z); a.w = fmaf(x.w, g, a.w);
-                    }
+                    for (int v = 0; v < kVecs; ++v) add(k, v, read(base + c, k, v), g);
                 }
         }
 #pragma unroll

@@ -79,6 +79,7 @@ struct Decode {
     static constexpr int kWordsK = D / 16, kWordsV = D / 32;
     static constexpr int kPitch = D + 4;                      // floats of a row in shared memory
     static constexpr int kBlocksPerSm = D == 256 ? 2 : NT == 2 ? 3 : 4;
+    static constexpr int kSetup = D >= 128 ? 2 : 256 / D;     // about 2.5 us in tiles of 128 D bytes at a block's share of HBM
     static constexpr int kStageBytes = 32 * D;                // 16 tokens of K, then of V
     static constexpr int kStages = D == 256 ? 3 : D == 128 ? 3 : D == 64 ? 6 : 8;
     static constexpr int kRing = kWarps * kStages * kStageBytes;
@@ -105,15 +106,15 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
     __shared__ uint32_t last_one;
     const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, g = lane / 4, t = lane % 4;
 
-    const uint32_t per_head = plan_units<kThreads, C::kRows, kTile>(p, prefix, scan);
+    const uint32_t per_head = plan_units<kThreads, C::kRows, kTile, C::kSetup>(p, prefix, scan);
     const uint64_t units = (uint64_t)per_head * (uint32_t)p.heads;
-    const uint64_t per = units_per_block(units, gridDim.x);
+    const uint64_t per = units_per_block<C::kSetup>(units, gridDim.x);
     uint64_t u = (uint64_t)blockIdx.x * per;
     const uint64_t u_end = min(u + per, units);
 
     while (u < u_end) {
-        const AttentionSegment w = locate<C::kRows, kTile>(p, prefix, u, u_end);
-        u += w.t1 - w.t0;
+        const AttentionSegment w = locate<C::kRows, kTile, C::kSetup>(p, prefix, u, u_end);
+        if (w.t0 == w.t1) continue;
         const int64_t kv_head = w.head;
 
         // The warp's own ring: 16 tokens of K and V a stage, copied some stages ahead. A lane looks up the block of

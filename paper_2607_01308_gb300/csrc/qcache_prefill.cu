@@ -47,6 +47,7 @@ struct Shape {
     // tensor memory, 512 columns: two tiles of scores, and the outputs
     static constexpr int kQTiles = D == 256 ? 1 : 2;
     static constexpr int kTile = D == 256 ? 64 : 128, kHalves = kTile / kHalf;   // tokens of a kv tile
+    static constexpr int kSetup = D == 256 ? 3 : 2;           // a segment's queries and its end, in tiles
     static constexpr int kBlocks = kTile / 16;                // scale entries of a tile
     static constexpr int kEntryTiles = 32 / kBlocks, kEntryStages = 2 * kEntryTiles;   // looked up at a time; held
     static constexpr int kScoreBuffers = 2 / kQTiles;         // for each query tile
@@ -392,23 +393,23 @@ __device__ __forceinline__ int visible_tiles(const QcacheAttentionParams &p, con
 
 struct Start {
     uint64_t u, end, per;
-    int request, row_tile, head, tile;
+    int request, row_tile, head, at;
 };
 
 // The walk through a block's share, and the segment that it is at: each warp makes it for itself, in
 // shared memory, so that neither takes registers from the loops.
-template <int ROWS, int TILE>
+template <int ROWS, int TILE, int SETUP>
 struct Walk {
     AttentionSegment w;
-    int left;                     // units of the share behind w
+    int at, left;                 // units: done of this (row tile, head), its setup first; of the share behind w
     bool more;
 
     __device__ void begin(const QcacheAttentionParams &p, const Start &start) {
         left = (int)(start.end > start.u ? start.end - start.u : 0);
         if (left == 0) return;
         w.request = start.request; w.head = start.head; w.row_tile = start.row_tile;
-        w.t1 = start.tile;        // an empty segment in front of the first
-        w.unit0 = start.u - start.tile;
+        at = start.at;
+        w.unit0 = start.u - start.at + SETUP;
         request(p);
     }
 
@@ -418,15 +419,15 @@ struct Walk {
         w.tiles = visible_tiles<ROWS, TILE>(p, s, w.row_tile);
     }
 
-    // The next segment into w, for the whole warp; false at the end.
+    // The next segment with tiles into w, for the whole warp; false at the end.
     __device__ __forceinline__ bool next(const QcacheAttentionParams &p) {
         __syncwarp();
         if (threadIdx.x % 32 == 0) {
-            more = left > 0;
-            if (more) {
-                if (w.t1 == w.tiles) {
-                    w.unit0 += w.tiles;
-                    w.t1 = 0;
+            more = false;
+            while (left > 0 && !more) {
+                if (at == w.tiles + SETUP) {
+                    w.unit0 += w.tiles + SETUP;
+                    at = 0;
                     if (++w.head == p.heads) {
                         w.head = 0;
                         if (++w.row_tile * ROWS >= w.rows) {
@@ -437,9 +438,12 @@ struct Walk {
                         }
                     }
                 }
-                w.t0 = w.t1;
-                w.t1 = min(w.tiles, w.t0 + left);
-                left -= w.t1 - w.t0;
+                const int n = min(w.tiles + SETUP - at, left);
+                w.t0 = max(0, at - SETUP);
+                at += n;
+                left -= n;
+                w.t1 = max(0, at - SETUP);
+                more = w.t1 > w.t0;
             }
         }
         __syncwarp();
@@ -476,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     __shared__ Entries<C::kBlocks> entries[C::kEntryStages];
     __shared__ uint32_t scan[kThreads / 32];
     __shared__ Start start;
-    __shared__ Walk<C::kRows, C::kTile> walks[kThreads / 32];
+    __shared__ Walk<C::kRows, C::kTile, C::kSetup> walks[kThreads / 32];
     __shared__ uint32_t tmem_base;
     __shared__ int failed;
     unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + C::kStages * C::kKvBytes;
@@ -490,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         uint32_t n = 0;
         if (r < p.requests) {
             const RequestShape s = request_shape<C::kRows, C::kTile>(p, r);
-            for (int rt = 0; rt < s.row_tiles; ++rt) n += visible_tiles<C::kRows, C::kTile>(p, s, rt);
+            for (int rt = 0; rt < s.row_tiles; ++rt) n += visible_tiles<C::kRows, C::kTile>(p, s, rt) + C::kSetup;
         }
         uint32_t a = n;
 #pragma unroll
@@ -534,10 +538,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         failed = 0;
         const uint64_t units = (uint64_t)total * (uint32_t)p.heads;
         Start s;
-        s.per = units_per_block(units, gridDim.x);
+        s.per = units_per_block<C::kSetup>(units, gridDim.x);
         s.u = (uint64_t)blockIdx.x * s.per;
         s.end = min(s.u + s.per, units);
-        s.request = s.row_tile = s.head = s.tile = 0;
+        s.request = s.row_tile = s.head = s.at = 0;
         if (s.u < s.end) {
             int lo = 0, hi = p.requests;
             while (hi - lo > 1) {
@@ -548,11 +552,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             uint64_t in = s.u - (uint64_t)prefix[lo] * (uint32_t)p.heads;
             s.request = lo;
             while (true) {
-                const uint32_t n = visible_tiles<C::kRows, C::kTile>(p, q, s.row_tile);
+                const uint32_t n = visible_tiles<C::kRows, C::kTile>(p, q, s.row_tile) + C::kSetup;
                 const uint64_t all = (uint64_t)n * (uint32_t)p.heads;
                 if (in < all) {
                     s.head = (int)(in / n);
-                    s.tile = (int)(in - (uint64_t)s.head * n);
+                    s.at = (int)(in - (uint64_t)s.head * n);
                     break;
                 }
                 in -= all;
@@ -568,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     // all 512 columns: they begin at 0, which is what the addresses below take them to do
     if (tmem_base != 0 && tid == 0) atomicOr(p.error, 1u);
     constexpr uint32_t tmem = 0;
-    Walk<C::kRows, C::kTile> &walk = walks[warp];
+    Walk<C::kRows, C::kTile, C::kSetup> &walk = walks[warp];
     const AttentionSegment &w = walk.w;
     if (lane == 0) walk.begin(p, start);
 
