@@ -61,7 +61,7 @@ struct Shape {
     static constexpr int kChunks = kHalf * D / 16 / kLoadThreads;   // 16-code loads of a thread for half a tile
     static constexpr size_t kSmem = kQBytes + 2 * kStages * kKvBytes;
     // registers of the softmax, the converting and the issuing warps
-    static constexpr int kSoftmaxRegs = D == 256 ? 120 : 168, kLoadRegs = D == 256 ? 88 : 48, kIssueRegs = D == 256 ? 64 : 48;
+    static constexpr int kSoftmaxRegs = D == 256 ? 120 : 144, kLoadRegs = D == 256 ? 88 : 64, kIssueRegs = 64;
     static_assert(256 * kSoftmaxRegs + 256 * kLoadRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs, "registers at launch");
     static_assert(kChunks >= 1, "every load thread has work");
     static_assert(kOColumn + kQTiles * D <= 512, "tensor memory");
@@ -247,48 +247,40 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return m;
 }
 
-// A kv tile of one row: scores to weights, as fp16 into the first 32 columns of each half, which `arrive` hands
-// over. left: columns that the row sees (only if `masked`, which is the warp's). Where the largest exponent of
-// some row passes its limit, that row's maximum is raised by as much, its sum and, unless this is the first tile
-// (behind `wait_output`), its output rescaled.
-template <int D, class Wait, class Arrive>
-__device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const Entries<Shape<D>::kBlocks> &entry, float factor, bool masked, int left,
-                                             bool first, RowState &r, Wait wait_output, Arrive arrive) {
-    using C = Shape<D>;
-    uint32_t x[C::kTile / 32][32];
-#pragma unroll
-    for (int c = 0; c < C::kTile / 32; ++c) tmem_ld(x[c], s_at + 32 * c);
-#pragma unroll
-    for (int c = 0; c < C::kTile / 32; ++c) ld_wait(x[c]);        // all of them; the others order their own registers
+// Half a kv tile of one row: scores x to weights w (fp16 pairs). left: columns that the row sees (only if
+// `masked`, which is the warp's). Where the largest exponent of some row passes its limit, that row's maximum is
+// raised by as much, its sum and, unless this is the first half tile (behind `wait_output`), its output rescaled.
+template <int D, class Wait>
+__device__ __forceinline__ void softmax_half(uint32_t (&x)[2][32], uint32_t (&w)[2][16], uint32_t o_at, const float4 *scale,
+                                             const float4 &inverse, float factor, bool masked, int left, bool first, RowState &r,
+                                             Wait wait_output) {
     const float base = kHeadroom - r.top;
-    float4 z;
 #pragma unroll
-    for (int b = 0; b < C::kBlocks; ++b) {
-        if (b % 2 == 0) z = *reinterpret_cast<const float4 *>(&entry.scale[b]);   // of two blocks
-        const float a = factor * (b % 2 ? z.z : z.x), d = (b % 2 ? z.w : z.y) + base;
-        const uint64_t a2 = pair(a, a), d2 = pair(d, d);
-        uint32_t *y = &x[b / 2][b % 2 * 16];
+    for (int c = 0; c < 2; ++c) {
+        const float4 z = scale[c];                                // of two blocks
 #pragma unroll
-        for (int k = 0; k < 16; k += 2) {
+        for (int k = 0; k < 32; k += 2) {
+            const float a = factor * (k < 16 ? z.x : z.z), d = (k < 16 ? z.y : z.w) + base;
             float e0, e1;
-            unpair(fma2(pair(__uint_as_float(y[k]), __uint_as_float(y[k + 1])), a2, d2), e0, e1);
-            y[k] = __float_as_uint(e0);
-            y[k + 1] = __float_as_uint(e1);
+            unpair(fma2(pair(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])), pair(a, a), pair(d, d)), e0, e1);
+            x[c][k] = __float_as_uint(e0);
+            x[c][k + 1] = __float_as_uint(e1);
         }
     }
     if (masked) {
 #pragma unroll
-        for (int k = 0; k < C::kTile; ++k)
+        for (int k = 0; k < kHalf; ++k)
             if (k >= left) x[k / 32][k % 32] = 0xff800000u;
     }
-    float most = -INFINITY;
+    float high[4];
 #pragma unroll
-    for (int c = 0; c < C::kTile / 32; ++c) {
-        float high[2] = {__uint_as_float(x[c][0]), __uint_as_float(x[c][1])};
+    for (int i = 0; i < 4; ++i) {
+        high[i] = __uint_as_float(x[i / 2][i % 2 * 16]);
 #pragma unroll
-        for (int k = 2; k < 32; k += 2) high[k / 2 & 1] = max3(high[k / 2 & 1], __uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1]));
-        most = max3(most, high[0], high[1]);
+        for (int k = 1; k < 15; k += 2) high[i] = max3(high[i], __uint_as_float(x[i / 2][i % 2 * 16 + k]), __uint_as_float(x[i / 2][i % 2 * 16 + k + 1]));
+        high[i] = fmaxf(high[i], __uint_as_float(x[i / 2][i % 2 * 16 + 15]));
     }
+    const float most = fmaxf(max3(high[0], high[1], high[2]), high[3]);
     if (__any_sync(~0u, most > r.limit)) {
         const bool raise = most > r.limit;
         const float by = raise ? most - kHeadroom : 0.f;
@@ -297,7 +289,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const
         r.sum *= f;
         if (raise) r.limit = kRaise + kHeadroom;
 #pragma unroll
-        for (int k = 0; k < C::kTile; ++k) x[k / 32][k % 32] = __float_as_uint(__uint_as_float(x[k / 32][k % 32]) - by);
+        for (int k = 0; k < kHalf; ++k) x[k / 32][k % 32] = __float_as_uint(__uint_as_float(x[k / 32][k % 32]) - by);
         if (!first) {
             wait_output();
             fence_after();
@@ -313,29 +305,20 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_at, uint32_t o_at, const
         }
     }
 #pragma unroll
-    for (int h = 0; h < C::kHalves; ++h) {
+    for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int c = 2 * h; c < 2 * h + 2; ++c) {
-            const float2 inverse = *reinterpret_cast<const float2 *>(&entry.v_inverse[2 * c]);
-            uint32_t w[16];
+        for (int b = 0; b < 2; ++b) {
+            uint64_t part = 0;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                uint64_t part = 0;
-#pragma unroll
-                for (int k = 16 * b; k < 16 * b + 16; k += 2) {
-                    const float e0 = exp2_fast(__uint_as_float(x[c][k])), e1 = exp2_fast(__uint_as_float(x[c][k + 1]));
-                    part = add2(part, pair(e0, e1));
-                    w[k / 2] = pack_half(e0, e1);
-                }
-                float p0, p1;
-                unpair(part, p0, p1);
-                r.sum = fmaf(p0 + p1, b ? inverse.y : inverse.x, r.sum);
+            for (int k = 16 * b; k < 16 * b + 16; k += 2) {
+                const float e0 = exp2_fast(__uint_as_float(x[c][k])), e1 = exp2_fast(__uint_as_float(x[c][k + 1]));
+                part = add2(part, pair(e0, e1));
+                w[c][k / 2] = pack_half(e0, e1);
             }
-            tmem_st16(s_at + h * kHalf + c % 2 * 16, w);
+            float p0, p1;
+            unpair(part, p0, p1);
+            r.sum = fmaf(p0 + p1, c ? (b ? inverse.w : inverse.z) : (b ? inverse.y : inverse.x), r.sum);
         }
-        st_wait();
-        arrive(h);
-    }
 }
 
 // The warp's 32 query rows, rows first .. first + 31 of the request, to fp16 with a power of two per row,
@@ -469,7 +452,8 @@ struct Barriers {
     uint64_t q_full[2], o_full[2];
     uint64_t s_full[2];                       // score buffer
     uint64_t p_full[2][2];                    // query tile; half, or score buffer where there are two
-    uint64_t o_done;                          // another tile is in the output (two score buffers only)
+    uint64_t a_done[2];                       // a tile's first half is in the output (query tile; two halves)
+    uint64_t o_done;                          // a tile is (two score buffers)
 };
 
 template <int D, int FORMAT>
@@ -534,6 +518,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             bar_init(&bars.o_full[i], 1);
         }
         bar_init(&bars.o_done, 1);
+        bar_init(&bars.a_done[0], 1);
+        bar_init(&bars.a_done[1], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
         const uint64_t units = (uint64_t)total * (uint32_t)p.heads;
@@ -610,16 +596,40 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
                 wait.warp(&bars.s_full[buffer], scored.use(buffer));
                 fence_after();
-                // the output holds the tile before: these scores came after it, unless they run two tiles ahead
-                auto output = [&] {
-                    if (C::kScoreBuffers == 2) wait.warp(&bars.o_done, (n_mine & 1) ^ 1);
-                };
-                softmax_tile<D>(s_at + buffer * C::kTile, o_at, entries[n_tile % C::kEntryStages], factor, (t + 1) * C::kTile > least,
-                                limit - t * C::kTile, t == t0, r, output,
-                                [&](int h) {
-                                    fence_before();
-                                    bar_arrive(&bars.p_full[qt][C::kHalves == 2 ? h : buffer]);
-                                });
+                const auto &entry = entries[n_tile % C::kEntryStages];
+                const uint32_t tile = s_at + buffer * C::kTile;
+                uint32_t x[2][32], y[2][16];
+                tmem_ld(x[0], tile);
+                tmem_ld(x[1], tile + 32);
+                ld_wait(x[0]);
+                ld_wait(x[1]);                                    // both: the second wait orders its own registers
+#pragma unroll 1
+                for (int h = 0; h < C::kHalves; ++h) {
+                    const int token = t * C::kTile + h * kHalf;
+                    const uint32_t half = tile + h * kHalf;
+                    // the half tile before is in the output: the second half of a tile waits for the first's product, and
+                    // scores that run two tiles ahead for the tile before; other scores came after it
+                    auto output = [&] {
+                        if (C::kHalves == 2 && h == 1) wait.warp(&bars.a_done[qt], n_mine & 1);
+                        if (C::kScoreBuffers == 2) wait.warp(&bars.o_done, (n_mine & 1) ^ 1);
+                    };
+                    softmax_half<D>(x, y, o_at, reinterpret_cast<const float4 *>(&entry.scale[h * kHalfBlocks]),
+                                    *reinterpret_cast<const float4 *>(&entry.v_inverse[h * kHalfBlocks]), factor, token + kHalf > least,
+                                    limit - token, t == t0 && h == 0, r, output);
+                    if (h + 1 < C::kHalves) {
+                        tmem_ld(x[0], half + kHalf);
+                        tmem_ld(x[1], half + kHalf + 32);
+                    }
+                    tmem_st16(half, y[0]);                        // into columns whose scores have been read
+                    tmem_st16(half + 16, y[1]);
+                    st_wait();
+                    fence_before();
+                    bar_arrive(&bars.p_full[qt][C::kHalves == 2 ? h : buffer]);
+                    if (h + 1 < C::kHalves) {
+                        ld_wait(x[0]);
+                        ld_wait(x[1]);
+                    }
+                }
             }
             const float top = r.top, sum = r.sum;
             wait.warp(&bars.o_full[qt], o_phase);
@@ -795,6 +805,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
 #pragma unroll
                             for (int j = 0; j < kHalf / 16; ++j)
                                 mma_ts(C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, j + h > 0 || i > 0, leader);
+                            if (C::kHalves == 2 && h == 0) commit(&bars.a_done[qt], leader);
                         }
                         if (C::kScoreBuffers == 2) commit(&bars.o_done, leader);
                         if (last) commit(&bars.v_empty[v], leader);
@@ -830,7 +841,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
 
 // The parts of ranges that were cut: a thread block for 16 rows of a range, which begins in block
 // blockIdx.x of the kernel before.
-constexpr int kJoinRows = 16, kJoinWarps = 4;
+constexpr int kJoinRows = 16, kJoinWarps = 16;
 
 template <int D>
 __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const __grid_constant__ QcacheAttentionParams p) {
@@ -843,7 +854,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const __grid_cons
     w.head = z.head;
     w.row0 = z.row0;
     const uint32_t c0 = blockIdx.x;
-    join_parts<D, kJoinWarps, 4>(p, w, first, min(kJoinRows, z.rows - first), c0, (uint32_t)z.last_block, kHeadroom, threadIdx.x / 32,
+    join_parts<D, kJoinWarps, 1>(p, w, first, min(kJoinRows, z.rows - first), c0, (uint32_t)z.last_block, kHeadroom, threadIdx.x / 32,
                                  [&](uint32_t c, int r) { return (2 * (int64_t)c + (c == c0)) * C::kRows + in_tile + r; });
 }
 
