@@ -5,19 +5,20 @@
 // One thread block per SM, on the tcgen05 tensor cores, with up to 256 query rows (rows are query
 // tokens x heads of a group) in two tiles of 128, so that each K and V tile that is brought in and
 // taken to fp16 serves both:
-//   warps 0-3, 4-7   softmax of query tile 0 and 1, one row per thread: half a kv tile (64 scores) from
-//                    tensor memory into registers, weights back into the same columns as fp16, the output
+//   warps 0-3, 4-7   softmax of query tile 0 and 1, one row per thread: a kv tile (64 scores) from tensor
+//                    memory into registers, weights back into the same columns as fp16, the output
 //                    rescaled when the running maximum is raised, the row normalised and written
 //   warps 8-11       K tiles, from global memory through registers to fp16 in shared memory, in the 128-byte
-//                    swizzle, the next half tile's codes on their way meanwhile
+//                    swizzle, the next tile's codes on their way meanwhile
 //   warps 12-15      V tiles
 //   warp 16          issues the matrix instructions: S = Q K^T (both operands from shared memory),
 //                    O += P V (P from tensor memory, V as it lies, tokens x head_dim)
 //   warp 17          looks up blocks and scales of every 16 tokens, several tiles ahead
-// Scores are products of 128 x 128 (64 columns at a time cost the tensor cores as much as 128); weights
-// go in by halves, so that the second half's softmax runs beside the first half's product, and one query
-// tile's softmax beside the other's products. At head_dim 256 the output of one query tile is all that
-// fits beside the scores: kv tiles are 64 tokens, with scores two tiles ahead in two buffers. A second, small kernel joins
+// Scores are computed two kv tiles ahead, into two buffers for each query tile, so that the softmax warps
+// always have a tile at hand while the tensor cores take the last one's weights. Products of 128 x 64 leave
+// a third of the tensor cores' time to the operands' way from shared memory; with tiles of 128 tokens, for
+// which there is one buffer, softmax and products waited for each other and took 4,100 to 5,000 cycles for
+// 256 x 128 scores. A second, small kernel joins
 // the ranges that were cut between thread blocks, over the whole GPU (one thread block alone took 95 us
 // for 256 rows in 19 parts). The softmax warps take
 // registers over from the others. Work is cut as in
@@ -39,29 +40,26 @@ constexpr int kLaunchRegs = 96;
 constexpr int kLoadThreads = kLoadWarps * 32;
 constexpr float kRaise = 8.f, kHeadroom = 7.f;
 
-constexpr int kHalf = 64;                   // tokens that go through the softmax at a time
-constexpr int kHalfBlocks = kHalf / 16;     // their scale entries
+constexpr int kTile = 64;                   // tokens of a kv tile
+constexpr int kBlocks = kTile / 16;         // its scale entries
+constexpr int kEntryTiles = 32 / kBlocks, kEntryStages = 2 * kEntryTiles;   // tiles looked up at a time; held
 
 template <int D>
 struct Shape {
-    // tensor memory, 512 columns: two tiles of scores, and the outputs
+    // tensor memory, 512 columns: two buffers of scores for each query tile, and the outputs
     static constexpr int kQTiles = D == 256 ? 1 : 2;
-    static constexpr int kTile = D == 256 ? 64 : 128, kHalves = kTile / kHalf;   // tokens of a kv tile
-    static constexpr int kSetup = D == 256 ? 3 : 2;           // a segment's queries and its end, in tiles
-    static constexpr int kBlocks = kTile / 16;                // scale entries of a tile
-    static constexpr int kEntryTiles = 32 / kBlocks, kEntryStages = 2 * kEntryTiles;   // looked up at a time; held
-    static constexpr int kScoreBuffers = 2 / kQTiles;         // for each query tile
     static constexpr int kRows = 128 * kQTiles;
-    static constexpr int kOColumn = 2 * kTile;
+    static constexpr int kOColumn = kQTiles * 2 * kTile;
+    static constexpr int kSetup = 3;                          // a segment's queries and its end, in tiles
     static constexpr int kPanels = D < 64 ? 1 : D / 64;       // 64 columns (128 bytes) of fp16 each
-    static constexpr int kStages = 2;                         // tiles of K, of V
+    static constexpr int kStages = D == 256 ? 2 : 4;          // tiles of K, of V
     static constexpr int kQPanel = 128 * 128, kKvPanel = kTile * 128;   // bytes
     static constexpr int kQBytes = kQTiles * kPanels * kQPanel;
     static constexpr int kKvBytes = kPanels * kKvPanel;       // a tile of K, of V
-    static constexpr int kChunks = kHalf * D / 16 / kLoadThreads;   // 16-code loads of a thread for half a tile
+    static constexpr int kChunks = kTile * D / 16 / kLoadThreads;   // 16-code loads of a thread for a tile
     static constexpr size_t kSmem = kQBytes + 2 * kStages * kKvBytes;
     // registers of the softmax, the converting and the issuing warps
-    static constexpr int kSoftmaxRegs = D == 256 ? 120 : 144, kLoadRegs = D == 256 ? 88 : 64, kIssueRegs = 64;
+    static constexpr int kSoftmaxRegs = 120, kLoadRegs = 88, kIssueRegs = 64;
     static_assert(256 * kSoftmaxRegs + 256 * kLoadRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs, "registers at launch");
     static_assert(kChunks >= 1, "every load thread has work");
     static_assert(kOColumn + kQTiles * D <= 512, "tensor memory");
@@ -227,13 +225,12 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 
 // What a tile needs to know of each 16 tokens: the scales, and where their codes begin in a head's plane, in
 // bytes (negative: in a block that is not there, or past the request's tokens).
-template <int BLOCKS>
 struct alignas(16) Entries {      // read 16 bytes at a time
-    float2 scale[BLOCKS];         // k_scale, log2 v_scale
-    float v_inverse[BLOCKS];
-    int64_t offset[BLOCKS];
+    float2 scale[kBlocks];        // k_scale, log2 v_scale
+    float v_inverse[kBlocks];
+    int64_t offset[kBlocks];
 };
-static_assert(sizeof(Entries<8>) % 16 == 0 && sizeof(Entries<4>) % 16 == 0, "every tile's entries are aligned alike");
+static_assert(sizeof(Entries) % 16 == 0 && kBlocks % 4 == 0, "every tile's entries are aligned alike");
 
 // What a softmax thread keeps of its row. The weights of a tile are 2^(t - top + headroom); `limit` is the
 // largest exponent that is let pass: without bound until the row has seen a token, which then sets `top`.
@@ -247,11 +244,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return m;
 }
 
-// Half a kv tile of one row: scores x to weights w (fp16 pairs). left: columns that the row sees (only if
+// A kv tile of one row: scores x to weights w (fp16 pairs). left: columns that the row sees (only if
 // `masked`, which is the warp's). Where the largest exponent of some row passes its limit, that row's maximum is
-// raised by as much, its sum and, unless this is the first half tile (behind `wait_output`), its output rescaled.
+// raised by as much, its sum and, unless this is the first tile (behind `wait_output`), its output rescaled.
 template <int D, class Wait>
-__device__ __forceinline__ void softmax_half(uint32_t (&x)[2][32], uint32_t (&w)[2][16], uint32_t o_at, const float4 *scale,
+__device__ __forceinline__ void softmax_tile(uint32_t (&x)[2][32], uint32_t (&w)[2][16], uint32_t o_at, const float4 *scale,
                                              const float4 &inverse, float factor, bool masked, int left, bool first, RowState &r,
                                              Wait wait_output) {
     const float base = kHeadroom - r.top;
@@ -269,7 +266,7 @@ __device__ __forceinline__ void softmax_half(uint32_t (&x)[2][32], uint32_t (&w)
     }
     if (masked) {
 #pragma unroll
-        for (int k = 0; k < kHalf; ++k)
+        for (int k = 0; k < kTile; ++k)
             if (k >= left) x[k / 32][k % 32] = 0xff800000u;
     }
     float high[4];
@@ -289,7 +286,7 @@ __device__ __forceinline__ void softmax_half(uint32_t (&x)[2][32], uint32_t (&w)
         r.sum *= f;
         if (raise) r.limit = kRaise + kHeadroom;
 #pragma unroll
-        for (int k = 0; k < kHalf; ++k) x[k / 32][k % 32] = __float_as_uint(__uint_as_float(x[k / 32][k % 32]) - by);
+        for (int k = 0; k < kTile; ++k) x[k / 32][k % 32] = __float_as_uint(__uint_as_float(x[k / 32][k % 32]) - by);
         if (!first) {
             wait_output();
             fence_after();
@@ -447,13 +444,11 @@ struct Parity {
 };
 
 struct Barriers {
-    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
-    uint64_t entry_full[16], entry_empty[16];
+    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
+    uint64_t entry_full[kEntryStages], entry_empty[kEntryStages];
     uint64_t q_full[2], o_full[2];
-    uint64_t s_full[2];                       // score buffer
-    uint64_t p_full[2][2];                    // query tile; half, or score buffer where there are two
-    uint64_t a_done[2];                       // a tile's first half is in the output (query tile; two halves)
-    uint64_t o_done;                          // a tile is (two score buffers)
+    uint64_t s_full[2][2], p_full[2][2];      // query tile, score buffer
+    uint64_t o_done[2];                       // another tile is in the output
 };
 
 template <int D, int FORMAT>
@@ -461,10 +456,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     using C = Shape<D>;
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ Barriers bars;
-    __shared__ Entries<C::kBlocks> entries[C::kEntryStages];
+    __shared__ Entries entries[kEntryStages];
     __shared__ uint32_t scan[kThreads / 32];
     __shared__ Start start;
-    __shared__ Walk<C::kRows, C::kTile, C::kSetup> walks[kThreads / 32];
+    __shared__ Walk<C::kRows, kTile, C::kSetup> walks[kThreads / 32];
     __shared__ uint32_t tmem_base;
     __shared__ int failed;
     unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + C::kStages * C::kKvBytes;
@@ -477,8 +472,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         const int r = r0 + tid;
         uint32_t n = 0;
         if (r < p.requests) {
-            const RequestShape s = request_shape<C::kRows, C::kTile>(p, r);
-            for (int rt = 0; rt < s.row_tiles; ++rt) n += visible_tiles<C::kRows, C::kTile>(p, s, rt) + C::kSetup;
+            const RequestShape s = request_shape<C::kRows, kTile>(p, r);
+            for (int rt = 0; rt < s.row_tiles; ++rt) n += visible_tiles<C::kRows, kTile>(p, s, rt) + C::kSetup;
         }
         uint32_t a = n;
 #pragma unroll
@@ -507,19 +502,19 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             bar_init(&bars.k_empty[i], 1);
             bar_init(&bars.v_empty[i], 1);
         }
-        for (int i = 0; i < C::kEntryStages; ++i) {
+        for (int i = 0; i < kEntryStages; ++i) {
             bar_init(&bars.entry_full[i], 1);
             bar_init(&bars.entry_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
-            for (int j = 0; j < 2; ++j) bar_init(&bars.p_full[i][j], 128);
-            bar_init(&bars.s_full[i], 1);
+            for (int j = 0; j < 2; ++j) {
+                bar_init(&bars.s_full[i][j], 1);
+                bar_init(&bars.p_full[i][j], 128);
+            }
             bar_init(&bars.q_full[i], 128);
             bar_init(&bars.o_full[i], 1);
+            bar_init(&bars.o_done[i], 1);
         }
-        bar_init(&bars.o_done, 1);
-        bar_init(&bars.a_done[0], 1);
-        bar_init(&bars.a_done[1], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
         const uint64_t units = (uint64_t)total * (uint32_t)p.heads;
@@ -534,11 +529,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 const int mid = (lo + hi) >> 1;
                 if ((uint64_t)prefix[mid] * (uint32_t)p.heads <= s.u) lo = mid; else hi = mid;
             }
-            const RequestShape q = request_shape<C::kRows, C::kTile>(p, lo);
+            const RequestShape q = request_shape<C::kRows, kTile>(p, lo);
             uint64_t in = s.u - (uint64_t)prefix[lo] * (uint32_t)p.heads;
             s.request = lo;
             while (true) {
-                const uint32_t n = visible_tiles<C::kRows, C::kTile>(p, q, s.row_tile) + C::kSetup;
+                const uint32_t n = visible_tiles<C::kRows, kTile>(p, q, s.row_tile) + C::kSetup;
                 const uint64_t all = (uint64_t)n * (uint32_t)p.heads;
                 if (in < all) {
                     s.head = (int)(in / n);
@@ -551,6 +546,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         }
         start = s;
     }
+    // the joining kernel may be set up from now on; it waits for this one's results by itself
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     fence_before();
     __syncthreads();
     fence_after();
@@ -558,7 +555,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     // all 512 columns: they begin at 0, which is what the addresses below take them to do
     if (tmem_base != 0 && tid == 0) atomicOr(p.error, 1u);
     constexpr uint32_t tmem = 0;
-    Walk<C::kRows, C::kTile, C::kSetup> &walk = walks[warp];
+    Walk<C::kRows, kTile, C::kSetup> &walk = walks[warp];
     const AttentionSegment &w = walk.w;
     if (lane == 0) walk.begin(p, start);
 
@@ -567,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftmaxRegs));
         const int qt = warp / 4, row = tid % 128;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
-        const uint32_t s_at = tmem + lanes, o_at = tmem + lanes + C::kOColumn + qt * D;
+        const uint32_t s_at = tmem + lanes + qt * 2 * kTile, o_at = tmem + lanes + C::kOColumn + qt * D;
         uint32_t n_tile = 0;          // kv tiles of the block so far
         uint32_t n_mine = 0, o_phase = 0;       // those with rows in this query tile
         Parity scored;
@@ -591,45 +588,26 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             RowState r{0.f, 0.f, -INFINITY};
             const int t0 = w.t0, t1 = w.t1;
             for (int t = t0; t < t1; ++t, ++n_tile, ++n_mine) {
-                // one buffer for each query tile, or two that take turns
-                const uint32_t buffer = C::kQTiles == 2 ? qt : (t - t0) & 1;
-                wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
-                wait.warp(&bars.s_full[buffer], scored.use(buffer));
+                const uint32_t buffer = (t - t0) & 1;
+                wait.warp(&bars.entry_full[n_tile % kEntryStages], n_tile / kEntryStages & 1);
+                wait.warp(&bars.s_full[qt][buffer], scored.use(buffer));
                 fence_after();
-                const auto &entry = entries[n_tile % C::kEntryStages];
-                const uint32_t tile = s_at + buffer * C::kTile;
+                const Entries &entry = entries[n_tile % kEntryStages];
+                const uint32_t tile = s_at + buffer * kTile;
                 uint32_t x[2][32], y[2][16];
                 tmem_ld(x[0], tile);
                 tmem_ld(x[1], tile + 32);
                 ld_wait(x[0]);
                 ld_wait(x[1]);                                    // both: the second wait orders its own registers
-#pragma unroll 1
-                for (int h = 0; h < C::kHalves; ++h) {
-                    const int token = t * C::kTile + h * kHalf;
-                    const uint32_t half = tile + h * kHalf;
-                    // the half tile before is in the output: the second half of a tile waits for the first's product, and
-                    // scores that run two tiles ahead for the tile before; other scores came after it
-                    auto output = [&] {
-                        if (C::kHalves == 2 && h == 1) wait.warp(&bars.a_done[qt], n_mine & 1);
-                        if (C::kScoreBuffers == 2) wait.warp(&bars.o_done, (n_mine & 1) ^ 1);
-                    };
-                    softmax_half<D>(x, y, o_at, reinterpret_cast<const float4 *>(&entry.scale[h * kHalfBlocks]),
-                                    *reinterpret_cast<const float4 *>(&entry.v_inverse[h * kHalfBlocks]), factor, token + kHalf > least,
-                                    limit - token, t == t0 && h == 0, r, output);
-                    if (h + 1 < C::kHalves) {
-                        tmem_ld(x[0], half + kHalf);
-                        tmem_ld(x[1], half + kHalf + 32);
-                    }
-                    tmem_st16(half, y[0]);                        // into columns whose scores have been read
-                    tmem_st16(half + 16, y[1]);
-                    st_wait();
-                    fence_before();
-                    bar_arrive(&bars.p_full[qt][C::kHalves == 2 ? h : buffer]);
-                    if (h + 1 < C::kHalves) {
-                        ld_wait(x[0]);
-                        ld_wait(x[1]);
-                    }
-                }
+                softmax_tile<D>(x, y, o_at, reinterpret_cast<const float4 *>(entry.scale), *reinterpret_cast<const float4 *>(entry.v_inverse),
+                                factor, (t + 1) * kTile > least, limit - t * kTile, t == t0, r,
+                                // the scores run ahead of the products: the tile before may not be in the output yet
+                                [&] { wait.warp(&bars.o_done[qt], (n_mine & 1) ^ 1); });
+                tmem_st16(tile, y[0]);                            // into columns whose scores have been read
+                tmem_st16(tile + 16, y[1]);
+                st_wait();
+                fence_before();
+                bar_arrive(&bars.p_full[qt][buffer]);
             }
             const float top = r.top, sum = r.sum;
             wait.warp(&bars.o_full[qt], o_phase);
@@ -685,12 +663,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         while (walk.next(p)) {
             const int tiles = w.t1 - w.t0;
             const uint8_t *head = codes + (int64_t)w.head * p.stride_head;
-            uint4 x[C::kChunks];
-            // half h of the segment's tile i; a token past the request's, or in a block that is not there, is zero
-            auto fetch = [&](int i, int h) {
-                if (h == 0) wait.warp(&bars.entry_full[(n_tile + i) % C::kEntryStages], (n_tile + i) / C::kEntryStages & 1);
-                const int64_t *offset = entries[(n_tile + i) % C::kEntryStages].offset + h * kHalfBlocks;
-                const int left = w.kv - (w.t0 + i) * C::kTile - h * kHalf;
+            // the segment's tile i; a token past the request's, or in a block that is not there, is zero
+            auto fetch = [&](uint4 (&x)[C::kChunks], int i) {
+                wait.warp(&bars.entry_full[(n_tile + i) % kEntryStages], (n_tile + i) / kEntryStages & 1);
+                const int64_t *offset = entries[(n_tile + i) % kEntryStages].offset;
+                const int left = w.kv - (w.t0 + i) * kTile;
 #pragma unroll
                 for (int c = 0; c < C::kChunks; ++c) {
                     const int r = row + c * kRowStep;
@@ -699,32 +676,40 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                     if (at >= 0 && r < left) x[c] = load_codes(head + at + (kRowStep % 16 ? c % 2 * 8 * p.stride_token : 0));
                 }
             };
-            fetch(0, 0);
-            for (int i = 0; i < tiles; ++i) {
-#pragma unroll 1
-                for (int h = 0; h < C::kHalves; ++h) {
-                    const uint32_t stage = i % C::kStages;
-                    const int to = stage * C::kKvBytes + h * kHalf * 128;
-                    if (h == 0) wait.warp(is_v ? &bars.v_empty[stage] : &bars.k_empty[stage], freed.use(stage) ^ 1);
+            auto convert = [&](uint4 (&x)[C::kChunks], int i) {
+                const uint32_t stage = i % C::kStages;
+                const int to = stage * C::kKvBytes;
+                wait.warp(is_v ? &bars.v_empty[stage] : &bars.k_empty[stage], freed.use(stage) ^ 1);
 #pragma unroll
-                    for (int c = 0; c < C::kChunks; ++c) {
-                        if (swap) x[c] = make_uint4(x[c].z, x[c].w, x[c].x, x[c].y);
-                        uint4 y0, y1;
-                        codes_to_half<FORMAT>(x[c].x, y0.x, y0.y);
-                        codes_to_half<FORMAT>(x[c].y, y0.z, y0.w);
-                        codes_to_half<FORMAT>(x[c].z, y1.x, y1.y);
-                        codes_to_half<FORMAT>(x[c].w, y1.z, y1.w);
-                        *reinterpret_cast<uint4 *>(to0 + to + c * kRowStep * 128) = y0;
-                        *reinterpret_cast<uint4 *>(to1 + to + c * kRowStep * 128) = y1;
-                    }
-                    if (h + 1 < C::kHalves) {
-                        fetch(i, h + 1);
-                    } else {
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(is_v ? &bars.v_full[stage] : &bars.k_full[stage]);
-                        if (i + 1 < tiles) fetch(i + 1, 0);
-                    }
+                for (int c = 0; c < C::kChunks; ++c) {
+                    if (swap) x[c] = make_uint4(x[c].z, x[c].w, x[c].x, x[c].y);
+                    uint4 y0, y1;
+                    codes_to_half<FORMAT>(x[c].x, y0.x, y0.y);
+                    codes_to_half<FORMAT>(x[c].y, y0.z, y0.w);
+                    codes_to_half<FORMAT>(x[c].z, y1.x, y1.y);
+                    codes_to_half<FORMAT>(x[c].w, y1.z, y1.w);
+                    *reinterpret_cast<uint4 *>(to0 + to + c * kRowStep * 128) = y0;
+                    *reinterpret_cast<uint4 *>(to1 + to + c * kRowStep * 128) = y1;
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) bar_arrive(is_v ? &bars.v_full[stage] : &bars.k_full[stage]);
+            };
+            // a tile's codes are on their way while the one before is converted, where there are registers for both
+            uint4 x[C::kChunks], y[C::kChunks];
+            fetch(x, 0);
+            if constexpr (C::kChunks <= 4) {
+                for (int i = 0; i < tiles; i += 2) {
+                    if (i + 1 < tiles) fetch(y, i + 1);
+                    convert(x, i);
+                    if (i + 1 == tiles) break;
+                    if (i + 2 < tiles) fetch(x, i + 2);
+                    convert(y, i + 1);
+                }
+            } else {
+                for (int i = 0; i < tiles; ++i) {
+                    convert(x, i);
+                    if (i + 1 < tiles) fetch(x, i + 1);
                 }
             }
             n_tile += tiles;
@@ -732,17 +717,17 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kIssueRegs));
       if (warp == kEntryWarp) {
-        // ------------------------------------------------ blocks and scales, C::kEntryTiles tiles at a time
+        // ------------------------------------------------ blocks and scales, kEntryTiles tiles at a time
         uint32_t n_tile = 0;
         while (walk.next(p)) {
             for (int t = w.t0; t < w.t1;) {
-                // up to the next multiple of C::kEntryTiles of the count, so that the stages stay together
-                const int n = min(w.t1 - t, (int)(C::kEntryTiles - n_tile % C::kEntryTiles));
-                const int mine = lane / C::kBlocks, group = lane % C::kBlocks;
-                const uint32_t slot = (n_tile + mine) % C::kEntryStages;
+                // up to the next multiple of kEntryTiles of the count, so that the stages stay together
+                const int n = min(w.t1 - t, (int)(kEntryTiles - n_tile % kEntryTiles));
+                const int mine = lane / kBlocks, group = lane % kBlocks;
+                const uint32_t slot = (n_tile + mine) % kEntryStages;
                 if (mine < n) {
-                    wait(&bars.entry_empty[slot], ((n_tile + mine) / C::kEntryStages & 1) ^ 1);
-                    const int64_t token = (int64_t)(t + mine) * C::kTile + group * 16;
+                    wait(&bars.entry_empty[slot], ((n_tile + mine) / kEntryStages & 1) ^ 1);
+                    const int64_t token = (int64_t)(t + mine) * kTile + group * 16;
                     const BlockEntry b = block_entry(p, w.request, w.head, token, w.kv);
                     // an absent block's tokens get weight 2^-inf
                     entries[slot].scale[group] = make_float2(b.k_scale, b.block < 0 ? -INFINITY : b.v_log2);
@@ -758,7 +743,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         }
       } else if (warp == kMmaWarp) {
         // ------------------------------------------------ the matrix instructions
-        constexpr uint32_t s_instruction = instruction(128, C::kTile, false), o_instruction = instruction(128, D, true);
+        constexpr uint32_t s_instruction = instruction(128, kTile, false), o_instruction = instruction(128, D, true);
         const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
         const uint32_t leader = elect();
         uint32_t n_tile = 0, segment = 0, second = 0;            // second: segments with rows in the second query tile
@@ -769,9 +754,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             const uint32_t a = operand_lo(q_at + qt * C::kPanels * C::kQPanel, 16), b = operand_lo(k_at + stage * C::kKvBytes, 16);
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
-                mma_ss(buffer * C::kTile, operand(a + k / 4 * (C::kQPanel / 16) + k % 4 * 2), operand(b + k / 4 * (C::kKvPanel / 16) + k % 4 * 2),
-                       s_instruction, k > 0, leader);
-            commit(&bars.s_full[buffer], leader);
+                mma_ss((qt * 2 + buffer) * kTile, operand(a + k / 4 * (C::kQPanel / 16) + k % 4 * 2),
+                       operand(b + k / 4 * (C::kKvPanel / 16) + k % 4 * 2), s_instruction, k > 0, leader);
+            commit(&bars.s_full[qt][buffer], leader);
         };
         while (__any_sync(~0u, walk.next(p))) {
             if (w.t0 == 0 && w.t1 < w.tiles) {
@@ -785,44 +770,37 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             const bool both = C::kQTiles == 2 && __any_sync(~0u, w.rows - w.row_tile * C::kRows > 128);
             wait.warp(&bars.q_full[0], segment++ & 1);
             if (both) wait.warp(&bars.q_full[1], second++ & 1);
-            constexpr int kAhead = C::kScoreBuffers;              // kv tiles that the scores are ahead
-            // One query tile's products after the other's: while they run, the other is in its softmax.
-            for (int i = -kAhead; __any_sync(~0u, i < tiles); ++i) {
+            // Scores two tiles ahead of the products, one query tile after the other.
+            for (int i = -2; __any_sync(~0u, i < tiles); ++i) {
+                const uint32_t buffer = i & 1, v = i & (C::kStages - 1), k = (i + 2) & (C::kStages - 1);
+                const bool ahead = __any_sync(~0u, i + 2 < tiles);
 #pragma unroll
                 for (int qt = 0; qt < C::kQTiles; ++qt) {
                     if (qt == 1 && !both) break;
                     const bool last = qt == 1 || !both;           // that reads this K and V
-                    const uint32_t buffer = C::kQTiles == 2 ? qt : i & 1;
                     if (i >= 0) {
-                        const uint32_t v = i % C::kStages;
                         if (qt == 0) wait.warp(&bars.v_full[v], v_full.use(v));
+                        wait.warp(&bars.p_full[qt][buffer], weighted[qt].use(buffer));
+                        fence_after();
+                        const uint32_t a = (qt * 2 + buffer) * kTile, b = operand_lo(v_at + v * C::kKvBytes, C::kKvPanel);
 #pragma unroll
-                        for (int h = 0; h < C::kHalves; ++h) {
-                            const uint32_t q = C::kHalves == 2 ? h : buffer;
-                            wait.warp(&bars.p_full[qt][q], weighted[qt].use(q));
-                            fence_after();
-                            const uint32_t a = buffer * C::kTile + h * kHalf, b = operand_lo(v_at + v * C::kKvBytes + h * kHalf * 128, C::kKvPanel);
-#pragma unroll
-                            for (int j = 0; j < kHalf / 16; ++j)
-                                mma_ts(C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, j + h > 0 || i > 0, leader);
-                            if (C::kHalves == 2 && h == 0) commit(&bars.a_done[qt], leader);
-                        }
-                        if (C::kScoreBuffers == 2) commit(&bars.o_done, leader);
+                        for (int j = 0; j < kTile / 16; ++j)
+                            mma_ts(C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, j > 0 || i > 0, leader);
+                        commit(&bars.o_done[qt], leader);
                         if (last) commit(&bars.v_empty[v], leader);
                         if (__any_sync(~0u, i + 1 == tiles)) commit(&bars.o_full[qt], leader);
-                        // every softmax thread has read the tile's entries, and so have the copies long before
+                        // every softmax thread has read the tile's entries, and so have the loads long before
                         if (last) {
-                            if (leader) bar_arrive(&bars.entry_empty[n_tile % C::kEntryStages]);
+                            if (leader) bar_arrive(&bars.entry_empty[n_tile % kEntryStages]);
                             ++n_tile;
                         }
                     }
-                    if (__any_sync(~0u, i + kAhead < tiles)) {
-                        const uint32_t k = (i + kAhead) % C::kStages;
+                    if (ahead) {
                         if (qt == 0) {
                             wait.warp(&bars.k_full[k], k_full.use(k));
                             fence_after();
                         }
-                        scores(qt, C::kQTiles == 2 ? qt : k, k);
+                        scores(qt, buffer, k);
                         if (last) commit(&bars.k_empty[k], leader);
                     }
                 }
@@ -839,9 +817,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512));
 }
 
-// The parts of ranges that were cut: a thread block for 16 rows of a range, which begins in block
+// The parts of ranges that were cut: a thread block for 8 rows of a range, which begins in block
 // blockIdx.x of the kernel before.
-constexpr int kJoinRows = 16, kJoinWarps = 16;
+constexpr int kJoinRows = 8, kJoinWarps = 8;
 
 template <int D>
 __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const __grid_constant__ QcacheAttentionParams p) {
