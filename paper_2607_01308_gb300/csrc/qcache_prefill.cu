@@ -436,6 +436,7 @@ struct Walk {
 // tensor instructions want.
 struct Parity {
     uint32_t bits = 0;
+    __device__ __forceinline__ uint32_t peek(uint32_t stage) const { return bits >> stage & 1; }
     __device__ __forceinline__ uint32_t use(uint32_t stage) {
         const uint32_t p = bits >> stage & 1;
         bits ^= 1u << stage;
@@ -444,11 +445,12 @@ struct Parity {
 };
 
 struct Barriers {
-    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
-    uint64_t entry_full[kEntryStages], entry_empty[kEntryStages];
+    // A step brings the K tile of the scores and the V tile of the weights, two tiles behind, in one stage.
+    uint64_t kv_full[4], kv_empty[4];
+    uint64_t entry_full[kEntryStages], entry_empty[2];   // tiles; half of the stages
     uint64_t q_full[2], o_full[2];
     uint64_t s_full[2][2], p_full[2][2];      // query tile, score buffer
-    uint64_t o_done[2];                       // another tile is in the output
+    uint64_t o_done[2];                       // all but the segment's last tile is in the output
 };
 
 template <int D, int FORMAT>
@@ -497,15 +499,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     }
     if (tid == 0) {
         for (int i = 0; i < C::kStages; ++i) {
-            bar_init(&bars.k_full[i], kLoadWarps);
-            bar_init(&bars.v_full[i], kLoadWarps);
-            bar_init(&bars.k_empty[i], 1);
-            bar_init(&bars.v_empty[i], 1);
+            bar_init(&bars.kv_full[i], 2 * kLoadWarps);
+            bar_init(&bars.kv_empty[i], 1);
         }
-        for (int i = 0; i < kEntryStages; ++i) {
-            bar_init(&bars.entry_full[i], 1);
-            bar_init(&bars.entry_empty[i], 1);
-        }
+        for (int i = 0; i < kEntryStages; ++i) bar_init(&bars.entry_full[i], 1);
         for (int i = 0; i < 2; ++i) {
             for (int j = 0; j < 2; ++j) {
                 bar_init(&bars.s_full[i][j], 1);
@@ -514,6 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             bar_init(&bars.q_full[i], 128);
             bar_init(&bars.o_full[i], 1);
             bar_init(&bars.o_done[i], 1);
+            bar_init(&bars.entry_empty[i], 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
@@ -566,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_at = tmem + lanes + qt * 2 * kTile, o_at = tmem + lanes + C::kOColumn + qt * D;
         uint32_t n_tile = 0;          // kv tiles of the block so far
-        uint32_t n_mine = 0, o_phase = 0;       // those with rows in this query tile
+        uint32_t o_phase = 0, done = 0;
         Parity scored;
         while (walk.next(p)) {
             const int first = w.row_tile * C::kRows + qt * 128;   // of the tile, among the request's rows
@@ -587,7 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             const int least = __reduce_min_sync(~0u, limit);      // of the warp's rows
             RowState r{0.f, 0.f, -INFINITY};
             const int t0 = w.t0, t1 = w.t1;
-            for (int t = t0; t < t1; ++t, ++n_tile, ++n_mine) {
+            for (int t = t0; t < t1; ++t, ++n_tile) {
                 const uint32_t buffer = (t - t0) & 1;
                 wait.warp(&bars.entry_full[n_tile % kEntryStages], n_tile / kEntryStages & 1);
                 wait.warp(&bars.s_full[qt][buffer], scored.use(buffer));
@@ -601,14 +599,18 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 ld_wait(x[1]);                                    // both: the second wait orders its own registers
                 softmax_tile<D>(x, y, o_at, reinterpret_cast<const float4 *>(entry.scale), *reinterpret_cast<const float4 *>(entry.v_inverse),
                                 factor, (t + 1) * kTile > least, limit - t * kTile, t == t0, r,
-                                // the scores run ahead of the products: the tile before may not be in the output yet
-                                [&] { wait.warp(&bars.o_done[qt], (n_mine & 1) ^ 1); });
+                                // the tile before is in the output when the next tile's scores are there, which came after it
+                                [&] {
+                                    if (t + 1 < t1) wait.warp(&bars.s_full[qt][buffer ^ 1], scored.peek(buffer ^ 1));
+                                    else wait.warp(&bars.o_done[qt], done);
+                                });
                 tmem_st16(tile, y[0]);                            // into columns whose scores have been read
                 tmem_st16(tile + 16, y[1]);
                 st_wait();
                 fence_before();
                 bar_arrive(&bars.p_full[qt][buffer]);
             }
+            if (t1 - t0 > 1) done ^= 1;
             const float top = r.top, sum = r.sum;
             wait.warp(&bars.o_full[qt], o_phase);
             o_phase ^= 1;
@@ -676,10 +678,21 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                     if (at >= 0 && r < left) x[c] = load_codes(head + at + (kRowStep % 16 ? c % 2 * 8 * p.stride_token : 0));
                 }
             };
+            auto begin_step = [&](int step) {
+                const uint32_t stage = step % C::kStages;
+                wait.warp(&bars.kv_empty[stage], freed.use(stage) ^ 1);
+                return stage;
+            };
+            auto end_step = [&](int step) {
+                __syncwarp();
+                if (lane == 0) bar_arrive(&bars.kv_full[step % C::kStages]);
+            };
+            auto empty_step = [&](int step) {                     // V has none in the first two steps, K in the last two
+                begin_step(step);
+                end_step(step);
+            };
             auto convert = [&](uint4 (&x)[C::kChunks], int i) {
-                const uint32_t stage = i % C::kStages;
-                const int to = stage * C::kKvBytes;
-                wait.warp(is_v ? &bars.v_empty[stage] : &bars.k_empty[stage], freed.use(stage) ^ 1);
+                const int to = begin_step(is_v ? i + 2 : i) * C::kKvBytes;
 #pragma unroll
                 for (int c = 0; c < C::kChunks; ++c) {
                     if (swap) x[c] = make_uint4(x[c].z, x[c].w, x[c].x, x[c].y);
@@ -692,12 +705,15 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                     *reinterpret_cast<uint4 *>(to1 + to + c * kRowStep * 128) = y1;
                 }
                 fence_async_smem();
-                __syncwarp();
-                if (lane == 0) bar_arrive(is_v ? &bars.v_full[stage] : &bars.k_full[stage]);
+                end_step(is_v ? i + 2 : i);
             };
             // a tile's codes are on their way while the one before is converted, where there are registers for both
             uint4 x[C::kChunks], y[C::kChunks];
             fetch(x, 0);
+            if (is_v) {
+                empty_step(0);
+                empty_step(1);
+            }
             if constexpr (C::kChunks <= 4) {
                 for (int i = 0; i < tiles; i += 2) {
                     if (i + 1 < tiles) fetch(y, i + 1);
@@ -712,8 +728,14 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                     if (i + 1 < tiles) fetch(x, i + 1);
                 }
             }
+            if (!is_v) {
+                empty_step(tiles);
+                empty_step(tiles + 1);
+            }
             n_tile += tiles;
         }
+        // no arrival of the tensor cores is under way when the block ends
+        for (int stage = 0; stage < C::kStages; ++stage) wait.warp(&bars.kv_empty[stage], freed.use(stage) ^ 1);
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kIssueRegs));
       if (warp == kEntryWarp) {
@@ -724,9 +746,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 // up to the next multiple of kEntryTiles of the count, so that the stages stay together
                 const int n = min(w.t1 - t, (int)(kEntryTiles - n_tile % kEntryTiles));
                 const int mine = lane / kBlocks, group = lane % kBlocks;
-                const uint32_t slot = (n_tile + mine) % kEntryStages;
+                const uint32_t half = n_tile / kEntryTiles % 2, slot = (n_tile + mine) % kEntryStages;
+                // the first tile of a half of the stages waits for that half
+                if (n_tile % kEntryTiles == 0) wait.warp(&bars.entry_empty[half], (n_tile / kEntryStages & 1) ^ 1);
                 if (mine < n) {
-                    wait(&bars.entry_empty[slot], ((n_tile + mine) / kEntryStages & 1) ^ 1);
                     const int64_t token = (int64_t)(t + mine) * kTile + group * 16;
                     const BlockEntry b = block_entry(p, w.request, w.head, token, w.kv);
                     // an absent block's tokens get weight 2^-inf
@@ -747,7 +770,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
         const uint32_t leader = elect();
         uint32_t n_tile = 0, segment = 0, second = 0;            // second: segments with rows in the second query tile
-        Parity k_full, v_full, weighted[2];
+        Parity filled, weighted[2];
         bool split = false;
         // scores of a query tile with the K tile in `stage`
         auto scores = [&](int qt, uint32_t buffer, uint32_t stage) {
@@ -772,37 +795,32 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             if (both) wait.warp(&bars.q_full[1], second++ & 1);
             // Scores two tiles ahead of the products, one query tile after the other.
             for (int i = -2; __any_sync(~0u, i < tiles); ++i) {
-                const uint32_t buffer = i & 1, v = i & (C::kStages - 1), k = (i + 2) & (C::kStages - 1);
+                const uint32_t buffer = i & 1, stage = (i + 2) & (C::kStages - 1);
                 const bool ahead = __any_sync(~0u, i + 2 < tiles);
+                wait.warp(&bars.kv_full[stage], filled.use(stage));
+                fence_after();
 #pragma unroll
                 for (int qt = 0; qt < C::kQTiles; ++qt) {
                     if (qt == 1 && !both) break;
-                    const bool last = qt == 1 || !both;           // that reads this K and V
                     if (i >= 0) {
-                        if (qt == 0) wait.warp(&bars.v_full[v], v_full.use(v));
                         wait.warp(&bars.p_full[qt][buffer], weighted[qt].use(buffer));
                         fence_after();
-                        const uint32_t a = (qt * 2 + buffer) * kTile, b = operand_lo(v_at + v * C::kKvBytes, C::kKvPanel);
+                        const uint32_t a = (qt * 2 + buffer) * kTile, b = operand_lo(v_at + stage * C::kKvBytes, C::kKvPanel);
 #pragma unroll
                         for (int j = 0; j < kTile / 16; ++j)
                             mma_ts(C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, j > 0 || i > 0, leader);
-                        commit(&bars.o_done[qt], leader);
-                        if (last) commit(&bars.v_empty[v], leader);
-                        if (__any_sync(~0u, i + 1 == tiles)) commit(&bars.o_full[qt], leader);
-                        // every softmax thread has read the tile's entries, and so have the loads long before
-                        if (last) {
-                            if (leader) bar_arrive(&bars.entry_empty[n_tile % kEntryStages]);
-                            ++n_tile;
+                        if (!ahead) {
+                            if (__any_sync(~0u, i + 2 == tiles)) commit(&bars.o_done[qt], leader);
+                            else commit(&bars.o_full[qt], leader);
                         }
                     }
-                    if (ahead) {
-                        if (qt == 0) {
-                            wait.warp(&bars.k_full[k], k_full.use(k));
-                            fence_after();
-                        }
-                        scores(qt, buffer, k);
-                        if (last) commit(&bars.k_empty[k], leader);
-                    }
+                    if (ahead) scores(qt, buffer, stage);
+                }
+                commit(&bars.kv_empty[stage], leader);
+                if (i >= 0) {
+                    // every softmax thread has read the tile's entries, and so have the loads long before
+                    if (n_tile % kEntryTiles == kEntryTiles - 1 && leader) bar_arrive(&bars.entry_empty[n_tile / kEntryTiles % 2]);
+                    ++n_tile;
                 }
             }
         }
