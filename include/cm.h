@@ -436,7 +436,8 @@ cm_status cm_measure_int_alu(int32_t device, double *xor3_tops, double *compress
  *     cm_qcache_schedule   block tables, slots and row starts from the requests' lengths
  *     cm_qcache_append     K and V rows (a render's, or a layer's new tokens) into their slots
  *     cm_qcache_attend     softmax(scale q K^T) V over each request's own tokens
- * All three enqueue one kernel on `stream` and return without waiting; they allocate nothing and
+ * Each enqueues one kernel on `stream` (cm_qcache_attend two when a request may bring more than 16
+ * query rows to a kv head) and returns without waiting; they allocate nothing and
  * keep nothing between calls, so they can be captured in a CUDA graph. Lengths, tables and slots
  * are DEVICE arrays that the host never reads; entries that name no block of the pool, and lengths
  * beyond the buffers, are left out rather than followed. Distinct arguments must not overlap
@@ -544,8 +545,9 @@ typedef struct cm_qcache_query {
  * anything. Sums and softmax statistics are fp32, weights fp16, the result is rounded once to bf16.
  * Bit for bit reproducible on one GPU.
  *   workspace   DEVICE, 16-byte aligned, at least cm_qcache_workspace() bytes: zeroed by the caller
- *               once, before its first use; each call leaves it ready for the next. Calls that may
- *               run at the same time (several streams) need one each.
+ *               once, before its first use; each call leaves it ready for the next, of any shape
+ *               and head_dim that it is large enough for. Calls that may run at the same time
+ *               (several streams) need one each.
  * Limits: R <= 4096; head_dim 32, 64, 128 or 256; num_q_heads / num_kv_heads <= 128; the step's work
  * (row tiles x tiles of 64 tokens of table_width) below 2^31. */
 cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t layer,

@@ -163,7 +163,7 @@ _SIGS = {
     "cm_qcache_append": (_c.c_int, [_P, _c.POINTER(cm_qcache), _c.c_int32, _c.c_int32, _P, _P,
                                     _c.c_int64, _c.c_int64, _c.c_int64, _P, _c.c_int64, _P]),
     "cm_qcache_attend": (_c.c_int, [_P, _c.POINTER(cm_qcache), _c.c_int32,
-                                    _c.POINTER(cm_qcache_batch), _c.POINTER(cm_qcache_query), _P,
+                                    _c.POINTER(cm_qcache_batch), _P, _P,   # the query: byref or its bytes
                                     _c.c_int64, _P]),
     "cm_qcache_workspace": (_c.c_int, [_P, _c.c_int32, _c.POINTER(_c.c_int64)]),
 }

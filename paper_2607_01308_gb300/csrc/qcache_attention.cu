@@ -393,16 +393,21 @@ static size_t part_rows(int head_dim, int num_sms) {
     return 2 * (decode > prefill ? decode : prefill);
 }
 
+// What comes first, at the same place for every head_dim: the arrival counters, which have to be
+// zero, and the splits.
+static size_t counter_bytes(int num_sms) { return (size_t)num_sms * kQcacheDecodeBlocksPerSm * 4; }
+static size_t head_bytes(int num_sms) { return counter_bytes(num_sms) + ((size_t)num_sms * sizeof(QcacheSplit) + 15) / 16 * 16; }
+
 size_t qcache_workspace_bytes(int head_dim, int num_sms) {
-    return part_rows(head_dim, num_sms) * ((size_t)head_dim + 2) * 4 + (size_t)num_sms * kQcacheDecodeBlocksPerSm * 4 +
-           (size_t)num_sms * sizeof(QcacheSplit);
+    return head_bytes(num_sms) + part_rows(head_dim, num_sms) * ((size_t)head_dim + 2) * 4;
 }
 
 void qcache_workspace_split(QcacheAttentionParams &p, void *workspace, int num_sms) {
-    p.part_o = static_cast<float *>(workspace);
+    unsigned char *at = static_cast<unsigned char *>(workspace);
+    p.arrived = reinterpret_cast<unsigned int *>(at);
+    p.splits = reinterpret_cast<QcacheSplit *>(at + counter_bytes(num_sms));
+    p.part_o = reinterpret_cast<float *>(at + head_bytes(num_sms));
     p.part_ml = p.part_o + part_rows(p.head_dim, num_sms) * p.head_dim;
-    p.arrived = reinterpret_cast<unsigned int *>(p.part_ml + part_rows(p.head_dim, num_sms) * 2);
-    p.splits = reinterpret_cast<QcacheSplit *>(p.arrived + (size_t)num_sms * kQcacheDecodeBlocksPerSm);
 }
 
 #define CM_EACH_DECODE(X) \

@@ -1,15 +1,21 @@
 """Torch-facing side of the 8-bit paged cache (cm_qcache_* of include/cm.h): argument checks and
 marshalling only. torch holds the memory; the library reads and writes it in place.
+
+A serving step makes these calls once for each layer, on kernels of a few microseconds: the
+checks are written for few interpreter steps (messages are only built for a refusal, descriptors
+of tensors that an object owns are filled once).
 """
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional, Tuple
 
-from ._binding import (Context, _check, _stream_handle, cm_qcache, cm_qcache_append, cm_qcache_batch,
-                       cm_qcache_query, cm_qcache_schedule, cm_qcache_workspace, lib)
+from ._binding import (Context, _check, _stream_handle, cm_qcache, cm_qcache_batch, cm_qcache_workspace,
+                       lib)
 
 _INT8, _E4M3 = 1, 0
+_pack_query = struct.Struct("@PPPqqqqiiiifi").pack     # a cm_qcache_query in one step
 
 
 def _require(ok: bool, what: str) -> None:
@@ -25,15 +31,14 @@ def _device(ctx: Context):
 def _strides(t, n: int, unit: int):
     """The first n strides of t; where a dimension has one entry its stride means nothing, and a
     multiple of `unit` stands for it."""
-    return [s if t.shape[i] > 1 else t.shape[-1] * unit for i, s in enumerate(t.stride()[:n])]
+    shape, stride = t.shape, t.stride()[:n]
+    if 1 not in shape:
+        return stride
+    return tuple([s if shape[i] > 1 else shape[-1] * unit for i, s in enumerate(stride)])
 
 
 def _same_layout(a, b, n: int) -> bool:
-    return a.shape == b.shape and _strides(a, n, 1) == _strides(b, n, 1)
-
-
-def _on_device(ctx: Context, t, what: str) -> None:
-    _require(t.is_cuda and t.device.index == ctx.device, f"{what} must be on the context's device")
+    return a.shape == b.shape and (a.stride() == b.stride() or _strides(a, n, 1) == _strides(b, n, 1))
 
 
 def _format(dtype) -> int:
@@ -59,6 +64,7 @@ class QBatch:
         _require(num_requests >= 0 and table_width >= 0 and max_rows >= 0, "sizes must not be negative")
         dev = _device(ctx)
         self.ctx = ctx
+        self._device, self._int32 = ctx.device, torch.int32
         self.max_rows = max_rows
         self.max_new: Optional[int] = None
         self.block_table = torch.full((num_requests, table_width), -1, dtype=torch.int32, device=dev)
@@ -69,30 +75,35 @@ class QBatch:
         self._c = cm_qcache_batch(num_requests, block_size, table_width, self.block_table.data_ptr() or None,
                                   self.row_starts.data_ptr(), self.kv_lens.data_ptr() or None)
         self._ref = ctypes.byref(self._c)
+        self._num_requests, self._slots, self._counts = num_requests, self.slot_map.data_ptr() or None, self.counts.data_ptr()
         self._workspace = None
-        self._workspace_dim = 0
+        self._workspace_ptr = self._workspace_bytes = 0
+        self._workspace_dims = set()
 
     def schedule(self, context_lens, new_lens, free_blocks, stream=None) -> "QBatch":
         """Block tables, row starts, lengths and slots from the requests' cached and new token counts
         (int32 CUDA tensors [R]); new blocks come from the front of free_blocks (int32)."""
-        import torch
-        for t, what in ((context_lens, "context_lens"), (new_lens, "new_lens"), (free_blocks, "free_blocks")):
-            _require(t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous(), f"{what} must be a contiguous int32 vector")
-            _on_device(self.ctx, t, what)
-        n = self._c.num_requests
-        _require(len(context_lens) == n and len(new_lens) == n, "one length per request")
-        cm_qcache_schedule(self.ctx.handle, self._c, context_lens.data_ptr() or None, new_lens.data_ptr() or None,
-                           free_blocks.data_ptr() or None, len(free_blocks), self.slot_map.data_ptr() or None,
-                           self.max_rows, self.counts.data_ptr(), stream)
+        n, dtype, device = self._num_requests, self._int32, self._device
+        for t in (context_lens, new_lens, free_blocks):
+            if t.dtype is not dtype or t.dim() != 1 or not t.is_contiguous() or t.get_device() != device:
+                raise ValueError("context_lens, new_lens and free_blocks must be contiguous int32 vectors on the context's device")
+        _require(context_lens.numel() == n and new_lens.numel() == n, "one length per request")
+        _check(lib.cm_qcache_schedule(self.ctx.handle, self._ref, context_lens.data_ptr() or None, new_lens.data_ptr() or None,
+                                      free_blocks.data_ptr() or None, free_blocks.numel(), self._slots, self.max_rows,
+                                      self._counts, _stream_handle(stream)))
         return self
 
     def _space(self, head_dim: int):
         import torch
+        """A workspace that does for head_dim as well."""
         need = cm_qcache_workspace(self.ctx.handle, head_dim)
-        self._workspace = torch.zeros(need, dtype=torch.uint8, device=_device(self.ctx))
-        torch.cuda.current_stream(self._workspace.device).synchronize()   # zero on every stream
-        self._workspace_dim = head_dim
-        return self._workspace
+        if need > self._workspace_bytes:
+            if self._workspace is not None:
+                torch.cuda.synchronize(self._workspace.device)                # the last call may still use the old one
+            self._workspace = torch.zeros(need, dtype=torch.uint8, device=_device(self.ctx))
+            torch.cuda.current_stream(self._workspace.device).synchronize()   # zero on every stream
+            self._workspace_ptr, self._workspace_bytes = self._workspace.data_ptr(), need
+        self._workspace_dims.add(head_dim)
 
 
 class QCache:
@@ -123,67 +134,63 @@ class QCache:
         import torch
         fmt = _format(k.dtype)
         _require(k.dim() == 5 and k.shape == v.shape and k.dtype == v.dtype, "k and v must both be [blocks, layers, kv_heads, block_size, head_dim]")
-        _require(_same_layout(k, v, 4) and k.stride(4) == 1, "k and v must have the same strides, head_dim contiguous")
+        _require(_same_layout(k, v, 5) and k.stride(4) == 1, "k and v must have the same strides, head_dim contiguous")
         _require(k_scale.dtype == torch.float32 and v_scale.dtype == torch.float32 and
                  tuple(k_scale.shape) == tuple(k.shape[:3]) and tuple(v_scale.shape) == tuple(k.shape[:3]) and
                  _same_layout(k_scale, v_scale, 3), "scales must be fp32 [blocks, layers, kv_heads] of the same strides")
-        for t in (k, v, k_scale, v_scale):
-            _on_device(ctx, t, "cache tensors")
+        _require(all(t.is_cuda and t.get_device() == ctx.device for t in (k, v, k_scale, v_scale)),
+                 "cache tensors must be on the context's device")
+        self._device = ctx.device
+        self._bf16, self._fp32, self._int64 = torch.bfloat16, torch.float32, torch.int64
         self.ctx, self.k, self.v, self.k_scale, self.v_scale = ctx, k, v, k_scale, v_scale
         nb, L, H, bs, d = k.shape
         s, z = _strides(k, 4, 16), _strides(k_scale, 3, 1)
         self._c = cm_qcache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), fmt, L, H, d, bs, 0,
                             nb, s[0], s[1], s[2], s[3], z[0], z[1], z[2])
-        self._query = cm_qcache_query()
-        self._query_ref = ctypes.byref(self._query)
+        self._heads, self._dim, self._scale = H, d, d ** -0.5
         self._ref = ctypes.byref(self._c)
 
     def append(self, K, V, slot_map, layer: int = 0, stream=None) -> None:
         """Rows K, V (bf16 CUDA tensors [layers, kv_heads, rows, head_dim] of the same strides, head_dim
         contiguous) into the slots [rows] (int64) of layers layer .. layer + layers - 1. A slot of -1 is
         skipped; slots of one block are consecutive and ascending."""
-        import torch
-        n = slot_map.shape[0]
-        _require(K.dtype == torch.bfloat16 and V.dtype == torch.bfloat16 and K.dim() == 4 and K.shape == V.shape and
-                 K.shape[1] == self._c.num_kv_heads and K.shape[3] == self._c.head_dim,
-                 "K and V must be bf16 [layers, kv_heads, rows, head_dim] of the cache's shape")
-        _require(_same_layout(K, V, 3) and K.stride(3) == 1, "K and V must have the same strides, head_dim contiguous")
-        _require(slot_map.dtype == torch.int64 and slot_map.dim() == 1 and slot_map.is_contiguous() and n <= K.shape[2],
-                 "slot_map must be a contiguous int64 vector of at most as many entries as there are rows")
-        for t in (K, V, slot_map):
-            _on_device(self.ctx, t, "rows and slots")
-        s = _strides(K, 3, 8)
-        cm_qcache_append(self.ctx.handle, self._c, layer, K.shape[0], K.data_ptr() or None, V.data_ptr() or None,
-                         s[0], s[1], s[2], slot_map.data_ptr() or None, n, stream)
+        shape, bf16, device = K.shape, self._bf16, self._device
+        if (K.dtype is not bf16 or V.dtype is not bf16 or len(shape) != 4 or shape != V.shape or
+                shape[1] != self._heads or shape[3] != self._dim):
+            raise ValueError("K and V must be bf16 [layers, kv_heads, rows, head_dim] of the cache's shape")
+        s = K.stride()
+        if s[3] != 1 or (s != V.stride() and not _same_layout(K, V, 4)):
+            raise ValueError("K and V must have the same strides, head_dim contiguous")
+        if slot_map.dtype is not self._int64 or slot_map.dim() != 1 or not slot_map.is_contiguous() or slot_map.numel() > shape[2]:
+            raise ValueError("slot_map must be a contiguous int64 vector of at most as many entries as there are rows")
+        if K.get_device() != device or V.get_device() != device or slot_map.get_device() != device:
+            raise ValueError("rows and slots must be on the context's device")
+        if 1 in shape:
+            s = _strides(K, 3, 8)
+        _check(lib.cm_qcache_append(self.ctx.handle, self._ref, layer, shape[0], K.data_ptr() or None, V.data_ptr() or None,
+                                    s[0], s[1], s[2], slot_map.data_ptr() or None, slot_map.numel(), _stream_handle(stream)))
 
     def attend(self, q, batch: QBatch, layer: int = 0, out=None, lse=None, softmax_scale: Optional[float] = None,
                causal: bool = True, stream=None) -> Tuple[object, object]:
         """(out, lse): softmax(softmax_scale * q K^T) V for the batch's rows, each over its own request's
         cached tokens. q, out: bf16 [rows, q_heads, head_dim] (q_heads a multiple of kv_heads, head_dim
         contiguous); lse: fp32 [rows, q_heads] or None to leave it out; out is made if not given."""
-        import torch
-        shape = q.shape
-        _require(q.dtype == torch.bfloat16 and q.dim() == 3 and shape[2] == self._c.head_dim and q.stride(2) == 1,
-                 "q must be bf16 [rows, q_heads, head_dim], head_dim contiguous")
-        _on_device(self.ctx, q, "q")
+        shape, bf16, device = q.shape, self._bf16, self._device
+        if q.dtype is not bf16 or len(shape) != 3 or shape[2] != self._dim or q.stride(2) != 1 or q.get_device() != device:
+            raise ValueError("q must be bf16 [rows, q_heads, head_dim] on the context's device, head_dim contiguous")
         if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
-        else:
-            _require(out.dtype == torch.bfloat16 and out.shape == shape and out.stride(2) == 1 and out.device == q.device,
-                     "out must be like q")
-        if lse is not None:
-            _require(lse.dtype == torch.float32 and lse.shape == shape[:2] and lse.is_contiguous() and lse.device == q.device,
-                     "lse must be a contiguous fp32 [rows, q_heads]")
-        space = batch._workspace
-        if space is None or batch._workspace_dim < self._c.head_dim:
-            space = batch._space(self._c.head_dim)
-        c, qs, os = self._query, _strides(q, 2, 8), _strides(out, 2, 8)
-        c.q, c.out, c.lse = q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None
-        c.q_stride_row, c.q_stride_head, c.out_stride_row, c.out_stride_head = qs[0], qs[1], os[0], os[1]
-        c.total_rows, c.num_q_heads = shape[0], shape[1]
-        c.max_rows_per_request = batch.max_new or 0
-        c.causal = 1 if causal else 0
-        c.softmax_scale = softmax_scale if softmax_scale is not None else self._c.head_dim ** -0.5
-        _check(lib.cm_qcache_attend(self.ctx.handle, self._ref, layer, batch._ref, self._query_ref,
-                                    space.data_ptr(), space.numel(), _stream_handle(stream)))
+            out = q.new_empty(shape)
+        elif out.dtype is not bf16 or out.shape != shape or out.stride(2) != 1 or out.get_device() != device:
+            raise ValueError("out must be like q")
+        if lse is not None and (lse.dtype is not self._fp32 or lse.shape != shape[:2] or not lse.is_contiguous() or
+                                lse.get_device() != device):
+            raise ValueError("lse must be a contiguous fp32 [rows, q_heads]")
+        if self._dim not in batch._workspace_dims:
+            batch._space(self._dim)
+        qs, os = _strides(q, 2, 8), _strides(out, 2, 8)
+        query = _pack_query(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), qs[0], qs[1], os[0], os[1],
+                            shape[0], shape[1], batch.max_new or 0, 1 if causal else 0,
+                            self._scale if softmax_scale is None else softmax_scale, 0)
+        _check(lib.cm_qcache_attend(self.ctx.handle, self._ref, layer, batch._ref, query,
+                                    batch._workspace_ptr, batch._workspace_bytes, _stream_handle(stream)))
         return out, lse

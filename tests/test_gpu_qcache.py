@@ -462,6 +462,28 @@ def test_attend_on_another_stream_and_in_a_graph(ctx):
 
 # ---------------------------------------------------------------- refusals
 
+def test_attend_one_batch_for_several_head_dims(ctx):
+    """A batch's workspace serves caches of any head_dim, in any order: same bits as with a batch of its own."""
+    caches = [_make_cache(ctx, "e4m3", 1, 1, d, 16, 160, d) for d in (256, 128, 64)]
+    g = torch.Generator().manual_seed(3)
+
+    def batch(rows):
+        b = cm.QBatch(ctx, 1, 160, rows, 16)
+        b.block_table.copy_(torch.arange(160)[None].int())
+        b.row_starts.copy_(_i32([0, rows]))
+        b.kv_lens.fill_(2500)
+        b.max_new = rows
+        return b
+
+    for rows in (1, 40):
+        queries = [torch.randn((rows, 4, c.k.shape[4]), generator=g).bfloat16().to(DEV) for c in caches]
+        own = [c.attend(q, batch(rows))[0] for c, q in zip(caches, queries)]
+        shared = batch(rows)
+        for i in (0, 1, 2, 1, 0, 2, 0, 1):
+            out = caches[i].attend(queries[i], shared)[0]
+            assert torch.equal(out, own[i])
+
+
 def test_refusals(ctx):
     cache = cm.QCache(ctx, 4, 16, 2, 2, 64)
     batch = cm.QBatch(ctx, 2, 4, 8, 16)
