@@ -508,7 +508,8 @@ cm_status cm_qcache_schedule(cm_context *ctx, const cm_qcache_batch *batch, cons
  * smallest 2^k, k in [-60, 60], with m <= 448 * 2^k (e4m3) or 127 * 2^k (int8), or stays if p > 0
  * and it is larger; codes are x / scale to nearest even, clamped to +-448 or +-127, NaN to 0; where
  * the scale grew, the codes of tokens 0 .. p - 1 are rounded again to it. The result is exactly that,
- * whatever the launch.
+ * whatever the launch (a kept scale that a caller wrote and that is no power of two is divided by
+ * with fp32's accuracy).
  *   slot_map    [num_rows] DEVICE: slots as cm_qcache_schedule writes them; one below 0 or beyond
  *               the pool is skipped. The rows of one block must be consecutive with ascending slots:
  *               a block that gets rows in two separate runs of one call ends up undefined.

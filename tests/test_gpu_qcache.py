@@ -217,6 +217,23 @@ def test_append_extreme_values(ctx, fmt, value):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dim,block", [(64, 16), (128, 32), (128, 64), (256, 128), (512, 256)])
+def test_append_not_finite_among_many(ctx, fmt, dim, block):
+    """A NaN and infinities in long runs and in a single token of a cache in use."""
+    requests = [(3, 2 * block + 5), (block - 1, 1)]
+
+    def values(x, which):
+        x[:, 0, 1, 3] = math.inf
+        x[:, 1, block + 2, dim - 1] = -math.inf
+        x[:, 1, block + 3, 0] = math.nan
+        x[:, 0, -1, which] = math.nan
+        return x
+
+    num_blocks = sum(-(-(o + n) // block) for o, n in requests) + 1
+    _check_append(ctx, fmt, 1, 2, dim, block, num_blocks, _slots_of(requests, block, num_blocks, dim), requests, k_values=values)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_append_skips_and_leaves_the_rest(ctx, fmt):
     slots = [-1, 3, 4, -1, 21, 22, 10 ** 12, 64, 35, 36, -5]      # four blocks: 64 is beyond the pool
     cache, before = _check_append(ctx, fmt, 1, 2, 32, 16, 4, slots, None)
