@@ -361,6 +361,23 @@ __device__ __forceinline__ float load_queries(const QcacheAttentionParams &p, co
     return fabsf(p.scale_log2) * pow2f(e - 14);
 }
 
+// The warp's 32 rows of 16-byte chunks, placed as load_queries places them, to their rows in global memory
+// (`row`: this lane's; null: none).
+template <int D>
+__device__ __forceinline__ void store_rows(uint16_t *row, const unsigned char *tile) {
+    using C = Shape<D>;
+    constexpr int kLanes = D / 8, kStep = 32 / kLanes;            // lanes to a row, rows of one store
+    const int lane = threadIdx.x % 32, sub = lane / kLanes, col = lane % kLanes;
+#pragma unroll 8
+    for (int k = 0; k < 32 / kStep; ++k) {
+        const int r = k * kStep + sub;
+        uint16_t *to = reinterpret_cast<uint16_t *>(__shfl_sync(~0u, reinterpret_cast<uint64_t>(row), r));
+        const uint4 x = *reinterpret_cast<const uint4 *>(tile + col / 8 * C::kQPanel + r * 128 + ((col % 8) ^ (r & 7)) * 16);
+        if (to) *reinterpret_cast<uint4 *>(to + col * 8) = x;
+    }
+    __syncwarp();
+}
+
 // ---------------------------------------------------------------- work
 
 // kv tiles that row tile rt of a request may see (one at least: its rows are written).
@@ -475,6 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         uint32_t n = 0;
         if (r < p.requests) {
             const RequestShape s = request_shape<C::kRows, kTile>(p, r);
+#pragma unroll 4
             for (int rt = 0; rt < s.row_tiles; ++rt) n += visible_tiles<C::kRows, kTile>(p, s, rt) + C::kSetup;
         }
         uint32_t a = n;
@@ -515,6 +533,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
+    }
+    if (warp == 1) {
+        // where the block's share begins: the request by halving, the row tile 32 at a time
         const uint64_t units = (uint64_t)total * (uint32_t)p.heads;
         Start s;
         s.per = units_per_block<C::kSetup>(units, gridDim.x);
@@ -527,22 +548,31 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 const int mid = (lo + hi) >> 1;
                 if ((uint64_t)prefix[mid] * (uint32_t)p.heads <= s.u) lo = mid; else hi = mid;
             }
+            s.request = lo;
             const RequestShape q = request_shape<C::kRows, kTile>(p, lo);
             uint64_t in = s.u - (uint64_t)prefix[lo] * (uint32_t)p.heads;
-            s.request = lo;
-            while (true) {
-                const uint32_t n = visible_tiles<C::kRows, kTile>(p, q, s.row_tile) + C::kSetup;
-                const uint64_t all = (uint64_t)n * (uint32_t)p.heads;
-                if (in < all) {
-                    s.head = (int)(in / n);
-                    s.at = (int)(in - (uint64_t)s.head * n);
+            for (int rt = 0; rt < q.row_tiles; rt += 32) {
+                const uint32_t n = visible_tiles<C::kRows, kTile>(p, q, min(rt + lane, q.row_tiles - 1)) + C::kSetup;
+                uint64_t all = (uint64_t)n * (uint32_t)p.heads;       // of the row tiles so far
+#pragma unroll
+                for (int d = 1; d < 32; d *= 2) {
+                    const uint64_t x = __shfl_up_sync(~0u, all, d);
+                    if (lane >= d) all += x;
+                }
+                const unsigned behind = __ballot_sync(~0u, in < all);
+                const int l = behind ? __ffs(behind) - 1 : 32;
+                if (l < 32 && rt + l < q.row_tiles) {
+                    const uint32_t n_l = __shfl_sync(~0u, n, l);
+                    const uint64_t in_l = in - (__shfl_sync(~0u, all, l) - (uint64_t)n_l * (uint32_t)p.heads);
+                    s.row_tile = rt + l;
+                    s.head = (int)(in_l / n_l);
+                    s.at = (int)(in_l - (uint64_t)s.head * n_l);
                     break;
                 }
-                in -= all;
-                ++s.row_tile;
+                in -= __shfl_sync(~0u, all, 31);
             }
         }
-        start = s;
+        if (lane == 0) start = s;
     }
     // the joining kernel may be set up from now on; it waits for this one's results by itself
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -616,34 +646,45 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             o_phase ^= 1;
             fence_after();
             const bool whole = w.t0 == 0 && w.t1 == w.tiles;
-            const int rows = min(128, w.rows - first);
-            const int64_t part = (2 * (int64_t)blockIdx.x + (w.t0 == 0)) * C::kRows + qt * 128;
-            const float scale = sum == 0.f ? 0.f : 1.f / sum;
-            uint16_t *to = p.out + token * p.out_stride_row + head * p.out_stride_head;
-            float *to_part = p.part_o + (part + row) * D;
+            const int64_t part = 2 * (int64_t)blockIdx.x + (w.t0 == 0);
+            if (whole) {
+                // through the query rows' places in shared memory, so that the warp stores whole rows
+                const float scale = sum == 0.f ? 0.f : 1.f / sum;
+                unsigned char *tile = q_smem + qt * C::kPanels * C::kQPanel + warp % 4 * 32 * 128;
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t x[32];
-                __syncwarp();
-                tmem_ld(x, o_at + 32 * c);
-                ld_wait(x);
-                if (valid && whole) {
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t x[32];
+                    tmem_ld(x, o_at + 32 * c);
+                    ld_wait(x);
 #pragma unroll
-                    for (int k = 0; k < 32; k += 8) {
+                    for (int k = 0; k < 4; ++k) {
                         uint32_t y[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
-                            y[j] = pack_bf16(__uint_as_float(x[k + 2 * j]) * scale, __uint_as_float(x[k + 2 * j + 1]) * scale);
-                        *reinterpret_cast<uint4 *>(to + 32 * c + k) = make_uint4(y[0], y[1], y[2], y[3]);
+                            y[j] = pack_bf16(__uint_as_float(x[8 * k + 2 * j]) * scale, __uint_as_float(x[8 * k + 2 * j + 1]) * scale);
+                        const int chunk = 4 * c + k;
+                        *reinterpret_cast<uint4 *>(tile + chunk / 8 * C::kQPanel + lane * 128 + ((chunk % 8) ^ (lane & 7)) * 16) =
+                            make_uint4(y[0], y[1], y[2], y[3]);
                     }
-                } else if (valid) {
+                }
+                __syncwarp();
+                store_rows<D>(valid ? p.out + token * p.out_stride_row + head * p.out_stride_head : nullptr, tile);
+            } else {
+                // 4 columns of all rows after another: a warp's stores lie together
+                float *to = p.part_o + (part * C::kRows * (D / 4) + qt * 128 + row) * 4;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t x[32];
+                    tmem_ld(x, o_at + 32 * c);
+                    ld_wait(x);
 #pragma unroll
                     for (int k = 0; k < 32; k += 4)
-                        __stcg(reinterpret_cast<uint4 *>(to_part + 32 * c + k), make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]));
+                        __stcg(reinterpret_cast<uint4 *>(to + (8 * c + k / 4) * (C::kRows * 4)), make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]));
                 }
             }
             if (valid && whole && p.lse) p.lse[token * ((int64_t)p.heads * p.group) + head] = log_sum(top, sum, kHeadroom);
-            if (valid && !whole) __stcg(reinterpret_cast<float2 *>(p.part_ml + (part + row) * 2), make_float2(sum == 0.f ? -INFINITY : top, sum));
+            if (!whole)
+                __stcg(reinterpret_cast<float2 *>(p.part_ml + (part * C::kRows + qt * 128 + row) * 2), make_float2(sum == 0.f ? -INFINITY : top, sum));
         }
     } else if (warp < kMmaWarp) {
         if constexpr (C::kLoadRegs < kLaunchRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kLoadRegs));
@@ -836,22 +877,66 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
 }
 
 // The parts of ranges that were cut: a thread block for 8 rows of a range, which begins in block
-// blockIdx.x of the kernel before.
-constexpr int kJoinRows = 8, kJoinWarps = 8;
+// blockIdx.x of the kernel before. A thread has 4 columns of a row (at head_dim 256 twice), a warp those
+// of 8 rows, whose parts lie together; the parts are weighed and added in the blocks' order.
+constexpr int kJoinRows = 8, kJoinThreads = 256, kJoinAhead = 4;   // parts that are read before they can be weighed
 
 template <int D>
-__global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const __grid_constant__ QcacheAttentionParams p) {
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ QcacheAttentionParams p) {
     using C = Shape<D>;
+    constexpr int kColumns = kJoinThreads / kJoinRows, kVecs = D / 4 > kColumns ? D / 4 / kColumns : 1;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const QcacheSplit z = p.splits[blockIdx.x];
-    const int in_tile = blockIdx.y * kJoinRows, first = z.row_tile * C::kRows + in_tile;
-    if (first >= z.rows) return;
+    const int row = blockIdx.y * kJoinRows + threadIdx.x % kJoinRows, column = threadIdx.x / kJoinRows;
+    if (z.row_tile * C::kRows + row >= z.rows || column >= D / 4) return;
+    const int n = z.last_block - (int)blockIdx.x + 1;
+    auto part = [&](int c) { return (2 * (int64_t)(blockIdx.x + c) + (c == 0)) * C::kRows; };
+    auto read_ml = [&](int c) { return __ldcg(reinterpret_cast<const float2 *>(p.part_ml + (part(c) + row) * 2)); };
+    auto read = [&](int c, int v) {
+        return __ldcg(reinterpret_cast<const float4 *>(p.part_o) + part(c) * (D / 4) + (int64_t)(column + v * kColumns) * C::kRows + row);
+    };
+    float2 ml[kJoinAhead];
+    float4 x[kJoinAhead][kVecs], acc[kVecs];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int c = 0; c < kJoinAhead; ++c) {
+        ml[c] = make_float2(-INFINITY, 0.f);
+        if (c < n) {
+            ml[c] = read_ml(c);
+#pragma unroll
+            for (int v = 0; v < kVecs; ++v) x[c][v] = read(c, v);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < kJoinAhead; ++c) m = fmaxf(m, ml[c].x);
+#pragma unroll 4
+    for (int c = kJoinAhead; c < n; ++c) m = fmaxf(m, read_ml(c).x);
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float2 &y, const float4 (&z)[kVecs]) {
+        const float f = y.x == m ? 1.f : exp2_fast(y.x - m);
+        l = fmaf(y.y, f, l);
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+            acc[v].x = fmaf(z[v].x, f, acc[v].x); acc[v].y = fmaf(z[v].y, f, acc[v].y);
+            acc[v].z = fmaf(z[v].z, f, acc[v].z); acc[v].w = fmaf(z[v].w, f, acc[v].w);
+        }
+    };
+#pragma unroll
+    for (int c = 0; c < kJoinAhead; ++c)
+        if (c < n) add(ml[c], x[c]);
+#pragma unroll 4
+    for (int c = kJoinAhead; c < n; ++c) {
+        float4 y[kVecs];
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) y[v] = read(c, v);
+        add(read_ml(c), y);
+    }
     AttentionSegment w{};
     w.head = z.head;
     w.row0 = z.row0;
-    const uint32_t c0 = blockIdx.x;
-    join_parts<D, kJoinWarps, 1>(p, w, first, min(kJoinRows, z.rows - first), c0, (uint32_t)z.last_block, kHeadroom, threadIdx.x / 32,
-                                 [&](uint32_t c, int r) { return (2 * (int64_t)c + (c == c0)) * C::kRows + in_tile + r; });
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) write_row(p, w, z.row_tile * C::kRows + row, (column + v * kColumns) * 4, acc[v], m, l, kHeadroom);
 }
 
 template <int D, int FORMAT>
@@ -873,7 +958,7 @@ cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cuda
     early.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t config{};
     config.gridDim = dim3(num_sms, C::kRows / kJoinRows);
-    config.blockDim = dim3(kJoinWarps * 32);
+    config.blockDim = dim3(kJoinThreads);
     config.stream = stream;
     config.attrs = &early;
     config.numAttrs = 1;
