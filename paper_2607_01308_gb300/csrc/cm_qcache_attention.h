@@ -178,92 +178,63 @@ __device__ __forceinline__ void write_row(const QcacheAttentionParams &p, const 
 
 // Joins the parts of rows [0, rows) of a segment's whole range, held by thread blocks c0 .. c1 of the
 // grid, in that order; row_at(c, row): the workspace row of block c's part; first: the rows' place
-// among the request's. WARPS warps share the rows, GROUP at a time to a warp: lanes weigh the parts,
-// then read them along head_dim.
-template <int D, int WARPS, int GROUP, class At>
+// among the request's. WARPS warps share the rows: lanes weigh the parts, then read them along head_dim.
+template <int D, int WARPS, class At>
 __device__ __forceinline__ void join_parts(const QcacheAttentionParams &p, const AttentionSegment &w, int first, int rows,
                                            uint32_t c0, uint32_t c1, float headroom, int warp, At row_at) {
-    constexpr int kGroup = GROUP, kVecs = D >= 128 ? D / 128 : 1;   // 16-byte vectors of a lane
-    constexpr int kAhead = 8 / kGroup;                          // parts that are read before they can be weighed
+    constexpr int kVecs = D >= 128 ? D / 128 : 1;   // 16-byte vectors of a lane
+    constexpr int kAhead = 8;                       // parts that are read before they can be weighed
     const int lane = threadIdx.x % 32, n = (int)(c1 - c0 + 1);
-    for (int r0 = warp; r0 < rows; r0 += WARPS * kGroup) {
-        float m[kGroup], l[kGroup];
-        float4 acc[kGroup][kVecs];
-        auto read = [&](int c, int k, int v) {
-            if ((D < 128 && lane >= D / 4) || c >= n) return make_float4(0.f, 0.f, 0.f, 0.f);
-            return __ldcg(reinterpret_cast<const float4 *>(p.part_o + row_at(c0 + c, min(r0 + k * WARPS, rows - 1)) * D) + lane + 32 * v);
+    for (int row = warp; row < rows; row += WARPS) {
+        auto read_ml = [&](int c) {
+            return c < n ? __ldcg(reinterpret_cast<const float2 *>(p.part_ml + row_at(c0 + c, row) * 2)) : make_float2(-INFINITY, 0.f);
         };
-        float2 ml[kGroup];
-        float4 early[kAhead][kGroup][kVecs];
-#pragma unroll
-        for (int k = 0; k < kGroup; ++k) {
-            ml[k] = make_float2(-INFINITY, 0.f);
-            if (lane < n) ml[k] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml + row_at(c0 + lane, min(r0 + k * WARPS, rows - 1)) * 2));
-        }
+        auto read = [&](int c, int v) {
+            if ((D < 128 && lane >= D / 4) || c >= n) return make_float4(0.f, 0.f, 0.f, 0.f);
+            return __ldcg(reinterpret_cast<const float4 *>(p.part_o + row_at(c0 + c, row) * D) + lane + 32 * v);
+        };
+        float2 ml = read_ml(lane);
+        float4 early[kAhead][kVecs], acc[kVecs];
 #pragma unroll
         for (int c = 0; c < kAhead; ++c)
 #pragma unroll
-            for (int k = 0; k < kGroup; ++k)
+            for (int v = 0; v < kVecs; ++v) early[c][v] = read(c, v);
+        float m = ml.x, l = 0.f;
+        for (int c = 32 + lane; c < n; c += 32) m = fmaxf(m, read_ml(c).x);
 #pragma unroll
-                for (int v = 0; v < kVecs; ++v) early[c][k][v] = read(c, k, v);
+        for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
 #pragma unroll
-        for (int k = 0; k < kGroup; ++k) {
-            m[k] = ml[k].x;
-            for (int c = 32 + lane; c < n; c += 32) m[k] = fmaxf(m[k], __ldcg(p.part_ml + row_at(c0 + c, min(r0 + k * WARPS, rows - 1)) * 2));
-#pragma unroll
-            for (int d = 16; d; d /= 2) m[k] = fmaxf(m[k], __shfl_xor_sync(~0u, m[k], d));
-            l[k] = 0.f;
-#pragma unroll
-            for (int v = 0; v < kVecs; ++v) acc[k][v] = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-        auto add = [&](int k, int v, const float4 &x, float g) {
-            float4 &a = acc[k][v];
-            a.x = fmaf(x.x, g, a.x); a.y = fmaf(x.y, g, a.y);
-            a.z = fmaf(x.z, g, a.z); a.w = fmaf(x.w, g, a.w);
+        for (int v = 0; v < kVecs; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto add = [&](int v, const float4 &x, float g) {
+            acc[v].x = fmaf(x.x, g, acc[v].x); acc[v].y = fmaf(x.y, g, acc[v].y);
+            acc[v].z = fmaf(x.z, g, acc[v].z); acc[v].w = fmaf(x.w, g, acc[v].w);
         };
         for (int base = 0; base < n; base += 32) {
-            float f[kGroup];
+            if (base > 0) ml = read_ml(base + lane);
+            const float f = ml.x == m ? 1.f : exp2_fast(ml.x - m);
+            float x = ml.y * f;
 #pragma unroll
-            for (int k = 0; k < kGroup; ++k) {
-                if (base > 0) {
-                    ml[k] = make_float2(-INFINITY, 0.f);
-                    if (base + lane < n)
-                        ml[k] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml + row_at(c0 + base + lane, min(r0 + k * WARPS, rows - 1)) * 2));
-                }
-                f[k] = ml[k].x == m[k] ? 1.f : exp2_fast(ml[k].x - m[k]);
-                float x = ml[k].y * f[k];
-#pragma unroll
-                for (int d = 16; d; d /= 2) x += __shfl_xor_sync(~0u, x, d);
-                l[k] += x;
-            }
+            for (int d = 16; d; d /= 2) x += __shfl_xor_sync(~0u, x, d);
+            l += x;
             if (base == 0) {
 #pragma unroll
-                for (int c = 0; c < kAhead; ++c)
+                for (int c = 0; c < kAhead; ++c) {
+                    const float g = __shfl_sync(~0u, f, c);
 #pragma unroll
-                    for (int k = 0; k < kGroup; ++k) {
-                        const float g = __shfl_sync(~0u, f[k], c);
-#pragma unroll
-                        for (int v = 0; v < kVecs; ++v) add(k, v, early[c][k][v], c < n ? g : 0.f);
-                    }
+                    for (int v = 0; v < kVecs; ++v) add(v, early[c][v], c < n ? g : 0.f);
+                }
             }
             const int most = min(32, n - base);
 #pragma unroll kAhead
-            for (int c = base == 0 ? kAhead : 0; c < most; ++c)
+            for (int c = base == 0 ? kAhead : 0; c < most; ++c) {
+                const float g = __shfl_sync(~0u, f, c);
 #pragma unroll
-                for (int k = 0; k < kGroup; ++k) {
-                    const float g = __shfl_sync(~0u, f[k], c);
-#pragma unroll
-                    for (int v = 0; v < kVecs; ++v) add(k, v, read(base + c, k, v), g);
-                }
+                for (int v = 0; v < kVecs; ++v) add(v, read(base + c, v), g);
+            }
         }
 #pragma unroll
-        for (int k = 0; k < kGroup; ++k) {
-            const int row = r0 + k * WARPS;
-            if (row >= rows) break;
-#pragma unroll
-            for (int v = 0; v < kVecs; ++v)
-                if (D >= 128 || lane < D / 4) write_row(p, w, first + row, (lane + 32 * v) * 4, acc[k][v], m[k], l[k], headroom);
-        }
+        for (int v = 0; v < kVecs; ++v)
+            if (D >= 128 || lane < D / 4) write_row(p, w, first + row, (lane + 32 * v) * 4, acc[v], m, l, headroom);
     }
 }
 

@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
             __syncthreads();
             if (last_one) {
                 __threadfence();
-                join_parts<D, kWarps, 1>(p, w, w.row_tile * C::kRows, rows, c0, c1, kHeadroom, warp,
+                join_parts<D, kWarps>(p, w, w.row_tile * C::kRows, rows, c0, c1, kHeadroom, warp,
                                       [&](uint32_t c, int n) { return (2 * (int64_t)c + (c == c0)) * C::kRows + n; });
             }
         }
@@ -416,7 +416,12 @@ void qcache_workspace_split(QcacheAttentionParams &p, void *workspace, int num_s
 
 cudaError_t launch_qcache_attention(const QcacheAttentionParams &p, int rows_per_request, int num_sms, int device,
                                     cudaStream_t stream) {
-    if (rows_per_request > 16) return launch_qcache_prefill(p, num_sms, device, stream);
+    // Rows of a request and kv head: to 8 in one fragment, to 16 in two at once, to 32 in two tiles of those,
+    // which read the cache twice; above, the other kernel. Measured, 32 requests of 4,096 tokens, 8 kv heads:
+    //   head_dim 128 e4m3   8 rows 55 us, as two fragments 57; 16 rows 61 us, as two tiles of one 99 or more;
+    //                       32 rows 100 us, by the other kernel 109
+    //   head_dim 64 int8    8 rows 36 us, as two fragments 42; 32 rows 73 us, by the other kernel 92
+    if (rows_per_request > 32) return launch_qcache_prefill(p, num_sms, device, stream);
 #define CM_LAUNCH(D, F) \
     if (p.head_dim == D && p.format == F) \
         return rows_per_request <= 8 ? launch<D, F, 1>(p, num_sms, device, stream) : launch<D, F, 2>(p, num_sms, device, stream);

@@ -876,15 +876,17 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512));
 }
 
-// The parts of ranges that were cut: a thread block for 8 rows of a range, which begins in block
-// blockIdx.x of the kernel before. A thread has 4 columns of a row (at head_dim 256 twice), a warp those
-// of 8 rows, whose parts lie together; the parts are weighed and added in the blocks' order.
-constexpr int kJoinRows = 8, kJoinThreads = 256, kJoinAhead = 4;   // parts that are read before they can be weighed
+// The parts of ranges that were cut: a thread block for a sixteenth of a row tile, of the range that begins
+// in block blockIdx.x of the kernel before. A thread has 4 columns of a row at a time, a warp those of 8 or
+// 16 rows, whose parts lie together; the parts are weighed and added in the blocks' order. Bound by
+// latency: the two reads and the launch. (Half as many rows, so twice the blocks: 1 us more where nothing
+// was cut, 11.6 us for 64 tokens; twice as many: 2 us more for the head_dim 256 prompts.)
+constexpr int kJoinThreads = 256, kJoinAhead = 4;   // parts that are read before they can be weighed
 
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ QcacheAttentionParams p) {
     using C = Shape<D>;
-    constexpr int kColumns = kJoinThreads / kJoinRows, kVecs = D / 4 > kColumns ? D / 4 / kColumns : 1;
+    constexpr int kJoinRows = C::kRows / 16, kColumns = kJoinThreads / kJoinRows, kVecs = D / 4 > kColumns ? D / 4 / kColumns : 1;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const QcacheSplit z = p.splits[blockIdx.x];
     const int row = blockIdx.y * kJoinRows + threadIdx.x % kJoinRows, column = threadIdx.x / kJoinRows;
@@ -957,7 +959,7 @@ cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cuda
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t config{};
-    config.gridDim = dim3(num_sms, C::kRows / kJoinRows);
+    config.gridDim = dim3(num_sms, 16);
     config.blockDim = dim3(kJoinThreads);
     config.stream = stream;
     config.attrs = &early;
