@@ -401,6 +401,14 @@ def test_attend_prompts(ctx, fmt, heads, group, dim, rows, kv):
     _check_attend(ctx, fmt, heads, group, dim, 16, [(kv, rows), (rows - 7, rows), (kv + 11, 2)], seed=rows)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,group,dim,fmt", [(1, 1, 128, "e4m3"), (2, 3, 64, "int8"), (1, 2, 32, "e4m3"), (1, 1, 256, "int8")])
+def test_attend_at_most_128_rows(ctx, heads, group, dim, fmt, causal):
+    """One query tile over 0 to 7 tiles of tokens: rows that see nothing, one tile for two halves, odd counts."""
+    requests = [(0, 33), (1, 40), (20, 42), (64, 33), (65, 34), (128, 42), (129, 36), (200, 35), (300, 42), (449, 33)]
+    _check_attend(ctx, fmt, heads, group, dim, 16, requests, causal=causal, seed=21)
+
+
 @pytest.mark.parametrize("rows", [1, 40])
 def test_attend_split_long_axis(ctx, rows):
     """Few rows over many tokens: the parts of several thread blocks are joined; the same bits each time."""
