@@ -11,7 +11,9 @@ moves a weight by as much) is below that. Hence
     |out - ref| <= 2^-8 |ref| * (1 + 2^-6) + (2^-11 + 2^-12 + 2^-19 size) * sum p |v|
     |lse - ref| <= 2^-19 * (1 + |ref| + size),   size = the largest sum |q||k| * softmax_scale
 """
+import importlib.util
 import math
+import os
 
 import numpy as np
 import pytest
@@ -549,3 +551,17 @@ def test_refusals(ctx):
     # nothing to do is no error
     cache.append(good[:, :, :0], good[:, :, :0], slots[:0])
     cache.attend(q[:0], batch)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_example_answers_from_merged_caches(fmt):
+    """Render, schedule, append and attend together. A value's rounding is at most 2^-4 of it (e4m3, three bits
+    behind the point) or 2^-6 of its block's largest (int8, power-of-two scale: up to 1 / 64), so an element is off
+    by no more than 1 / 16 of a typical one, K and V each; three times both bounds any row's result."""
+    path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "examples", "answer_from_merge.py")
+    spec = importlib.util.spec_from_file_location("answer_from_merge", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    r = example.main(requests=3, layers=2, kv_heads=2, group=4, dim=64, tokens=(20, 130), question=21, steps=3, fmt=fmt)
+    assert r["merged_tokens"] > 3 * 40
+    assert 0.0 < r["relative_error"] < 3 * 2 / 16
