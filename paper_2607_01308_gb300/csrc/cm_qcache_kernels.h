@@ -87,4 +87,29 @@ cudaError_t launch_qcache_attention(const QcacheAttentionParams &p, int rows_per
 cudaError_t launch_qcache_prefill(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream);
 size_t qcache_prefill_part_rows(int head_dim);
 
+#ifdef __CUDACC__
+// Launches a kernel that may be set up while the one before it in the stream ends. Its threads call
+// after_kernels_before() before they read or write global memory; nothing else is relaxed.
+template <class... Params, class... Args>
+cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, unsigned int threads, size_t shared, cudaStream_t stream, const Args &...args) {
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = grid;
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = shared;
+    config.stream = stream;
+    config.attrs = &early;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, args...);
+}
+
+// Waits until the kernels before this one have ended and their writes are seen, and lets the next one
+// be set up.
+__device__ __forceinline__ void after_kernels_before() {
+    asm volatile("griddepcontrol.wait;\ngriddepcontrol.launch_dependents;" ::: "memory");
+}
+#endif
+
 }  // namespace cm

@@ -269,6 +269,7 @@ __global__ void __launch_bounds__(kBlockWarps<TEAM> * 32, (VECS < 8 ? 32 : 24) /
     __shared__ Run runs[32];
     __shared__ int num_runs;
     constexpr int kHeads = TEAM == 1 ? 2 : 1;  // per thread block
+    after_kernels_before();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     if (warp == 0) {
         const int64_t row0 = (int64_t)blockIdx.x * p.window;
@@ -298,8 +299,8 @@ __global__ void __launch_bounds__(kBlockWarps<TEAM> * 32, (VECS < 8 ? 32 : 24) /
 }
 
 template <int FORMAT, int TEAM, int VECS>
-void launch(const QcacheAppendParams &p, const dim3 &grid, cudaStream_t stream) {
-    append_kernel<FORMAT, TEAM, VECS><<<grid, kBlockWarps<TEAM> * 32, 0, stream>>>(p);
+cudaError_t launch(const QcacheAppendParams &p, const dim3 &grid, cudaStream_t stream) {
+    return launch_behind(append_kernel<FORMAT, TEAM, VECS>, grid, kBlockWarps<TEAM> * 32, 0, stream, p);
 }
 
 }  // namespace
@@ -326,11 +327,10 @@ cudaError_t launch_qcache_append(QcacheAppendParams p, int num_sms, cudaStream_t
     p.window = window;
     const dim3 grid((unsigned)((p.num_rows + window - 1) / window), (unsigned)head_groups, (unsigned)p.layers);
     const bool e4m3 = p.format == CM_QCACHE_E4M3;
-    if (block <= 1024) e4m3 ? launch<CM_QCACHE_E4M3, 1, 4>(p, grid, stream) : launch<CM_QCACHE_INT8, 1, 4>(p, grid, stream);
-    else if (team == 1) e4m3 ? launch<CM_QCACHE_E4M3, 1, 8>(p, grid, stream) : launch<CM_QCACHE_INT8, 1, 8>(p, grid, stream);
-    else if (team == 4) e4m3 ? launch<CM_QCACHE_E4M3, 4, 8>(p, grid, stream) : launch<CM_QCACHE_INT8, 4, 8>(p, grid, stream);
-    else e4m3 ? launch<CM_QCACHE_E4M3, 8, 8>(p, grid, stream) : launch<CM_QCACHE_INT8, 8, 8>(p, grid, stream);
-    return cudaGetLastError();
+    if (block <= 1024) return e4m3 ? launch<CM_QCACHE_E4M3, 1, 4>(p, grid, stream) : launch<CM_QCACHE_INT8, 1, 4>(p, grid, stream);
+    if (team == 1) return e4m3 ? launch<CM_QCACHE_E4M3, 1, 8>(p, grid, stream) : launch<CM_QCACHE_INT8, 1, 8>(p, grid, stream);
+    if (team == 4) return e4m3 ? launch<CM_QCACHE_E4M3, 4, 8>(p, grid, stream) : launch<CM_QCACHE_INT8, 4, 8>(p, grid, stream);
+    return e4m3 ? launch<CM_QCACHE_E4M3, 8, 8>(p, grid, stream) : launch<CM_QCACHE_INT8, 8, 8>(p, grid, stream);
 }
 
 }  // namespace cm

@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
     __shared__ uint32_t scan[kWarps];
     __shared__ uint32_t last_one;
     const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, g = lane / 4, t = lane % 4;
+    after_kernels_before();
 
     const uint32_t per_head = plan_units<kThreads, C::kRows, kTile, C::kSetup>(p, prefix, scan);
     const uint64_t units = (uint64_t)per_head * (uint32_t)p.heads;
@@ -381,8 +382,7 @@ cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cuda
         if (e != cudaSuccess) return e;
         if (device < 64) allowed.fetch_or(1ull << device);
     }
-    decode_kernel<D, FORMAT, NT><<<num_sms * C::kBlocksPerSm, kThreads, smem, stream>>>(p);
-    return cudaGetLastError();
+    return launch_behind(decode_kernel<D, FORMAT, NT>, dim3(num_sms * C::kBlocksPerSm), kThreads, smem, stream, p);
 }
 
 }  // namespace

@@ -484,6 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + C::kStages * C::kKvBytes;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
 
+    after_kernels_before();
     // the plan: one thread per request, prefix sums in the (still unused) tile memory
     uint32_t *prefix = reinterpret_cast<uint32_t *>(smem);
     uint32_t total = 0;
@@ -574,8 +575,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         }
         if (lane == 0) start = s;
     }
-    // the joining kernel may be set up from now on; it waits for this one's results by itself
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     fence_before();
     __syncthreads();
     fence_after();
@@ -887,7 +886,7 @@ template <int D>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ QcacheAttentionParams p) {
     using C = Shape<D>;
     constexpr int kJoinRows = C::kRows / 16, kColumns = kJoinThreads / kJoinRows, kVecs = D / 4 > kColumns ? D / 4 / kColumns : 1;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    after_kernels_before();
     const QcacheSplit z = p.splits[blockIdx.x];
     const int row = blockIdx.y * kJoinRows + threadIdx.x % kJoinRows, column = threadIdx.x / kJoinRows;
     if (z.row_tile * C::kRows + row >= z.rows || column >= D / 4) return;
@@ -952,19 +951,8 @@ cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cuda
         if (e != cudaSuccess) return e;
         if (device < 64) allowed.fetch_or(1ull << device);
     }
-    prefill_kernel<D, FORMAT><<<num_sms, kThreads, smem, stream>>>(p);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    cudaLaunchAttribute early;                  // it may be set up while the kernel before it ends
-    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    early.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t config{};
-    config.gridDim = dim3(num_sms, 16);
-    config.blockDim = dim3(kJoinThreads);
-    config.stream = stream;
-    config.attrs = &early;
-    config.numAttrs = 1;
-    return cudaLaunchKernelEx(&config, join_kernel<D>, p);
+    const cudaError_t e = launch_behind(prefill_kernel<D, FORMAT>, dim3(num_sms), kThreads, smem, stream, p);
+    return e != cudaSuccess ? e : launch_behind(join_kernel<D>, dim3(num_sms, 16), kJoinThreads, 0, stream, p);
 }
 
 }  // namespace

@@ -50,6 +50,7 @@ __device__ __forceinline__ int owner(const int32_t *starts, int n, int32_t x) {
 }
 
 __global__ void __launch_bounds__(kThreads) tables_kernel(const QcacheTablesParams p) {
+    after_kernels_before();
     extern __shared__ int32_t prefix[];   // row starts, then block starts, of the requests
     int32_t *row_start = prefix, *block_start = prefix + p.requests;
     __shared__ int64_t warp_rows[kWarps], warp_blocks[kWarps];
@@ -127,8 +128,7 @@ cudaError_t launch_qcache_tables(const QcacheTablesParams &p, int num_sms, cudaS
     }
     const int64_t want = (p.max_rows + kThreads - 1) / kThreads;
     const int grid = (int)(want < 1 ? 1 : want > 2 * num_sms ? 2 * num_sms : want);
-    tables_kernel<<<grid, kThreads, smem, stream>>>(p);
-    return cudaGetLastError();
+    return launch_behind(tables_kernel, dim3(grid), kThreads, smem, stream, p);
 }
 
 }  // namespace cm
