@@ -105,10 +105,11 @@ cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, unsigned int thr
     return cudaLaunchKernelEx(&config, kernel, args...);
 }
 
-// Waits until the kernels before this one have ended and their writes are seen, and lets the next one
-// be set up.
+// Waits until the kernels before this one have ended and their writes are seen. The next kernel is set up
+// when this one's blocks have ended: letting it in from the start held up short kernels (one token over
+// 1,041 cached: 8.4 us against 9.3).
 __device__ __forceinline__ void after_kernels_before() {
-    asm volatile("griddepcontrol.wait;\ngriddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 #endif
 
