@@ -183,53 +183,50 @@ template <int D, int WARPS, class At>
 __device__ __forceinline__ void join_parts(const QcacheAttentionParams &p, const AttentionSegment &w, int first, int rows,
                                            uint32_t c0, uint32_t c1, float headroom, int warp, At row_at) {
     constexpr int kVecs = D >= 128 ? D / 128 : 1;   // 16-byte vectors of a lane
-    constexpr int kAhead = 8;                       // parts that are read before they can be weighed
+    constexpr int kAhead = 8;              // parts that are read together, the first before they can be weighed
     const int lane = threadIdx.x % 32, n = (int)(c1 - c0 + 1);
     for (int row = warp; row < rows; row += WARPS) {
         auto read_ml = [&](int c) {
             return c < n ? __ldcg(reinterpret_cast<const float2 *>(p.part_ml + row_at(c0 + c, row) * 2)) : make_float2(-INFINITY, 0.f);
         };
-        auto read = [&](int c, int v) {
-            if ((D < 128 && lane >= D / 4) || c >= n) return make_float4(0.f, 0.f, 0.f, 0.f);
-            return __ldcg(reinterpret_cast<const float4 *>(p.part_o + row_at(c0 + c, row) * D) + lane + 32 * v);
+        float4 x[kAhead][kVecs], acc[kVecs];
+        auto read = [&](int c) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+                for (int v = 0; v < kVecs; ++v)
+                    x[k][v] = (D < 128 && lane >= D / 4) || c + k >= n
+                                  ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                  : __ldcg(reinterpret_cast<const float4 *>(p.part_o + row_at(c0 + c + k, row) * D) + lane + 32 * v);
         };
         float2 ml = read_ml(lane);
-        float4 early[kAhead][kVecs], acc[kVecs];
-#pragma unroll
-        for (int c = 0; c < kAhead; ++c)
-#pragma unroll
-            for (int v = 0; v < kVecs; ++v) early[c][v] = read(c, v);
+        read(0);
         float m = ml.x, l = 0.f;
         for (int c = 32 + lane; c < n; c += 32) m = fmaxf(m, read_ml(c).x);
 #pragma unroll
         for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-        auto add = [&](int v, const float4 &x, float g) {
-            acc[v].x = fmaf(x.x, g, acc[v].x); acc[v].y = fmaf(x.y, g, acc[v].y);
-            acc[v].z = fmaf(x.z, g, acc[v].z); acc[v].w = fmaf(x.w, g, acc[v].w);
-        };
-        for (int base = 0; base < n; base += 32) {
-            if (base > 0) ml = read_ml(base + lane);
-            const float f = ml.x == m ? 1.f : exp2_fast(ml.x - m);
-            float x = ml.y * f;
+        float f = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < n; c += kAhead) {
+            if (c > 0) read(c);
+            if (c % 32 == 0) {                      // the factors of the next 32 parts, one a lane
+                if (c > 0) ml = read_ml(c + lane);
+                f = ml.x == m ? 1.f : exp2_fast(ml.x - m);
+                float y = ml.y * f;
 #pragma unroll
-            for (int d = 16; d; d /= 2) x += __shfl_xor_sync(~0u, x, d);
-            l += x;
-            if (base == 0) {
-#pragma unroll
-                for (int c = 0; c < kAhead; ++c) {
-                    const float g = __shfl_sync(~0u, f, c);
-#pragma unroll
-                    for (int v = 0; v < kVecs; ++v) add(v, early[c][v], c < n ? g : 0.f);
-                }
+                for (int d = 16; d; d /= 2) y += __shfl_xor_sync(~0u, y, d);
+                l += y;
             }
-            const int most = min(32, n - base);
-#pragma unroll kAhead
-            for (int c = base == 0 ? kAhead : 0; c < most; ++c) {
-                const float g = __shfl_sync(~0u, f, c);
 #pragma unroll
-                for (int v = 0; v < kVecs; ++v) add(v, read(base + c, v), g);
+            for (int k = 0; k < kAhead; ++k) {
+                const float g = __shfl_sync(~0u, f, (c + k) % 32);
+#pragma unroll
+                for (int v = 0; v < kVecs; ++v) {
+                    acc[v].x = fmaf(x[k][v].x, g, acc[v].x); acc[v].y = fmaf(x[k][v].y, g, acc[v].y);
+                    acc[v].z = fmaf(x[k][v].z, g, acc[v].z); acc[v].w = fmaf(x[k][v].w, g, acc[v].w);
+                }
             }
         }
 #pragma unroll

@@ -13,14 +13,18 @@
 // down to 2^-28 of it), w to fp16 with M set so that w <= 2^15 (11 bits; w below 2^-40 of the
 // largest are lost), the result to bf16.
 //
-// Layout. A warp takes 16 tokens at a time through a ring of its own in shared memory, copied two or
-// more stages ahead (about 130 KB on their way per SM), into the fragments of mma.m16n8k16: scores as
+// Layout. A warp takes 16 tokens at a time through a ring of its own in shared memory, copied one to
+// three stages ahead (64 KB and more on their way per SM), into the fragments of mma.m16n8k16: scores as
 // K (16 tokens) x Q^T (8 rows), outputs as V^T (16 of head_dim) x w^T. Which element of head_dim a
 // fragment position stands for is free as long as K and Q (V and the output) agree, so every lane
-// reads whole vectors and no code is transposed. The work, every (request, kv head, tile of 64 tokens), is laid out on one line and cut
-// evenly over a grid that just fills the GPU; where a cut falls inside a (request, head), the
+// reads whole vectors and no code is transposed. The work, every (request, kv head, tile of 64 tokens),
+// is laid out on one line and cut evenly over a grid that just fills the GPU; where a cut falls inside a (request, head), the
 // parts meet in the workspace and whoever comes last joins them in their order, so that the
 // result does not depend on timing.
+//
+// Bound by HBM once the requests are long (above), by the chain of dependent reads (lengths, table, scales,
+// tokens, parts) when they are short: one token over 1,041 cached 8.4 us, over 131,072 57 us; 64 requests of
+// 600 to 12,000 tokens 84 us (5.9 TB/s); 29 requests, int8 drafts of 3 or 4 rows, 18 us.
 #include "cm_qcache_kernels.h"
 
 #include <atomic>
@@ -81,7 +85,10 @@ struct Decode {
     static constexpr int kBlocksPerSm = D == 256 ? 2 : NT == 2 ? 3 : 4;
     static constexpr int kSetup = D >= 128 ? 2 : 256 / D;     // about 2.5 us in tiles of 128 D bytes at a block's share of HBM
     static constexpr int kStageBytes = 32 * D;                // 16 tokens of K, then of V
-    static constexpr int kStages = D == 256 ? 3 : D == 128 ? 3 : D == 64 ? 6 : 8;
+    // More on its way at once is slower: 32 requests of 16,384 tokens, head_dim 128, take 167 us (6.4 TB/s) with two
+    // stages, 180 with three; head_dim 64 91 us with three, 95 with four, 103 with two; head_dim 256 170 with two, 181
+    // with three. So are more blocks with fewer registers (head_dim 64: five 101 us) and fewer blocks (three 103).
+    static constexpr int kStages = D >= 128 ? 2 : D == 64 ? 3 : 4;
     static constexpr int kRing = kWarps * kStages * kStageBytes;
     static constexpr int kMerge = kWarps * kRows * (kPitch + 2) * 4;   // over the ring, once it has been read
     static constexpr size_t kShared = kRing > kMerge ? kRing : kMerge;
