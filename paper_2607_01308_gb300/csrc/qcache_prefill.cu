@@ -11,21 +11,25 @@
 //   warps 8-11       K tiles, from global memory through registers to fp16 in shared memory, in the 128-byte
 //                    swizzle, the next tile's codes on their way meanwhile
 //   warps 12-15      V tiles
-//   warp 16          issues the matrix instructions: S = Q K^T (both operands from shared memory),
-//                    O += P V (P from tensor memory, V as it lies, tokens x head_dim)
+//   warp 16 (, 18)   issue the matrix instructions (at head_dim 128 a warp for each query tile):
+//                    S = Q K^T (both operands from shared memory), O += P V (P from tensor memory, V as it
+//                    lies, tokens x head_dim)
 //   warp 17          looks up blocks and scales of every 16 tokens, several tiles ahead
 // Scores are computed two kv tiles ahead, into two buffers for each query tile, so that the softmax warps
 // always have a tile at hand while the tensor cores take the last one's weights. Products of 128 x 64 leave
 // a third of the tensor cores' time to the operands' way from shared memory; with tiles of 128 tokens, for
-// which there is one buffer, softmax and products waited for each other and took 4,100 to 5,000 cycles for
-// 256 x 128 scores. A second, small kernel joins
-// the ranges that were cut between thread blocks, over the whole GPU (one thread block alone took 95 us
-// for 256 rows in 19 parts). The softmax warps take
-// registers over from the others. Work is cut as in
-// qcache_attention.cu, over kv tiles that the rows of a tile may see at all.
+// which there is one buffer, softmax and products wait for each other (513 us against 467 for the chunk
+// below). The softmax warps take registers over from the others. Work is cut as in qcache_attention.cu, over
+// kv tiles that the rows of a tile may see at all; a second, small kernel joins the ranges that were cut
+// between thread blocks, over the whole GPU (one thread block alone took 95 us for 256 rows in 19 parts).
+//
+// Bound by the tensor cores and the softmax's latency together (the tensor pipe is 55 to 60 % busy): 2,048
+// rows x 4 heads of a group over 16,384 tokens, 8 kv heads of 128, 467 us (1,250 TFLOP/s); by latency where
+// prompts are short: 64 tokens 10.5 us, five ragged ones of head_dim 256 50 us.
 #include "cm_qcache_kernels.h"
 
 #include <atomic>
+#include <type_traits>
 
 #include "cm_qcache_attention.h"
 #include "cm_qcache_codes.h"
@@ -34,7 +38,7 @@ namespace cm {
 namespace {
 
 constexpr int kSoftmaxWarps = 8, kLoadWarps = 4;              // load warps: for K, and as many for V
-constexpr int kMmaWarp = kSoftmaxWarps + 2 * kLoadWarps, kEntryWarp = kMmaWarp + 1;
+constexpr int kMmaWarp = kSoftmaxWarps + 2 * kLoadWarps, kEntryWarp = kMmaWarp + 1, kSecondMmaWarp = kMmaWarp + 2;
 constexpr int kThreads = 20 * 32;           // whole warpgroups: registers change hands by warpgroup
 constexpr int kLaunchRegs = 96;
 constexpr int kLoadThreads = kLoadWarps * 32;
@@ -48,6 +52,10 @@ template <int D>
 struct Shape {
     // tensor memory, 512 columns: two buffers of scores for each query tile, and the outputs
     static constexpr int kQTiles = D == 256 ? 1 : 2;
+    // Warps that issue: one for each query tile at head_dim 128, where one for both waits for the weights of one
+    // tile while those of the other are there (2,048 tokens over 16,384: 467 us against 520); below, where the
+    // products are short, one (head_dim 64: 433 us against 461), which keeps the two tiles' softmax apart.
+    static constexpr int kIssuers = D == 128 ? 2 : 1;
     static constexpr int kRows = 128 * kQTiles;
     static constexpr int kOColumn = kQTiles * 2 * kTile;
     static constexpr int kSetup = 3;                          // a segment's queries and its end, in tiles
@@ -519,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     if (tid == 0) {
         for (int i = 0; i < C::kStages; ++i) {
             bar_init(&bars.kv_full[i], 2 * kLoadWarps);
-            bar_init(&bars.kv_empty[i], 1);
+            bar_init(&bars.kv_empty[i], C::kIssuers);
         }
         for (int i = 0; i < kEntryStages; ++i) bar_init(&bars.entry_full[i], 1);
         for (int i = 0; i < 2; ++i) {
@@ -530,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             bar_init(&bars.q_full[i], 128);
             bar_init(&bars.o_full[i], 1);
             bar_init(&bars.o_done[i], 1);
-            bar_init(&bars.entry_empty[i], 1);
+            bar_init(&bars.entry_empty[i], C::kIssuers);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
@@ -778,6 +786,72 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         for (int stage = 0; stage < C::kStages; ++stage) wait.warp(&bars.kv_empty[stage], freed.use(stage) ^ 1);
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kIssueRegs));
+      // ------------------------------------------------ the matrix instructions of query tiles Q0 .. Q1 - 1
+      // (a whole warp goes through it, one of its threads issues)
+      auto issue = [&](auto q0, auto q1) {
+        constexpr int Q0 = decltype(q0)::value, Q1 = decltype(q1)::value;
+        constexpr uint32_t s_instruction = instruction(128, kTile, false), o_instruction = instruction(128, D, true);
+        const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
+        const uint32_t leader = elect();
+        uint32_t n_tile = 0, segment[2] = {0, 0};                // segment: those with rows in the query tile
+        Parity filled, weighted[2];
+        bool split = false;
+        while (__any_sync(~0u, walk.next(p))) {
+            if (Q0 == 0 && w.t0 == 0 && w.t1 < w.tiles) {
+                // the part that begins a range which the next blocks go on with: for the joining kernel
+                split = true;
+                if (leader)
+                    p.splits[blockIdx.x] = {w.request, w.head, w.row_tile, w.row0, w.rows, (int)((w.unit0 + w.tiles - 1) / start.per)};
+            }
+            // votes, so that the branches are uniform
+            const int tiles = w.t1 - w.t0;
+            const bool both = C::kQTiles == 2 && __any_sync(~0u, w.rows - w.row_tile * C::kRows > 128);
+#pragma unroll
+            for (int qt = Q0; qt < Q1; ++qt)
+                if (qt == 0 || both) wait.warp(&bars.q_full[qt], segment[qt]++ & 1);
+            // Scores two tiles ahead of the products, one query tile after the other.
+            for (int i = -2; __any_sync(~0u, i < tiles); ++i) {
+                const uint32_t buffer = i & 1, stage = (i + 2) & (C::kStages - 1);
+                const bool ahead = __any_sync(~0u, i + 2 < tiles);
+                wait.warp(&bars.kv_full[stage], filled.use(stage));
+                fence_after();
+#pragma unroll
+                for (int qt = Q0; qt < Q1; ++qt) {
+                    if (qt == 1 && !both) break;
+                    if (i >= 0) {
+                        wait.warp(&bars.p_full[qt][buffer], weighted[qt].use(buffer));
+                        fence_after();
+                        const uint32_t a = (qt * 2 + buffer) * kTile, b = operand_lo(v_at + stage * C::kKvBytes, C::kKvPanel);
+#pragma unroll
+                        for (int j = 0; j < kTile / 16; ++j)
+                            mma_ts(C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, j > 0 || i > 0, leader);
+                        if (!ahead) {
+                            if (__any_sync(~0u, i + 2 == tiles)) commit(&bars.o_done[qt], leader);
+                            else commit(&bars.o_full[qt], leader);
+                        }
+                    }
+                    if (ahead) {
+                        const uint32_t a = operand_lo(q_at + qt * C::kPanels * C::kQPanel, 16), b = operand_lo(k_at + stage * C::kKvBytes, 16);
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)
+                            mma_ss((qt * 2 + buffer) * kTile, operand(a + k / 4 * (C::kQPanel / 16) + k % 4 * 2),
+                                   operand(b + k / 4 * (C::kKvPanel / 16) + k % 4 * 2), s_instruction, k > 0, leader);
+                        commit(&bars.s_full[qt][buffer], leader);
+                    }
+                }
+                commit(&bars.kv_empty[stage], leader);
+                if (i >= 0) {
+                    // these tiles' softmax threads have read the kv tile's entries, and so have the loads long before
+                    if (n_tile % kEntryTiles == kEntryTiles - 1 && leader) bar_arrive(&bars.entry_empty[n_tile / kEntryTiles % 2]);
+                    ++n_tile;
+                }
+            }
+        }
+        if (Q0 == 0 && !split && leader) p.splits[blockIdx.x].rows = 0;
+      };
+      using First = std::integral_constant<int, 0>;
+      using Second = std::integral_constant<int, 1>;
+      using All = std::integral_constant<int, C::kQTiles>;
       if (warp == kEntryWarp) {
         // ------------------------------------------------ blocks and scales, kEntryTiles tiles at a time
         uint32_t n_tile = 0;
@@ -805,66 +879,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             }
         }
       } else if (warp == kMmaWarp) {
-        // ------------------------------------------------ the matrix instructions
-        constexpr uint32_t s_instruction = instruction(128, kTile, false), o_instruction = instruction(128, D, true);
-        const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
-        const uint32_t leader = elect();
-        uint32_t n_tile = 0, segment = 0, second = 0;            // second: segments with rows in the second query tile
-        Parity filled, weighted[2];
-        bool split = false;
-        // scores of a query tile with the K tile in `stage`
-        auto scores = [&](int qt, uint32_t buffer, uint32_t stage) {
-            const uint32_t a = operand_lo(q_at + qt * C::kPanels * C::kQPanel, 16), b = operand_lo(k_at + stage * C::kKvBytes, 16);
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                mma_ss((qt * 2 + buffer) * kTile, operand(a + k / 4 * (C::kQPanel / 16) + k % 4 * 2),
-                       operand(b + k / 4 * (C::kKvPanel / 16) + k % 4 * 2), s_instruction, k > 0, leader);
-            commit(&bars.s_full[qt][buffer], leader);
-        };
-        while (__any_sync(~0u, walk.next(p))) {
-            if (w.t0 == 0 && w.t1 < w.tiles) {
-                // the part that begins a range which the next blocks go on with: for the joining kernel
-                split = true;
-                if (leader)
-                    p.splits[blockIdx.x] = {w.request, w.head, w.row_tile, w.row0, w.rows, (int)((w.unit0 + w.tiles - 1) / start.per)};
-            }
-            // votes, so that the branches are uniform
-            const int tiles = w.t1 - w.t0;
-            const bool both = C::kQTiles == 2 && __any_sync(~0u, w.rows - w.row_tile * C::kRows > 128);
-            wait.warp(&bars.q_full[0], segment++ & 1);
-            if (both) wait.warp(&bars.q_full[1], second++ & 1);
-            // Scores two tiles ahead of the products, one query tile after the other.
-            for (int i = -2; __any_sync(~0u, i < tiles); ++i) {
-                const uint32_t buffer = i & 1, stage = (i + 2) & (C::kStages - 1);
-                const bool ahead = __any_sync(~0u, i + 2 < tiles);
-                wait.warp(&bars.kv_full[stage], filled.use(stage));
-                fence_after();
-#pragma unroll
-                for (int qt = 0; qt < C::kQTiles; ++qt) {
-                    if (qt == 1 && !both) break;
-                    if (i >= 0) {
-                        wait.warp(&bars.p_full[qt][buffer], weighted[qt].use(buffer));
-                        fence_after();
-                        const uint32_t a = (qt * 2 + buffer) * kTile, b = operand_lo(v_at + stage * C::kKvBytes, C::kKvPanel);
-#pragma unroll
-                        for (int j = 0; j < kTile / 16; ++j)
-                            mma_ts(C::kOColumn + qt * D, a + j * 8, operand(b + j * 128), o_instruction, j > 0 || i > 0, leader);
-                        if (!ahead) {
-                            if (__any_sync(~0u, i + 2 == tiles)) commit(&bars.o_done[qt], leader);
-                            else commit(&bars.o_full[qt], leader);
-                        }
-                    }
-                    if (ahead) scores(qt, buffer, stage);
-                }
-                commit(&bars.kv_empty[stage], leader);
-                if (i >= 0) {
-                    // every softmax thread has read the tile's entries, and so have the loads long before
-                    if (n_tile % kEntryTiles == kEntryTiles - 1 && leader) bar_arrive(&bars.entry_empty[n_tile / kEntryTiles % 2]);
-                    ++n_tile;
-                }
-            }
-        }
-        if (!split && leader) p.splits[blockIdx.x].rows = 0;
+        if constexpr (C::kIssuers == 2) issue(First{}, Second{});
+        else issue(First{}, All{});
+      } else if (warp == kSecondMmaWarp) {
+        if constexpr (C::kIssuers == 2) issue(Second{}, All{});
       }
     }
     fence_before();
