@@ -1,6 +1,6 @@
 // Host side of the 8-bit paged cache (cm_qcache_* of include/cm.h): every argument that the host
-// can see is checked before the one launch of each call. Nothing is allocated or kept, so the calls
-// take no lock.
+// can see is checked before anything is launched. Nothing is allocated or kept, so the calls take
+// no lock.
 #include "cm.h"
 
 #include <cmath>

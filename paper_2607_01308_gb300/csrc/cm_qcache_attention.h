@@ -35,9 +35,9 @@ template <int ROWS, int TILE>
 __device__ __forceinline__ RequestShape request_shape(const QcacheAttentionParams &p, int r) {
     RequestShape s;
     const int64_t cap = min(p.table_width << p.log2_block, (int64_t)INT32_MAX - 1024);
-    s.row0 = min(max(__ldg(p.row_starts + r), 0), p.total_rows);
-    s.q_len = min(max(__ldg(p.row_starts + r + 1), s.row0), p.total_rows) - s.row0;
-    s.kv = (int)min((int64_t)max(__ldg(p.kv_lens + r), 0), cap);
+    s.row0 = min(max(p.row_starts[r], 0), p.total_rows);
+    s.q_len = min(max(p.row_starts[r + 1], s.row0), p.total_rows) - s.row0;
+    s.kv = (int)min((int64_t)max(p.kv_lens[r], 0), cap);
     s.rows = s.q_len * p.group;
     s.row_tiles = (s.rows + ROWS - 1) / ROWS;
     s.tiles = max(1, (s.kv + TILE - 1) / TILE);   // one without tokens too: its rows are written
@@ -134,13 +134,13 @@ struct BlockEntry {
 __device__ __forceinline__ BlockEntry block_entry(const QcacheAttentionParams &p, int request, int64_t head, int64_t token, int kv) {
     BlockEntry e{-1, 0.f, 0.f, 0.f};
     if (token < kv) {
-        const int b = __ldg(p.block_table + request * p.table_width + (token >> p.log2_block));
+        const int b = p.block_table[request * p.table_width + (token >> p.log2_block)];
         if (b >= 0 && b < p.num_blocks) {
             const int64_t at = (int64_t)b * p.scale_stride_block + head * p.scale_stride_head;
             // V scales are read within [2^-60, 2^60], where w / scale stays in fp32's range
-            const float v = fminf(fmaxf(__ldg(p.v_scale + at), 0x1p-60f), 0x1p60f);
+            const float v = fminf(fmaxf(p.v_scale[at], 0x1p-60f), 0x1p60f);
             e.block = b;
-            e.k_scale = __ldg(p.k_scale + at);
+            e.k_scale = p.k_scale[at];
             e.v_log2 = __log2f(v);
             e.v_inverse = __frcp_rn(v);
         }

@@ -89,7 +89,9 @@ size_t qcache_prefill_part_rows(int head_dim);
 
 #ifdef __CUDACC__
 // Launches a kernel that may be set up while the one before it in the stream ends. Its threads call
-// after_kernels_before() before they read or write global memory; nothing else is relaxed.
+// after_kernels_before() before they read or write global memory; nothing else is relaxed. (The
+// kernels read with plain loads throughout: what a kernel before still writes while this one is set up is not
+// read-only for its life, as the non-coherent loads ask.)
 template <class... Params, class... Args>
 cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, unsigned int threads, size_t shared, cudaStream_t stream, const Args &...args) {
     cudaLaunchAttribute early;

@@ -225,12 +225,12 @@ struct Run {
 __device__ __forceinline__ int find_runs(const QcacheAppendParams &p, int64_t row0, int64_t row1, Run *runs) {
     const int lane = threadIdx.x % 32;
     const int64_t r = row0 + lane, mask = ((int64_t)1 << p.log2_block) - 1;
-    const int64_t slot = r < p.num_rows ? __ldg(p.slots + r) : -1;
-    const int64_t after = r + 32 < p.num_rows ? __ldg(p.slots + r + 32) : -1;   // where the runs may go on
+    const int64_t slot = r < p.num_rows ? p.slots[r] : -1;
+    const int64_t after = r + 32 < p.num_rows ? p.slots[r + 32] : -1;   // where the runs may go on
     int64_t before = __shfl_up_sync(~0u, slot, 1), after_before = __shfl_up_sync(~0u, after, 1);
     const int64_t last = __shfl_sync(~0u, slot, 31);
     if (lane == 0) {
-        before = r > 0 ? __ldg(p.slots + r - 1) : -1;
+        before = r > 0 ? p.slots[r - 1] : -1;
         after_before = last;
     }
     auto goes_on = [&](int64_t x, int64_t b) { return b >= 0 && x == b + 1 && (x & mask) != 0; };
@@ -248,7 +248,7 @@ __device__ __forceinline__ int find_runs(const QcacheAppendParams &p, int64_t ro
         int m = 64 - l;
         unsigned more = ~0u;
         while (more == ~0u && m < limit) {
-            more = __ballot_sync(~0u, m + lane < limit && __ldg(p.slots + row0 + l + m + lane) == first + m + lane);
+            more = __ballot_sync(~0u, m + lane < limit && p.slots[row0 + l + m + lane] == first + m + lane);
             m += more == ~0u ? 32 : __ffs(~more) - 1;
         }
         if (lane == l) n = m;

@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
             for (int c = 0; c < D / (4 * C::kVecK); ++c)
 #pragma unroll
                 for (int e = 0; e < C::kVecK / 8; ++e) {
-                    const uint4 x = valid ? __ldg(reinterpret_cast<const uint4 *>(q + c * 4 * C::kVecK + t * C::kVecK + e * 8))
+                    const uint4 x = valid ? *reinterpret_cast<const uint4 *>(q + c * 4 * C::kVecK + t * C::kVecK + e * 8)
                                           : make_uint4(0, 0, 0, 0);
                     const int at = c * C::kVecK / 2 + e * 4;
                     raw[at] = x.x; raw[at + 1] = x.y; raw[at + 2] = x.z; raw[at + 3] = x.w;

@@ -553,6 +553,54 @@ def test_refusals(ctx):
     cache.attend(q[:0], batch)
 
 
+@pytest.mark.parametrize("rows", [1, 40])
+def test_steps_in_a_row_equal_steps_with_waits_between(ctx, rows):
+    """Each call reads what the one before it wrote (tables, slots, codes, scales), with nothing between them that
+    waits: the same bits as with a synchronisation after every call."""
+    R, H, G, d, block, steps = 5, 2, 4, 64, 16, 24
+    width = -(-(steps * rows + 200) // block)
+
+    def run(wait):
+        g = torch.Generator(device=DEV).manual_seed(17)
+        cache = cm.QCache(ctx, R * width, block, 1, H, d)
+        b = cm.QBatch(ctx, R, width, R * rows, block)
+        b.max_new = rows
+        free = torch.randperm(R * width, generator=torch.Generator().manual_seed(3)).int().to(DEV)
+        held = [3 * r for r in range(R)]
+        first = cm.QBatch(ctx, R, width, sum(held), block)
+        first.schedule(_i32([0] * R), _i32(held), free)
+        free = free[sum(-(-h // block) for h in held):].contiguous()
+        b.block_table.copy_(first.block_table)
+        x = torch.randn((2, 1, H, sum(held), d), generator=g, device=DEV).bfloat16()
+        cache.append(x[0], x[1], first.slot_map)
+        lens, new = _i32(held), _i32([rows] * R)
+        inputs = [torch.randn((2, 1, H, R * rows, d), generator=g, device=DEV).bfloat16() for _ in range(steps)]
+        queries = [torch.randn((R * rows, H * G, d), generator=g, device=DEV).bfloat16() for _ in range(steps)]
+        frees = []
+        for _ in range(steps):
+            frees.append(free)
+            free = free[sum(-(-(h + rows) // block) - -(-h // block) for h in held):].contiguous()
+            held = [h + rows for h in held]
+        lengths = [lens + t * rows for t in range(steps)]
+        torch.cuda.synchronize()
+        outs = []
+        for t in range(steps):
+            b.schedule(lengths[t], new, frees[t])
+            if wait:
+                torch.cuda.synchronize()
+            cache.append(inputs[t][0], inputs[t][1], b.slot_map)
+            if wait:
+                torch.cuda.synchronize()
+            outs.append(cache.attend(queries[t], b)[0])
+            if wait:
+                torch.cuda.synchronize()
+        ctx.check()
+        return outs
+
+    for a, c in zip(run(True), run(False)):
+        assert torch.equal(a, c)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_example_answers_from_merged_caches(fmt):
     """Render, schedule, append and attend together. A value's rounding is at most 2^-4 of it (e4m3, three bits
