@@ -25,7 +25,7 @@
 //
 // Bound by the tensor cores and the softmax's latency together (the tensor pipe is 55 to 60 % busy): 2,048
 // rows x 4 heads of a group over 16,384 tokens, 8 kv heads of 128, 467 us (1,250 TFLOP/s); by latency where
-// prompts are short: 64 tokens 10.5 us, five ragged ones of head_dim 256 50 us.
+// prompts are short: 64 tokens 10.5 us, five ragged ones of head_dim 256 47 us.
 #include "cm_qcache_kernels.h"
 
 #include <atomic>
@@ -58,7 +58,7 @@ struct Shape {
     static constexpr int kIssuers = D == 128 ? 2 : 1;
     static constexpr int kRows = 128 * kQTiles;
     static constexpr int kOColumn = kQTiles * 2 * kTile;
-    static constexpr int kSetup = 3;                          // a segment's queries and its end, in tiles
+    static constexpr int kSetup = 4;                          // a segment's queries and its end, in tiles: 8,700 to 11,000 cycles
     static constexpr int kPanels = D < 64 ? 1 : D / 64;       // 64 columns (128 bytes) of fp16 each
     static constexpr int kStages = D == 256 ? 2 : 4;          // tiles of K, of V
     static constexpr int kQPanel = 128 * 128, kKvPanel = kTile * 128;   // bytes
