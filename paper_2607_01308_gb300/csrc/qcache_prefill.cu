@@ -24,7 +24,7 @@
 // between thread blocks, over the whole GPU (one thread block alone took 95 us for 256 rows in 19 parts).
 //
 // Bound by the tensor cores and the softmax's latency together (the tensor pipe is 55 to 60 % busy): 2,048
-// rows x 4 heads of a group over 16,384 tokens, 8 kv heads of 128, 467 us (1,250 TFLOP/s); by latency where
+// rows x 4 heads of a group over 16,384 tokens, 8 kv heads of 128, 464 us (1,260 TFLOP/s); by latency where
 // prompts are short: 64 tokens 10.5 us, five ragged ones of head_dim 256 47 us.
 #include "cm_qcache_kernels.h"
 
@@ -161,12 +161,14 @@ __device__ __forceinline__ void tmem_ld(uint32_t (&x)[8], uint32_t at) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]) : "r"(at));
 }
+// Waits for the loads; what is done with x comes after that, copies of its registers too.
 __device__ __forceinline__ void ld_wait(uint32_t (&x)[32]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" : CM_INOUT16(x, 0), CM_INOUT16(x, 16) :: "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    asm volatile("" : CM_INOUT16(x, 0), CM_INOUT16(x, 16) :: "memory");
 }
 __device__ __forceinline__ void ld_wait(uint32_t (&x)[8]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]) :: "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    asm volatile("" : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]) :: "memory");
 }
 __device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&x)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -255,14 +257,15 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // A kv tile of one row: scores x to weights w (fp16 pairs). left: columns that the row sees (only if
 // `masked`, which is the warp's). Where the largest exponent of some row passes its limit, that row's maximum is
 // raised by as much, its sum and, unless this is the first tile (behind `wait_output`), its output rescaled.
-template <int D, class Wait>
+template <int D, class Wait, class Store>
 __device__ __forceinline__ void softmax_tile(uint32_t (&x)[2][32], uint32_t (&w)[2][16], uint32_t o_at, const float4 *scale,
                                              const float4 &inverse, float factor, bool masked, int left, bool first, RowState &r,
-                                             Wait wait_output) {
+                                             Wait wait_output, Store store) {
     const float base = kHeadroom - r.top;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         const float4 z = scale[c];                                // of two blocks
+        if (c == 1) ld_wait(x[1]);
 #pragma unroll
         for (int k = 0; k < 32; k += 2) {
             const float a = factor * (k < 16 ? z.x : z.z), d = (k < 16 ? z.y : z.w) + base;
@@ -310,7 +313,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t (&x)[2][32], uint32_t (&w)
         }
     }
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < 2; ++c) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             uint64_t part = 0;
@@ -324,6 +327,8 @@ __device__ __forceinline__ void softmax_tile(uint32_t (&x)[2][32], uint32_t (&w)
             unpair(part, p0, p1);
             r.sum = fmaf(p0 + p1, c ? (b ? inverse.w : inverse.z) : (b ? inverse.y : inverse.x), r.sum);
         }
+        store(c);
+    }
 }
 
 // The warp's 32 query rows, rows first .. first + 31 of the request, to fp16 with a power of two per row,
@@ -631,18 +636,17 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 const uint32_t tile = s_at + buffer * kTile;
                 uint32_t x[2][32], y[2][16];
                 tmem_ld(x[0], tile);
-                tmem_ld(x[1], tile + 32);
                 ld_wait(x[0]);
-                ld_wait(x[1]);                                    // both: the second wait orders its own registers
+                tmem_ld(x[1], tile + 32);                         // on its way while the first half is scaled
                 softmax_tile<D>(x, y, o_at, reinterpret_cast<const float4 *>(entry.scale), *reinterpret_cast<const float4 *>(entry.v_inverse),
                                 factor, (t + 1) * kTile > least, limit - t * kTile, t == t0, r,
                                 // the tile before is in the output when the next tile's scores are there, which came after it
                                 [&] {
                                     if (t + 1 < t1) wait.warp(&bars.s_full[qt][buffer ^ 1], scored.peek(buffer ^ 1));
                                     else wait.warp(&bars.o_done[qt], done);
-                                });
-                tmem_st16(tile, y[0]);                            // into columns whose scores have been read
-                tmem_st16(tile + 16, y[1]);
+                                },
+                                // into columns whose scores have been read, the first half while the second is computed
+                                [&](int c) { tmem_st16(tile + 16 * c, y[c]); });
                 st_wait();
                 fence_before();
                 bar_arrive(&bars.p_full[qt][buffer]);
