@@ -15,8 +15,8 @@
 // block finds the runs that begin in its window of rows; then a warp takes a run of one head, K or
 // V: it reads it into registers, reduces the magnitude, writes the scale and the codes, so that every
 // element is read once. Bound by HBM: 2 bytes in and 1 out per element. Measured: 36 layers of 8
-// heads of 128, 5,208 tokens (1,153 MB): 183 us, 6.3 TB/s; 10,300 ragged int8 rows of 12 heads of 64
-// (47 MB, two waves of thread blocks): 13.9 us; one token of 48 requests: 2.6 us, a launch's latency.
+// heads of 128, 5,208 tokens (1,153 MB): 175 us, 6.6 TB/s; 10,300 ragged int8 rows of 12 heads of 64
+// (47 MB, two waves of thread blocks): 13.8 us; one token of 48 requests: 2.6 us, a launch's latency.
 #include "cm_qcache_kernels.h"
 
 #include "cm_qcache_codes.h"
@@ -308,8 +308,8 @@ cudaError_t launch(const QcacheAppendParams &p, const dim3 &grid, cudaStream_t s
 cudaError_t launch_qcache_append(QcacheAppendParams p, int num_sms, cudaStream_t stream) {
     if (p.num_rows == 0) return cudaSuccess;
     // Who holds a run in registers, by the elements of a block of one head:
-    //   to 1024    a warp with 4 vectors a lane, 32 warps to an SM (blocks of 16 x 64, 302 MB of int8:
-    //              180 us; 226 us with 40 warps, 212 with 24)
+    //   to 1024    a warp with 4 vectors a lane, 32 warps to an SM (blocks of 16 x 64, 886 MB of int8:
+    //              158 us; with 40 warps a quarter more, with 24 a sixth)
     //   to 4096    a warp with 8 vectors a lane, 24 warps to an SM
     //   above      four warps, of more than 16384 eight (blocks of 128 x 256: 242 us, with four 257,
     //              with sixteen, of which fewer fit an SM, 381); all head_dim above 256 are here. Short
@@ -318,12 +318,13 @@ cudaError_t launch_qcache_append(QcacheAppendParams p, int num_sms, cudaStream_t
     const int64_t block = (int64_t)p.head_dim << p.log2_block;
     const int team = block <= 4096 ? 1 : block <= 16384 ? 4 : 8, per = team == 1 ? 2 : 1;
     const int head_groups = (p.heads + per - 1) / per;
-    // Rows per thread block: one while that leaves every SM less than about 16 thread blocks
-    // (single tokens: each row is a run of its own), up to a block of tokens, which is one run
-    // of a prompt. (With 64 thread blocks the ragged int8 rows take 16.1 us, with 16 13.9.)
+    // Rows per thread block: one while that leaves every SM less than about 16 thread blocks (single
+    // tokens: each row is a run of its own), up to 32, of which a warp looks at the slots in one go. (With 64
+    // thread blocks to an SM the ragged int8 rows take 16.1 us, with 16 13.8; with windows of no more than a block
+    // of tokens the merge takes 183 us, with 32 rows 175, with 64 the same.)
     const int64_t blocks_of_one = p.num_rows * head_groups * p.layers;
     int window = 1;
-    while (window < 32 && window < (1 << p.log2_block) && blocks_of_one / window > 16ll * num_sms) window *= 2;
+    while (window < 32 && blocks_of_one / window > 16ll * num_sms) window *= 2;
     p.window = window;
     const dim3 grid((unsigned)((p.num_rows + window - 1) / window), (unsigned)head_groups, (unsigned)p.layers);
     const bool e4m3 = p.format == CM_QCACHE_E4M3;

@@ -18,7 +18,7 @@
 // Scores are computed two kv tiles ahead, into two buffers for each query tile, so that the softmax warps
 // always have a tile at hand while the tensor cores take the last one's weights. Products of 128 x 64 leave
 // a third of the tensor cores' time to the operands' way from shared memory; with tiles of 128 tokens, for
-// which there is one buffer, softmax and products wait for each other (513 us against 467 for the chunk
+// which there is one buffer, softmax and products wait for each other (513 us against 464 for the chunk
 // below). The softmax warps take registers over from the others. Work is cut as in qcache_attention.cu, over
 // kv tiles that the rows of a tile may see at all; a second, small kernel joins the ranges that were cut
 // between thread blocks, over the whole GPU (one thread block alone took 95 us for 256 rows in 19 parts).
