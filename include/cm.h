@@ -437,7 +437,7 @@ cm_status cm_measure_int_alu(int32_t device, double *xor3_tops, double *compress
  *     cm_qcache_append     K and V rows (a render's, or a layer's new tokens) into their slots
  *     cm_qcache_attend     softmax(scale q K^T) V over each request's own tokens
  * Each enqueues one kernel on `stream` (cm_qcache_attend two when a request may bring more than 32
- * query rows to a kv head) and returns without waiting; they allocate nothing and
+ * query rows to a kv head, 16 at head_dim 256) and returns without waiting; they allocate nothing and
  * keep nothing between calls, so they can be captured in a CUDA graph. Lengths, tables and slots
  * are DEVICE arrays that the host never reads; entries that name no block of the pool, and lengths
  * beyond the buffers, are left out rather than followed. Distinct arguments must not overlap

@@ -423,12 +423,14 @@ void qcache_workspace_split(QcacheAttentionParams &p, void *workspace, int num_s
 
 cudaError_t launch_qcache_attention(const QcacheAttentionParams &p, int rows_per_request, int num_sms, int device,
                                     cudaStream_t stream) {
-    // Rows of a request and kv head: to 8 in one fragment, to 16 in two at once, to 32 in two tiles of those,
-    // which read the cache twice; above, the other kernel. Measured, 32 requests of 4,096 tokens, 8 kv heads:
+    // Rows of a request and kv head: to 8 in one fragment, to 16 in two at once, to 32 (not at head_dim 256) in two
+    // tiles of those, which read the cache twice; above, the other kernel. Measured, 32 requests of 4,096 tokens, 8 kv heads:
     //   head_dim 128 e4m3   8 rows 55 us, as two fragments 57; 16 rows 61 us, as two tiles of one 99 or more;
     //                       32 rows 100 us, by the other kernel 109
     //   head_dim 64 int8    8 rows 36 us, as two fragments 42; 32 rows 73 us, by the other kernel 92
-    if (rows_per_request > 32) return launch_qcache_prefill(p, num_sms, device, stream);
+    //   head_dim 32 e4m3    32 rows 51 us, by the other kernel 82
+    //   head_dim 256 e4m3   (16 requests, 4 kv heads) 32 rows 59 us, by the other kernel 48
+    if (rows_per_request > (p.head_dim == 256 ? 16 : 32)) return launch_qcache_prefill(p, num_sms, device, stream);
 #define CM_LAUNCH(D, F) \
     if (p.head_dim == D && p.format == F) \
         return rows_per_request <= 8 ? launch<D, F, 1>(p, num_sms, device, stream) : launch<D, F, 2>(p, num_sms, device, stream);
