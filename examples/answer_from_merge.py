@@ -127,10 +127,10 @@ def main(requests=16, layers=8, kv_heads=8, group=4, dim=128, tokens=(300, 900),
         positions = (torch.tensor(held).cuda()[:, None] + torch.arange(rows, device="cuda")).reshape(-1)
         for layer in range(layers):
             q, k, v = model.project(layer, x, positions)
-            # [rows, heads, d] as [1, heads, rows, d]; K and V are views of one projection's strides or their own
-            k, v = k.contiguous(), v.contiguous()
+            v = v.contiguous()                            # strides as K's, which its rotation has laid out anew
+            # [rows, heads, d] is taken as it is, as a view [1, heads, rows, d]
             cache.append(k.transpose(0, 1)[None], v.transpose(0, 1)[None], batch.slot_map, layer=layer)
-            out, _ = cache.attend(q.contiguous(), batch, layer=layer)
+            out, _ = cache.attend(q, batch, layer=layer)
             if check:
                 for r in range(requests):
                     mine = slice(r * rows, (r + 1) * rows)
