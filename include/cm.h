@@ -493,11 +493,20 @@ typedef struct cm_qcache_batch {
  *   counts          [2]: blocks needed (taken from the front of free_blocks, if there were as many)
  *                   and rows
  * Tokens beyond the table's width get no block (kv_lens stops there); rows beyond max_rows are not
- * written (row_starts stops there). context_lens must not be batch->kv_lens. Limits:
+ * written (row_starts stops there). The two no longer fit together for a request that is cut short so: its attention
+ * needs its context length besides (cm_qcache_query.context_lens). context_lens must not be batch->kv_lens. Limits:
  * R <= 16384, max_rows < 2^31, block_size as for cm_qcache. */
 cm_status cm_qcache_schedule(cm_context *ctx, const cm_qcache_batch *batch, const int32_t *context_lens,
                              const int32_t *new_lens, const int32_t *free_blocks, int64_t num_free,
                              int64_t *slot_map, int64_t max_rows, int64_t *counts, cm_stream_t stream);
+
+/* As cm_qcache_schedule, and writes what cm_qcache_query.context_lens takes: context_out [R] (nullable DEVICE, none of
+ * the other arrays) becomes the tokens that request r held where the table's width or max_rows cut it
+ * short, and -1 elsewhere. */
+cm_status cm_qcache_schedule_cut(cm_context *ctx, const cm_qcache_batch *batch, const int32_t *context_lens,
+                                 const int32_t *new_lens, const int32_t *free_blocks, int64_t num_free,
+                                 int64_t *slot_map, int64_t max_rows, int64_t *counts, int32_t *context_out,
+                                 cm_stream_t stream);
 
 /* K and V rows into their slots, for layers [layer, layer + num_layers) of the cache. Row i of
  * head h of the j-th of those layers has head_dim bf16 values, contiguous, at element
@@ -531,11 +540,21 @@ typedef struct cm_qcache_query {
     int32_t num_q_heads;                 /* a multiple of num_kv_heads */
     int32_t max_rows_per_request;        /* the most query rows of one request that are expected;
                                             it chooses the kernel, not the result */
-    int32_t causal;                      /* nonzero: row i of a request's n rows sees its first
-                                            kv_len - n + i + 1 tokens; 0: all kv_len */
+    int32_t causal;                      /* nonzero: a row sees its request's tokens up to its own, row i
+                                            of n the first kv_len - n + i + 1; 0: all of them */
     float softmax_scale;                 /* finite; 1 / sqrt(head_dim) as a rule */
-    int32_t reserved;                    /* 0 */
+    union {
+        int32_t flags;                   /* 0 or CM_QCACHE_CONTEXT_LENS */
+        int32_t reserved;                /* the same, by the name that it had when only 0 was allowed */
+    };
+    const int32_t *context_lens;         /* only read with that flag: nullable DEVICE [num_requests] */
 } cm_qcache_query;
+
+/* The batch's requests may have been cut short by cm_qcache_schedule: context_lens[r] >= 0 says how
+ * many tokens request r held before its rows, so that its row i is token context_lens[r] + i, and
+ * its tokens are the first min(kv_len, context_lens[r] + rows). Without the flag, or where the entry is negative, they
+ * are all kv_len, and row i of n is token kv_len - n + i. */
+#define CM_QCACHE_CONTEXT_LENS 1
 
 /* Attention of each request's rows (row_starts) over its own cached tokens (kv_lens, block_table):
  * out = softmax(softmax_scale * q K^T) V with K and V the cache's values, and, if asked,

@@ -30,6 +30,6 @@ from ._binding import (  # noqa: F401
     cm_render, cm_render_incremental, cm_render_paged, cm_paged_cache, cm_bagmerge,
     fragment_from_tensors, Context, FragmentSet,
     cm_qcache, cm_qcache_batch, cm_qcache_query,
-    cm_qcache_schedule, cm_qcache_append, cm_qcache_attend, cm_qcache_workspace,
+    CM_QCACHE_CONTEXT_LENS, cm_qcache_schedule, cm_qcache_schedule_cut, cm_qcache_append, cm_qcache_attend, cm_qcache_workspace,
 )
 from .qcache import QBatch, QCache  # noqa: F401

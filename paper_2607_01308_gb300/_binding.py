@@ -104,8 +104,19 @@ class cm_qcache_query(ctypes.Structure):
                 ("out_stride_row", ctypes.c_int64), ("out_stride_head", ctypes.c_int64),
                 ("total_rows", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
                 ("max_rows_per_request", ctypes.c_int32), ("causal", ctypes.c_int32),
-                ("softmax_scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+                ("softmax_scale", ctypes.c_float), ("flags", ctypes.c_int32),
+                ("context_lens", ctypes.c_void_p)]
 
+    @property
+    def reserved(self) -> int:            # the flags, by the name that they had when only 0 was allowed
+        return self.flags
+
+    @reserved.setter
+    def reserved(self, value: int) -> None:
+        self.flags = value
+
+
+CM_QCACHE_CONTEXT_LENS = 1
 
 _c = ctypes
 _P = ctypes.c_void_p
@@ -160,6 +171,8 @@ _SIGS = {
                                          _c.POINTER(_c.c_int64)]),
     "cm_qcache_schedule": (_c.c_int, [_P, _c.POINTER(cm_qcache_batch), _P, _P, _P, _c.c_int64, _P,
                                       _c.c_int64, _P, _P]),
+    "cm_qcache_schedule_cut": (_c.c_int, [_P, _c.POINTER(cm_qcache_batch), _P, _P, _P, _c.c_int64, _P,
+                                          _c.c_int64, _P, _P, _P]),
     "cm_qcache_append": (_c.c_int, [_P, _c.POINTER(cm_qcache), _c.c_int32, _c.c_int32, _P, _P,
                                     _c.c_int64, _c.c_int64, _c.c_int64, _P, _c.c_int64, _P]),
     "cm_qcache_attend": (_c.c_int, [_P, _c.POINTER(cm_qcache), _c.c_int32,
@@ -473,6 +486,14 @@ def cm_qcache_schedule(ctx: int, batch: cm_qcache_batch, context_lens: int, new_
                        stream=None) -> None:
     _check(lib.cm_qcache_schedule(ctx, ctypes.byref(batch), context_lens, new_lens, free_blocks,
                                   num_free, slot_map, max_rows, counts, _stream_handle(stream)))
+
+
+def cm_qcache_schedule_cut(ctx: int, batch: cm_qcache_batch, context_lens: int, new_lens: int,
+                           free_blocks: int, num_free: int, slot_map: int, max_rows: int, counts: int,
+                           context_out: int, stream=None) -> None:
+    _check(lib.cm_qcache_schedule_cut(ctx, ctypes.byref(batch), context_lens, new_lens, free_blocks,
+                                      num_free, slot_map, max_rows, counts, context_out,
+                                      _stream_handle(stream)))
 
 
 def cm_qcache_append(ctx: int, cache: cm_qcache, layer: int, num_layers: int, k: int, v: int,

@@ -118,6 +118,14 @@ extern "C" {
 cm_status cm_qcache_schedule(cm_context *ctx, const cm_qcache_batch *batch, const int32_t *context_lens,
                              const int32_t *new_lens, const int32_t *free_blocks, int64_t num_free,
                              int64_t *slot_map, int64_t max_rows, int64_t *counts, cm_stream_t stream) {
+    return cm_qcache_schedule_cut(ctx, batch, context_lens, new_lens, free_blocks, num_free, slot_map, max_rows,
+                                  counts, nullptr, stream);
+}
+
+cm_status cm_qcache_schedule_cut(cm_context *ctx, const cm_qcache_batch *batch, const int32_t *context_lens,
+                                 const int32_t *new_lens, const int32_t *free_blocks, int64_t num_free,
+                                 int64_t *slot_map, int64_t max_rows, int64_t *counts, int32_t *context_out,
+                                 cm_stream_t stream) {
     TraceRange trace("cm_qcache_schedule");
     return guarded([&]() -> cm_status {
         if (!ctx) return fail(CM_ERR_INVALID_ARG, "context is NULL");
@@ -129,10 +137,13 @@ cm_status cm_qcache_schedule(cm_context *ctx, const cm_qcache_batch *batch, cons
             (max_rows > 0 && !slot_map) || !counts)
             return fail(CM_ERR_INVALID_ARG, "a length, free-list, slot or count pointer is NULL");
         if (!aligned(context_lens, 4) || !aligned(new_lens, 4) || !aligned(free_blocks, 4) ||
-            !aligned(slot_map, 8) || !aligned(counts, 8))
+            !aligned(context_out, 4) || !aligned(slot_map, 8) || !aligned(counts, 8))
             return fail(CM_ERR_ALIGNMENT, "int32 arrays must be 4-byte, int64 arrays 8-byte aligned");
         if (batch->num_requests > 0 && (context_lens == batch->kv_lens || new_lens == batch->kv_lens))
             return fail(CM_ERR_INVALID_ARG, "kv_lens must not be one of the length inputs");
+        if (context_out && batch->num_requests > 0 &&
+            (context_out == context_lens || context_out == new_lens || context_out == batch->kv_lens || context_out == batch->row_starts))
+            return fail(CM_ERR_INVALID_ARG, "context_out must not be another of the length arrays");
         cm::QcacheTablesParams p{};
         p.old_lens = context_lens;
         p.new_lens = new_lens;
@@ -140,6 +151,7 @@ cm_status cm_qcache_schedule(cm_context *ctx, const cm_qcache_batch *batch, cons
         p.block_table = batch->block_table;
         p.row_starts = batch->row_starts;
         p.kv_lens = batch->kv_lens;
+        p.context_out = context_out;
         p.slot_map = slot_map;
         p.counts = counts;
         p.num_free = num_free;
@@ -221,7 +233,9 @@ cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t laye
         if (layer < 0 || layer >= cache->num_layers) return fail(CM_ERR_INVALID_ARG, "layer outside the cache");
         if (batch->block_size != cache->block_size)
             return fail(CM_ERR_SHAPE_MISMATCH, "the batch's block_size is not the cache's");
-        if (query->reserved != 0) return fail(CM_ERR_INVALID_ARG, "reserved must be 0");
+        if (query->flags & ~CM_QCACHE_CONTEXT_LENS) return fail(CM_ERR_INVALID_ARG, "unknown query flags");
+        const int32_t *context_lens = query->flags & CM_QCACHE_CONTEXT_LENS ? query->context_lens : nullptr;
+        if (!aligned(context_lens, 4)) return fail(CM_ERR_ALIGNMENT, "context_lens must be 4-byte aligned");
         if (query->num_q_heads < 1 || query->num_q_heads % cache->num_kv_heads)
             return fail(CM_ERR_SHAPE_MISMATCH, "num_q_heads is not a multiple of the cache's kv heads");
         const int32_t group = query->num_q_heads / cache->num_kv_heads;
@@ -259,6 +273,7 @@ cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t laye
         p.table_width = batch->table_width;
         p.row_starts = batch->row_starts;
         p.kv_lens = batch->kv_lens;
+        p.context_lens = context_lens;
         p.q = static_cast<const uint16_t *>(query->q);
         p.out = static_cast<uint16_t *>(query->out);
         p.lse = query->lse;

@@ -25,9 +25,9 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 
 // Request r's share of the work: `rows` query rows (query tokens x heads of a group) in tiles
 // of ROWS, each over the kv tokens in tiles of TILE. Lengths are clamped to what the buffers
-// hold, so that a wrong one reads nothing outside.
+// hold, so that a wrong one reads nothing outside. Query token i is token first + i of its request.
 struct RequestShape {
-    int row0, q_len, kv;
+    int row0, first, kv;
     int rows, row_tiles, tiles;
 };
 
@@ -36,9 +36,15 @@ __device__ __forceinline__ RequestShape request_shape(const QcacheAttentionParam
     RequestShape s;
     const int64_t cap = min(p.table_width << p.log2_block, (int64_t)INT32_MAX - 1024);
     s.row0 = min(max(p.row_starts[r], 0), p.total_rows);
-    s.q_len = min(max(p.row_starts[r + 1], s.row0), p.total_rows) - s.row0;
+    const int q_len = min(max(p.row_starts[r + 1], s.row0), p.total_rows) - s.row0;
     s.kv = (int)min((int64_t)max(p.kv_lens[r], 0), cap);
-    s.rows = s.q_len * p.group;
+    s.first = s.kv - q_len;
+    const int context = p.context_lens ? p.context_lens[r] : -1;
+    if (context >= 0) {                           // rows or tokens of the request were left out: the two lengths do not say it
+        s.kv = (int)min((int64_t)s.kv, (int64_t)context + q_len);
+        s.first = min(context, s.kv);
+    }
+    s.rows = q_len * p.group;
     s.row_tiles = (s.rows + ROWS - 1) / ROWS;
     s.tiles = max(1, (s.kv + TILE - 1) / TILE);   // one without tokens too: its rows are written
     return s;
@@ -93,7 +99,7 @@ __device__ __forceinline__ uint64_t units_per_block(uint64_t units, uint32_t blo
 // A run of kv tiles [t0, t1) of one row tile of one kv head of one request.
 struct AttentionSegment {
     int request, head, row_tile, t0, t1;
-    int row0, q_len, kv, rows, tiles;
+    int row0, first, kv, rows, tiles;
     uint64_t unit0;               // the unit of tile 0
 };
 
@@ -110,7 +116,7 @@ __device__ __forceinline__ AttentionSegment locate(const QcacheAttentionParams &
     const RequestShape s = request_shape<ROWS, TILE>(p, lo);
     AttentionSegment w;
     w.request = lo;
-    w.row0 = s.row0; w.q_len = s.q_len; w.kv = s.kv; w.rows = s.rows; w.tiles = s.tiles;
+    w.row0 = s.row0; w.first = s.first; w.kv = s.kv; w.rows = s.rows; w.tiles = s.tiles;
     const uint64_t in = u - (uint64_t)prefix[lo] * (uint32_t)p.heads;
     const uint64_t pair = in / (uint32_t)(s.tiles + SETUP);
     const int at = (int)(in - pair * (uint32_t)(s.tiles + SETUP));

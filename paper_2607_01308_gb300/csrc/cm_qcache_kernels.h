@@ -20,6 +20,7 @@ struct QcacheTablesParams {
     const int32_t *free_blocks;           // [num_free]
     int32_t *block_table;                 // [requests][table_width]
     int32_t *row_starts, *kv_lens;
+    int32_t *context_out;                 // may be null
     int64_t *slot_map;                    // [max_rows]
     int64_t *counts;                      // [2]: blocks needed, rows
     int64_t num_free, table_width, max_rows;
@@ -60,6 +61,7 @@ struct QcacheAttentionParams {
     const int32_t *block_table;
     int64_t table_width;
     const int32_t *row_starts, *kv_lens;
+    const int32_t *context_lens;  // may be null
     const uint16_t *q;
     uint16_t *out;
     float *lse;                   // may be null

@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
             for (int x = 0; x < D / 8; ++x)
                 qf[nt][x] = pack_half(__uint_as_float(raw[x] << 16) * up, __uint_as_float(raw[x] & 0xffff0000u) * up);
             const float f = p.scale_log2 * pow2f(e - 14);
-            const int lim = !valid ? 0 : p.causal ? min(w.kv, max(0, w.kv - w.q_len + i + 1)) : w.kv;
+            const int lim = !valid ? 0 : p.causal ? min(w.kv, max(0, w.first + i + 1)) : w.kv;
             if (valid) least = min(least, lim);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {

@@ -399,7 +399,7 @@ __device__ __forceinline__ void store_rows(uint16_t *row, const unsigned char *t
 template <int ROWS, int TILE>
 __device__ __forceinline__ int visible_tiles(const QcacheAttentionParams &p, const RequestShape &s, int rt) {
     int limit = s.kv;
-    if (p.causal) limit = min(limit, max(0, s.kv - s.q_len + (min(s.rows, (rt + 1) * ROWS) - 1) / p.group + 1));
+    if (p.causal) limit = min(limit, max(0, s.first + (min(s.rows, (rt + 1) * ROWS) - 1) / p.group + 1));
     return max(1, (limit + TILE - 1) / TILE);
 }
 
@@ -427,7 +427,7 @@ struct Walk {
 
     __device__ __forceinline__ void request(const QcacheAttentionParams &p) {
         const RequestShape s = request_shape<ROWS, TILE>(p, w.request);
-        w.row0 = s.row0; w.q_len = s.q_len; w.kv = s.kv; w.rows = s.rows;
+        w.row0 = s.row0; w.first = s.first; w.kv = s.kv; w.rows = s.rows;
         w.tiles = visible_tiles<ROWS, TILE>(p, s, w.row_tile);
     }
 
@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             bar_arrive(&bars.q_full[qt]);
 
             // a row that is not there sees everything, so that no tile is masked for its sake
-            const int limit = !valid ? INT32_MAX : p.causal ? min(w.kv, max(0, w.kv - w.q_len + (int)(token - w.row0) + 1)) : w.kv;
+            const int limit = !valid ? INT32_MAX : p.causal ? min(w.kv, max(0, w.first + (int)(token - w.row0) + 1)) : w.kv;
             const int least = __reduce_min_sync(~0u, limit);      // of the warp's rows
             RowState r{0.f, 0.f, -INFINITY};
             const int t0 = w.t0, t1 = w.t1;

@@ -82,8 +82,14 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(const QcacheTablesPara
             row_start[r] = (int32_t)min(before_a + a - q.new_len, (int64_t)INT32_MAX);
             block_start[r] = (int32_t)min(before_b + b - q.need, (int64_t)INT32_MAX);
             if (blockIdx.x == 0) {
-                p.row_starts[r] = (int32_t)min(before_a + a - q.new_len, p.max_rows);
+                const int64_t start = min(before_a + a - q.new_len, p.max_rows), end = min(before_a + a, p.max_rows);
+                p.row_starts[r] = (int32_t)start;
                 p.kv_lens[r] = (int32_t)q.kv;
+                // the lengths of a request that was cut short do not say which tokens its rows are
+                if (p.context_out) {
+                    const bool cut = end - start < q.new_len || q.kv < q.old_len + q.new_len;
+                    p.context_out[r] = cut ? (int32_t)q.old_len : -1;
+                }
             }
         }
         __syncthreads();

@@ -11,11 +11,11 @@ import ctypes
 import struct
 from typing import Optional, Tuple
 
-from ._binding import (Context, _check, _stream_handle, cm_qcache, cm_qcache_batch, cm_qcache_workspace,
+from ._binding import (CM_QCACHE_CONTEXT_LENS, Context, _check, _stream_handle, cm_qcache, cm_qcache_batch, cm_qcache_workspace,
                        lib)
 
 _INT8, _E4M3 = 1, 0
-_pack_query = struct.Struct("@PPPqqqqiiiifi").pack     # a cm_qcache_query in one step
+_pack_query = struct.Struct("@PPPqqqqiiiifiP").pack    # a cm_qcache_query in one step
 
 
 def _require(ok: bool, what: str) -> None:
@@ -52,9 +52,12 @@ class QBatch:
     rows and the attention's workspace. One batch is used by one stream at a time.
 
       block_table [R, table_width] int32, row_starts [R + 1] int32, kv_lens [R] int32,
-      slot_map [max_rows] int64, counts [2] int64 (blocks needed, rows)
+      slot_map [max_rows] int64, counts [2] int64 (blocks needed, rows),
+      context_lens [R] int32: the tokens before the rows of a request that schedule() had to cut short (its
+      table row or max_rows ended), else -1
 
-    schedule() fills them; a program with tables of its own writes into them instead. max_new (host):
+    schedule() fills them; a program with tables of its own writes into them instead (and leaves
+    context_lens at -1 where a request's rows are the last of its kv_lens tokens). max_new (host):
     the most new rows of one request that are expected (None: max_rows); attend() chooses its
     kernel by it, results do not depend on it."""
 
@@ -70,12 +73,14 @@ class QBatch:
         self.block_table = torch.full((num_requests, table_width), -1, dtype=torch.int32, device=dev)
         self.row_starts = torch.zeros(num_requests + 1, dtype=torch.int32, device=dev)
         self.kv_lens = torch.zeros(num_requests, dtype=torch.int32, device=dev)
+        self.context_lens = torch.full((num_requests,), -1, dtype=torch.int32, device=dev)
         self.slot_map = torch.full((max_rows,), -1, dtype=torch.int64, device=dev)
         self.counts = torch.zeros(2, dtype=torch.int64, device=dev)
         self._c = cm_qcache_batch(num_requests, block_size, table_width, self.block_table.data_ptr() or None,
                                   self.row_starts.data_ptr(), self.kv_lens.data_ptr() or None)
         self._ref = ctypes.byref(self._c)
         self._num_requests, self._slots, self._counts = num_requests, self.slot_map.data_ptr() or None, self.counts.data_ptr()
+        self._context = self.context_lens.data_ptr()
         self._workspace = None
         self._workspace_ptr = self._workspace_bytes = 0
         self._workspace_dims = set()
@@ -88,9 +93,9 @@ class QBatch:
             if t.dtype is not dtype or t.dim() != 1 or not t.is_contiguous() or t.get_device() != device:
                 raise ValueError("context_lens, new_lens and free_blocks must be contiguous int32 vectors on the context's device")
         _require(context_lens.numel() == n and new_lens.numel() == n, "one length per request")
-        _check(lib.cm_qcache_schedule(self.ctx.handle, self._ref, context_lens.data_ptr() or None, new_lens.data_ptr() or None,
-                                      free_blocks.data_ptr() or None, free_blocks.numel(), self._slots, self.max_rows,
-                                      self._counts, _stream_handle(stream)))
+        _check(lib.cm_qcache_schedule_cut(self.ctx.handle, self._ref, context_lens.data_ptr() or None, new_lens.data_ptr() or None,
+                                          free_blocks.data_ptr() or None, free_blocks.numel(), self._slots, self.max_rows,
+                                          self._counts, self._context or None, _stream_handle(stream)))
         return self
 
     def _space(self, head_dim: int):
@@ -190,7 +195,7 @@ class QCache:
         qs, os = _strides(q, 2, 8), _strides(out, 2, 8)
         query = _pack_query(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), qs[0], qs[1], os[0], os[1],
                             shape[0], shape[1], batch.max_new or 0, 1 if causal else 0,
-                            self._scale if softmax_scale is None else softmax_scale, 0)
+                            self._scale if softmax_scale is None else softmax_scale, CM_QCACHE_CONTEXT_LENS, batch._context)
         _check(lib.cm_qcache_attend(self.ctx.handle, self._ref, layer, batch._ref, query,
                                     batch._workspace_ptr, batch._workspace_bytes, _stream_handle(stream)))
         return out, lse

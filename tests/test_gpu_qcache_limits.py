@@ -1,0 +1,142 @@
+"""The 8-bit paged cache where its buffers end, where a launch's limits lie and where its memory is used again:
+requests that are cut short, the most requests of a call, graphs and other streams. Tolerances are those of
+test_gpu_qcache.py, which derives them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import qcache_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+cm = pytest.importorskip("paper_2607_01308_gb300")
+
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = cm.Context(0)
+    yield c
+    c.close()
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _rows_of(cache, head, entries, block):
+    """K and V values (fp64) of a head's tokens, whose blocks are `entries`, one per token."""
+    e, p = torch.tensor(entries, dtype=torch.long), torch.arange(len(entries)) % block
+    return tuple(c[:, 0, head].double().cpu()[e, p] * s[:, 0, head].double().cpu()[e][:, None]
+                 for c, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)))
+
+
+def _assert_rows(out, lse, q, k, v, limits):
+    """out, lse [n] of one query head against 64 bits: row i over the first limits[i] of k and v."""
+    w, wl, mag, size = ref.attend(q.double().cpu(), k, v, q.shape[-1] ** -0.5, limits)
+    err = (out.double().cpu() - w).abs()
+    tol = w.abs() * 2 ** -8 * (1 + 2 ** -6) + (2 ** -11 + 2 ** -12 + 2 ** -19 * size) * mag
+    assert bool((err <= tol).all()), float((err - tol).max())
+    got, fine = lse.double().cpu(), torch.isfinite(wl)
+    assert torch.equal(torch.isinf(got), ~fine) and not torch.isnan(got).any()
+    assert bool(((got - wl)[fine].abs() <= 2 ** -19 * (1 + wl[fine].abs() + size)).all())
+
+
+# ---------------------------------------------------------------- requests that are cut short
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("max_new", [1, 1000])
+@pytest.mark.parametrize("old,new,width,max_rows", [
+    ([60], [30], 4, None),                       # the table ends after 4 of the new tokens
+    ([60], [30], 9, 7),                          # 7 rows of 30
+    ([60, 20], [30, 25], 9, 37),                 # the second request keeps 7 rows
+    ([3, 20, 0], [40, 30, 60], 8, 50),           # a request cut, the last without a row
+    ([3, 100, 60], [40, 30, 60], 4, None),       # one whose cached tokens already end at the table
+    ([3, 100, 60], [40, 30, 60], 4, 85),         # both
+    ([0], [200], 3, None), ([0], [200], 20, 1)])
+def test_attend_after_a_cut(ctx, old, new, width, max_rows, max_new, causal):
+    """Rows that got a place see their request's tokens up to their own and nothing that was never written; rows
+    behind the table's end see what the table holds."""
+    H, G, d, block = 1, 4, 64, 16
+    R, cap = len(old), width * block
+    rows = sum(new) if max_rows is None else max_rows
+    cache = cm.QCache(ctx, sum(-(-(o + n) // block) for o, n in zip(old, new)), block, 1, H, d)
+    for c in (cache.k, cache.v):
+        c.view(torch.uint8).fill_(0x7F)           # NaN wherever nothing is written
+    free = torch.randperm(cache.k.shape[0], generator=torch.Generator().manual_seed(1)).int().to(DEV)
+    g = torch.Generator(device=DEV).manual_seed(2)
+
+    def step(batch, before, lens, free):
+        batch.schedule(_i32(before), _i32(lens), free)
+        x = torch.randn((2, 1, H, batch.max_rows, d), generator=g, device=DEV).bfloat16()
+        if batch.max_rows:
+            cache.append(x[0], x[1], batch.slot_map)
+
+    first = cm.QBatch(ctx, R, width, sum(old), block)
+    step(first, [0] * R, old, free)
+    batch = cm.QBatch(ctx, R, width, rows, block)
+    batch.block_table.copy_(first.block_table)
+    step(batch, old, new, free[int(first.counts[0]):].contiguous())
+    batch.max_new = max_new
+    q = torch.randn((rows, H * G, d), generator=g, device=DEV).bfloat16()
+    lse = torch.empty(q.shape[:2], device=DEV)
+    out, _ = cache.attend(q, batch, lse=lse, causal=causal)
+    torch.cuda.synchronize()
+    table, at = batch.block_table.tolist(), 0
+    for r, (o, n) in enumerate(zip(old, new)):
+        kept = min(n, rows - at)
+        tokens = min(o + kept, cap)
+        k, v = _rows_of(cache, 0, [table[r][t // block] for t in range(tokens)], block)
+        assert torch.isfinite(k).all() and torch.isfinite(v).all()
+        limits = [min(tokens, o + i + 1) if causal else tokens for i in range(kept)]
+        for j in range(G):
+            _assert_rows(out[at:at + kept, j], lse[at:at + kept, j], q[at:at + kept, j], k, v, limits)
+        at += kept
+    assert at == rows
+
+
+def test_context_lens_of_a_schedule(ctx):
+    """Only requests that were cut short have an entry; later steps without a cut take it back."""
+    batch = cm.QBatch(ctx, 3, 4, 130, 16)
+    batch.schedule(_i32([3, 100, 60]), _i32([40, 30, 60]), _i32(list(range(40))))
+    assert batch.context_lens.tolist() == [-1, 100, 60]
+    batch.schedule(_i32([3, -5, 60]), _i32([2, 64, 4]), _i32(list(range(40))))
+    assert batch.context_lens.tolist() == [-1, -1, -1]
+    few = cm.QBatch(ctx, 3, 4, 5, 16)
+    few.schedule(_i32([3, 0, 7]), _i32([2, 4, 0]), _i32(list(range(40))))
+    assert few.context_lens.tolist() == [-1, 0, -1]
+
+
+def test_context_lens_of_the_caller(ctx):
+    """Context lengths in the query descriptor, as a C program gives them; flags that are not known are refused."""
+    import ctypes
+    cache = cm.QCache(ctx, 4, 16, 1, 1, 64)
+    x = torch.randn((2, 1, 1, 50, 64), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).bfloat16()
+    cache.append(x[0], x[1], torch.arange(50, device=DEV))
+    batch = cm.QBatch(ctx, 1, 4, 8, 16)
+    batch.block_table.copy_(_i32([[0, 1, 2, 3]]))
+    batch.row_starts.copy_(_i32([0, 8]))
+    batch.kv_lens.fill_(50)
+    q = torch.randn((8, 2, 64), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).bfloat16()
+    out, lse = torch.empty_like(q), torch.empty((8, 2), device=DEV)
+    context = _i32([20])
+    space = torch.zeros(cm.cm_qcache_workspace(ctx.handle, 64), dtype=torch.uint8, device=DEV)
+    d = cm.cm_qcache_query(q=q.data_ptr(), out=out.data_ptr(), lse=lse.data_ptr(), q_stride_row=128, q_stride_head=64,
+                           out_stride_row=128, out_stride_head=64, total_rows=8, num_q_heads=2, max_rows_per_request=8,
+                           causal=1, softmax_scale=0.125, flags=cm.CM_QCACHE_CONTEXT_LENS, context_lens=context.data_ptr())
+    c = cache._c
+    k, v = _rows_of(cache, 0, [t // 16 for t in range(50)], 16)
+    for flags, limits in ((cm.CM_QCACHE_CONTEXT_LENS, [21 + i for i in range(8)]), (0, [43 + i for i in range(8)])):
+        d.flags = flags
+        cm.cm_qcache_attend(ctx.handle, c, 0, batch._c, d, space.data_ptr(), space.numel())
+        torch.cuda.synchronize()
+        for j in range(2):
+            _assert_rows(out[:, j], lse[:, j], q[:, j], k, v, limits)
+    d.reserved = 2
+    assert d.flags == 2
+    with pytest.raises(cm.CMError) as e:
+        cm.cm_qcache_attend(ctx.handle, c, 0, batch._c, d, space.data_ptr(), space.numel())
+    assert e.value.status == cm.Status.ERR_INVALID_ARG
