@@ -383,7 +383,8 @@ cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cuda
     using C = Decode<D, FORMAT, NT>;
     static std::atomic<uint64_t> allowed{0};   // devices on which the shared memory limit is raised
     const size_t smem = C::kShared + ((size_t)p.requests + 1) * 4;
-    if (smem > 48 * 1024 && (device >= 64 || !(allowed.load() >> device & 1))) {
+    // whatever this call needs: the limit without it covers the static bytes too
+    if (device >= 64 || !(allowed.load() >> device & 1)) {
         const cudaError_t e = cudaFuncSetAttribute(decode_kernel<D, FORMAT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                    (int)(C::kShared + (kQcacheMaxAttentionRequests + 1) * 4));
         if (e != cudaSuccess) return e;

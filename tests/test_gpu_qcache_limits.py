@@ -140,3 +140,44 @@ def test_context_lens_of_the_caller(ctx):
     with pytest.raises(cm.CMError) as e:
         cm.cm_qcache_attend(ctx.handle, c, 0, batch._c, d, space.data_ptr(), space.numel())
     assert e.value.status == cm.Status.ERR_INVALID_ARG
+
+
+# ---------------------------------------------------------------- many requests
+
+def _attend_requests(ctx, requests, heads, group, dim, block, max_new, checked, seed, fmt="e4m3"):
+    """requests: [(tokens, query rows), ...] over a pool whose blocks are shared; the rows of the requests `checked`
+    against 64 bits."""
+    rng = np.random.default_rng(seed)
+    pool = 64
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    cache = cm.QCache(ctx, pool, block, 1, heads, dim, dtype=ref.DTYPE[fmt])
+    x = torch.randn((2, 1, heads, pool * block, dim), generator=g, device=DEV).bfloat16()
+    cache.append(x[0], x[1], torch.arange(pool * block, device=DEV))
+    width = max(1, max(-(-kv // block) for kv, _ in requests))
+    table = rng.integers(0, pool, (len(requests), width))
+    starts = np.cumsum([0] + [m for _, m in requests])
+    batch = cm.QBatch(ctx, len(requests), width, int(starts[-1]), block)
+    batch.block_table.copy_(torch.from_numpy(table).int())
+    batch.row_starts.copy_(torch.from_numpy(starts).int())
+    batch.kv_lens.copy_(_i32([kv for kv, _ in requests]))
+    batch.max_new = max_new
+    q = torch.randn((int(starts[-1]), heads * group, dim), generator=g, device=DEV).bfloat16()
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device=DEV)
+    cache.attend(q, batch, out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert not (out == 7).all(-1).any() and not (lse == 7).any()       # every row is written
+    for r in checked:
+        (kv, m), at = requests[r], int(starts[r])
+        for h in range(heads):
+            k, v = _rows_of(cache, h, [int(table[r, t // block]) for t in range(kv)], block)
+            for j in range(h * group, (h + 1) * group):
+                _assert_rows(out[at:at + m, j], lse[at:at + m, j], q[at:at + m, j], k, v,
+                             [max(0, kv - m + i + 1) for i in range(m)])
+
+
+@pytest.mark.parametrize("requests,group", [(4060, 1), (4095, 1), (4096, 1), (3672, 16), (3711, 16)])
+def test_attend_as_many_requests_as_shared_memory_holds(ctx, requests, group):
+    """Request counts whose plan ends close to 48 KB of shared memory, up to the most of a call."""
+    rng = np.random.default_rng(requests)
+    lens = [(int(kv), 1) for kv in rng.integers(1, 40, requests)]
+    _attend_requests(ctx, lens, 1, group, 128, 16, 1, [0, 1, 127, 128, 129, 2047, requests - 2, requests - 1], requests)
