@@ -542,7 +542,7 @@ typedef struct cm_qcache_query {
                                             it chooses the kernel, not the result */
     int32_t causal;                      /* nonzero: a row sees its request's tokens up to its own, row i
                                             of n the first kv_len - n + i + 1; 0: all of them */
-    float softmax_scale;                 /* finite; 1 / sqrt(head_dim) as a rule */
+    float softmax_scale;                 /* to 2.3e38 in size; 1 / sqrt(head_dim) as a rule */
     union {
         int32_t flags;                   /* 0 or CM_QCACHE_CONTEXT_LENS */
         int32_t reserved;                /* the same, by the name that it had when only 0 was allowed */

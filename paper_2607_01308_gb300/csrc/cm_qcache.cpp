@@ -242,7 +242,8 @@ cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t laye
         if (group > 128) return fail(CM_ERR_UNSUPPORTED, "more than 128 query heads to a kv head");
         if (query->total_rows < 0 || query->max_rows_per_request < 0)
             return fail(CM_ERR_INVALID_ARG, "total_rows < 0 or max_rows_per_request < 0");
-        if (!std::isfinite(query->softmax_scale)) return fail(CM_ERR_INVALID_ARG, "softmax_scale is not finite");
+        const float scale_log2 = query->softmax_scale * 1.44269504088896340736f;
+        if (!std::isfinite(scale_log2)) return fail(CM_ERR_INVALID_ARG, "softmax_scale (times log2 e) is not finite");
         if (query->total_rows == 0 || batch->num_requests == 0) return CM_OK;
         if (!query->q || !query->out || !workspace) return fail(CM_ERR_INVALID_ARG, "q, out or workspace is NULL");
         if (!aligned(query->q, 16) || !aligned(query->out, 16) || !aligned(query->lse, 4) || !aligned(workspace, 16))
@@ -281,7 +282,7 @@ cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t laye
         p.q_stride_head = query->q_stride_head;
         p.out_stride_row = query->out_stride_row;
         p.out_stride_head = query->out_stride_head;
-        p.scale_log2 = query->softmax_scale * 1.44269504088896340736f;
+        p.scale_log2 = scale_log2;
         p.requests = batch->num_requests;
         p.heads = cache->num_kv_heads;
         p.group = group;

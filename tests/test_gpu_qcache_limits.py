@@ -181,3 +181,25 @@ def test_attend_as_many_requests_as_shared_memory_holds(ctx, requests, group):
     rng = np.random.default_rng(requests)
     lens = [(int(kv), 1) for kv in rng.integers(1, 40, requests)]
     _attend_requests(ctx, lens, 1, group, 128, 16, 1, [0, 1, 127, 128, 129, 2047, requests - 2, requests - 1], requests)
+
+
+# ---------------------------------------------------------------- refusals
+
+def _small(ctx, rows=3, heads=2, dim=64):
+    cache = cm.QCache(ctx, 2, 16, 1, 1, dim)
+    batch = cm.QBatch(ctx, 1, 1, rows, 16)
+    batch.block_table.fill_(1)
+    batch.row_starts.copy_(_i32([0, rows]))
+    batch.kv_lens.fill_(rows)
+    return cache, batch, torch.zeros((rows, heads, dim), dtype=torch.bfloat16, device=DEV)
+
+
+@pytest.mark.parametrize("scale", [3e38, -3e38, math.inf, math.nan])
+def test_scales_that_overflow_are_refused(ctx, scale):
+    """A scale that is finite itself but not times log2 e would make every score NaN."""
+    cache, batch, q = _small(ctx)
+    with pytest.raises(cm.CMError) as e:
+        cache.attend(q, batch, softmax_scale=scale)
+    assert e.value.status == cm.Status.ERR_INVALID_ARG
+    out, _ = cache.attend(q, batch, softmax_scale=math.copysign(2.3e38, scale))
+    assert bool((out == 0).all())
