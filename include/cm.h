@@ -535,7 +535,8 @@ typedef struct cm_qcache_query {
     const void *q;                       /* DEVICE, 16-byte aligned, bf16 */
     void *out;                           /* DEVICE, 16-byte aligned, bf16 */
     float *lse;                          /* nullable DEVICE [total_rows][num_q_heads] */
-    int64_t q_stride_row, q_stride_head, out_stride_row, out_stride_head;   /* multiples of 8 */
+    int64_t q_stride_row, q_stride_head;       /* multiples of 8 */
+    int64_t out_stride_row, out_stride_head;   /* multiples of 8, head_dim at least where there are several */
     int32_t total_rows;                  /* rows of q, out and lse */
     int32_t num_q_heads;                 /* a multiple of num_kv_heads */
     int32_t max_rows_per_request;        /* the most query rows of one request that are expected;

@@ -252,6 +252,9 @@ cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t laye
             if (s < 0) return fail(CM_ERR_INVALID_ARG, "row strides must not be negative");
             if (s % 8) return fail(CM_ERR_ALIGNMENT, "row strides must be multiples of 8 elements");
         }
+        if ((query->total_rows > 1 && query->out_stride_row < cache->head_dim) ||
+            (query->num_q_heads > 1 && query->out_stride_head < cache->head_dim))
+            return fail(CM_ERR_INVALID_ARG, "rows of out lie on one another");
         const int num_sms = cm::context_num_sms(ctx);
         if (workspace_bytes < 0 || (uint64_t)workspace_bytes < cm::qcache_workspace_bytes(cache->head_dim, num_sms))
             return fail(CM_ERR_CAPACITY, "workspace is smaller than cm_qcache_workspace says");

@@ -203,3 +203,18 @@ def test_scales_that_overflow_are_refused(ctx, scale):
     assert e.value.status == cm.Status.ERR_INVALID_ARG
     out, _ = cache.attend(q, batch, softmax_scale=math.copysign(2.3e38, scale))
     assert bool((out == 0).all())
+
+
+def test_results_that_lie_on_one_another_are_refused(ctx):
+    """An expanded tensor has no place of its own for every row; an expanded query is fine."""
+    cache, batch, q = _small(ctx)
+    one = torch.empty((1, 2, 64), dtype=torch.bfloat16, device=DEV)
+    for out in (one.expand(3, 2, 64), one[:, :1].expand(1, 2, 64).expand(3, 2, 64), torch.empty_like(q)[:, :1].expand(3, 2, 64),
+                torch.empty(400, dtype=torch.bfloat16, device=DEV).as_strided((3, 2, 64), (128, 32, 1))):
+        with pytest.raises(cm.CMError) as e:
+            cache.attend(q, batch, out=out)
+        assert e.value.status == cm.Status.ERR_INVALID_ARG
+    out, _ = cache.attend(q[:1].expand(3, 2, 64), batch)
+    assert bool((out == 0).all())
+    # a single row or head has no stride to speak of
+    cache.attend(q[:1, :1], batch, out=one[:, :1])
