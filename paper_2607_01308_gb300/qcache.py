@@ -15,6 +15,7 @@ from ._binding import (CM_QCACHE_CONTEXT_LENS, Context, _check, _stream_handle, 
                        lib)
 
 _INT8, _E4M3 = 1, 0
+_ATTENTION_DIMS = (32, 64, 128, 256)
 _pack_query = struct.Struct("@PPPqqqqiiiifiP").pack    # a cm_qcache_query in one step
 
 
@@ -59,7 +60,10 @@ class QBatch:
     schedule() fills them; a program with tables of its own writes into them instead (and leaves
     context_lens at -1 where a request's rows are the last of its kv_lens tokens). max_new (host):
     the most new rows of one request that are expected (None: max_rows); attend() chooses its
-    kernel by it, results do not depend on it."""
+    kernel by it, results do not depend on it.
+
+    The workspace (some 40 MB) is made with the batch and stays where it is, for every head_dim, so that
+    graphs which were captured with the batch can be replayed as long as it lives."""
 
     def __init__(self, ctx: Context, num_requests: int, table_width: int, max_rows: int,
                  block_size: int):
@@ -81,9 +85,11 @@ class QBatch:
         self._ref = ctypes.byref(self._c)
         self._num_requests, self._slots, self._counts = num_requests, self.slot_map.data_ptr() or None, self.counts.data_ptr()
         self._context = self.context_lens.data_ptr()
-        self._workspace = None
-        self._workspace_ptr = self._workspace_bytes = 0
-        self._workspace_dims = set()
+        self._workspace_bytes = max(cm_qcache_workspace(ctx.handle, d) for d in _ATTENTION_DIMS)
+        self._workspace = torch.zeros(self._workspace_bytes, dtype=torch.uint8, device=dev)
+        self._workspace_ptr = self._workspace.data_ptr()
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(dev).synchronize()      # set on every stream
 
     def schedule(self, context_lens, new_lens, free_blocks, stream=None) -> "QBatch":
         """Block tables, row starts, lengths and slots from the requests' cached and new token counts
@@ -97,18 +103,6 @@ class QBatch:
                                           free_blocks.data_ptr() or None, free_blocks.numel(), self._slots, self.max_rows,
                                           self._counts, self._context or None, _stream_handle(stream)))
         return self
-
-    def _space(self, head_dim: int):
-        import torch
-        """A workspace that does for head_dim as well."""
-        need = cm_qcache_workspace(self.ctx.handle, head_dim)
-        if need > self._workspace_bytes:
-            if self._workspace is not None:
-                torch.cuda.synchronize(self._workspace.device)                # the last call may still use the old one
-            self._workspace = torch.zeros(need, dtype=torch.uint8, device=_device(self.ctx))
-            torch.cuda.current_stream(self._workspace.device).synchronize()   # zero on every stream
-            self._workspace_ptr, self._workspace_bytes = self._workspace.data_ptr(), need
-        self._workspace_dims.add(head_dim)
 
 
 class QCache:
@@ -190,8 +184,6 @@ class QCache:
         if lse is not None and (lse.dtype is not self._fp32 or lse.shape != shape[:2] or not lse.is_contiguous() or
                                 lse.get_device() != device):
             raise ValueError("lse must be a contiguous fp32 [rows, q_heads]")
-        if self._dim not in batch._workspace_dims:
-            batch._space(self._dim)
         qs, os = _strides(q, 2, 8), _strides(out, 2, 8)
         query = _pack_query(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), qs[0], qs[1], os[0], os[1],
                             shape[0], shape[1], batch.max_new or 0, 1 if causal else 0,

@@ -218,3 +218,103 @@ def test_results_that_lie_on_one_another_are_refused(ctx):
     assert bool((out == 0).all())
     # a single row or head has no stride to speak of
     cache.attend(q[:1, :1], batch, out=one[:, :1])
+
+
+# ---------------------------------------------------------------- memory that is used again
+
+def _steps(ctx, rows, dim, seed=5):
+    """A cache of some 2,500 tokens, a batch of one request that reads all of it, and a query."""
+    block, tokens = 16, 2500
+    n = -(-tokens // block)
+    cache = cm.QCache(ctx, n, block, 1, 1, dim)
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn((2, 1, 1, tokens, dim), generator=g, device=DEV).bfloat16()
+    cache.append(x[0], x[1], torch.arange(tokens, device=DEV))
+    batch = cm.QBatch(ctx, 1, n, rows, block)
+    batch.block_table.copy_(torch.arange(n)[None].int())
+    batch.row_starts.copy_(_i32([0, rows]))
+    batch.kv_lens.fill_(tokens)
+    batch.max_new = rows
+    return cache, batch, torch.randn((rows, 4, dim), generator=g, device=DEV).bfloat16()
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_a_captured_attend_outlives_calls_of_other_head_dims(ctx, rows):
+    """The first attend of a batch is captured; then the batch serves a larger head_dim; the graph still writes
+    into memory that is the batch's, and gives the same bits."""
+    cache, batch, q = _steps(ctx, rows, 64)
+    wide, _, q_wide = _steps(ctx, rows, 128)
+    want = cache.attend(q, _same(ctx, batch))[0]
+    want_wide = wide.attend(q_wide, _same(ctx, batch))[0]
+    out = torch.zeros_like(q)
+    space = batch._workspace_ptr
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.attend(q, batch, out=out)
+    assert torch.equal(wide.attend(q_wide, batch)[0], want_wide)
+    assert batch._workspace_ptr == space == batch._workspace.data_ptr()
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        assert torch.equal(wide.attend(q_wide, batch)[0], want_wide)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+def _same(ctx, batch):
+    """Another batch of the same requests."""
+    b = cm.QBatch(ctx, batch.kv_lens.numel(), batch.block_table.shape[1], batch.max_rows, 16)
+    for a, c in ((b.block_table, batch.block_table), (b.row_starts, batch.row_starts), (b.kv_lens, batch.kv_lens)):
+        a.copy_(c)
+    b.max_new = batch.max_new
+    return b
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_a_captured_step_is_the_step(ctx, rows):
+    """schedule, append and attend in one graph, replayed over new inputs: the bits of the plain calls. The first
+    calls of the batch are the captured ones."""
+    R, H, G, d, block, width = 3, 2, 4, 64, 16, 40
+    old = [3, 16, 200]
+    g = torch.Generator(device=DEV).manual_seed(31)
+    caches = [cm.QCache(ctx, R * width, block, 1, H, d) for _ in range(2)]
+    batches = [cm.QBatch(ctx, R, width, R * rows, block) for _ in range(2)]
+    first = cm.QBatch(ctx, R, width, sum(old), block)
+    free = torch.randperm(R * width, generator=torch.Generator().manual_seed(3)).int().to(DEV)
+    first.schedule(_i32([0] * R), _i32(old), free)
+    x = torch.randn((2, 1, H, sum(old), d), generator=g, device=DEV).bfloat16()
+    for c, b in zip(caches, batches):
+        c.append(x[0], x[1], first.slot_map)
+        b.block_table.copy_(first.block_table)
+        b.max_new = rows
+    lens, new = _i32(old), _i32([rows] * R)
+    left = free[sum(-(-o // block) for o in old):].contiguous()
+    kv = torch.empty((2, 1, H, R * rows, d), dtype=torch.bfloat16, device=DEV)
+    q = torch.empty((R * rows, H * G, d), dtype=torch.bfloat16, device=DEV)
+    outs = [torch.zeros_like(q) for _ in range(2)]
+
+    def step(i):
+        batches[i].schedule(lens, new, left)
+        caches[i].append(kv[0], kv[1], batches[i].slot_map)
+        caches[i].attend(q, batches[i], out=outs[i])
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(0)
+    held = list(old)
+    for _ in range(3):
+        kv.copy_(torch.randn(kv.shape, generator=g, device=DEV))
+        q.copy_(torch.randn(q.shape, generator=g, device=DEV))
+        graph.replay()
+        step(1)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1]) and bool(outs[0].abs().sum() > 0)
+        for a, b in ((caches[0].k, caches[1].k), (caches[0].v, caches[1].v)):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+        lens += rows                                  # the next step's, in the same memory
+        taken = sum(-(-(h + rows) // block) - -(-h // block) for h in held)
+        held = [h + rows for h in held]
+        left.copy_(torch.cat([left[taken:], left[:taken]]))
+    ctx.check()
