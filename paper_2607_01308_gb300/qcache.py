@@ -42,6 +42,18 @@ def _same_layout(a, b, n: int) -> bool:
     return a.shape == b.shape and (a.stride() == b.stride() or _strides(a, n, 1) == _strides(b, n, 1))
 
 
+def _new_on(stream, q):
+    """An empty tensor like q (its strides left aside) from the memory of the stream that will write it: what other
+    streams may still do with that memory is done."""
+    if stream is None:
+        return q.new_empty(q.shape)
+    import torch
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, q.device) if stream else torch.cuda.default_stream(q.device)
+    with torch.cuda.stream(stream):
+        return q.new_empty(q.shape)
+
+
 def _format(dtype) -> int:
     import torch
     _require(dtype in (torch.float8_e4m3fn, torch.int8), "a cache holds float8_e4m3fn or int8 codes")
@@ -173,12 +185,12 @@ class QCache:
                causal: bool = True, stream=None) -> Tuple[object, object]:
         """(out, lse): softmax(softmax_scale * q K^T) V for the batch's rows, each over its own request's
         cached tokens. q, out: bf16 [rows, q_heads, head_dim] (q_heads a multiple of kv_heads, head_dim
-        contiguous); lse: fp32 [rows, q_heads] or None to leave it out; out is made if not given."""
+        contiguous); lse: fp32 [rows, q_heads] or None to leave it out; out is made if not given, on `stream`."""
         shape, bf16, device = q.shape, self._bf16, self._device
         if q.dtype is not bf16 or len(shape) != 3 or shape[2] != self._dim or q.stride(2) != 1 or q.get_device() != device:
             raise ValueError("q must be bf16 [rows, q_heads, head_dim] on the context's device, head_dim contiguous")
         if out is None:
-            out = q.new_empty(shape)
+            out = _new_on(stream, q)
         elif out.dtype is not bf16 or out.shape != shape or out.stride(2) != 1 or out.get_device() != device:
             raise ValueError("out must be like q")
         if lse is not None and (lse.dtype is not self._fp32 or lse.shape != shape[:2] or not lse.is_contiguous() or

@@ -318,3 +318,25 @@ def test_a_captured_step_is_the_step(ctx, rows):
         held = [h + rows for h in held]
         left.copy_(torch.cat([left[taken:], left[:taken]]))
     ctx.check()
+
+
+@pytest.mark.parametrize("handle", [False, True])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_results_are_made_on_the_stream_that_writes_them(ctx, rows, handle):
+    """With stream= and no out, the result is memory of that stream: the current stream neither has it still in use nor
+    gets it when the result is dropped."""
+    cache, batch, q = _steps(ctx, rows, 64)
+    want = cache.attend(q, batch)[0]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    out, _ = cache.attend(q, batch, stream=side.cuda_stream if handle else side)
+    side.synchronize()
+    assert torch.equal(out, want)
+    torch.cuda.synchronize()
+    at = out.data_ptr()
+    del out
+    assert torch.empty_like(q).data_ptr() != at           # of the current stream
+    with torch.cuda.stream(side):
+        assert torch.empty_like(q).data_ptr() == at
+    assert torch.equal(cache.attend(q, batch, stream=0)[0], want)     # the default stream
