@@ -75,7 +75,9 @@ class QBatch:
     kernel by it, results do not depend on it.
 
     The workspace (some 40 MB) is made with the batch and stays where it is, for every head_dim, so that
-    graphs which were captured with the batch can be replayed as long as it lives."""
+    graphs which were captured with the batch can be replayed as long as it lives. The batch's memory is
+    given back when the torch streams that its calls ran on are through with it; a stream given as a bare handle has to be
+    through with it before the batch is dropped."""
 
     def __init__(self, ctx: Context, num_requests: int, table_width: int, max_rows: int,
                  block_size: int):
@@ -102,6 +104,19 @@ class QBatch:
         self._workspace_ptr = self._workspace.data_ptr()
         if not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream(dev).synchronize()      # set on every stream
+        self._streams = {_stream_handle(torch.cuda.current_stream(dev))}
+
+    def _on(self, stream) -> Optional[int]:
+        """The stream's handle; the first time, its use of the batch's memory is made known to torch."""
+        handle = _stream_handle(stream)
+        if handle not in self._streams and not isinstance(stream, int):
+            import torch
+            stream = stream or torch.cuda.current_stream(self._device)
+            for t in (self.block_table, self.row_starts, self.kv_lens, self.context_lens, self.slot_map, self.counts,
+                      self._workspace):
+                t.record_stream(stream)
+            self._streams.add(handle)
+        return handle
 
     def schedule(self, context_lens, new_lens, free_blocks, stream=None) -> "QBatch":
         """Block tables, row starts, lengths and slots from the requests' cached and new token counts
@@ -113,7 +128,7 @@ class QBatch:
         _require(context_lens.numel() == n and new_lens.numel() == n, "one length per request")
         _check(lib.cm_qcache_schedule_cut(self.ctx.handle, self._ref, context_lens.data_ptr() or None, new_lens.data_ptr() or None,
                                           free_blocks.data_ptr() or None, free_blocks.numel(), self._slots, self.max_rows,
-                                          self._counts, self._context or None, _stream_handle(stream)))
+                                          self._counts, self._context or None, self._on(stream)))
         return self
 
 
@@ -201,5 +216,5 @@ class QCache:
                             shape[0], shape[1], batch.max_new or 0, 1 if causal else 0,
                             self._scale if softmax_scale is None else softmax_scale, CM_QCACHE_CONTEXT_LENS, batch._context)
         _check(lib.cm_qcache_attend(self.ctx.handle, self._ref, layer, batch._ref, query,
-                                    batch._workspace_ptr, batch._workspace_bytes, _stream_handle(stream)))
+                                    batch._workspace_ptr, batch._workspace_bytes, batch._on(stream)))
         return out, lse

@@ -340,3 +340,27 @@ def test_results_are_made_on_the_stream_that_writes_them(ctx, rows, handle):
     with torch.cuda.stream(side):
         assert torch.empty_like(q).data_ptr() == at
     assert torch.equal(cache.attend(q, batch, stream=0)[0], want)     # the default stream
+
+
+@pytest.mark.parametrize("current", [False, True])
+def test_a_dropped_batch_keeps_its_memory_from_others_until_its_stream_is_done(ctx, current):
+    """A batch made on one stream, used on another (named, or the current one) and dropped while that one is busy:
+    nobody else gets its memory before."""
+    cache, batch, q = _steps(ctx, 1, 64)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    spaces = {t.data_ptr(): t.numel() for t in (batch._workspace, batch.block_table)}
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)                    # some 0.1 s
+    if current:
+        with torch.cuda.stream(side):
+            out, _ = cache.attend(q, batch)
+    else:
+        out, _ = cache.attend(q, batch, stream=side)
+    del batch
+    big = torch.empty(max(spaces.values()), dtype=torch.uint8, device=DEV)
+    small = torch.empty(min(spaces.values()), dtype=torch.int32, device=DEV)
+    assert not side.query()                               # it was still busy
+    assert not {big.data_ptr(), small.data_ptr()} & set(spaces)
+    side.synchronize()
+    assert torch.isfinite(out).all()
