@@ -277,7 +277,8 @@ cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t laye
         p.table_width = batch->table_width;
         p.row_starts = batch->row_starts;
         p.kv_lens = batch->kv_lens;
-        p.context_lens = context_lens;
+        p.context_lens = context_lens ? context_lens : batch->kv_lens;
+        p.no_context = context_lens ? 0 : -1;
         p.q = static_cast<const uint16_t *>(query->q);
         p.out = static_cast<uint16_t *>(query->out);
         p.lse = query->lse;

@@ -37,13 +37,12 @@ __device__ __forceinline__ RequestShape request_shape(const QcacheAttentionParam
     const int64_t cap = min(p.table_width << p.log2_block, (int64_t)INT32_MAX - 1024);
     s.row0 = min(max(p.row_starts[r], 0), p.total_rows);
     const int q_len = min(max(p.row_starts[r + 1], s.row0), p.total_rows) - s.row0;
-    s.kv = (int)min((int64_t)max(p.kv_lens[r], 0), cap);
-    s.first = s.kv - q_len;
-    const int context = p.context_lens ? p.context_lens[r] : -1;
-    if (context >= 0) {                           // rows or tokens of the request were left out: the two lengths do not say it
-        s.kv = (int)min((int64_t)s.kv, (int64_t)context + q_len);
-        s.first = min(context, s.kv);
-    }
+    const int kv = (int)min((int64_t)max(p.kv_lens[r], 0), cap);
+    // a request that was cut short: the two lengths do not say which tokens its rows are (loaded with the others; without
+    // context_lens a length, which counts as negative)
+    const int context = p.context_lens[r] | p.no_context;
+    s.kv = context < 0 ? kv : (int)min((uint32_t)kv, (uint32_t)context + (uint32_t)q_len);
+    s.first = context < 0 ? kv - q_len : min(context, s.kv);
     s.rows = q_len * p.group;
     s.row_tiles = (s.rows + ROWS - 1) / ROWS;
     s.tiles = max(1, (s.kv + TILE - 1) / TILE);   // one without tokens too: its rows are written

@@ -61,7 +61,7 @@ struct QcacheAttentionParams {
     const int32_t *block_table;
     int64_t table_width;
     const int32_t *row_starts, *kv_lens;
-    const int32_t *context_lens;  // may be null
+    const int32_t *context_lens;  // [requests]
     const uint16_t *q;
     uint16_t *out;
     float *lse;                   // may be null
@@ -74,6 +74,7 @@ struct QcacheAttentionParams {
     float scale_log2;             // softmax scale * log2(e)
     int32_t requests, heads, group, head_dim, log2_block;
     int32_t total_rows, causal, format;
+    int32_t no_context;           // -1: context_lens is another array of that size, and no request was cut short; else 0
 };
 
 // The workspace holds, for every thread block of a launch, two partial results and an arrival
