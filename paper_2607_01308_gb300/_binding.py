@@ -162,6 +162,9 @@ _SIGS = {
     "cm_bagmerge": (_c.c_int, [_P, _c.POINTER(cm_fragment), _c.c_int32, _P, _P, _c.c_int64, _P,
                                _c.POINTER(_c.c_int64)]),
     "cm_testing_render_withheld_load": (_c.c_int, [_P, _P, _P, _c.c_int64, _P]),
+    "cm_testing_qcache_attend_withheld": (_c.c_int, [_P, _c.POINTER(cm_qcache), _c.c_int32,
+                                                     _c.POINTER(cm_qcache_batch), _P, _P, _c.c_int64,
+                                                     _c.c_int32, _P]),
     "cm_testing_bounds_violations": (_c.c_int, [_c.c_int32, _c.POINTER(_c.c_uint64),
                                                 _c.POINTER(_c.c_int32)]),
     "cm_render_paged": (_c.c_int, [_P, _c.POINTER(cm_paged_cache), _P, _c.POINTER(_c.c_int64),

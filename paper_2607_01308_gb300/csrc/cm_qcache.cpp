@@ -2,6 +2,7 @@
 // can see is checked before anything is launched. Nothing is allocated or kept, so the calls take
 // no lock.
 #include "cm.h"
+#include "cm_testing.h"
 
 #include <cmath>
 #include <exception>
@@ -109,6 +110,99 @@ cm_status check_batch(const cm_qcache_batch *b, int32_t most) {
     if (!aligned(b->row_starts, 4) || !aligned(b->kv_lens, 4) || !aligned(b->block_table, 4))
         return fail(CM_ERR_ALIGNMENT, "batch arrays must be 4-byte aligned");
     return CM_OK;
+}
+
+// withhold: 0, or what the many-rows kernel is to wait for in vain (failure injection; that kernel then runs
+// whatever the rows).
+cm_status attend(cm_context *ctx, const cm_qcache *cache, int32_t layer, const cm_qcache_batch *batch,
+                 const cm_qcache_query *query, void *workspace, int64_t workspace_bytes, cm_stream_t stream,
+                 int32_t withhold) {
+    TraceRange trace("cm_qcache_attend");
+    return guarded([&]() -> cm_status {
+        if (!ctx) return fail(CM_ERR_INVALID_ARG, "context is NULL");
+        cm_status st = check_cache(cache);
+        if (st != CM_OK) return st;
+        st = check_batch(batch, cm::kQcacheMaxAttentionRequests);
+        if (st != CM_OK) return st;
+        if (!query) return fail(CM_ERR_INVALID_ARG, "query descriptor is NULL");
+        if (cache->head_dim < 32 || cache->head_dim > 256)
+            return fail(CM_ERR_UNSUPPORTED, "attention needs head_dim 32, 64, 128 or 256");
+        if (layer < 0 || layer >= cache->num_layers) return fail(CM_ERR_INVALID_ARG, "layer outside the cache");
+        if (batch->block_size != cache->block_size)
+            return fail(CM_ERR_SHAPE_MISMATCH, "the batch's block_size is not the cache's");
+        if (query->flags & ~CM_QCACHE_CONTEXT_LENS) return fail(CM_ERR_INVALID_ARG, "unknown query flags");
+        const int32_t *context_lens = query->flags & CM_QCACHE_CONTEXT_LENS ? query->context_lens : nullptr;
+        if (!aligned(context_lens, 4)) return fail(CM_ERR_ALIGNMENT, "context_lens must be 4-byte aligned");
+        if (query->num_q_heads < 1 || query->num_q_heads % cache->num_kv_heads)
+            return fail(CM_ERR_SHAPE_MISMATCH, "num_q_heads is not a multiple of the cache's kv heads");
+        const int32_t group = query->num_q_heads / cache->num_kv_heads;
+        if (group > 128) return fail(CM_ERR_UNSUPPORTED, "more than 128 query heads to a kv head");
+        if (query->total_rows < 0 || query->max_rows_per_request < 0)
+            return fail(CM_ERR_INVALID_ARG, "total_rows < 0 or max_rows_per_request < 0");
+        const float scale_log2 = query->softmax_scale * 1.44269504088896340736f;
+        if (!std::isfinite(scale_log2)) return fail(CM_ERR_INVALID_ARG, "softmax_scale (times log2 e) is not finite");
+        if (query->total_rows == 0 || batch->num_requests == 0) return CM_OK;
+        if (!query->q || !query->out || !workspace) return fail(CM_ERR_INVALID_ARG, "q, out or workspace is NULL");
+        if (!aligned(query->q, 16) || !aligned(query->out, 16) || !aligned(query->lse, 4) || !aligned(workspace, 16))
+            return fail(CM_ERR_ALIGNMENT, "q, out and workspace must be 16-byte aligned");
+        for (int64_t s : {query->q_stride_row, query->q_stride_head, query->out_stride_row, query->out_stride_head}) {
+            if (s < 0) return fail(CM_ERR_INVALID_ARG, "row strides must not be negative");
+            if (s % 8) return fail(CM_ERR_ALIGNMENT, "row strides must be multiples of 8 elements");
+        }
+        if ((query->total_rows > 1 && query->out_stride_row < cache->head_dim) ||
+            (query->num_q_heads > 1 && query->out_stride_head < cache->head_dim))
+            return fail(CM_ERR_INVALID_ARG, "rows of out lie on one another");
+        const int num_sms = cm::context_num_sms(ctx);
+        if (workspace_bytes < 0 || (uint64_t)workspace_bytes < cm::qcache_workspace_bytes(cache->head_dim, num_sms))
+            return fail(CM_ERR_CAPACITY, "workspace is smaller than cm_qcache_workspace says");
+        const double tiles = (double)batch->table_width * batch->block_size / 64 + 9;   // and their setup
+        const double row_tiles = (double)query->total_rows * group / 8 + batch->num_requests;
+        if (tiles * row_tiles >= 2147483648.0)
+            return fail(CM_ERR_UNSUPPORTED, "too much work for one call: split the rows");
+        cm::QcacheAttentionParams p{};
+        p.k = static_cast<const uint8_t *>(cache->k_codes) + layer * cache->stride_layer;
+        p.v = static_cast<const uint8_t *>(cache->v_codes) + layer * cache->stride_layer;
+        p.k_scale = cache->k_scales + layer * cache->scale_stride_layer;
+        p.v_scale = cache->v_scales + layer * cache->scale_stride_layer;
+        p.stride_block = cache->stride_block;
+        p.stride_head = cache->stride_head;
+        p.stride_token = cache->stride_token;
+        p.scale_stride_block = cache->scale_stride_block;
+        p.scale_stride_head = cache->scale_stride_head;
+        p.num_blocks = cache->num_blocks;
+        p.block_table = batch->block_table;
+        p.table_width = batch->table_width;
+        p.row_starts = batch->row_starts;
+        p.kv_lens = batch->kv_lens;
+        p.context_lens = context_lens ? context_lens : batch->kv_lens;
+        p.no_context = context_lens ? 0 : -1;
+        p.q = static_cast<const uint16_t *>(query->q);
+        p.out = static_cast<uint16_t *>(query->out);
+        p.lse = query->lse;
+        p.q_stride_row = query->q_stride_row;
+        p.q_stride_head = query->q_stride_head;
+        p.out_stride_row = query->out_stride_row;
+        p.out_stride_head = query->out_stride_head;
+        p.scale_log2 = scale_log2;
+        p.requests = batch->num_requests;
+        p.heads = cache->num_kv_heads;
+        p.group = group;
+        p.head_dim = cache->head_dim;
+        p.log2_block = log2_of(cache->block_size);
+        p.total_rows = query->total_rows;
+        p.causal = query->causal != 0;
+        p.format = cache->format;
+        p.error = cm::context_error_word(ctx);
+        p.withhold = withhold;
+        cm::qcache_workspace_split(p, workspace, num_sms);
+        const int64_t rows = (int64_t)(query->max_rows_per_request ? query->max_rows_per_request : query->total_rows) * group;
+        return on_device(ctx, "attention launch", [&] {
+            const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+            if (withhold) return cm::launch_qcache_prefill(p, num_sms, cm::context_device(ctx), s);
+            return cm::launch_qcache_attention(p, (int)(rows < INT32_MAX ? rows : INT32_MAX), num_sms,
+                                               cm::context_device(ctx), s);
+        });
+    });
 }
 
 }  // namespace
@@ -220,89 +314,15 @@ cm_status cm_qcache_append(cm_context *ctx, const cm_qcache *cache, int32_t laye
 cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t layer,
                            const cm_qcache_batch *batch, const cm_qcache_query *query, void *workspace,
                            int64_t workspace_bytes, cm_stream_t stream) {
-    TraceRange trace("cm_qcache_attend");
-    return guarded([&]() -> cm_status {
-        if (!ctx) return fail(CM_ERR_INVALID_ARG, "context is NULL");
-        cm_status st = check_cache(cache);
-        if (st != CM_OK) return st;
-        st = check_batch(batch, cm::kQcacheMaxAttentionRequests);
-        if (st != CM_OK) return st;
-        if (!query) return fail(CM_ERR_INVALID_ARG, "query descriptor is NULL");
-        if (cache->head_dim < 32 || cache->head_dim > 256)
-            return fail(CM_ERR_UNSUPPORTED, "attention needs head_dim 32, 64, 128 or 256");
-        if (layer < 0 || layer >= cache->num_layers) return fail(CM_ERR_INVALID_ARG, "layer outside the cache");
-        if (batch->block_size != cache->block_size)
-            return fail(CM_ERR_SHAPE_MISMATCH, "the batch's block_size is not the cache's");
-        if (query->flags & ~CM_QCACHE_CONTEXT_LENS) return fail(CM_ERR_INVALID_ARG, "unknown query flags");
-        const int32_t *context_lens = query->flags & CM_QCACHE_CONTEXT_LENS ? query->context_lens : nullptr;
-        if (!aligned(context_lens, 4)) return fail(CM_ERR_ALIGNMENT, "context_lens must be 4-byte aligned");
-        if (query->num_q_heads < 1 || query->num_q_heads % cache->num_kv_heads)
-            return fail(CM_ERR_SHAPE_MISMATCH, "num_q_heads is not a multiple of the cache's kv heads");
-        const int32_t group = query->num_q_heads / cache->num_kv_heads;
-        if (group > 128) return fail(CM_ERR_UNSUPPORTED, "more than 128 query heads to a kv head");
-        if (query->total_rows < 0 || query->max_rows_per_request < 0)
-            return fail(CM_ERR_INVALID_ARG, "total_rows < 0 or max_rows_per_request < 0");
-        const float scale_log2 = query->softmax_scale * 1.44269504088896340736f;
-        if (!std::isfinite(scale_log2)) return fail(CM_ERR_INVALID_ARG, "softmax_scale (times log2 e) is not finite");
-        if (query->total_rows == 0 || batch->num_requests == 0) return CM_OK;
-        if (!query->q || !query->out || !workspace) return fail(CM_ERR_INVALID_ARG, "q, out or workspace is NULL");
-        if (!aligned(query->q, 16) || !aligned(query->out, 16) || !aligned(query->lse, 4) || !aligned(workspace, 16))
-            return fail(CM_ERR_ALIGNMENT, "q, out and workspace must be 16-byte aligned");
-        for (int64_t s : {query->q_stride_row, query->q_stride_head, query->out_stride_row, query->out_stride_head}) {
-            if (s < 0) return fail(CM_ERR_INVALID_ARG, "row strides must not be negative");
-            if (s % 8) return fail(CM_ERR_ALIGNMENT, "row strides must be multiples of 8 elements");
-        }
-        if ((query->total_rows > 1 && query->out_stride_row < cache->head_dim) ||
-            (query->num_q_heads > 1 && query->out_stride_head < cache->head_dim))
-            return fail(CM_ERR_INVALID_ARG, "rows of out lie on one another");
-        const int num_sms = cm::context_num_sms(ctx);
-        if (workspace_bytes < 0 || (uint64_t)workspace_bytes < cm::qcache_workspace_bytes(cache->head_dim, num_sms))
-            return fail(CM_ERR_CAPACITY, "workspace is smaller than cm_qcache_workspace says");
-        const double tiles = (double)batch->table_width * batch->block_size / 64 + 9;   // and their setup
-        const double row_tiles = (double)query->total_rows * group / 8 + batch->num_requests;
-        if (tiles * row_tiles >= 2147483648.0)
-            return fail(CM_ERR_UNSUPPORTED, "too much work for one call: split the rows");
-        cm::QcacheAttentionParams p{};
-        p.k = static_cast<const uint8_t *>(cache->k_codes) + layer * cache->stride_layer;
-        p.v = static_cast<const uint8_t *>(cache->v_codes) + layer * cache->stride_layer;
-        p.k_scale = cache->k_scales + layer * cache->scale_stride_layer;
-        p.v_scale = cache->v_scales + layer * cache->scale_stride_layer;
-        p.stride_block = cache->stride_block;
-        p.stride_head = cache->stride_head;
-        p.stride_token = cache->stride_token;
-        p.scale_stride_block = cache->scale_stride_block;
-        p.scale_stride_head = cache->scale_stride_head;
-        p.num_blocks = cache->num_blocks;
-        p.block_table = batch->block_table;
-        p.table_width = batch->table_width;
-        p.row_starts = batch->row_starts;
-        p.kv_lens = batch->kv_lens;
-        p.context_lens = context_lens ? context_lens : batch->kv_lens;
-        p.no_context = context_lens ? 0 : -1;
-        p.q = static_cast<const uint16_t *>(query->q);
-        p.out = static_cast<uint16_t *>(query->out);
-        p.lse = query->lse;
-        p.q_stride_row = query->q_stride_row;
-        p.q_stride_head = query->q_stride_head;
-        p.out_stride_row = query->out_stride_row;
-        p.out_stride_head = query->out_stride_head;
-        p.scale_log2 = scale_log2;
-        p.requests = batch->num_requests;
-        p.heads = cache->num_kv_heads;
-        p.group = group;
-        p.head_dim = cache->head_dim;
-        p.log2_block = log2_of(cache->block_size);
-        p.total_rows = query->total_rows;
-        p.causal = query->causal != 0;
-        p.format = cache->format;
-        p.error = cm::context_error_word(ctx);
-        cm::qcache_workspace_split(p, workspace, num_sms);
-        const int64_t rows = (int64_t)(query->max_rows_per_request ? query->max_rows_per_request : query->total_rows) * group;
-        return on_device(ctx, "attention launch", [&] {
-            return cm::launch_qcache_attention(p, (int)(rows < INT32_MAX ? rows : INT32_MAX), num_sms,
-                                               cm::context_device(ctx), reinterpret_cast<cudaStream_t>(stream));
-        });
-    });
+    return attend(ctx, cache, layer, batch, query, workspace, workspace_bytes, stream, 0);
+}
+
+cm_status cm_testing_qcache_attend_withheld(cm_context *ctx, const cm_qcache *cache, int32_t layer,
+                                            const cm_qcache_batch *batch, const cm_qcache_query *query,
+                                            void *workspace, int64_t workspace_bytes, int32_t what,
+                                            cm_stream_t stream) {
+    if (what != cm::kQcacheWithholdQueries) return fail(CM_ERR_INVALID_ARG, "nothing that can be withheld");
+    return attend(ctx, cache, layer, batch, query, workspace, workspace_bytes, stream, what);
 }
 
 cm_status cm_qcache_workspace(cm_context *ctx, int32_t head_dim, int64_t *out_bytes) {

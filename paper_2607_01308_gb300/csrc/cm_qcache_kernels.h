@@ -75,7 +75,10 @@ struct QcacheAttentionParams {
     int32_t requests, heads, group, head_dim, log2_block;
     int32_t total_rows, causal, format;
     int32_t no_context;           // -1: context_lens is another array of that size, and no request was cut short; else 0
+    int32_t withhold;             // prefill, failure injection: an arrival that does not come, in thread block 0
 };
+
+constexpr int kQcacheWithholdQueries = 1;   // of the query rows
 
 // The workspace holds, for every thread block of a launch, two partial results and an arrival
 // counter or a QcacheSplit.

@@ -483,6 +483,7 @@ struct Barriers {
     uint64_t q_full[2], o_full[2];
     uint64_t s_full[2][2], p_full[2][2];      // query tile, score buffer
     uint64_t o_done[2];                       // all but the segment's last tile is in the output
+    uint64_t drained[2];                      // all that an issuing warp has issued is done
 };
 
 template <int D, int FORMAT>
@@ -542,9 +543,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 bar_init(&bars.s_full[i][j], 1);
                 bar_init(&bars.p_full[i][j], 128);
             }
-            bar_init(&bars.q_full[i], 128);
+            bar_init(&bars.q_full[i], 128 + (p.withhold == kQcacheWithholdQueries && blockIdx.x == 0));   // one more never comes
             bar_init(&bars.o_full[i], 1);
             bar_init(&bars.o_done[i], 1);
+            bar_init(&bars.drained[i], 1);
             bar_init(&bars.entry_empty[i], C::kIssuers);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -851,6 +853,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             }
         }
         if (Q0 == 0 && !split && leader) p.splits[blockIdx.x].rows = 0;
+        // whatever waits were passed over before, nothing is under way into this block's memory when it ends
+        int late = 0;
+        commit(&bars.drained[Q0], leader);
+        if (!bar_try(&bars.drained[Q0], 0)) bar_wait_slow(&bars.drained[Q0], 0, &late, p.error);
+        __syncwarp();
       };
       using First = std::integral_constant<int, 0>;
       using Second = std::integral_constant<int, 1>;

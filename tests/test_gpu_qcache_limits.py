@@ -222,11 +222,11 @@ def test_results_that_lie_on_one_another_are_refused(ctx):
 
 # ---------------------------------------------------------------- memory that is used again
 
-def _steps(ctx, rows, dim, seed=5):
+def _steps(ctx, rows, dim, seed=5, fmt="e4m3"):
     """A cache of some 2,500 tokens, a batch of one request that reads all of it, and a query."""
     block, tokens = 16, 2500
     n = -(-tokens // block)
-    cache = cm.QCache(ctx, n, block, 1, 1, dim)
+    cache = cm.QCache(ctx, n, block, 1, 1, dim, dtype=ref.DTYPE[fmt])
     g = torch.Generator(device=DEV).manual_seed(seed)
     x = torch.randn((2, 1, 1, tokens, dim), generator=g, device=DEV).bfloat16()
     cache.append(x[0], x[1], torch.arange(tokens, device=DEV))
@@ -364,3 +364,35 @@ def test_a_dropped_batch_keeps_its_memory_from_others_until_its_stream_is_done(c
     assert not {big.data_ptr(), small.data_ptr()} & set(spaces)
     side.synchronize()
     assert torch.isfinite(out).all()
+
+
+# ---------------------------------------------------------------- waits that run out
+
+def _withheld(ctx, cache, batch, q, out, what):
+    """Attention with an arrival withheld: the host learns of it, once. Returns the call's time in ms."""
+    n, heads, dim = q.shape
+    d = cm.cm_qcache_query(q=q.data_ptr(), out=out.data_ptr(), q_stride_row=q.stride(0), q_stride_head=q.stride(1),
+                           out_stride_row=out.stride(0), out_stride_head=out.stride(1), total_rows=n, num_q_heads=heads,
+                           max_rows_per_request=n, causal=1, softmax_scale=dim ** -0.5)
+    begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    begin.record()
+    st = cm.lib.cm_testing_qcache_attend_withheld(ctx.handle, cache._ref, 0, batch._ref, bytes(d), batch._workspace_ptr,
+                                                  batch._workspace_bytes, what, torch.cuda.current_stream().cuda_stream or None)
+    end.record()
+    assert st == cm.Status.OK
+    with pytest.raises(cm.CMError) as e:
+        ctx.check()
+    assert e.value.status == cm.Status.ERR_TIMEOUT
+    ctx.check()
+    return begin.elapsed_time(end)
+
+
+@pytest.mark.parametrize("dim,fmt", [(32, "e4m3"), (64, "int8"), (128, "e4m3"), (256, "int8")])
+def test_withheld_queries_time_out_and_the_next_call_is_right(ctx, dim, fmt):
+    cache, batch, q = _steps(ctx, 70, dim, fmt=fmt)
+    want = cache.attend(q, batch)[0]
+    out = torch.zeros_like(q)
+    for _ in range(2):
+        _withheld(ctx, cache, batch, q, out, 1)
+        assert torch.equal(cache.attend(q, batch)[0], want)
+    ctx.check()
