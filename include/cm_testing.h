@@ -26,7 +26,8 @@ cm_status cm_testing_render_withheld_load(const cm_set *set, void *k_out, void *
                                           int64_t capacity_tokens, cm_stream_t stream);
 
 /* cm_qcache_attend by its many-rows kernel (whatever the rows), in whose first thread block an arrival that
- * others wait for never comes: `what` 1, that the query rows are there. Takes about a
+ * others wait for never comes: `what` 1, that the query rows are there; 2, that the tiles' blocks and scales are
+ * looked up (and they are not). Takes about a
  * second of device time; the output is incomplete, and cm_context_check then returns CM_ERR_TIMEOUT. */
 cm_status cm_testing_qcache_attend_withheld(cm_context *ctx, const cm_qcache *cache, int32_t layer,
                                             const cm_qcache_batch *batch, const cm_qcache_query *query,

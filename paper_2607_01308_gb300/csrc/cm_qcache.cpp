@@ -321,7 +321,8 @@ cm_status cm_testing_qcache_attend_withheld(cm_context *ctx, const cm_qcache *ca
                                             const cm_qcache_batch *batch, const cm_qcache_query *query,
                                             void *workspace, int64_t workspace_bytes, int32_t what,
                                             cm_stream_t stream) {
-    if (what != cm::kQcacheWithholdQueries) return fail(CM_ERR_INVALID_ARG, "nothing that can be withheld");
+    if (what != cm::kQcacheWithholdQueries && what != cm::kQcacheWithholdEntries)
+        return fail(CM_ERR_INVALID_ARG, "nothing that can be withheld");
     return attend(ctx, cache, layer, batch, query, workspace, workspace_bytes, stream, what);
 }
 

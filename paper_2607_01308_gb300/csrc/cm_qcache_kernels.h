@@ -79,6 +79,7 @@ struct QcacheAttentionParams {
 };
 
 constexpr int kQcacheWithholdQueries = 1;   // of the query rows
+constexpr int kQcacheWithholdEntries = 2;   // of every tile's blocks and scales, which are not looked up either
 
 // The workspace holds, for every thread block of a launch, two partial results and an arrival
 // counter or a QcacheSplit.

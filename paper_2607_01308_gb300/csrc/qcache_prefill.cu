@@ -552,6 +552,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
     }
+    // after a wait that ran out the loads may come to a tile that was never looked up: it is one without blocks
+    for (int i = tid; i < kEntryStages * kBlocks; i += kThreads) entries[i / kBlocks].offset[i % kBlocks] = -1;
     if (warp == 1) {
         // where the block's share begins: the request by halving, the row tile 32 at a time
         const uint64_t units = (uint64_t)total * (uint32_t)p.heads;
@@ -865,7 +867,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
       if (warp == kEntryWarp) {
         // ------------------------------------------------ blocks and scales, kEntryTiles tiles at a time
         uint32_t n_tile = 0;
-        while (walk.next(p)) {
+        const bool withheld = p.withhold == kQcacheWithholdEntries && blockIdx.x == 0;
+        while (!withheld && walk.next(p)) {
             for (int t = w.t0; t < w.t1;) {
                 // up to the next multiple of kEntryTiles of the count, so that the stages stay together
                 const int n = min(w.t1 - t, (int)(kEntryTiles - n_tile % kEntryTiles));

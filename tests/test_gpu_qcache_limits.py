@@ -396,3 +396,24 @@ def test_withheld_queries_time_out_and_the_next_call_is_right(ctx, dim, fmt):
         _withheld(ctx, cache, batch, q, out, 1)
         assert torch.equal(cache.attend(q, batch)[0], want)
     ctx.check()
+
+
+@pytest.mark.parametrize("dim,fmt", [(32, "e4m3"), (64, "int8"), (128, "e4m3"), (256, "int8")])
+def test_withheld_lookups_time_out_and_read_nothing_outside(ctx, dim, fmt):
+    """The loads go on without the places of their codes: they read none. (Shared memory that was never written is no
+    address; what a wrong one would do is not tried.)"""
+    cache, batch, q = _steps(ctx, 70, dim, fmt=fmt)
+    want = cache.attend(q, batch)[0]
+    out = torch.zeros_like(q)
+    for _ in range(2):
+        _withheld(ctx, cache, batch, q, out, 2)
+        assert torch.equal(cache.attend(q, batch)[0], want)
+    ctx.check()
+
+
+def test_unknown_arrivals_are_not_withheld(ctx):
+    cache, batch, q = _steps(ctx, 1, 64)
+    for what in (0, 3, -1):
+        assert cm.lib.cm_testing_qcache_attend_withheld(ctx.handle, cache._ref, 0, batch._ref, bytes(cm.cm_qcache_query()),
+                                                        batch._workspace_ptr, batch._workspace_bytes, what,
+                                                        None) == cm.Status.ERR_INVALID_ARG
