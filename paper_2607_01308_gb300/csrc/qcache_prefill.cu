@@ -94,9 +94,9 @@ __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity) {
     return ok != 0;
 }
 
-// Waits for the phase of the given parity. A wait that runs out (about a second) is recorded, and
-// every later one then gives up at once, so that the block runs to its end with a wrong result that
-// the host can learn of.
+// Waits for the phase of the given parity. A wait that runs out (2 * 10^9 cycles, about a second) is recorded, and every
+// later one then gives up after two tries (measured: 864 tiles of three such waits end 7 ms after the first), so that the
+// block runs to its end with a wrong result that the host can learn of.
 __device__ __forceinline__ void bar_wait_slow(uint64_t *b, uint32_t parity, volatile int *failed, unsigned int *error) {
     const long long t0 = clock64();
     while (!bar_try(b, parity)) {

@@ -417,3 +417,21 @@ def test_unknown_arrivals_are_not_withheld(ctx):
         assert cm.lib.cm_testing_qcache_attend_withheld(ctx.handle, cache._ref, 0, batch._ref, bytes(cm.cm_qcache_query()),
                                                         batch._workspace_ptr, batch._workspace_bytes, what,
                                                         None) == cm.Status.ERR_INVALID_ARG
+
+
+def test_after_a_wait_ran_out_the_others_do_not_add_up(ctx):
+    """A block with 64 * 2,052 / 152 = 864 tiles that are never looked up: the first wait takes 2e9 cycles (0.97 s at
+    2,070 MHz, 1.43 s at 1,400), the three of each tile after it some microseconds (a millisecond each, which a try may take, would be 2.6 s)."""
+    block, tokens, heads, dim, rows = 16, 1 << 17, 64, 32, 40
+    n = tokens // block
+    cache = cm.QCache(ctx, n, block, 1, heads, dim)
+    batch = cm.QBatch(ctx, 1, n, rows, block)
+    batch.block_table.copy_(torch.arange(n)[None].int())
+    batch.row_starts.copy_(_i32([0, rows]))
+    batch.kv_lens.fill_(tokens)
+    q = torch.zeros((rows, heads, dim), dtype=torch.bfloat16, device=DEV)
+    out = torch.zeros_like(q)
+    assert 900 < _withheld(ctx, cache, batch, q, out, 2) < 1600
+    cache.attend(q, batch, out=out)
+    ctx.check()
+    assert bool((out == 0).all())
