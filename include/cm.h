@@ -475,7 +475,8 @@ typedef struct cm_qcache_batch {
     int32_t block_size;                  /* the cache's */
     int64_t table_width;                 /* entries of a request's row of block_table */
     int32_t *block_table;                /* [R][table_width]: block of token t at entry t / block_size */
-    int32_t *row_starts;                 /* [R + 1]: first row of each request's new tokens; ascending */
+    int32_t *row_starts;                 /* [R + 1]: first row of each request's new tokens; ascending
+                                            (attention leaves rows that several requests claim undefined) */
     int32_t *kv_lens;                    /* [R]: tokens cached, the new ones included */
 } cm_qcache_batch;
 

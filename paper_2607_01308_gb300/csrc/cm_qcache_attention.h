@@ -49,6 +49,12 @@ __device__ __forceinline__ RequestShape request_shape(const QcacheAttentionParam
     return s;
 }
 
+// Sums of units in 32 bits. The host refuses calls whose requests could come to 2^31 units together, so only
+// row starts that do not ascend (rows that several requests claim) reach that: the sum stays there, and such a call
+// does nothing, where one that wrapped around would send blocks to places outside the requests.
+constexpr uint32_t kTooMany = 0x7fffffffu;
+__device__ __forceinline__ uint32_t add_units(uint32_t a, uint32_t b) { return min(a + b, kTooMany); }
+
 // A unit of work is a kv tile of one row tile and kv head. What beginning and ending a (row tile, head)
 // costs besides its tiles (the query rows, the first copies, the parts' meeting) counts as SETUP units in
 // front of them, or short requests would come to the same few thread blocks.
@@ -70,22 +76,22 @@ __device__ __forceinline__ uint32_t plan_units(const QcacheAttentionParams &p, u
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) {
             const uint32_t x = __shfl_up_sync(~0u, a, d);
-            if (lane >= d) a += x;
+            if (lane >= d) a = add_units(a, x);
         }
         if (lane == 31) scan[warp] = a;
         __syncthreads();
         uint32_t before = total;
 #pragma unroll
         for (int w = 0; w < THREADS / 32; ++w) {
-            if (w < warp) before += scan[w];
-            total += scan[w];
+            if (w < warp) before = add_units(before, scan[w]);
+            total = add_units(total, scan[w]);
         }
         if (r < p.requests) prefix[r] = before + a - n;
         __syncthreads();
     }
     if (tid == 0) prefix[p.requests] = total;
     __syncthreads();
-    return total;
+    return total < kTooMany ? total : 0;
 }
 
 // Units of one thread block: an even share, but no less than a few tiles, below which joining the

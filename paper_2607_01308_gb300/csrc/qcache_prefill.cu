@@ -516,18 +516,19 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) {
             const uint32_t x = __shfl_up_sync(~0u, a, d);
-            if (lane >= d) a += x;
+            if (lane >= d) a = add_units(a, x);
         }
         if (lane == 31) scan[warp] = a;
         __syncthreads();
         uint32_t before = total;
         for (int w = 0; w < kThreads / 32; ++w) {
-            if (w < warp) before += scan[w];
-            total += scan[w];
+            if (w < warp) before = add_units(before, scan[w]);
+            total = add_units(total, scan[w]);
         }
         if (r < p.requests) prefix[r] = before + a - n;
         __syncthreads();
     }
+    if (total >= kTooMany) total = 0;
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "n"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");

@@ -183,6 +183,29 @@ def test_attend_as_many_requests_as_shared_memory_holds(ctx, requests, group):
     _attend_requests(ctx, lens, 1, group, 128, 16, 1, [0, 1, 127, 128, 129, 2047, requests - 2, requests - 1], requests)
 
 
+@pytest.mark.parametrize("max_new,T", [(1, 8192), (1000, 65536)])
+def test_row_starts_that_do_not_ascend(ctx, max_new, T):
+    """2,048 requests that claim all of the rows, in tiles of 8 or of 256: more work than 32 bits count. Such a call does
+    nothing, and the batch can be used on."""
+    R, width, group, dim, block = 4096, 256, 8, 32, 256
+    assert 2048 * (T * group // (8 if max_new == 1 else 256)) * (width * block // 64) >= 2 ** 32
+    cache = cm.QCache(ctx, width, block, 1, 1, dim)
+    batch = cm.QBatch(ctx, R, width, T, block)
+    batch.block_table.copy_(torch.arange(width, dtype=torch.int32)[None].expand(R, width))
+    batch.row_starts.copy_((torch.arange(R + 1) % 2 * T).int())
+    batch.kv_lens.fill_(width * block)
+    batch.max_new = max_new
+    q = torch.zeros((T, group, dim), dtype=torch.bfloat16, device=DEV)
+    out = torch.full_like(q, 7.0)
+    cache.attend(q, batch, out=out)
+    ctx.check()
+    assert bool((out == 7).all())
+    batch.row_starts.copy_(torch.arange(R + 1, dtype=torch.int32))
+    cache.attend(q, batch, out=out)
+    ctx.check()
+    assert bool((out[:R] == 0).all()) and bool((out[R:] == 7).all())
+
+
 # ---------------------------------------------------------------- refusals
 
 def _small(ctx, rows=3, heads=2, dim=64):
