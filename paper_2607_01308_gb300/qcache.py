@@ -60,6 +60,14 @@ def _format(dtype) -> int:
     return _INT8 if dtype == torch.int8 else _E4M3
 
 
+def _fixed(name: str):
+    """A tensor whose address the library holds: it can be written into (+= too), but not replaced."""
+    def keep(self, value):
+        if value is not getattr(self, name):
+            raise AttributeError("%s is the memory that the calls use: write into it" % name[1:])
+    return property(lambda self: getattr(self, name), keep)
+
+
 class QBatch:
     """The requests of a step: block table, row starts and lengths on the GPU, the slots of the new
     rows and the attention's workspace. One batch is used by one stream at a time.
@@ -79,6 +87,18 @@ class QBatch:
     given back when the torch streams that its calls ran on are through with it; a stream given as a bare handle has to be
     through with it before the batch is dropped."""
 
+    block_table, row_starts, kv_lens = _fixed("_block_table"), _fixed("_row_starts"), _fixed("_kv_lens")
+    context_lens, slot_map, counts = _fixed("_context_lens"), _fixed("_slot_map"), _fixed("_counts")
+
+    @property
+    def max_rows(self) -> int:
+        return self._max_rows
+
+    @max_rows.setter
+    def max_rows(self, rows: int) -> None:
+        _require(0 <= rows <= self._slot_map.numel(), "max_rows must not pass the slot map's size")
+        self._max_rows = rows
+
     def __init__(self, ctx: Context, num_requests: int, table_width: int, max_rows: int,
                  block_size: int):
         import torch
@@ -86,18 +106,18 @@ class QBatch:
         dev = _device(ctx)
         self.ctx = ctx
         self._device, self._int32 = ctx.device, torch.int32
-        self.max_rows = max_rows
+        self._max_rows = max_rows
         self.max_new: Optional[int] = None
-        self.block_table = torch.full((num_requests, table_width), -1, dtype=torch.int32, device=dev)
-        self.row_starts = torch.zeros(num_requests + 1, dtype=torch.int32, device=dev)
-        self.kv_lens = torch.zeros(num_requests, dtype=torch.int32, device=dev)
-        self.context_lens = torch.full((num_requests,), -1, dtype=torch.int32, device=dev)
-        self.slot_map = torch.full((max_rows,), -1, dtype=torch.int64, device=dev)
-        self.counts = torch.zeros(2, dtype=torch.int64, device=dev)
+        self._block_table = torch.full((num_requests, table_width), -1, dtype=torch.int32, device=dev)
+        self._row_starts = torch.zeros(num_requests + 1, dtype=torch.int32, device=dev)
+        self._kv_lens = torch.zeros(num_requests, dtype=torch.int32, device=dev)
+        self._context_lens = torch.full((num_requests,), -1, dtype=torch.int32, device=dev)
+        self._slot_map = torch.full((max_rows,), -1, dtype=torch.int64, device=dev)
+        self._counts = torch.zeros(2, dtype=torch.int64, device=dev)
         self._c = cm_qcache_batch(num_requests, block_size, table_width, self.block_table.data_ptr() or None,
                                   self.row_starts.data_ptr(), self.kv_lens.data_ptr() or None)
         self._ref = ctypes.byref(self._c)
-        self._num_requests, self._slots, self._counts = num_requests, self.slot_map.data_ptr() or None, self.counts.data_ptr()
+        self._num_requests, self._slots, self._count_ptr = num_requests, self.slot_map.data_ptr() or None, self.counts.data_ptr()
         self._context = self.context_lens.data_ptr()
         self._workspace_bytes = max(cm_qcache_workspace(ctx.handle, d) for d in _ATTENTION_DIMS)
         self._workspace = torch.zeros(self._workspace_bytes, dtype=torch.uint8, device=dev)
@@ -127,8 +147,8 @@ class QBatch:
                 raise ValueError("context_lens, new_lens and free_blocks must be contiguous int32 vectors on the context's device")
         _require(context_lens.numel() == n and new_lens.numel() == n, "one length per request")
         _check(lib.cm_qcache_schedule_cut(self.ctx.handle, self._ref, context_lens.data_ptr() or None, new_lens.data_ptr() or None,
-                                          free_blocks.data_ptr() or None, free_blocks.numel(), self._slots, self.max_rows,
-                                          self._counts, self._context or None, self._on(stream)))
+                                          free_blocks.data_ptr() or None, free_blocks.numel(), self._slots, self._max_rows,
+                                          self._count_ptr, self._context or None, self._on(stream)))
         return self
 
 
@@ -136,6 +156,8 @@ class QCache:
     """A paged KV cache held in 8 bits: codes k, v [num_blocks, layers, kv_heads, block_size, head_dim]
     (float8_e4m3fn or int8) and one fp32 scale for each block, layer and head, k_scale, v_scale
     [num_blocks, layers, kv_heads]; a stored value is code * scale."""
+
+    k, v, k_scale, v_scale = _fixed("_k"), _fixed("_v"), _fixed("_k_scale"), _fixed("_v_scale")
 
     def __init__(self, ctx: Context, num_blocks: int, block_size: int, num_layers: int,
                  num_kv_heads: int, head_dim: int, dtype=None):
@@ -168,7 +190,7 @@ class QCache:
                  "cache tensors must be on the context's device")
         self._device = ctx.device
         self._bf16, self._fp32, self._int64 = torch.bfloat16, torch.float32, torch.int64
-        self.ctx, self.k, self.v, self.k_scale, self.v_scale = ctx, k, v, k_scale, v_scale
+        self.ctx, self._k, self._v, self._k_scale, self._v_scale = ctx, k, v, k_scale, v_scale
         nb, L, H, bs, d = k.shape
         s, z = _strides(k, 4, 16), _strides(k_scale, 3, 1)
         self._c = cm_qcache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), fmt, L, H, d, bs, 0,

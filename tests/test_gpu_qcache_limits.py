@@ -458,3 +458,25 @@ def test_after_a_wait_ran_out_the_others_do_not_add_up(ctx):
     cache.attend(q, batch, out=out)
     ctx.check()
     assert bool((out == 0).all())
+
+
+def test_tensors_that_the_library_holds_cannot_be_replaced(ctx):
+    """Assigning another tensor would leave the calls with the old one's memory; writing into it is the way."""
+    cache, batch, q = _small(ctx)
+    for obj, names in ((batch, ("block_table", "row_starts", "kv_lens", "context_lens", "slot_map", "counts")),
+                       (cache, ("k", "v", "k_scale", "v_scale"))):
+        for name in names:
+            with pytest.raises(AttributeError):
+                setattr(obj, name, getattr(obj, name).clone())
+    batch.kv_lens[0] = 2
+    batch.kv_lens += 1
+    cache.k_scale *= 2
+    assert batch.kv_lens.tolist() == [3]
+    # fewer rows than the slot map has are fine, more are not
+    batch.max_rows = 2
+    for rows in (4, -1):
+        with pytest.raises(ValueError):
+            batch.max_rows = rows
+    batch.slot_map.fill_(-9)
+    batch.schedule(_i32([0]), _i32([5]), _i32([1]))
+    assert batch.slot_map.tolist() == [16, 17, -9] and batch.row_starts.tolist() == [0, 2]
