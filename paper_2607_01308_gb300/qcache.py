@@ -233,6 +233,8 @@ class QCache:
         if lse is not None and (lse.dtype is not self._fp32 or lse.shape != shape[:2] or not lse.is_contiguous() or
                                 lse.get_device() != device):
             raise ValueError("lse must be a contiguous fp32 [rows, q_heads]")
+        if batch._device != device:
+            raise ValueError("the batch must be on the cache's device")
         qs, os = _strides(q, 2, 8), _strides(out, 2, 8)
         query = _pack_query(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), qs[0], qs[1], os[0], os[1],
                             shape[0], shape[1], batch.max_new or 0, 1 if causal else 0,

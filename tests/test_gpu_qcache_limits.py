@@ -480,3 +480,11 @@ def test_tensors_that_the_library_holds_cannot_be_replaced(ctx):
     batch.slot_map.fill_(-9)
     batch.schedule(_i32([0]), _i32([5]), _i32([1]))
     assert batch.slot_map.tolist() == [16, 17, -9] and batch.row_starts.tolist() == [0, 2]
+
+
+def test_a_batch_of_another_device_is_refused(ctx):
+    """Its addresses mean nothing here. (One GPU: a batch that says it is elsewhere.)"""
+    cache, batch, q = _small(ctx)
+    batch._device = 1
+    with pytest.raises(ValueError):
+        cache.attend(q, batch)
