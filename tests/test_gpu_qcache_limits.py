@@ -183,6 +183,50 @@ def test_attend_as_many_requests_as_shared_memory_holds(ctx, requests, group):
     _attend_requests(ctx, lens, 1, group, 128, 16, 1, [0, 1, 127, 128, 129, 2047, requests - 2, requests - 1], requests)
 
 
+@pytest.mark.parametrize("requests", [129, 300, 700])
+@pytest.mark.parametrize("heads,group,dim,fmt", [(2, 4, 64, "e4m3"), (1, 2, 256, "int8"), (1, 8, 32, "e4m3")])
+@pytest.mark.parametrize("max_new", [1, 1000])
+def test_attend_more_requests_than_the_plan_scans_at_a_time(ctx, requests, heads, group, dim, fmt, max_new):
+    """Ragged requests, some without rows or tokens, beyond 128 (few-rows kernel) and 640 (many-rows kernel)."""
+    rng = np.random.default_rng(requests + dim)
+    lens = [(int(kv), int(m)) for kv, m in zip(rng.integers(0, 400, requests), rng.choice([0, 1, 1, 2, 5], requests))]
+    lens[0], lens[128], lens[requests - 1] = (33, 1), (70, 2), (129, 1)
+    checked = sorted({0, 1, 127, 128, requests // 2, requests - 2, requests - 1} | ({639, 640, 641} if requests > 641 else set()))
+    _attend_requests(ctx, lens, heads, group, dim, 16, max_new, checked, requests, fmt)
+
+
+@pytest.mark.parametrize("tokens,kv,group,dim,heads", [(1100, 1300, 8, 32, 1), (1100, 1100, 8, 64, 2), (600, 700, 16, 256, 1)])
+def test_attend_more_row_tiles_than_a_warp_searches_at_a_time(ctx, tokens, kv, group, dim, heads):
+    """More than 32 row tiles of a request and kv head, between requests of other sizes; a sample of the rows."""
+    requests = [(50, 3), (kv, tokens), (0, 2), (77, 77)]
+    block, pool = 16, 128
+    g = torch.Generator(device=DEV).manual_seed(tokens + dim)
+    cache = cm.QCache(ctx, pool, block, 1, heads, dim)
+    x = torch.randn((2, 1, heads, pool * block, dim), generator=g, device=DEV).bfloat16()
+    cache.append(x[0], x[1], torch.arange(pool * block, device=DEV))
+    width = -(-kv // block)
+    table = np.random.default_rng(dim).integers(0, pool, (len(requests), width))
+    starts = np.cumsum([0] + [m for _, m in requests])
+    batch = cm.QBatch(ctx, len(requests), width, int(starts[-1]), block)
+    batch.block_table.copy_(torch.from_numpy(table).int())
+    batch.row_starts.copy_(torch.from_numpy(starts).int())
+    batch.kv_lens.copy_(_i32([n for n, _ in requests]))
+    q = torch.randn((int(starts[-1]), heads * group, dim), generator=g, device=DEV).bfloat16()
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device=DEV)
+    cache.attend(q, batch, out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert not (out == 7).all(-1).any() and not (lse == 7).any()
+    assert tokens * group > 32 * (128 if dim == 256 else 256)
+    for r, (n, m) in enumerate(requests):
+        rows = sorted({0, 1, m // 3, m // 2, m - 2, m - 1, *([m - 60, 32 * 256 // group - 1, 32 * 256 // group] if m > 500 else [])})
+        rows = [i for i in rows if 0 <= i < m]
+        at = torch.tensor(rows) + int(starts[r])
+        for h in range(heads):
+            k, v = _rows_of(cache, h, [int(table[r, t // block]) for t in range(n)], block)
+            for j in range(h * group, (h + 1) * group):
+                _assert_rows(out[at, j], lse[at, j], q[at, j], k, v, [max(0, n - m + i + 1) for i in rows])
+
+
 @pytest.mark.parametrize("max_new,T", [(1, 8192), (1000, 65536)])
 def test_row_starts_that_do_not_ascend(ctx, max_new, T):
     """2,048 requests that claim all of the rows, in tiles of 8 or of 256: more work than 32 bits count. Such a call does
