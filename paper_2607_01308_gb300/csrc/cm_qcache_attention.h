@@ -38,11 +38,23 @@ __device__ __forceinline__ RequestShape request_shape(const QcacheAttentionParam
     s.row0 = min(max(p.row_starts[r], 0), p.total_rows);
     const int q_len = min(max(p.row_starts[r + 1], s.row0), p.total_rows) - s.row0;
     const int kv = (int)min((int64_t)max(p.kv_lens[r], 0), cap);
-    // a request that was cut short: the two lengths do not say which tokens its rows are (loaded with the others; without
-    // context_lens a length, which counts as negative)
-    const int context = p.context_lens[r] | p.no_context;
-    s.kv = context < 0 ? kv : (int)min((uint32_t)kv, (uint32_t)context + (uint32_t)q_len);
-    s.first = context < 0 ? kv - q_len : min(context, s.kv);
+    // A request that was cut short: the two lengths do not say which tokens its rows are. Its context length is loaded with
+    // the others and selected by (without context_lens it is a length, made negative), except with two query tiles, where a
+    // test keeps the issuing loop shorter: 8 prompts of 700 tokens, 8 kv heads x 4 of 128, 80 us against 84; the other
+    // way round 29 requests of 3 rows take 19.7 us instead of 19.2, prompts of head_dim 256 49.3 instead of 48.2.
+    s.kv = kv;
+    s.first = kv - q_len;
+    if constexpr (ROWS == 256) {
+        const int context = p.no_context ? -1 : p.context_lens[r];
+        if (context >= 0) {
+            s.kv = (int)min((uint32_t)kv, (uint32_t)context + (uint32_t)q_len);
+            s.first = min(context, s.kv);
+        }
+    } else {
+        const int context = p.context_lens[r] | p.no_context;
+        s.kv = context < 0 ? kv : (int)min((uint32_t)kv, (uint32_t)context + (uint32_t)q_len);
+        s.first = context < 0 ? kv - q_len : min(context, s.kv);
+    }
     s.rows = q_len * p.group;
     s.row_tiles = (s.rows + ROWS - 1) / ROWS;
     s.tiles = max(1, (s.kv + TILE - 1) / TILE);   // one without tokens too: its rows are written
