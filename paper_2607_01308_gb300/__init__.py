@@ -16,7 +16,8 @@ What decodes from a merged cache reads it in 8 bits (QCache, QBatch):
     batch = cm.QBatch(ctx, requests, table_width, max_rows, 16)
     batch.schedule(context_lens, new_lens, free_blocks)       # block tables and slots
     cache.append(k_out, v_out, batch.slot_map)                # the merged cache into its blocks
-    out, lse = cache.attend(q, batch, layer=0)                # softmax(q K^T / sqrt(d)) V
+    batch.max_new = 1                                         # if no request brings more rows than this
+    out, _ = cache.attend(q, batch, layer=0)                  # softmax(q K^T / sqrt(d)) V
 """
 from ._binding import (  # noqa: F401
     CMError, Status, cm_id, cm_fragment, lib, LIB_PATH, EXPORTED,

@@ -13,10 +13,13 @@
 // Rows of one block are consecutive in the call (slots ascend by one), so the first of them (its
 // slot does not continue the row before it inside one block) stands for the whole run. A thread
 // block finds the runs that begin in its window of rows; then a warp takes a run of one head, K or
-// V: it reads it into registers, reduces the magnitude, writes the scale and the codes, so that every
-// element is read once. Bound by HBM: 2 bytes in and 1 out per element. Measured: 36 layers of 8
-// heads of 128, 5,208 tokens (1,153 MB): 175 us, 6.6 TB/s; 10,300 ragged int8 rows of 12 heads of 64
-// (47 MB, two waves of thread blocks): 13.8 us; one token of 48 requests: 2.6 us, a launch's latency.
+// V: it reads it into registers, reduces the magnitude, writes the scale and the codes. A run that fits the registers
+// (2,048 elements of a warp, 8,192 of four, 16,384 of eight) is read once; of a longer one all but the last
+// part is read a second time for its codes (blocks of 128 x 128 and 128 x 256: 1.5 times in all, 256 x 256: 1.75).
+// Bound by HBM: 2 bytes in and 1 out per element. Measured: 36 layers of 8 heads of 128, 5,208 tokens in blocks of
+// 16 (1,153 MB): 175 us, 6.6 TB/s; 5,000 tokens in blocks of 64 184 us (6.0 TB/s), of 128 217 us (5.1), where a thread
+// block's warps write K and V one after the other; 10,300 ragged int8 rows of 12 heads of 64 (47 MB, 2.1 waves of thread
+// blocks): 13.5 us; one token of 48 requests: 2.5 us, a launch's latency.
 #include "cm_qcache_kernels.h"
 
 #include "cm_qcache_codes.h"
@@ -314,7 +317,7 @@ cudaError_t launch_qcache_append(QcacheAppendParams p, int num_sms, cudaStream_t
     //   above      four warps, of more than 16384 eight (blocks of 128 x 256: 242 us, with four 257,
     //              with sixteen, of which fewer fit an SM, 381); all head_dim above 256 are here. Short
     //              runs in such blocks go to single warps all the same (one token of 128 requests, 36
-    //              layers, blocks of 128 x 128: 49 us against 142)
+    //              layers, blocks of 128 x 128: 48 us against 142)
     const int64_t block = (int64_t)p.head_dim << p.log2_block;
     const int team = block <= 4096 ? 1 : block <= 16384 ? 4 : 8, per = team == 1 ? 2 : 1;
     const int head_groups = (p.heads + per - 1) / per;

@@ -23,8 +23,9 @@
 // result does not depend on timing.
 //
 // Bound by HBM once the requests are long (above), by the chain of dependent reads (lengths, table, scales,
-// tokens, parts) when they are short: one token over 1,041 cached 8.4 us, over 131,072 57 us; 64 requests of
-// 600 to 12,000 tokens 84 us (5.9 TB/s); 29 requests, int8 drafts of 3 or 4 rows, 18 us.
+// tokens, parts) when they are short: one token over 1,041 cached 8.8 us; 64 requests of 600 to 12,000 tokens 84 us
+// (5.9 TB/s); 29 requests, int8 drafts of 3 or 4 rows, 18 us. At head_dim 32 and 64 neither HBM nor issue is full (64: 47
+// and 52 % over 32 x 4,096 tokens): a warp's own chain of copy, conversion and products per 16 tokens.
 #include "cm_qcache_kernels.h"
 
 #include <atomic>
@@ -426,10 +427,10 @@ cudaError_t launch_qcache_attention(const QcacheAttentionParams &p, int rows_per
                                     cudaStream_t stream) {
     // Rows of a request and kv head: to 8 in one fragment, to 16 in two at once, to 32 (not at head_dim 256) in two
     // tiles of those, which read the cache twice; above, the other kernel. Measured, 32 requests of 4,096 tokens, 8 kv heads:
-    //   head_dim 128 e4m3   8 rows 55 us, as two fragments 57; 16 rows 61 us, as two tiles of one 99 or more;
-    //                       32 rows 100 us, by the other kernel 109
-    //   head_dim 64 int8    8 rows 36 us, as two fragments 42; 32 rows 73 us, by the other kernel 92
-    //   head_dim 32 e4m3    32 rows 51 us, by the other kernel 82
+    //   head_dim 128 e4m3   8 rows 52 us, as two fragments 56; 16 rows 60 us, as two tiles of one 91;
+    //                       32 rows 97 us, by the other kernel 105 (one request of 131,072 tokens: 101 by either)
+    //   head_dim 64 int8    8 rows 33 us, as two fragments 40; 32 rows 72 us, by the other kernel 90
+    //   head_dim 32 e4m3    32 rows 50 us, by the other kernel 83
     //   head_dim 256 e4m3   (16 requests, 4 kv heads) 32 rows 59 us, by the other kernel 48
     if (rows_per_request > (p.head_dim == 256 ? 16 : 32)) return launch_qcache_prefill(p, num_sms, device, stream);
 #define CM_LAUNCH(D, F) \

@@ -23,9 +23,10 @@
 // kv tiles that the rows of a tile may see at all; a second, small kernel joins the ranges that were cut
 // between thread blocks, over the whole GPU (one thread block alone took 95 us for 256 rows in 19 parts).
 //
-// Bound by the tensor cores and the softmax's latency together (the tensor pipe is 55 to 60 % busy): 2,048
-// rows x 4 heads of a group over 16,384 tokens, 8 kv heads of 128, 464 us (1,260 TFLOP/s); by latency where
-// prompts are short: 64 tokens 10.5 us, five ragged ones of head_dim 256 47 us.
+// Bound by the tensor cores and the softmax's latency together (the tensor pipe is 56 % busy with 1,024 rows x 4 over
+// 8,192 tokens): 2,048 rows x 4 heads of a group over 16,384 tokens, 8 kv heads of 128, 465 us (1,256 TFLOP/s); by
+// latency where prompts are short: 64 tokens of that shape 17.6 us, eight of 700 80 us, five ragged ones of
+// head_dim 256 48 us. What a range costs besides its tiles is spent in series: output out, queries in, first product.
 #include "cm_qcache_kernels.h"
 
 #include <atomic>
@@ -620,6 +621,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         while (walk.next(p)) {
             const int first = w.row_tile * C::kRows + qt * 128;   // of the tile, among the request's rows
             if (first >= w.rows) {
+                // Counted on without waiting, n_tile may get a round and more ahead of the lookups, and the wait for the
+                // entries below then end early, on the parity of the round before. They are there all the same once the tile's
+                // scores are: the loads had them before the products could begin.
                 n_tile += w.t1 - w.t0;
                 continue;
             }

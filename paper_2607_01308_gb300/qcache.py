@@ -78,9 +78,10 @@ class QBatch:
       table row or max_rows ended), else -1
 
     schedule() fills them; a program with tables of its own writes into them instead (and leaves
-    context_lens at -1 where a request's rows are the last of its kv_lens tokens). max_new (host):
-    the most new rows of one request that are expected (None: max_rows); attend() chooses its
-    kernel by it, results do not depend on it.
+    context_lens at -1 where a request's rows are the last of its kv_lens tokens). max_new (host, not
+    set by schedule()): the most new rows of one request that are expected; attend() chooses the kernel of the whole
+    call by it, and is right whatever it says. None counts as all rows of the call: a step of single tokens
+    then goes to the kernel for prompts, at some twice its time.
 
     The workspace (some 40 MB) is made with the batch and stays where it is, for every head_dim, so that
     graphs which were captured with the batch can be replayed as long as it lives. The batch's memory is
