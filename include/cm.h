@@ -579,6 +579,124 @@ cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t laye
 /* Bytes of workspace that cm_qcache_attend needs on ctx's device at a head_dim. */
 cm_status cm_qcache_workspace(cm_context *ctx, int32_t head_dim, int64_t *out_bytes);
 
+/* ------------------------------------------------------------------ trees of drafted tokens
+ *
+ * Several tokens a step: a drafter proposes a tree of tokens for each request, one pass of the model over all of them
+ * says what the target thinks of each, and the path that it accepts stays in the 8-bit cache. A step is
+ *     cm_qcache_schedule     slots for the rows of every tree
+ *     cm_qcache_tree         which rows are a row's ancestors, and its position, from the rows' parents
+ *     cm_qk_rotate           a layer's q and k: norm of each head, rotation to the position
+ *     cm_qcache_append       K and V of all rows into their slots
+ *     cm_qcache_attend_tree  a row attends to its request's context, its ancestors and itself
+ *     cm_tree_verify         the accepted path and the token behind it, from probabilities and random numbers
+ *     cm_qcache_keep         the path's rows to the front, the blocks behind them given back
+ * The rows of request r are row_starts[r] .. row_starts[r + 1] - 1 of a batch. Its row 0 is the root, the token that
+ * the step before has chosen; parents[row] is the place, among its request's rows, of the row that it was drafted behind: before its
+ * own, or it counts as having none (negative: behind the context alone). All of these calls enqueue one kernel
+ * (cm_qcache_attend_tree: as cm_qcache_attend), allocate nothing, and can be captured in a CUDA graph. As
+ * with the calls above the host never reads DEVICE arrays, entries that name nothing are left out rather than followed, and distinct
+ * arguments must not overlap unless said otherwise. */
+
+/* Masks and positions.
+ *   batch           row_starts alone is read
+ *   context_lens    [R] DEVICE: tokens of each request in front of its rows (negative counts as 0)
+ *   parents         [total_rows] DEVICE, or NULL: every row's parent is the one before it
+ *   words           32-bit words of a mask, 1 to 8: the first 32 * words rows of a request can be a tree. Rows behind them have
+ *                   no bit and an empty mask; their position is the context's length, without parents that and their place
+ *   mask            nullable [total_rows][words] DEVICE: bit j of a row (bit j % 32 of word j / 32) is set if row j of its
+ *                   request is the row itself or one of its ancestors
+ *   positions       nullable [total_rows] DEVICE: context length + number of ancestors, to 2^31 - 1
+ * Rows of no request are left untouched. Limits: R <= 16384. */
+cm_status cm_qcache_tree(cm_context *ctx, const cm_qcache_batch *batch, const int32_t *context_lens, const int32_t *parents,
+                         int32_t total_rows, int32_t words, uint32_t *mask, int32_t *positions, cm_stream_t stream);
+
+/* Rows of cm_qk_rotate. Row i, head h of q has head_dim bf16 values, contiguous, at element i * q_stride_row +
+ * h * q_stride_head; k, q_out and k_out likewise. */
+typedef struct cm_qk_rows {
+    const void *q, *k;                         /* DEVICE, 16-byte aligned, bf16 */
+    void *q_out, *k_out;                       /* DEVICE, 16-byte aligned, bf16; may be q and k themselves */
+    const void *q_weight, *k_weight;           /* nullable DEVICE [head_dim], 16-byte aligned, bf16; NULL: no norm */
+    const int32_t *positions;                  /* DEVICE [num_rows], any int32 */
+    int64_t q_stride_row, q_stride_head;       /* elements, multiples of 8 */
+    int64_t k_stride_row, k_stride_head;
+    int64_t q_out_stride_row, q_out_stride_head;   /* head_dim at least where there are several */
+    int64_t k_out_stride_row, k_out_stride_head;
+    int64_t num_rows;                          /* below 2^31 */
+    int32_t num_q_heads, num_kv_heads;         /* 0 to 65535 */
+    int32_t head_dim;                          /* a power of two in [16, 512] */
+    float eps;
+    int32_t reserved;                          /* 0 */
+} cm_qk_rows;
+
+/* q_out and k_out: every head's row x of q and k, y = x / sqrt(mean x^2 + eps) * weight (0 where the root is 0), rotated to its
+ * row's position as the keys of a fragment are: (y_j, y_{j + head_dim / 2}) by position * theta^(-2j / head_dim), theta the
+ * context's. fp32, rounded once to bf16; angles are exact to some 2^-24 turns at any position. Squares are fp32's: a row
+ * with elements beyond some 1e18 is not normed right. q_out may be q, with the same strides, and k_out k. */
+cm_status cm_qk_rotate(cm_context *ctx, const cm_qk_rows *rows, cm_stream_t stream);
+
+/* As cm_qcache_attend, for trees: row i of a request sees the tokens in front of the request's rows (kv_len - n of them, n its
+ * rows, or its context length as for cm_qcache_attend) and, of its n rows, those whose bit is set in row i of mask ([total_rows][words] DEVICE,
+ * words 1 to 8, as cm_qcache_tree writes it or any other). Rows beyond 32 * words have no bit: no row sees them.
+ * query->causal is not read. */
+cm_status cm_qcache_attend_tree(cm_context *ctx, const cm_qcache *cache, int32_t layer,
+                                const cm_qcache_batch *batch, const cm_qcache_query *query, const uint32_t *mask,
+                                int32_t words, void *workspace, int64_t workspace_bytes, cm_stream_t stream);
+
+typedef enum cm_prob_type {
+    CM_PROB_F32 = 0,
+    CM_PROB_BF16 = 1
+} cm_prob_type;
+
+/* Arguments of cm_tree_verify; all pointers DEVICE. Row i of target (draft) is vocab elements from element
+ * i * target_stride (draft_stride) on. */
+typedef struct cm_tree_drafts {
+    const int32_t *row_starts;                 /* [R + 1] */
+    const int32_t *parents, *tokens;           /* [total_rows] */
+    const void *target;                        /* the target's probabilities of what follows each row */
+    const void *draft;                         /* nullable: those from which the rows behind each row were drawn */
+    const float *accept;                       /* [total_rows]: uniform random numbers of [0, 1) */
+    const float *sample;                       /* [R]: likewise */
+    int32_t *path;                             /* [total_rows]: written */
+    int32_t *kept, *next_token;                /* [R]: written */
+    int64_t target_stride, draft_stride;
+    int32_t num_requests, total_rows;
+    int32_t vocab;                             /* 1 to 2^20 */
+    int32_t max_nodes;                         /* rows of a request that are looked at, 1 to 256 */
+    int32_t type;                              /* cm_prob_type of target and draft */
+} cm_tree_drafts;
+
+/* The accepted path of each request, and the token behind it, so that the tokens are distributed as the target's own.
+ * The walk begins at row 0. At a row: w is its row of target, z = 1. The rows behind it, in their order, are accepted where
+ *     accept[row] * q(token) * z < w(token)
+ * q being the row's row of draft (1 without draft); the walk goes on at the first that is. One that is not leaves w = max(w - q z, 0)
+ * and z = sum w, unless that sum is 0; without draft it leaves w(token) = 0 and z less by w(token) (what was drafted without chance is
+ * accepted with the target's probability). Where no row is left, next_token is the first t with w(0) + .. + w(t) > sample * sum w; if w is
+ * all 0, of the row of target as it was; -1 if that is too, and for a request without rows.
+ *   path        the places of the accepted rows among their request's, row 0 first, from path[row_starts[r]] on; -1 behind them
+ *   kept        their number
+ * Probabilities are taken to [0, 1] (NaN: 0); a row whose token is not in [0, vocab) is no row. Arithmetic, so that the same numbers give the
+ * same tokens everywhere: elements fp32, each operation rounded; sums exact, of floor(w * 2^42); z rounded to fp32 where it multiplies a row of
+ * draft; the test's products in fp64. A draft row must be what the rows behind it were drawn from, one after the other, with
+ * replacement. */
+cm_status cm_tree_verify(cm_context *ctx, const cm_tree_drafts *drafts, cm_stream_t stream);
+
+/* The rows of each request's path to the front of its rows, in all layers of the cache: token context_lens[r] + path_i becomes token
+ * context_lens[r] + i, path_i = path[row_starts[r] + i], i < kept[r]. In each block, layer and head that takes rows, and for K and V on their own, the
+ * scale becomes the largest of its own, if tokens in front of the moved ones are in it, and of those of the blocks that they come from; codes whose
+ * scale changes are rounded again, the others are copied. Tokens behind the path keep whatever they are.
+ *   path            ascending places among the request's rows; it ends before an entry that is not, that is beyond the
+ *                   request's rows or tokens, or whose blocks are not of the pool, and after 256
+ *   context_lens    [R]: as given to cm_qcache_schedule (negative counts as 0)
+ *   lens_out        [R]: context_lens[r] + the rows of its path; none of the arrays that are read. batch is not changed: its tables go
+ *                   on naming the blocks that are given back, until cm_qcache_schedule writes others over them
+ *   freed           [max_freed]: the blocks of which no token is left, ceil(lens_out / B) .. ceil(kv_len / B) - 1 of
+ *                   each request's table row, in the requests' order; -1 behind the last. requests + total_rows / B are enough
+ *   freed_count     [1]: their number (freed holds as many as fit)
+ * A block must not be named by two requests where one of them moves rows in it. Limits: R <= 16384. */
+cm_status cm_qcache_keep(cm_context *ctx, const cm_qcache *cache, const cm_qcache_batch *batch, const int32_t *context_lens,
+                         const int32_t *path, const int32_t *kept, int32_t total_rows, int32_t *lens_out, int32_t *freed,
+                         int64_t max_freed, int64_t *freed_count, cm_stream_t stream);
+
 /* Static name of a status code. */
 const char *cm_status_string(cm_status status);
 

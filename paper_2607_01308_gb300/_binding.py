@@ -116,7 +116,28 @@ class cm_qcache_query(ctypes.Structure):
         self.flags = value
 
 
+class cm_qk_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("q_stride_row", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+                ("k_stride_row", ctypes.c_int64), ("k_stride_head", ctypes.c_int64),
+                ("q_out_stride_row", ctypes.c_int64), ("q_out_stride_head", ctypes.c_int64),
+                ("k_out_stride_row", ctypes.c_int64), ("k_out_stride_head", ctypes.c_int64),
+                ("num_rows", ctypes.c_int64), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class cm_tree_drafts(ctypes.Structure):
+    _fields_ = [("row_starts", ctypes.c_void_p), ("parents", ctypes.c_void_p), ("tokens", ctypes.c_void_p),
+                ("target", ctypes.c_void_p), ("draft", ctypes.c_void_p), ("accept", ctypes.c_void_p),
+                ("sample", ctypes.c_void_p), ("path", ctypes.c_void_p), ("kept", ctypes.c_void_p),
+                ("next_token", ctypes.c_void_p), ("target_stride", ctypes.c_int64), ("draft_stride", ctypes.c_int64),
+                ("num_requests", ctypes.c_int32), ("total_rows", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("max_nodes", ctypes.c_int32), ("type", ctypes.c_int32)]
+
+
 CM_QCACHE_CONTEXT_LENS = 1
+CM_PROB_F32, CM_PROB_BF16 = 0, 1
 
 _c = ctypes
 _P = ctypes.c_void_p
@@ -182,6 +203,13 @@ _SIGS = {
                                     _c.POINTER(cm_qcache_batch), _P, _P,   # the query: byref or its bytes
                                     _c.c_int64, _P]),
     "cm_qcache_workspace": (_c.c_int, [_P, _c.c_int32, _c.POINTER(_c.c_int64)]),
+    "cm_qcache_tree": (_c.c_int, [_P, _c.POINTER(cm_qcache_batch), _P, _P, _c.c_int32, _c.c_int32, _P, _P, _P]),
+    "cm_qk_rotate": (_c.c_int, [_P, _P, _P]),                              # the rows: byref or their bytes
+    "cm_qcache_attend_tree": (_c.c_int, [_P, _c.POINTER(cm_qcache), _c.c_int32, _c.POINTER(cm_qcache_batch), _P, _P,
+                                         _c.c_int32, _P, _c.c_int64, _P]),
+    "cm_tree_verify": (_c.c_int, [_P, _P, _P]),                            # the drafts: likewise
+    "cm_qcache_keep": (_c.c_int, [_P, _c.POINTER(cm_qcache), _c.POINTER(cm_qcache_batch), _P, _P, _P, _c.c_int32, _P, _P,
+                                  _c.c_int64, _P, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(lib, _name)
@@ -518,6 +546,32 @@ def cm_qcache_workspace(ctx: int, head_dim: int) -> int:
     out = ctypes.c_int64()
     _check(lib.cm_qcache_workspace(ctx, head_dim, ctypes.byref(out)))
     return out.value
+
+
+def cm_qcache_tree(ctx: int, batch: cm_qcache_batch, context_lens: int, parents: Optional[int], total_rows: int, words: int,
+                   mask: Optional[int], positions: Optional[int], stream=None) -> None:
+    _check(lib.cm_qcache_tree(ctx, ctypes.byref(batch), context_lens, parents, total_rows, words, mask, positions,
+                              _stream_handle(stream)))
+
+
+def cm_qk_rotate(ctx: int, rows: cm_qk_rows, stream=None) -> None:
+    _check(lib.cm_qk_rotate(ctx, ctypes.byref(rows), _stream_handle(stream)))
+
+
+def cm_qcache_attend_tree(ctx: int, cache: cm_qcache, layer: int, batch: cm_qcache_batch, query: cm_qcache_query, mask: int,
+                          words: int, workspace: int, workspace_bytes: int, stream=None) -> None:
+    _check(lib.cm_qcache_attend_tree(ctx, ctypes.byref(cache), layer, ctypes.byref(batch), ctypes.byref(query), mask, words,
+                                     workspace, workspace_bytes, _stream_handle(stream)))
+
+
+def cm_tree_verify(ctx: int, drafts: cm_tree_drafts, stream=None) -> None:
+    _check(lib.cm_tree_verify(ctx, ctypes.byref(drafts), _stream_handle(stream)))
+
+
+def cm_qcache_keep(ctx: int, cache: cm_qcache, batch: cm_qcache_batch, context_lens: int, path: int, kept: int, total_rows: int,
+                   lens_out: int, freed: int, max_freed: int, freed_count: int, stream=None) -> None:
+    _check(lib.cm_qcache_keep(ctx, ctypes.byref(cache), ctypes.byref(batch), context_lens, path, kept, total_rows, lens_out,
+                              freed, max_freed, freed_count, _stream_handle(stream)))
 
 
 # ---------------------------------------------------------------- torch-facing helpers

@@ -1,6 +1,6 @@
 """Builds libcm.so in-tree (next to this file) for sm_103a with nvcc and g++.
 
-Ten translation units compiled in parallel, then one shared-library link:
+Fifteen translation units compiled in parallel, then one shared-library link:
   csrc/cm_host.cpp       host core (g++, C++17, no floating-point contraction)
   csrc/blake2s_tree.cu   content-address kernels (nvcc, sm_103a)
   csrc/render.cu         render kernel (nvcc, sm_103a)
@@ -11,6 +11,11 @@ Ten translation units compiled in parallel, then one shared-library link:
   csrc/qcache_append.cu  rows into the 8-bit cache (nvcc, sm_103a)
   csrc/qcache_attention.cu  attention over the 8-bit cache, few rows per request (nvcc, sm_103a)
   csrc/qcache_prefill.cu    the same, many rows per request (nvcc, sm_103a)
+  csrc/cm_tree.cpp       trees of drafted tokens: argument checks and launches (g++)
+  csrc/tree_plan.cu      ancestor masks and positions (nvcc, sm_103a)
+  csrc/rotate.cu         norm and rotation of q and k (nvcc, sm_103a)
+  csrc/tree_verify.cu    drafted tokens against the target's probabilities (nvcc, sm_103a)
+  csrc/qcache_keep.cu    accepted rows to the front, blocks given back (nvcc, sm_103a)
 The CUDA runtime is linked statically into libcm.so and only the cm_* symbols
 are exported (csrc/libcm.map).
 
@@ -42,8 +47,9 @@ CXX_FLAGS = ["-std=c++17", "-O2", "-fPIC", "-ffp-contract=off", "-Wall", "-Wextr
              "-I" + INCLUDE, "-I" + CSRC]
 
 CUDA_SOURCES = ["blake2s_tree.cu", "render.cu", "dedup.cu", "readback.cu", "qcache_tables.cu",
-                "qcache_append.cu", "qcache_attention.cu", "qcache_prefill.cu"]
-CXX_SOURCES = ["cm_host.cpp", "cm_qcache.cpp"]
+                "qcache_append.cu", "qcache_attention.cu", "qcache_prefill.cu", "tree_plan.cu", "rotate.cu",
+                "tree_verify.cu", "qcache_keep.cu"]
+CXX_SOURCES = ["cm_host.cpp", "cm_qcache.cpp", "cm_tree.cpp"]
 
 
 def _cuda_home() -> str:

@@ -125,6 +125,7 @@ struct cm_context {
     int num_sms = 0;
     int leaf_blocks_per_sm = 0;   // leaf-hash blocks resident on one SM at once
     unsigned int *d_error = nullptr;   // set by a kernel whose bounded wait timed out
+    uint64_t *d_turns = nullptr;       // the rotation's angles for each head_dim (context_turns)
     std::mutex mu;
     // hashing scratch (device): leaf digests, inner levels, Q[t], compare flag
     uint8_t *d_scratch = nullptr;
@@ -1130,6 +1131,18 @@ void union_into(cm_set *dst, const cm_set *src) {
     }
 }
 
+// What a position adds to angle j of a head of d elements, theta^(-2j/d) / 2 pi turns, as the fraction of a turn in
+// units of 2^-64: for d = 16, 32, ... 512 one behind the other, those of d from entry d / 2 - 8 on.
+std::vector<uint64_t> turn_table(double theta) {
+    std::vector<uint64_t> turns;
+    for (int d = 16; d <= 512; d *= 2)
+        for (int j = 0; j < d / 2; ++j) {
+            const long double turn = std::pow((long double)theta, -(2.0L * j) / d) / 6.283185307179586476925286766559L;
+            turns.push_back((uint64_t)((turn - std::floor(turn)) * 0x1p64L));
+        }
+    return turns;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1178,6 +1191,9 @@ cm_status cm_context_create(int32_t device, double rope_theta, int32_t routing_l
         ctx->leaf_blocks_per_sm = cm::leaf_hash_blocks_per_sm();
         CM_CUDA_TRY(cudaMalloc(&ctx->d_error, sizeof(unsigned int)), "error word allocation");
         CM_CUDA_TRY(cudaMemset(ctx->d_error, 0, sizeof(unsigned int)), "error word reset");
+        const std::vector<uint64_t> turns = turn_table(rope_theta);
+        CM_CUDA_TRY(cudaMalloc(&ctx->d_turns, turns.size() * sizeof(uint64_t)), "angle table allocation");
+        CM_CUDA_TRY(cudaMemcpy(ctx->d_turns, turns.data(), turns.size() * sizeof(uint64_t), cudaMemcpyHostToDevice), "angle table");
         *out = ctx.release();
         return CM_OK;
     });
@@ -1192,6 +1208,7 @@ cm_status cm_context_destroy(cm_context *ctx) {
         if (ctx->d_scratch) cudaFree(ctx->d_scratch);
         if (ctx->h_pinned) cudaFreeHost(ctx->h_pinned);
         if (ctx->d_error) cudaFree(ctx->d_error);
+        if (ctx->d_turns) cudaFree(ctx->d_turns);
         if (ctx->side) cudaStreamDestroy(ctx->side);
         if (ctx->side_begin) cudaEventDestroy(ctx->side_begin);
         if (ctx->side_end) cudaEventDestroy(ctx->side_end);
@@ -1928,5 +1945,7 @@ int context_device(const cm_context *ctx) { return ctx->device; }
 int context_num_sms(const cm_context *ctx) { return ctx->num_sms; }
 
 unsigned int *context_error_word(const cm_context *ctx) { return ctx->d_error; }
+
+const uint64_t *context_turns(const cm_context *ctx, int head_dim) { return ctx->d_turns + head_dim / 2 - 8; }
 
 }  // namespace cm

@@ -5,119 +5,27 @@
 #include "cm_testing.h"
 
 #include <cmath>
-#include <exception>
-#include <string>
 
-#include <cuda_runtime.h>
-#include <nvtx3/nvToolsExt.h>
-
-#include "cm_hash_kernels.h"
-#include "cm_qcache_kernels.h"
-
-namespace cm {
-// cm_host.cpp
-int context_device(const cm_context *ctx);
-int context_num_sms(const cm_context *ctx);
-unsigned int *context_error_word(const cm_context *ctx);
-}  // namespace cm
+#include "cm_host_checks.h"
+#include "cm_tree_kernels.h"
 
 namespace {
 
-struct TraceRange {
-    explicit TraceRange(const char *name) { nvtxRangePushA(name); }
-    ~TraceRange() { nvtxRangePop(); }
+using namespace cm::checks;
+
+// What a call asks for besides causal or whole attention.
+struct Extras {
+    int32_t withhold;             // 0, or what the many-rows kernel is to wait for in vain (failure injection; that kernel
+                                  // then runs whatever the rows)
+    bool trees;                   // rows see their context and the rows that tree_mask names
+    const uint32_t *tree_mask;
+    int32_t tree_words;
 };
 
-cm_status fail(cm_status st, const char *msg) { return cm::report_error(st, msg); }
-
-bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-bool is_pow2(int64_t x) { return x > 0 && (x & (x - 1)) == 0; }
-
-int log2_of(int64_t x) {
-    int k = 0;
-    while (((int64_t)1 << k) < x) ++k;
-    return k;
-}
-
-// Makes ctx's device current for a launch and puts the caller's back.
-template <class F>
-cm_status on_device(const cm_context *ctx, const char *what, F &&launch) {
-    int before = 0;
-    const int device = cm::context_device(ctx);
-    cudaError_t e = cudaGetDevice(&before);
-    if (e == cudaSuccess && before != device) e = cudaSetDevice(device);
-    if (e == cudaSuccess) {
-        e = launch();
-        if (before != device) cudaSetDevice(before);
-    }
-    if (e == cudaSuccess) return CM_OK;
-    return fail(CM_ERR_CUDA, (std::string(what) + ": " + cudaGetErrorString(e)).c_str());
-}
-
-template <class F>
-cm_status guarded(F &&f) {
-    try {
-        return f();
-    } catch (const std::bad_alloc &) {
-        return fail(CM_ERR_OOM, "host allocation failed");
-    } catch (...) {
-        return fail(CM_ERR_INVALID_ARG, "unexpected internal error");
-    }
-}
-
-bool block_size_ok(int32_t b) { return is_pow2(b) && b >= 16 && b <= 256; }
-
-cm_status check_cache(const cm_qcache *c) {
-    if (!c) return fail(CM_ERR_INVALID_ARG, "cache descriptor is NULL");
-    if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales)
-        return fail(CM_ERR_INVALID_ARG, "a cache pointer is NULL");
-    if (c->format != CM_QCACHE_E4M3 && c->format != CM_QCACHE_INT8)
-        return fail(CM_ERR_INVALID_ARG, "unknown cache format");
-    if (c->num_layers < 1 || c->num_layers > 65535 || c->num_kv_heads < 1 || c->num_kv_heads > 65535)
-        return fail(CM_ERR_INVALID_ARG, "cache layers and kv heads must be in [1, 65535]");
-    if (!is_pow2(c->head_dim) || c->head_dim < 16 || c->head_dim > 512)
-        return fail(CM_ERR_INVALID_ARG, "head_dim must be a power of two in [16, 512]");
-    if (!block_size_ok(c->block_size))
-        return fail(CM_ERR_UNSUPPORTED, "block_size must be a power of two in [16, 256]");
-    if (c->num_blocks < 1 || c->num_blocks > INT32_MAX)
-        return fail(CM_ERR_INVALID_ARG, "num_blocks must be in [1, 2^31 - 1]");
-    if (c->reserved != 0) return fail(CM_ERR_INVALID_ARG, "reserved must be 0");
-    if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16))
-        return fail(CM_ERR_ALIGNMENT, "codes must be 16-byte aligned");
-    if (!aligned(c->k_scales, 4) || !aligned(c->v_scales, 4))
-        return fail(CM_ERR_ALIGNMENT, "scales must be 4-byte aligned");
-    for (int64_t s : {c->stride_block, c->stride_layer, c->stride_head, c->stride_token}) {
-        if (s < 1) return fail(CM_ERR_INVALID_ARG, "cache strides must be positive");
-        if (s % 16) return fail(CM_ERR_ALIGNMENT, "code strides must be multiples of 16 bytes");
-    }
-    if (c->stride_token < c->head_dim) return fail(CM_ERR_INVALID_ARG, "stride_token is below head_dim");
-    for (int64_t s : {c->scale_stride_block, c->scale_stride_layer, c->scale_stride_head})
-        if (s < 1) return fail(CM_ERR_INVALID_ARG, "scale strides must be positive");
-    return CM_OK;
-}
-
-cm_status check_batch(const cm_qcache_batch *b, int32_t most) {
-    if (!b) return fail(CM_ERR_INVALID_ARG, "batch descriptor is NULL");
-    if (b->num_requests < 0) return fail(CM_ERR_INVALID_ARG, "num_requests < 0");
-    if (b->num_requests > most) return fail(CM_ERR_UNSUPPORTED, "too many requests for one call");
-    if (!block_size_ok(b->block_size))
-        return fail(CM_ERR_UNSUPPORTED, "block_size must be a power of two in [16, 256]");
-    if (b->table_width < 0 || b->table_width > INT32_MAX)
-        return fail(CM_ERR_INVALID_ARG, "table_width must be in [0, 2^31 - 1]");
-    if (!b->row_starts || (b->num_requests > 0 && (!b->kv_lens || (b->table_width > 0 && !b->block_table))))
-        return fail(CM_ERR_INVALID_ARG, "a batch pointer is NULL");
-    if (!aligned(b->row_starts, 4) || !aligned(b->kv_lens, 4) || !aligned(b->block_table, 4))
-        return fail(CM_ERR_ALIGNMENT, "batch arrays must be 4-byte aligned");
-    return CM_OK;
-}
-
-// withhold: 0, or what the many-rows kernel is to wait for in vain (failure injection; that kernel then runs
-// whatever the rows).
 cm_status attend(cm_context *ctx, const cm_qcache *cache, int32_t layer, const cm_qcache_batch *batch,
                  const cm_qcache_query *query, void *workspace, int64_t workspace_bytes, cm_stream_t stream,
-                 int32_t withhold) {
-    TraceRange trace("cm_qcache_attend");
+                 const Extras &extras) {
+    TraceRange trace(extras.trees ? "cm_qcache_attend_tree" : "cm_qcache_attend");
     return guarded([&]() -> cm_status {
         if (!ctx) return fail(CM_ERR_INVALID_ARG, "context is NULL");
         cm_status st = check_cache(cache);
@@ -141,7 +49,11 @@ cm_status attend(cm_context *ctx, const cm_qcache *cache, int32_t layer, const c
             return fail(CM_ERR_INVALID_ARG, "total_rows < 0 or max_rows_per_request < 0");
         const float scale_log2 = query->softmax_scale * 1.44269504088896340736f;
         if (!std::isfinite(scale_log2)) return fail(CM_ERR_INVALID_ARG, "softmax_scale (times log2 e) is not finite");
+        if (extras.trees && (extras.tree_words < 1 || extras.tree_words > cm::kTreeMaxWords))
+            return fail(CM_ERR_INVALID_ARG, "a mask has 1 to 8 words a row");
         if (query->total_rows == 0 || batch->num_requests == 0) return CM_OK;
+        if (extras.trees && !extras.tree_mask) return fail(CM_ERR_INVALID_ARG, "mask is NULL");
+        if (!aligned(extras.tree_mask, 4)) return fail(CM_ERR_ALIGNMENT, "mask must be 4-byte aligned");
         if (!query->q || !query->out || !workspace) return fail(CM_ERR_INVALID_ARG, "q, out or workspace is NULL");
         if (!aligned(query->q, 16) || !aligned(query->out, 16) || !aligned(query->lse, 4) || !aligned(workspace, 16))
             return fail(CM_ERR_ALIGNMENT, "q, out and workspace must be 16-byte aligned");
@@ -190,15 +102,17 @@ cm_status attend(cm_context *ctx, const cm_qcache *cache, int32_t layer, const c
         p.head_dim = cache->head_dim;
         p.log2_block = log2_of(cache->block_size);
         p.total_rows = query->total_rows;
-        p.causal = query->causal != 0;
+        p.causal = query->causal != 0 && !extras.trees;
+        p.tree = extras.tree_mask;
+        p.tree_words = extras.tree_words;
         p.format = cache->format;
         p.error = cm::context_error_word(ctx);
-        p.withhold = withhold;
+        p.withhold = extras.withhold;
         cm::qcache_workspace_split(p, workspace, num_sms);
         const int64_t rows = (int64_t)(query->max_rows_per_request ? query->max_rows_per_request : query->total_rows) * group;
         return on_device(ctx, "attention launch", [&] {
             const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-            if (withhold) return cm::launch_qcache_prefill(p, num_sms, cm::context_device(ctx), s);
+            if (extras.withhold) return cm::launch_qcache_prefill(p, num_sms, cm::context_device(ctx), s);
             return cm::launch_qcache_attention(p, (int)(rows < INT32_MAX ? rows : INT32_MAX), num_sms,
                                                cm::context_device(ctx), s);
         });
@@ -314,7 +228,13 @@ cm_status cm_qcache_append(cm_context *ctx, const cm_qcache *cache, int32_t laye
 cm_status cm_qcache_attend(cm_context *ctx, const cm_qcache *cache, int32_t layer,
                            const cm_qcache_batch *batch, const cm_qcache_query *query, void *workspace,
                            int64_t workspace_bytes, cm_stream_t stream) {
-    return attend(ctx, cache, layer, batch, query, workspace, workspace_bytes, stream, 0);
+    return attend(ctx, cache, layer, batch, query, workspace, workspace_bytes, stream, Extras{});
+}
+
+cm_status cm_qcache_attend_tree(cm_context *ctx, const cm_qcache *cache, int32_t layer,
+                                const cm_qcache_batch *batch, const cm_qcache_query *query, const uint32_t *mask,
+                                int32_t words, void *workspace, int64_t workspace_bytes, cm_stream_t stream) {
+    return attend(ctx, cache, layer, batch, query, workspace, workspace_bytes, stream, Extras{0, true, mask, words});
 }
 
 cm_status cm_testing_qcache_attend_withheld(cm_context *ctx, const cm_qcache *cache, int32_t layer,
@@ -323,7 +243,7 @@ cm_status cm_testing_qcache_attend_withheld(cm_context *ctx, const cm_qcache *ca
                                             cm_stream_t stream) {
     if (what != cm::kQcacheWithholdQueries && what != cm::kQcacheWithholdEntries)
         return fail(CM_ERR_INVALID_ARG, "nothing that can be withheld");
-    return attend(ctx, cache, layer, batch, query, workspace, workspace_bytes, stream, what);
+    return attend(ctx, cache, layer, batch, query, workspace, workspace_bytes, stream, Extras{what, false, nullptr, 0});
 }
 
 cm_status cm_qcache_workspace(cm_context *ctx, int32_t head_dim, int64_t *out_bytes) {

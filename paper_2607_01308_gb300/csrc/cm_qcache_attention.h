@@ -176,6 +176,14 @@ __device__ __forceinline__ BlockEntry shuffle(const BlockEntry &e, int lane) {
             __shfl_sync(~0u, e.v_inverse, lane)};
 }
 
+// Trees. A row sees every token in front of its request's rows, and of those rows the ones whose bit is set in
+// its mask. 32 tokens from the one that is number j of the rows (negative: in front of them), one bit each:
+__device__ __forceinline__ uint32_t tree_window(const uint32_t *mask, int words, int j) {
+    const int w = j >> 5;
+    const uint32_t lo = w < 0 ? ~0u : w < words ? mask[w] : 0u, hi = w + 1 < 0 ? ~0u : w + 1 < words ? mask[w + 1] : 0u;
+    return __funnelshift_r(lo, hi, j & 31);
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t w;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));

@@ -76,6 +76,8 @@ struct QcacheAttentionParams {
     int32_t total_rows, causal, format;
     int32_t no_context;           // -1: context_lens is another array of that size, and no request was cut short; else 0
     int32_t withhold;             // prefill, failure injection: an arrival that does not come, in thread block 0
+    const uint32_t *tree;         // [total_rows][tree_words]; null: no trees. With them causal is 0
+    int32_t tree_words;
 };
 
 constexpr int kQcacheWithholdQueries = 1;   // of the query rows

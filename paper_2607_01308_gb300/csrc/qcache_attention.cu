@@ -101,7 +101,7 @@ struct Decode {
     }
 };
 
-template <int D, int FORMAT, int NT>
+template <int D, int FORMAT, int NT, bool TREE>
 __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
     decode_kernel(const __grid_constant__ QcacheAttentionParams p) {
     using C = Decode<D, FORMAT, NT>;
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
                 limit[nt][b] = __shfl_sync(~0u, lim, (2 * t + b) * 4);
             }
         }
-        least = __reduce_min_sync(~0u, least);
+        least = TREE ? min(least, w.first) : __reduce_min_sync(~0u, least);
 
         float o[D / 16][NT][4];
         float top[NT][2], sum[NT][2];
@@ -251,7 +251,17 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
                 s[nt][1] = fmaf(s[nt][1], f1, b.v_log2);
                 s[nt][2] = fmaf(s[nt][2], f0, b.v_log2);
                 s[nt][3] = fmaf(s[nt][3], f1, b.v_log2);
-                if (token + 16 > least) {
+                if (TREE && token + 16 > least) {
+                    // rare (the last tiles of a request), so that nothing of it is kept in registers
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int n = w.row_tile * C::kRows + nt * 8 + 2 * t + b;
+                        uint32_t seen = 0;
+                        if (n < w.rows) seen = tree_window(p.tree + (int64_t)(w.row0 + n / p.group) * p.tree_words, p.tree_words, token - w.first);
+                        if (!(seen >> g & 1) || token + g >= w.kv) s[nt][b] = -INFINITY;
+                        if (!(seen >> (g + 8) & 1) || token + g + 8 >= w.kv) s[nt][2 + b] = -INFINITY;
+                    }
+                } else if (token + 16 > least) {
                     if (token + g >= limit[nt][0]) s[nt][0] = -INFINITY;
                     if (token + g >= limit[nt][1]) s[nt][1] = -INFINITY;
                     if (token + g + 8 >= limit[nt][0]) s[nt][2] = -INFINITY;
@@ -379,19 +389,19 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
     }
 }
 
-template <int D, int FORMAT, int NT>
+template <int D, int FORMAT, int NT, bool TREE>
 cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream) {
     using C = Decode<D, FORMAT, NT>;
     static std::atomic<uint64_t> allowed{0};   // devices on which the shared memory limit is raised
     const size_t smem = C::kShared + ((size_t)p.requests + 1) * 4;
     // whatever this call needs: the limit without it covers the static bytes too
     if (device >= 64 || !(allowed.load() >> device & 1)) {
-        const cudaError_t e = cudaFuncSetAttribute(decode_kernel<D, FORMAT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        const cudaError_t e = cudaFuncSetAttribute(decode_kernel<D, FORMAT, NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                    (int)(C::kShared + (kQcacheMaxAttentionRequests + 1) * 4));
         if (e != cudaSuccess) return e;
         if (device < 64) allowed.fetch_or(1ull << device);
     }
-    return launch_behind(decode_kernel<D, FORMAT, NT>, dim3(num_sms * C::kBlocksPerSm), kThreads, smem, stream, p);
+    return launch_behind(decode_kernel<D, FORMAT, NT, TREE>, dim3(num_sms * C::kBlocksPerSm), kThreads, smem, stream, p);
 }
 
 }  // namespace
@@ -435,7 +445,8 @@ cudaError_t launch_qcache_attention(const QcacheAttentionParams &p, int rows_per
     if (rows_per_request > (p.head_dim == 256 ? 16 : 32)) return launch_qcache_prefill(p, num_sms, device, stream);
 #define CM_LAUNCH(D, F) \
     if (p.head_dim == D && p.format == F) \
-        return rows_per_request <= 8 ? launch<D, F, 1>(p, num_sms, device, stream) : launch<D, F, 2>(p, num_sms, device, stream);
+        return rows_per_request <= 8 ? p.tree ? launch<D, F, 1, true>(p, num_sms, device, stream) : launch<D, F, 1, false>(p, num_sms, device, stream) \
+               : p.tree ? launch<D, F, 2, true>(p, num_sms, device, stream) : launch<D, F, 2, false>(p, num_sms, device, stream);
     CM_EACH_DECODE(CM_LAUNCH)
 #undef CM_LAUNCH
     return cudaErrorInvalidValue;

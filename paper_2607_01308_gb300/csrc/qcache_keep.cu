@@ -1,0 +1,204 @@
+// The rows of an accepted path to the front of their request's new tokens, in every layer of an 8-bit paged
+// cache, and the blocks behind them.
+//
+// Request r holds c tokens in front of its new rows; path_i, ascending, is the i-th accepted one: token c + path_i becomes
+// token c + i. Rows in front of the first with path_i > i stay as they are. For each block that takes others, of
+// each layer and head, and for K and V on their own:
+//   scale' = max(the block's scale if tokens in front of the moved ones stay in it, the scales of the blocks they come from)
+//   code'  = code * (scale of its block / scale') to nearest even; as it is where the ratio is 1
+// so a value that moves is rounded once more at most, and not at all if the scales are alike.
+//
+// path_i >= i, so what a block takes comes from itself or from later blocks, and a warp that goes through one
+// (layer, head, K or V) of a request block by block, and reads 16 rows or so before it writes them, never reads what it
+// has written. A thread block looks up where a request's rows lie once, for several layers and heads. One more thread
+// block adds up the lengths and lists the blocks given back. Bound by the chain of dependent reads (lengths, path,
+// table, codes and scales): a step of a few accepted rows moves little.
+#include "cm_tree_kernels.h"
+
+#include "cm_qcache_codes.h"
+
+namespace cm {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kHeld = 4;                      // vectors of a lane that are read before they are written
+
+// What entry i of a request's path names: places of the row's present and new slot, negative if there are none.
+struct Place {
+    int block, at;                            // the token's block and its place in it
+};
+
+struct Request {
+    int first, n;                             // rows
+    int64_t context, kv;
+};
+
+__device__ __forceinline__ Request request(const QcacheKeepParams &p, int r) {
+    const RequestRows q = request_rows(p.row_starts, r, p.total_rows);
+    const int64_t cap = min(p.table_width << p.log2_block, (int64_t)INT32_MAX);
+    return {q.first, q.n, max(p.context_lens[r], 0), min((int64_t)max(p.kv_lens[r], 0), cap)};
+}
+
+__device__ __forceinline__ Place place(const QcacheKeepParams &p, int r, const Request &q, int64_t token) {
+    if (token >= q.kv) return {-1, 0};
+    const int b = p.block_table[r * p.table_width + (token >> p.log2_block)];
+    return {b >= 0 && b < p.num_blocks ? b : -1, (int)(token & ((1 << p.log2_block) - 1))};
+}
+
+// Whether path entry `now` (after `before`) is one more accepted row that the cache holds.
+__device__ __forceinline__ bool follows(const Request &q, int before, int now) { return now > before && now < q.n; }
+
+template <int FORMAT>
+__device__ __forceinline__ uint4 rescale(const uint4 &x, float ratio) {
+    if (ratio == 1.f) return x;
+    return make_uint4(shrink<FORMAT>(x.x, ratio), shrink<FORMAT>(x.y, ratio), shrink<FORMAT>(x.z, ratio), shrink<FORMAT>(x.w, ratio));
+}
+
+// One (layer, head) of K or V of a request by a warp.
+template <int FORMAT>
+__device__ __forceinline__ void move_rows(const QcacheKeepParams &p, int kv, int64_t layer, int64_t head, const Place *from, const Place *to,
+                                          int begin, int end) {
+    const int lane = threadIdx.x % 32;
+    const int log2_vecs = 31 - __clz(p.head_dim) - 4, row = lane >> log2_vecs, rows = 32 >> log2_vecs;
+    uint8_t *codes = p.codes[kv] + layer * p.stride_layer + head * p.stride_head + (lane & ((1 << log2_vecs) - 1)) * 16;
+    float *scales = p.scales[kv] + layer * p.scale_stride_layer + head * p.scale_stride_head;
+    auto code_at = [&](int block, int at) { return reinterpret_cast<uint4 *>(codes + block * p.stride_block + at * p.stride_token); };
+    for (int i0 = begin; i0 < end;) {
+        const Place first = to[i0];
+        const int i1 = min(end, i0 + (1 << p.log2_block) - first.at);
+        float *scale = scales + first.block * p.scale_stride_block;
+        // the first rows are on their way while the scales are looked at
+        uint4 x[kHeld];
+        float s[kHeld];
+        auto load = [&](int base) {
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) {
+                const int i = base + j * rows + row;
+                if (i < i1) {
+                    const Place f = from[i];
+                    x[j] = *code_at(f.block, f.at);
+                    s[j] = scales[f.block * p.scale_stride_block];
+                }
+            }
+        };
+        load(i0);
+        const float old = first.at ? *scale : 0.f;
+        float now = old;
+        for (int i = i0 + lane; i < i1; i += 32) now = fmaxf(now, scales[from[i].block * p.scale_stride_block]);
+#pragma unroll
+        for (int d = 16; d; d /= 2) now = fmaxf(now, __shfl_xor_sync(~0u, now, d));
+        for (int base = i0; base < i1; base += kHeld * rows) {
+            if (base != i0) load(base);
+            __syncwarp();                     // all of them are read before one is written over
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) {
+                const int i = base + j * rows + row;
+                if (i < i1) *code_at(first.block, first.at + i - i0) = rescale<FORMAT>(x[j], s[j] == now ? 1.f : __fdiv_rn(s[j], now));
+            }
+        }
+        if (first.at && now > old) {          // the tokens that stay in the block
+            const float ratio = __fdiv_rn(old, now);
+#pragma unroll 2
+            for (int t = row; t < first.at; t += rows) {
+                uint4 *at = code_at(first.block, t);
+                *at = rescale<FORMAT>(*at, ratio);
+            }
+        }
+        __syncwarp();                         // every lane has read the scales
+        if (lane == 0) *scale = now;
+        __syncwarp();
+        i0 = i1;
+    }
+}
+
+// The last thread block: new lengths, and the blocks that no token is left in, in the requests' order.
+__device__ __forceinline__ void count_blocks(const QcacheKeepParams &p) {
+    __shared__ int64_t warp_sum[kWarps];
+    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    int64_t total = 0;
+    for (int r0 = 0; r0 < p.requests; r0 += kThreads) {
+        const int r = r0 + tid;
+        int64_t begin = 0, n = 0;
+        if (r < p.requests) {
+            const Request q = request(p, r);
+            const int most = min(min(max(p.kept[r], 0), q.n), kTreeMaxNodes);
+            int kept = 0, before = -1;
+            for (; kept < most; ++kept) {
+                const int now = p.path[q.first + kept];
+                if (!follows(q, before, now) || place(p, r, q, q.context + now).block < 0 || place(p, r, q, q.context + kept).block < 0) break;
+                before = now;
+            }
+            const int64_t length = q.context + kept, mask = ((int64_t)1 << p.log2_block) - 1;
+            p.lens_out[r] = (int32_t)min(length, (int64_t)INT32_MAX);
+            begin = (length + mask) >> p.log2_block;
+            n = max(((q.kv + mask) >> p.log2_block) - begin, (int64_t)0);
+        }
+        int64_t upto = n;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int64_t x = __shfl_up_sync(~0u, upto, d);
+            if (lane >= d) upto += x;
+        }
+        if (lane == 31) warp_sum[warp] = upto;
+        __syncthreads();
+        int64_t at = total + upto - n;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) at += warp_sum[w];
+            total += warp_sum[w];
+        }
+        for (int64_t j = 0; j < n && at + j < p.max_freed; ++j) p.freed[at + j] = p.block_table[r * p.table_width + begin + j];
+        __syncthreads();
+    }
+    for (int64_t j = total + tid; j < p.max_freed; j += kThreads) p.freed[j] = -1;
+    if (tid == 0) *p.freed_count = total;
+}
+
+template <int FORMAT>
+__global__ void __launch_bounds__(kThreads) keep_kernel(const __grid_constant__ QcacheKeepParams p) {
+    __shared__ Place from[kTreeMaxNodes], to[kTreeMaxNodes];
+    __shared__ int first_moved, first_wrong;
+    after_kernels_before();
+    const int r = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
+    if (r == p.requests) {
+        count_blocks(p);
+        return;
+    }
+    if (threadIdx.x == 0) first_moved = first_wrong = kTreeMaxNodes;
+    __syncthreads();
+    const Request q = request(p, r);
+    const int most = min(min(max(p.kept[r], 0), q.n), kTreeMaxNodes);
+    for (int i = threadIdx.x; i < most; i += kThreads) {
+        const int now = p.path[q.first + i], before = i ? p.path[q.first + i - 1] : -1;
+        Place f{-1, 0}, t{-1, 0};
+        if (follows(q, before, now)) {
+            f = place(p, r, q, q.context + now);
+            t = place(p, r, q, q.context + i);
+        }
+        from[i] = f;
+        to[i] = t;
+        if (f.block < 0 || t.block < 0) atomicMin(&first_wrong, i);
+        if (now != i) atomicMin(&first_moved, i);
+    }
+    __syncthreads();
+    const int begin = first_moved, end = min(most, first_wrong);
+    if (begin >= end) return;
+    const int tasks = p.layers * p.heads * 2;
+    for (int task = chunk * kWarps + threadIdx.x / 32; task < tasks; task += p.chunks * kWarps) {
+        const int which = task & 1, at = task >> 1;
+        move_rows<FORMAT>(p, which, at / p.heads, at % p.heads, from, to, begin, end);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_qcache_keep(QcacheKeepParams p, int num_sms, cudaStream_t stream) {
+    const int64_t warps = ((int64_t)p.layers * p.heads * 2 + kWarps - 1) / kWarps;      // thread blocks of one task a warp
+    const int64_t fair = p.requests ? (8ll * num_sms + p.requests - 1) / p.requests : 1;
+    p.chunks = (int)(warps < fair ? warps : fair);
+    const dim3 grid((unsigned)(p.requests * p.chunks + 1));
+    return p.format == CM_QCACHE_E4M3 ? launch_behind(keep_kernel<CM_QCACHE_E4M3>, grid, kThreads, 0, stream, p)
+                                      : launch_behind(keep_kernel<CM_QCACHE_INT8>, grid, kThreads, 0, stream, p);
+}
+
+}  // namespace cm

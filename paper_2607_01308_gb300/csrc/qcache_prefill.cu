@@ -258,12 +258,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // A kv tile of one row: scores x to weights w (fp16 pairs). left: columns that the row sees (only if
-// `masked`, which is the warp's). Where the largest exponent of some row passes its limit, that row's maximum is
+// `masked`, which is the warp's), of these, with trees, the ones in the row's mask, from bit tree_at on (no mask: all). Where the largest exponent of some row passes its limit, that row's maximum is
 // raised by as much, its sum and, unless this is the first tile (behind `wait_output`), its output rescaled.
-template <int D, class Wait, class Store>
+template <int D, bool TREE, class Wait, class Store>
 __device__ __forceinline__ void softmax_tile(uint32_t (&x)[2][32], uint32_t (&w)[2][16], uint32_t o_at, const float4 *scale,
-                                             const float4 &inverse, float factor, bool masked, int left, bool first, RowState &r,
-                                             Wait wait_output, Store store) {
+                                             const float4 &inverse, float factor, bool masked, int left, const uint32_t *tree,
+                                             int tree_words, int tree_at, bool first, RowState &r, Wait wait_output, Store store) {
     const float base = kHeadroom - r.top;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
@@ -278,7 +278,17 @@ __device__ __forceinline__ void softmax_tile(uint32_t (&x)[2][32], uint32_t (&w)
             x[c][k + 1] = __float_as_uint(e1);
         }
     }
-    if (masked) {
+    if (TREE && masked) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int n = min(max(left - 32 * c, 0), 32);         // columns with tokens
+            uint32_t seen = tree ? tree_window(tree, tree_words, tree_at + 32 * c) : ~0u;
+            if (n < 32) seen &= (1u << n) - 1;
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+                if (!(seen >> k & 1)) x[c][k] = 0xff800000u;
+        }
+    } else if (masked) {
 #pragma unroll
         for (int k = 0; k < kTile; ++k)
             if (k >= left) x[k / 32][k % 32] = 0xff800000u;
@@ -487,7 +497,7 @@ struct Barriers {
     uint64_t drained[2];                      // all that an issuing warp has issued is done
 };
 
-template <int D, int FORMAT>
+template <int D, int FORMAT, bool TREE>
 __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_constant__ QcacheAttentionParams p) {
     using C = Shape<D>;
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -637,7 +647,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
 
             // a row that is not there sees everything, so that no tile is masked for its sake
             const int limit = !valid ? INT32_MAX : p.causal ? min(w.kv, max(0, w.first + (int)(token - w.row0) + 1)) : w.kv;
-            const int least = __reduce_min_sync(~0u, limit);      // of the warp's rows
+            const int least = TREE ? min(w.kv, w.first) : __reduce_min_sync(~0u, limit);   // of the warp's rows
+            const uint32_t *tree = TREE && valid ? p.tree + token * p.tree_words : nullptr;
             RowState r{0.f, 0.f, -INFINITY};
             const int t0 = w.t0, t1 = w.t1;
             for (int t = t0; t < t1; ++t, ++n_tile) {
@@ -651,8 +662,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 tmem_ld(x[0], tile);
                 ld_wait(x[0]);
                 tmem_ld(x[1], tile + 32);                         // on its way while the first half is scaled
-                softmax_tile<D>(x, y, o_at, reinterpret_cast<const float4 *>(entry.scale), *reinterpret_cast<const float4 *>(entry.v_inverse),
-                                factor, (t + 1) * kTile > least, limit - t * kTile, t == t0, r,
+                softmax_tile<D, TREE>(x, y, o_at, reinterpret_cast<const float4 *>(entry.scale), *reinterpret_cast<const float4 *>(entry.v_inverse),
+                                factor, (t + 1) * kTile > least, limit - t * kTile, tree, p.tree_words, t * kTile - w.first, t == t0, r,
                                 // the tile before is in the output when the next tile's scores are there, which came after it
                                 [&] {
                                     if (t + 1 < t1) wait.warp(&bars.s_full[qt][buffer ^ 1], scored.peek(buffer ^ 1));
@@ -976,18 +987,18 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     for (int v = 0; v < kVecs; ++v) write_row(p, w, z.row_tile * C::kRows + row, (column + v * kColumns) * 4, acc[v], m, l, kHeadroom);
 }
 
-template <int D, int FORMAT>
+template <int D, int FORMAT, bool TREE>
 cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream) {
     using C = Shape<D>;
     // more than half of an SM's shared memory: one block per SM, which holds all of its tensor memory
     const size_t smem = C::kSmem > 120 * 1024 ? C::kSmem : 120 * 1024;
     static std::atomic<uint64_t> allowed{0};   // devices on which the shared memory limit is raised
     if (device >= 64 || !(allowed.load() >> device & 1)) {
-        const cudaError_t e = cudaFuncSetAttribute(prefill_kernel<D, FORMAT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = cudaFuncSetAttribute(prefill_kernel<D, FORMAT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         if (device < 64) allowed.fetch_or(1ull << device);
     }
-    const cudaError_t e = launch_behind(prefill_kernel<D, FORMAT>, dim3(num_sms), kThreads, smem, stream, p);
+    const cudaError_t e = launch_behind(prefill_kernel<D, FORMAT, TREE>, dim3(num_sms), kThreads, smem, stream, p);
     return e != cudaSuccess ? e : launch_behind(join_kernel<D>, dim3(num_sms, 16), kJoinThreads, 0, stream, p);
 }
 
@@ -997,9 +1008,12 @@ size_t qcache_prefill_part_rows(int head_dim) { return head_dim == 256 ? 128 : 2
 
 cudaError_t launch_qcache_prefill(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream) {
 #define CM_LAUNCH(D) \
-    if (p.head_dim == D) \
-        return p.format == CM_QCACHE_E4M3 ? launch<D, CM_QCACHE_E4M3>(p, num_sms, device, stream) \
-                                          : launch<D, CM_QCACHE_INT8>(p, num_sms, device, stream);
+    if (p.head_dim == D) { \
+        if (p.tree) return p.format == CM_QCACHE_E4M3 ? launch<D, CM_QCACHE_E4M3, true>(p, num_sms, device, stream) \
+                                                      : launch<D, CM_QCACHE_INT8, true>(p, num_sms, device, stream); \
+        return p.format == CM_QCACHE_E4M3 ? launch<D, CM_QCACHE_E4M3, false>(p, num_sms, device, stream) \
+                                          : launch<D, CM_QCACHE_INT8, false>(p, num_sms, device, stream); \
+    }
     CM_LAUNCH(32) CM_LAUNCH(64) CM_LAUNCH(128) CM_LAUNCH(256)
 #undef CM_LAUNCH
     return cudaErrorInvalidValue;

@@ -220,10 +220,12 @@ class QCache:
                                     s[0], s[1], s[2], slot_map.data_ptr() or None, slot_map.numel(), _stream_handle(stream)))
 
     def attend(self, q, batch: QBatch, layer: int = 0, out=None, lse=None, softmax_scale: Optional[float] = None,
-               causal: bool = True, stream=None) -> Tuple[object, object]:
+               causal: bool = True, stream=None, tree=None) -> Tuple[object, object]:
         """(out, lse): softmax(softmax_scale * q K^T) V for the batch's rows, each over its own request's
         cached tokens. q, out: bf16 [rows, q_heads, head_dim] (q_heads a multiple of kv_heads, head_dim
-        contiguous); lse: fp32 [rows, q_heads] or None to leave it out; out is made if not given, on `stream`."""
+        contiguous); lse: fp32 [rows, q_heads] or None to leave it out; out is made if not given, on `stream`.
+        With a tree (QTree) a row sees the tokens in front of its request's rows and the rows in its mask, whatever
+        `causal` says."""
         shape, bf16, device = q.shape, self._bf16, self._device
         if q.dtype is not bf16 or len(shape) != 3 or shape[2] != self._dim or q.stride(2) != 1 or q.get_device() != device:
             raise ValueError("q must be bf16 [rows, q_heads, head_dim] on the context's device, head_dim contiguous")
@@ -240,6 +242,28 @@ class QCache:
         query = _pack_query(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), qs[0], qs[1], os[0], os[1],
                             shape[0], shape[1], batch.max_new or 0, 1 if causal else 0,
                             self._scale if softmax_scale is None else softmax_scale, CM_QCACHE_CONTEXT_LENS, batch._context)
-        _check(lib.cm_qcache_attend(self.ctx.handle, self._ref, layer, batch._ref, query,
-                                    batch._workspace_ptr, batch._workspace_bytes, batch._on(stream)))
+        if tree is None:
+            _check(lib.cm_qcache_attend(self.ctx.handle, self._ref, layer, batch._ref, query,
+                                        batch._workspace_ptr, batch._workspace_bytes, batch._on(stream)))
+            return out, lse
+        if tree._device != device or tree._max_rows < shape[0]:
+            raise ValueError("the tree must be on the cache's device and have a mask for every row")
+        tree._on(stream)
+        _check(lib.cm_qcache_attend_tree(self.ctx.handle, self._ref, layer, batch._ref, query, tree._mask_ptr, tree._words,
+                                         batch._workspace_ptr, batch._workspace_bytes, batch._on(stream)))
         return out, lse
+
+    def keep(self, batch: QBatch, tree, context_lens, stream=None) -> None:
+        """The rows that tree.path and tree.kept name to the front of their requests' rows, in every layer; tree.lens,
+        tree.freed and tree.freed_count are written: the tokens that each request holds now, the blocks that none is left in, and
+        their number. context_lens: as schedule() took them (int32 CUDA tensor [R], not tree.lens itself)."""
+        n, device = batch._num_requests, self._device
+        if (context_lens.dtype is not batch._int32 or context_lens.dim() != 1 or not context_lens.is_contiguous() or
+                context_lens.numel() != n or context_lens.get_device() != device):
+            raise ValueError("context_lens must be a contiguous int32 vector with a length for each request, on the context's device")
+        if batch._device != device or tree._device != device or tree._num_requests != n:
+            raise ValueError("batch and tree must be on the cache's device and have the same requests")
+        tree._on(stream)
+        _check(lib.cm_qcache_keep(self.ctx.handle, self._ref, batch._ref, context_lens.data_ptr() or None, tree._path_ptr,
+                                  tree._kept_ptr, tree._max_rows, tree._lens_ptr, tree._freed_ptr, tree._max_freed,
+                                  tree._count_ptr, batch._on(stream)))

@@ -1,0 +1,157 @@
+"""Torch-facing side of the operators around a tree of drafted tokens (cm_qcache_tree, cm_qk_rotate and
+cm_tree_verify of include/cm.h): argument checks and marshalling only, in few interpreter steps, as in qcache.py."""
+from __future__ import annotations
+
+import struct
+from typing import Optional, Tuple
+
+from ._binding import CM_PROB_BF16, CM_PROB_F32, Context, _check, _stream_handle, lib
+from .qcache import QBatch, _fixed, _new_on, _require, _strides
+
+_pack_rows = struct.Struct("@PPPPPPPqqqqqqqqqiiifi4x").pack      # a cm_qk_rows in one step
+_pack_drafts = struct.Struct("@PPPPPPPPPPqqiiiii4x").pack        # a cm_tree_drafts
+
+
+class QTree:
+    """Trees of drafted tokens, one for each request of a batch: what is known of their rows, on the GPU.
+
+      mask [max_rows, words] int32 (bit j: row j of the request is the row or an ancestor) and positions [max_rows]
+      int32: written by plan()
+      path [max_rows], kept [R], next_token [R] int32: written by verify(), the accepted rows of each request, from
+      its first row's place on, their number and the token behind them
+      lens [R] int32, freed [max_freed] int32, freed_count [1] int64: written by QCache.keep(), the tokens that
+      each request holds then, the blocks that none is left in (-1 behind the last) and their number
+
+    max_nodes: the most rows of one request, to 256; rows behind it are seen by none and never accepted. A program with masks or
+    paths of its own writes into these tensors instead. One tree is used by one stream at a time; its memory is
+    given back as a QBatch's is."""
+
+    mask, positions, path, kept = _fixed("_mask"), _fixed("_positions"), _fixed("_path"), _fixed("_kept")
+    next_token, lens = _fixed("_next_token"), _fixed("_lens")
+    freed, freed_count = _fixed("_freed"), _fixed("_freed_count")
+
+    def __init__(self, batch: QBatch, max_nodes: int):
+        import torch
+        _require(1 <= max_nodes <= 256, "max_nodes must be in [1, 256]")
+        dev = batch.row_starts.device
+        rows, n = batch.slot_map.numel(), batch._num_requests
+        self.batch, self.ctx = batch, batch.ctx
+        self.max_nodes = max_nodes
+        self._device, self._max_rows, self._num_requests = batch._device, rows, n
+        self._words, self._max_freed = (max_nodes + 31) // 32, n + rows // batch._c.block_size
+        self._int32, self._fp32, self._bf16 = torch.int32, torch.float32, torch.bfloat16
+
+        def whole(*shape, fill=-1, dtype=torch.int32):
+            return torch.full(shape, fill, dtype=dtype, device=dev)
+
+        self._mask, self._positions = whole(rows, self._words, fill=0), whole(rows, fill=0)
+        self._path, self._kept, self._next_token = whole(rows), whole(n, fill=0), whole(n)
+        self._lens, self._freed, self._freed_count = whole(n, fill=0), whole(self._max_freed), whole(1, fill=0, dtype=torch.int64)
+        self._mask_ptr, self._positions_ptr = self._mask.data_ptr() or None, self._positions.data_ptr() or None
+        self._path_ptr, self._kept_ptr, self._next_ptr = self._path.data_ptr() or None, self._kept.data_ptr() or None, self._next_token.data_ptr() or None
+        self._lens_ptr, self._freed_ptr, self._count_ptr = self._lens.data_ptr() or None, self._freed.data_ptr() or None, self._freed_count.data_ptr()
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(dev).synchronize()      # set on every stream
+        self._streams = {_stream_handle(torch.cuda.current_stream(dev))}
+
+    def _on(self, stream) -> Optional[int]:
+        """The stream's handle; the first time, its use of the tree's memory is made known to torch."""
+        handle = _stream_handle(stream)
+        if handle not in self._streams and not isinstance(stream, int):
+            import torch
+            stream = stream or torch.cuda.current_stream(self._device)
+            for t in (self._mask, self._positions, self._path, self._kept, self._next_token, self._lens, self._freed, self._freed_count):
+                t.record_stream(stream)
+            self._streams.add(handle)
+        return handle
+
+    def _vector(self, t, dtype, n, what: str):
+        if t.dtype is not dtype or t.dim() != 1 or not t.is_contiguous() or t.numel() != n or t.get_device() != self._device:
+            raise ValueError(what)
+        return t.data_ptr() or None
+
+    def plan(self, parents, context_lens, stream=None) -> "QTree":
+        """mask and positions from the rows' parents (int32 CUDA tensor [rows], at most as many as the batch has; the
+        place of each row's parent among its request's rows, -1 for none) and the tokens in front of each request's rows
+        (int32 [R]). parents None: every row follows the one before it."""
+        rows = self._max_rows
+        if parents is not None:
+            rows = parents.numel()
+            _require(rows <= self._max_rows, "more parents than the batch has rows")
+            parents = self._vector(parents, self._int32, rows, "parents must be a contiguous int32 vector on the context's device")
+        context = self._vector(context_lens, self._int32, self._num_requests,
+                               "context_lens must be a contiguous int32 vector with a length for each request, on the context's device")
+        self.batch._on(stream)
+        _check(lib.cm_qcache_tree(self.ctx.handle, self.batch._ref, context, parents, rows, self._words, self._mask_ptr,
+                                  self._positions_ptr, self._on(stream)))
+        return self
+
+    def verify(self, parents, tokens, target, accept, sample, draft=None, stream=None) -> "QTree":
+        """path, kept and next_token from the drafted tokens (int32 [rows]), the target's probabilities of what follows each row,
+        those that the rows behind it were drawn from (target, draft: fp32 or bf16 [rows, vocab], vocab contiguous; draft
+        None: drafted without chance) and uniform random numbers of [0, 1): accept [rows], sample [R] (fp32). What is
+        accepted and chosen is distributed as the target's own tokens are."""
+        rows, shape, dtype, device = parents.numel(), target.shape, target.dtype, self._device
+        _require(rows <= self._max_rows, "more parents than the batch has rows")
+        if (dtype is not self._fp32 and dtype is not self._bf16) or len(shape) != 2 or shape[0] < rows or target.get_device() != device:
+            raise ValueError("target must be fp32 or bf16 [rows, vocab] on the context's device")
+        if draft is not None and (draft.dtype is not dtype or draft.shape != shape or draft.get_device() != device):
+            raise ValueError("draft must be like target")
+        if shape[1] > 1 and (target.stride(1) != 1 or (draft is not None and draft.stride(1) != 1)):
+            raise ValueError("the vocabulary must be contiguous")
+        what = "parents and tokens (int32), accept (fp32) must be contiguous vectors of the same size, sample (fp32) one with a number for each request, on the context's device"
+        int32, fp32 = self._int32, self._fp32
+        parents, tokens = self._vector(parents, int32, rows, what), self._vector(tokens, int32, rows, what)
+        accept, sample = self._vector(accept, fp32, rows, what), self._vector(sample, fp32, self._num_requests, what)
+        batch = self.batch
+        drafts = _pack_drafts(batch._c.row_starts, parents or 0, tokens or 0, target.data_ptr(), 0 if draft is None else draft.data_ptr(), accept or 0,
+                              sample or 0, self._path_ptr or 0, self._kept_ptr or 0, self._next_ptr or 0, target.stride(0),
+                              0 if draft is None else draft.stride(0), self._num_requests, rows, shape[1], self.max_nodes,
+                              CM_PROB_F32 if dtype is fp32 else CM_PROB_BF16)
+        batch._on(stream)
+        _check(lib.cm_tree_verify(self.ctx.handle, drafts, self._on(stream)))
+        return self
+
+
+def rotate_qk(ctx: Context, q, k, positions, q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None, k_out=None,
+              stream=None) -> Tuple[object, object]:
+    """(q_out, k_out): every head's row of q and k (bf16 CUDA tensors [rows, heads, head_dim], head_dim contiguous; views of a
+    fused projection, say), normed (x / sqrt(mean x^2 + eps) * weight; a weight of None: not) and rotated to
+    positions [rows] (int32), as the keys of a fragment are, with the context's rope_theta. Either of q and k may be None. q_out
+    and k_out are made if not given, on `stream`; they may be q and k themselves."""
+    import torch
+    bf16, device = torch.bfloat16, ctx.device
+    like = q if q is not None else k
+    _require(like is not None, "q or k must be given")
+    rows, d = like.shape[0], like.shape[-1]
+    if positions.dtype is not torch.int32 or positions.dim() != 1 or not positions.is_contiguous() or positions.numel() != rows or positions.get_device() != device:
+        raise ValueError("positions must be a contiguous int32 vector with one for each row, on the context's device")
+    pointers, strides, heads, outs = [], [], [], []
+    for x, out, weight in ((q, q_out, q_weight), (k, k_out, k_weight)):
+        if x is None:
+            _require(out is None and weight is None, "an output or a weight without its rows")
+            pointers.append((0, 0, 0))
+            strides.append((0, 0, 0, 0))
+            heads.append(0)
+            outs.append(None)
+            continue
+        shape = x.shape
+        if x.dtype is not bf16 or len(shape) != 3 or shape[0] != rows or shape[2] != d or x.stride(2) != 1 or x.get_device() != device:
+            raise ValueError("q and k must be bf16 [rows, heads, head_dim] of the same rows and head_dim, contiguous in it, on the context's device")
+        if out is None:
+            out = _new_on(stream, x)
+        elif out.dtype is not bf16 or out.shape != shape or out.stride(2) != 1 or out.get_device() != device:
+            raise ValueError("q_out and k_out must be like q and k")
+        if weight is not None and (weight.dtype is not bf16 or weight.dim() != 1 or weight.numel() != d or not weight.is_contiguous() or
+                                   weight.get_device() != device):
+            raise ValueError("weights must be contiguous bf16 [head_dim] on the context's device")
+        pointers.append((x.data_ptr(), out.data_ptr(), 0 if weight is None else weight.data_ptr()))
+        strides.append(_strides(x, 2, 8) + _strides(out, 2, 8))
+        heads.append(shape[1])
+        outs.append(out)
+    (qp, qo, qw), (kp, ko, kw) = pointers
+    qs, ks = strides
+    desc = _pack_rows(qp, kp, qo, ko, qw, kw, positions.data_ptr(), qs[0], qs[1], ks[0], ks[1], qs[2], qs[3], ks[2], ks[3], rows,
+                      heads[0], heads[1], d, eps, 0)
+    _check(lib.cm_qk_rotate(ctx.handle, desc, _stream_handle(stream)))
+    return outs[0], outs[1]
