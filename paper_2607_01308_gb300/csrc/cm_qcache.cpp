@@ -112,7 +112,7 @@ cm_status attend(cm_context *ctx, const cm_qcache *cache, int32_t layer, const c
         const int64_t rows = (int64_t)(query->max_rows_per_request ? query->max_rows_per_request : query->total_rows) * group;
         return on_device(ctx, "attention launch", [&] {
             const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-            if (extras.withhold) return cm::launch_qcache_prefill(p, num_sms, cm::context_device(ctx), s);
+            if (extras.withhold) return cm::launch_qcache_prefill(p, INT32_MAX, num_sms, cm::context_device(ctx), s);
             return cm::launch_qcache_attention(p, (int)(rows < INT32_MAX ? rows : INT32_MAX), num_sms,
                                                cm::context_device(ctx), s);
         });

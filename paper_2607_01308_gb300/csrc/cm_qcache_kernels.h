@@ -93,7 +93,7 @@ void qcache_workspace_split(QcacheAttentionParams &p, void *workspace, int num_s
 cudaError_t launch_qcache_attention(const QcacheAttentionParams &p, int rows_per_request, int num_sms, int device,
                                     cudaStream_t stream);
 // The kernel for more rows per request, and the part rows of one of its thread blocks.
-cudaError_t launch_qcache_prefill(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream);
+cudaError_t launch_qcache_prefill(const QcacheAttentionParams &p, int rows_per_request, int num_sms, int device, cudaStream_t stream);
 size_t qcache_prefill_part_rows(int head_dim);
 
 #ifdef __CUDACC__

@@ -442,7 +442,10 @@ cudaError_t launch_qcache_attention(const QcacheAttentionParams &p, int rows_per
     //   head_dim 64 int8    8 rows 33 us, as two fragments 40; 32 rows 72 us, by the other kernel 90
     //   head_dim 32 e4m3    32 rows 50 us, by the other kernel 83
     //   head_dim 256 e4m3   (16 requests, 4 kv heads) 32 rows 59 us, by the other kernel 48
-    if (rows_per_request > (p.head_dim == 256 ? 16 : 32)) return launch_qcache_prefill(p, num_sms, device, stream);
+    // Trees, whose other kernel has two streams for up to 128 rows:
+    //   head_dim 128 e4m3   32 rows 103 us, by the other kernel 95; int8 115 and 99
+    //   head_dim 64 e4m3    32 rows 69 us, by the other kernel 71; head_dim 32 53 and 66
+    if (rows_per_request > (p.head_dim == 256 || (p.tree && p.head_dim == 128) ? 16 : 32)) return launch_qcache_prefill(p, rows_per_request, num_sms, device, stream);
 #define CM_LAUNCH(D, F) \
     if (p.head_dim == D && p.format == F) \
         return rows_per_request <= 8 ? p.tree ? launch<D, F, 1, true>(p, num_sms, device, stream) : launch<D, F, 1, false>(p, num_sms, device, stream) \

@@ -47,18 +47,23 @@ constexpr float kRaise = 8.f, kHeadroom = 7.f;
 
 constexpr int kTile = 64;                   // tokens of a kv tile
 constexpr int kBlocks = kTile / 16;         // its scale entries
-constexpr int kEntryTiles = 32 / kBlocks, kEntryStages = 2 * kEntryTiles;   // tiles looked up at a time; held
+constexpr int kEntryTiles = 32 / kBlocks;   // looked up at a time
+constexpr int kMostEntryGroups = 4;         // of so many tiles that are held
 
-template <int D>
+template <int D, int QT = D == 256 ? 1 : 2>
 struct Shape {
     // tensor memory, 512 columns: two buffers of scores for each query tile, and the outputs
-    static constexpr int kQTiles = D == 256 ? 1 : 2;
+    static constexpr int kQTiles = QT;
+    // One query tile leaves room for a second stream: the two halves of the softmax warps take the kv tiles in turn, each with
+    // scores, maximum, sum and output of its own, and the two outputs are joined when a segment ends.
+    static constexpr int kStreams = QT == 1 && D < 256 ? 2 : 1;
+    static constexpr int kLanes = kQTiles * kStreams;             // halves of the softmax warps that have work
     // Warps that issue: one for each query tile at head_dim 128, where one for both waits for the weights of one
     // tile while those of the other are there (2,048 tokens over 16,384: 467 us against 520); below, where the
     // products are short, one (head_dim 64: 433 us against 461), which keeps the two tiles' softmax apart.
-    static constexpr int kIssuers = D == 128 ? 2 : 1;
+    static constexpr int kIssuers = (D == 128 && kQTiles == 2) || kStreams == 2 ? 2 : 1;
     static constexpr int kRows = 128 * kQTiles;
-    static constexpr int kOColumn = kQTiles * 2 * kTile;
+    static constexpr int kOColumn = kLanes * 2 * kTile;
     static constexpr int kSetup = 4;                          // a segment's queries and its end, in tiles: 8,700 to 11,000 cycles
     static constexpr int kPanels = D < 64 ? 1 : D / 64;       // 64 columns (128 bytes) of fp16 each
     static constexpr int kStages = D == 256 ? 2 : 4;          // tiles of K, of V
@@ -66,14 +71,19 @@ struct Shape {
     static constexpr int kQBytes = kQTiles * kPanels * kQPanel;
     static constexpr int kKvBytes = kPanels * kKvPanel;       // a tile of K, of V
     static constexpr int kChunks = kTile * D / 16 / kLoadThreads;   // 16-code loads of a thread for a tile
+    static constexpr int kBehind = 2 * kStreams;                  // V tiles behind the K tiles of their steps
+    // Lookups that are held: with two streams the loads are some eight tiles ahead of the products, and with two groups they
+    // waited 1,400 cycles of every four tiles for a lookup.
+    static constexpr int kEntryGroups = kStreams == 2 ? 4 : 2, kEntryStages = kEntryGroups * kEntryTiles;
+    static constexpr int kTileWarps = D == 128 ? 2 : 1;           // that load a tile of K, of V, with two streams
     static constexpr size_t kSmem = kQBytes + 2 * kStages * kKvBytes;
     // registers of the softmax, the converting and the issuing warps; where the second half of the softmax
     // warps has no tile, the converting ones have its
-    static constexpr int kSoftmaxRegs = 120, kIdleRegs = 32, kLoadRegs = kQTiles == 1 ? 128 : 88, kIssueRegs = 64;
-    static_assert(128 * kSoftmaxRegs + 128 * (kQTiles == 1 ? kIdleRegs : kSoftmaxRegs) + 256 * kLoadRegs + 128 * kIssueRegs <=
+    static constexpr int kSoftmaxRegs = 120, kIdleRegs = 32, kLoadRegs = kLanes == 1 ? 128 : 88, kIssueRegs = 64;
+    static_assert(128 * kSoftmaxRegs + 128 * (kLanes == 1 ? kIdleRegs : kSoftmaxRegs) + 256 * kLoadRegs + 128 * kIssueRegs <=
                       kThreads * kLaunchRegs, "registers at launch");
     static_assert(kChunks >= 1, "every load thread has work");
-    static_assert(kOColumn + kQTiles * D <= 512, "tensor memory");
+    static_assert(kOColumn + kLanes * D <= 512, "tensor memory");
 };
 
 // ---------------------------------------------------------------- barriers, bounded
@@ -389,11 +399,11 @@ __device__ __forceinline__ float load_queries(const QcacheAttentionParams &p, co
 
 // The warp's 32 rows of 16-byte chunks, placed as load_queries places them, to their rows in global memory
 // (`row`: this lane's; null: none).
-template <int D>
-__device__ __forceinline__ void store_rows(uint16_t *row, const unsigned char *tile) {
+template <int D, int COLUMNS = D>
+__device__ __forceinline__ void store_rows(uint16_t *row, const unsigned char *tile, int first_chunk = 0) {
     using C = Shape<D>;
-    constexpr int kLanes = D / 8, kStep = 32 / kLanes;            // lanes to a row, rows of one store
-    const int lane = threadIdx.x % 32, sub = lane / kLanes, col = lane % kLanes;
+    constexpr int kLanes = COLUMNS / 8, kStep = 32 / kLanes;      // lanes to a row, rows of one store
+    const int lane = threadIdx.x % 32, sub = lane / kLanes, col = first_chunk + lane % kLanes;
 #pragma unroll 8
     for (int k = 0; k < 32 / kStep; ++k) {
         const int r = k * kStep + sub;
@@ -490,24 +500,26 @@ struct Parity {
 struct Barriers {
     // A step brings the K tile of the scores and the V tile of the weights, two tiles behind, in one stage.
     uint64_t kv_full[4], kv_empty[4];
-    uint64_t entry_full[kEntryStages], entry_empty[2];   // tiles; half of the stages
+    uint64_t entry_full[kMostEntryGroups * kEntryTiles], entry_empty[kMostEntryGroups];   // tiles; those looked up together
     uint64_t q_full[2], o_full[2];
     uint64_t s_full[2][2], p_full[2][2];      // query tile, score buffer
     uint64_t o_done[2];                       // all but the segment's last tile is in the output
     uint64_t drained[2];                      // all that an issuing warp has issued is done
 };
 
-template <int D, int FORMAT, bool TREE>
+template <int D, int FORMAT, bool TREE, int QT>
 __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_constant__ QcacheAttentionParams p) {
-    using C = Shape<D>;
+    using C = Shape<D, QT>;
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ Barriers bars;
-    __shared__ Entries entries[kEntryStages];
+    __shared__ Entries entries[C::kEntryStages];
     __shared__ uint32_t scan[kThreads / 32];
     __shared__ Start start;
     __shared__ Walk<C::kRows, kTile, C::kSetup> walks[kThreads / 32];
     __shared__ uint32_t tmem_base;
     __shared__ int failed;
+    __shared__ float row_factor[C::kStreams == 2 ? 128 : 1];      // of the streams' rows, which one half loads
+    __shared__ float2 row_state[2][C::kStreams == 2 ? 128 : 1];   // maximum and sum of each stream
     unsigned char *q_smem = smem, *k_smem = q_smem + C::kQBytes, *v_smem = k_smem + C::kStages * C::kKvBytes;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
 
@@ -546,10 +558,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     }
     if (tid == 0) {
         for (int i = 0; i < C::kStages; ++i) {
-            bar_init(&bars.kv_full[i], 2 * kLoadWarps);
-            bar_init(&bars.kv_empty[i], C::kIssuers);
+            bar_init(&bars.kv_full[i], C::kStreams == 2 ? 2 * C::kTileWarps : 2 * kLoadWarps);
+            bar_init(&bars.kv_empty[i], C::kStreams == 2 ? 1 : C::kIssuers);
         }
-        for (int i = 0; i < kEntryStages; ++i) bar_init(&bars.entry_full[i], 1);
+        for (int i = 0; i < C::kEntryStages; ++i) bar_init(&bars.entry_full[i], 1);
         for (int i = 0; i < 2; ++i) {
             for (int j = 0; j < 2; ++j) {
                 bar_init(&bars.s_full[i][j], 1);
@@ -559,13 +571,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             bar_init(&bars.o_full[i], 1);
             bar_init(&bars.o_done[i], 1);
             bar_init(&bars.drained[i], 1);
-            bar_init(&bars.entry_empty[i], C::kIssuers);
         }
+        for (int i = 0; i < C::kEntryGroups; ++i) bar_init(&bars.entry_empty[i], C::kIssuers);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
     }
     // after a wait that ran out the loads may come to a tile that was never looked up: it is one without blocks
-    for (int i = tid; i < kEntryStages * kBlocks; i += kThreads) entries[i / kBlocks].offset[i % kBlocks] = -1;
+    for (int i = tid; i < C::kEntryStages * kBlocks; i += kThreads) entries[i / kBlocks].offset[i % kBlocks] = -1;
     if (warp == 1) {
         // where the block's share begins: the request by halving, the row tile 32 at a time
         const uint64_t units = (uint64_t)total * (uint32_t)p.heads;
@@ -617,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
     const AttentionSegment &w = walk.w;
     if (lane == 0) walk.begin(p, start);
 
-    if (C::kQTiles == 1 && warp >= 4 && warp < kSoftmaxWarps) {
+    if (C::kLanes == 1 && warp >= 4 && warp < kSoftmaxWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kIdleRegs));
     } else if (warp < kSoftmaxWarps) {
         // ------------------------------------------------ softmax: one row per thread
@@ -628,6 +640,100 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         uint32_t n_tile = 0;          // kv tiles of the block so far
         uint32_t o_phase = 0, done = 0;
         Parity scored;
+        if constexpr (C::kStreams == 2) {
+            auto both_halves = [] {
+                fence_before();
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                fence_after();
+            };
+            while (walk.next(p)) {
+                const int n = w.row_tile * C::kRows + row, tiles = w.t1 - w.t0, mine = (tiles + 1 - qt) / 2;
+                const bool valid = n < w.rows;
+                const int64_t token = w.row0 + n / p.group, head = (int64_t)w.head * p.group + n % p.group;
+                both_halves();                                    // the rows' place has been read, and the states before
+                if (qt == 0) {
+                    row_factor[row] = load_queries<D>(p, valid ? p.q + token * p.q_stride_row + head * p.q_stride_head : nullptr, q_smem, warp % 4 * 32);
+                    fence_async_smem();
+                    bar_arrive(&bars.q_full[0]);
+                }
+                both_halves();
+                const float factor = row_factor[row];
+                const int limit = !valid ? INT32_MAX : p.causal ? min(w.kv, max(0, w.first + (int)(token - w.row0) + 1)) : w.kv;
+                const int least = TREE ? min(w.kv, w.first) : __reduce_min_sync(~0u, limit);
+                const uint32_t *tree = TREE && valid ? p.tree + token * p.tree_words : nullptr;
+                RowState r{0.f, 0.f, -INFINITY};
+                for (int i = 0; i < mine; ++i) {
+                    const uint32_t buffer = i & 1, at = n_tile + 2 * i + qt;
+                    const int t = w.t0 + 2 * i + qt;
+                    // those looked up together are there together
+                    if (i == 0 || (at - 2) / kEntryTiles != at / kEntryTiles) wait.warp(&bars.entry_full[at % C::kEntryStages], at / C::kEntryStages & 1);
+                    wait.warp(&bars.s_full[qt][buffer], scored.use(buffer));
+                    fence_after();
+                    const Entries &entry = entries[at % C::kEntryStages];
+                    const uint32_t tile = s_at + buffer * kTile;
+                    uint32_t x[2][32], y[2][16];
+                    tmem_ld(x[0], tile);
+                    ld_wait(x[0]);
+                    tmem_ld(x[1], tile + 32);
+                    softmax_tile<D, TREE>(x, y, o_at, reinterpret_cast<const float4 *>(entry.scale), *reinterpret_cast<const float4 *>(entry.v_inverse),
+                                          factor, (t + 1) * kTile > least, limit - t * kTile, tree, p.tree_words, t * kTile - w.first, i == 0, r,
+                                          [&] {
+                                              if (i + 1 < mine) wait.warp(&bars.s_full[qt][buffer ^ 1], scored.peek(buffer ^ 1));
+                                              else wait.warp(&bars.o_done[qt], done);
+                                          },
+                                          [&](int c) { tmem_st16(tile + 16 * c, y[c]); });
+                    st_wait();
+                    fence_before();
+                    bar_arrive(&bars.p_full[qt][buffer]);
+                }
+                n_tile += tiles;
+                if (mine > 1) done ^= 1;
+                row_state[qt][row] = make_float2(r.sum == 0.f ? -INFINITY : r.top, r.sum);
+                wait.warp(&bars.o_full[qt], o_phase);             // of a stream without tiles too
+                o_phase ^= 1;
+                both_halves();
+                // each half of the warps joins half of the columns; the second stream may have had no tile
+                const float2 a = row_state[0][row], b = row_state[1][row];
+                const float top = fmaxf(a.x, b.x), fa = a.x == top ? 1.f : exp2_fast(a.x - top), fb = b.x == top ? 1.f : exp2_fast(b.x - top);
+                const float sum = a.y * fa + b.y * fb;
+                const bool whole = w.t0 == 0 && w.t1 == w.tiles;
+                const float scale = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum, ga = a.y == 0.f ? 0.f : fa * scale, gb = b.y == 0.f ? 0.f : fb * scale;
+                const int64_t part = 2 * (int64_t)blockIdx.x + (w.t0 == 0);
+                const uint32_t columns = tmem + lanes + C::kOColumn + qt * (D / 2);
+                unsigned char *stage = q_smem + warp % 4 * 32 * 128;
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    uint32_t x[8], y[8];
+                    tmem_ld(x, columns + 8 * c);
+                    if (tiles > 1) tmem_ld(y, columns + D + 8 * c);
+                    ld_wait(x);
+                    float o[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) o[k] = __uint_as_float(x[k]) * ga;
+                    if (tiles > 1) {
+                        ld_wait(y);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) o[k] = fmaf(__uint_as_float(y[k]), gb, o[k]);
+                    }
+                    if (whole) {
+                        const int chunk = qt * (D / 16) + c;
+                        *reinterpret_cast<uint4 *>(stage + chunk / 8 * C::kQPanel + lane * 128 + ((chunk % 8) ^ (lane & 7)) * 16) =
+                            make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
+                    } else {
+                        float *to = p.part_o + (part * C::kRows * (D / 4) + row) * 4 + (qt * (D / 8) + 2 * c) * (C::kRows * 4);
+                        __stcg(reinterpret_cast<float4 *>(to), make_float4(o[0], o[1], o[2], o[3]));
+                        __stcg(reinterpret_cast<float4 *>(to + C::kRows * 4), make_float4(o[4], o[5], o[6], o[7]));
+                    }
+                }
+                __syncwarp();
+                if (whole) {
+                    store_rows<D, D / 2>(valid ? p.out + token * p.out_stride_row + head * p.out_stride_head : nullptr, stage, qt * (D / 16));
+                    if (valid && qt == 0 && p.lse) p.lse[token * ((int64_t)p.heads * p.group) + head] = log_sum(top, sum, kHeadroom);
+                } else if (qt == 0) {
+                    __stcg(reinterpret_cast<float2 *>(p.part_ml + (part * C::kRows + row) * 2), make_float2(sum == 0.f ? -INFINITY : top, sum));
+                }
+            }
+        } else
         while (walk.next(p)) {
             const int first = w.row_tile * C::kRows + qt * 128;   // of the tile, among the request's rows
             if (first >= w.rows) {
@@ -653,10 +759,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             const int t0 = w.t0, t1 = w.t1;
             for (int t = t0; t < t1; ++t, ++n_tile) {
                 const uint32_t buffer = (t - t0) & 1;
-                wait.warp(&bars.entry_full[n_tile % kEntryStages], n_tile / kEntryStages & 1);
+                wait.warp(&bars.entry_full[n_tile % C::kEntryStages], n_tile / C::kEntryStages & 1);
                 wait.warp(&bars.s_full[qt][buffer], scored.use(buffer));
                 fence_after();
-                const Entries &entry = entries[n_tile % kEntryStages];
+                const Entries &entry = entries[n_tile % C::kEntryStages];
                 const uint32_t tile = s_at + buffer * kTile;
                 uint32_t x[2][32], y[2][16];
                 tmem_ld(x[0], tile);
@@ -744,8 +850,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             const uint8_t *head = codes + (int64_t)w.head * p.stride_head;
             // the segment's tile i; a token past the request's, or in a block that is not there, is zero
             auto fetch = [&](uint4 (&x)[C::kChunks], int i) {
-                wait.warp(&bars.entry_full[(n_tile + i) % kEntryStages], (n_tile + i) / kEntryStages & 1);
-                const int64_t *offset = entries[(n_tile + i) % kEntryStages].offset;
+                wait.warp(&bars.entry_full[(n_tile + i) % C::kEntryStages], (n_tile + i) / C::kEntryStages & 1);
+                const int64_t *offset = entries[(n_tile + i) % C::kEntryStages].offset;
                 const int left = w.kv - (w.t0 + i) * kTile;
 #pragma unroll
                 for (int c = 0; c < C::kChunks; ++c) {
@@ -784,6 +890,60 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 fence_async_smem();
                 end_step(is_v ? i + 2 : i);
             };
+            if constexpr (C::kStreams == 2) {
+                // A tile for a warp (head_dim 128: for two) in turn, so that what a tile costs besides its codes (three waits, a fence) is
+                // not spent by each of four. The next tile's codes are asked for together, when all of this one have been used: a load that
+                // is waited for is waited for with those that were asked for after it.
+                constexpr int kWarpsOf = C::kTileWarps, kTurns = kLoadWarps / kWarpsOf, kStep = 32 * kWarpsOf / kPerRow;   // tokens between a thread's loads
+                constexpr int kLoads = kTile / kStep;
+                const int turn = warp % kLoadWarps / kWarpsOf, row = (warp % kWarpsOf * 32 + lane) / kPerRow;
+                const uint8_t *plane = head - (lt / kPerRow) % 16 * p.stride_token;       // at the thread's columns, a block's first token
+                unsigned char *to = (is_v ? v_smem : k_smem) + d / 64 * C::kKvPanel + row * 128;
+                const int x0 = (at16 ^ (row & 7)) * 16, x1 = ((at16 ^ 1) ^ (row & 7)) * 16;
+                uint4 x[kLoads];
+                // a token past the request's, or in a block that is not there, is zero
+                auto ask = [&](int i) {
+                    const uint32_t n = n_tile + i;
+                    // those looked up together are there together
+                    if (i == turn || n / kEntryTiles != (n - kTurns) / kEntryTiles) wait.warp(&bars.entry_full[n % C::kEntryStages], n / C::kEntryStages & 1);
+                    const int64_t *offset = entries[n % C::kEntryStages].offset;
+                    const int left = w.kv - (w.t0 + i) * kTile;
+#pragma unroll
+                    for (int c = 0; c < kLoads; ++c) {
+                        const int r = row + c * kStep;
+                        const int64_t at = offset[r / 16];
+                        x[c] = make_uint4(0, 0, 0, 0);
+                        if (at >= 0 && r < left) x[c] = load_codes(plane + at + r % 16 * p.stride_token);
+                    }
+                };
+                if (turn < tiles) ask(turn);
+                if (is_v)
+                    for (int i = turn; i < C::kBehind; i += kTurns) empty_step(i);
+                for (int i = turn; i < tiles; i += kTurns) {
+                    const int step = is_v ? i + C::kBehind : i;
+                    unsigned char *stage = to + begin_step(step) * C::kKvBytes;
+#pragma unroll
+                    for (int c = 0; c < kLoads; ++c) {
+                        const uint4 z = swap ? make_uint4(x[c].z, x[c].w, x[c].x, x[c].y) : x[c];
+                        uint4 y0, y1;
+                        codes_to_half<FORMAT>(z.x, y0.x, y0.y);
+                        codes_to_half<FORMAT>(z.y, y0.z, y0.w);
+                        codes_to_half<FORMAT>(z.z, y1.x, y1.y);
+                        codes_to_half<FORMAT>(z.w, y1.z, y1.w);
+                        *reinterpret_cast<uint4 *>(stage + c * kStep * 128 + x0) = y0;
+                        *reinterpret_cast<uint4 *>(stage + c * kStep * 128 + x1) = y1;
+                    }
+                    fence_async_smem();
+                    end_step(step);
+                    asm volatile("" ::: "memory");
+                    if (i + kTurns < tiles) ask(i + kTurns);
+                }
+                if (!is_v)
+                    for (int i = tiles; i < tiles + C::kBehind; ++i)
+                        if (i % kTurns == turn) empty_step(i);
+                n_tile += tiles;
+                continue;
+            }
             // a tile's codes are on their way while the one before is converted (at head_dim 256, with registers for one
             // tile, 2,048 tokens over 16,384 take 1,134 us instead of 1,059)
             uint4 x[C::kChunks], y[C::kChunks];
@@ -806,7 +966,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             n_tile += tiles;
         }
         // no arrival of the tensor cores is under way when the block ends
-        for (int stage = 0; stage < C::kStages; ++stage) wait.warp(&bars.kv_empty[stage], freed.use(stage) ^ 1);
+        constexpr int kTurns = C::kStreams == 2 ? kLoadWarps / C::kTileWarps : 1;
+        for (int stage = C::kStreams == 2 ? warp % kLoadWarps / C::kTileWarps : 0; stage < C::kStages; stage += kTurns) wait.warp(&bars.kv_empty[stage], freed.use(stage) ^ 1);
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kIssueRegs));
       // ------------------------------------------------ the matrix instructions of query tiles Q0 .. Q1 - 1
@@ -865,7 +1026,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 commit(&bars.kv_empty[stage], leader);
                 if (i >= 0) {
                     // these tiles' softmax threads have read the kv tile's entries, and so have the loads long before
-                    if (n_tile % kEntryTiles == kEntryTiles - 1 && leader) bar_arrive(&bars.entry_empty[n_tile / kEntryTiles % 2]);
+                    if (n_tile % kEntryTiles == kEntryTiles - 1 && leader) bar_arrive(&bars.entry_empty[n_tile / kEntryTiles % C::kEntryGroups]);
                     ++n_tile;
                 }
             }
@@ -875,6 +1036,68 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         int late = 0;
         commit(&bars.drained[Q0], leader);
         if (!bar_try(&bars.drained[Q0], 0)) bar_wait_slow(&bars.drained[Q0], 0, &late, p.error);
+        __syncwarp();
+      };
+      // The same for a stream of one query tile: every second kv tile, K of one beside V of the stream's second before it. Steps of both
+      // streams lie in turn in the stages.
+      auto issue_stream = [&](auto which) {
+        constexpr int S = decltype(which)::value;
+        constexpr uint32_t s_instruction = instruction(128, kTile, false), o_instruction = instruction(128, D, true);
+        const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
+        const uint32_t leader = elect();
+        uint32_t n_tile = 0, passed = 0, segment = 0;             // passed: tiles that this stream needs no more entries of
+        Parity filled, weighted;
+        bool split = false;
+        auto pass = [&](uint32_t to) {
+            if (to / kEntryTiles != passed / kEntryTiles && leader) bar_arrive(&bars.entry_empty[passed / kEntryTiles % C::kEntryGroups]);
+            passed = to;
+        };
+        while (__any_sync(~0u, walk.next(p))) {
+            if (S == 0 && w.t0 == 0 && w.t1 < w.tiles) {
+                split = true;
+                if (leader)
+                    p.splits[blockIdx.x] = {w.request, w.head, w.row_tile, w.row0, w.rows, (int)((w.unit0 + w.tiles - 1) / start.per)};
+            }
+            const int all = w.t1 - w.t0, tiles = (all + 1 - S) / 2;
+            if (S == 1) pass(n_tile + 1);                         // the first is the other's
+            wait.warp(&bars.q_full[0], segment++ & 1);
+            for (int i = -2; __any_sync(~0u, i < tiles); ++i) {
+                const uint32_t buffer = i & 1, stage = 2 * buffer + S;
+                const bool ahead = __any_sync(~0u, i + 2 < tiles);
+                wait.warp(&bars.kv_full[stage], filled.use(stage));
+                fence_after();
+                if (i >= 0) {
+                    wait.warp(&bars.p_full[S][buffer], weighted.use(buffer));
+                    fence_after();
+                    const uint32_t a = (S * 2 + buffer) * kTile, b = operand_lo(v_at + stage * C::kKvBytes, C::kKvPanel);
+#pragma unroll
+                    for (int j = 0; j < kTile / 16; ++j)
+                        mma_ts(C::kOColumn + S * D, a + j * 8, operand(b + j * 128), o_instruction, j > 0 || i > 0, leader);
+                    if (!ahead) {
+                        if (__any_sync(~0u, i + 2 == tiles)) commit(&bars.o_done[S], leader);
+                        else commit(&bars.o_full[S], leader);
+                    }
+                }
+                if (ahead) {
+                    const uint32_t a = operand_lo(q_at, 16), b = operand_lo(k_at + stage * C::kKvBytes, 16);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        mma_ss((S * 2 + buffer) * kTile, operand(a + k / 4 * (C::kQPanel / 16) + k % 4 * 2),
+                               operand(b + k / 4 * (C::kKvPanel / 16) + k % 4 * 2), s_instruction, k > 0, leader);
+                    commit(&bars.s_full[S][buffer], leader);
+                }
+                commit(&bars.kv_empty[stage], leader);
+                if (i >= 0) pass(n_tile + min(2 * i + S + 2, all));
+            }
+            // a segment does not end without this stream: it would fall more than one behind in the queries' barrier
+            if (__any_sync(~0u, tiles == 0)) commit(&bars.o_full[S], leader);
+            n_tile += all;
+            pass(n_tile);
+        }
+        if (S == 0 && !split && leader) p.splits[blockIdx.x].rows = 0;
+        int late = 0;
+        commit(&bars.drained[S], leader);
+        if (!bar_try(&bars.drained[S], 0)) bar_wait_slow(&bars.drained[S], 0, &late, p.error);
         __syncwarp();
       };
       using First = std::integral_constant<int, 0>;
@@ -889,9 +1112,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 // up to the next multiple of kEntryTiles of the count, so that the stages stay together
                 const int n = min(w.t1 - t, (int)(kEntryTiles - n_tile % kEntryTiles));
                 const int mine = lane / kBlocks, group = lane % kBlocks;
-                const uint32_t half = n_tile / kEntryTiles % 2, slot = (n_tile + mine) % kEntryStages;
-                // the first tile of a half of the stages waits for that half
-                if (n_tile % kEntryTiles == 0) wait.warp(&bars.entry_empty[half], (n_tile / kEntryStages & 1) ^ 1);
+                const uint32_t group_of = n_tile / kEntryTiles % C::kEntryGroups, slot = (n_tile + mine) % C::kEntryStages;
+                // the first tile of those looked up together waits for their stages
+                if (n_tile % kEntryTiles == 0) wait.warp(&bars.entry_empty[group_of], (n_tile / C::kEntryStages & 1) ^ 1);
                 if (mine < n) {
                     const int64_t token = (int64_t)(t + mine) * kTile + group * 16;
                     const BlockEntry b = block_entry(p, w.request, w.head, token, w.kv);
@@ -908,10 +1131,12 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             }
         }
       } else if (warp == kMmaWarp) {
-        if constexpr (C::kIssuers == 2) issue(First{}, Second{});
+        if constexpr (C::kStreams == 2) issue_stream(First{});
+        else if constexpr (C::kIssuers == 2) issue(First{}, Second{});
         else issue(First{}, All{});
       } else if (warp == kSecondMmaWarp) {
-        if constexpr (C::kIssuers == 2) issue(Second{}, All{});
+        if constexpr (C::kStreams == 2) issue_stream(Second{});
+        else if constexpr (C::kIssuers == 2) issue(Second{}, All{});
       }
     }
     fence_before();
@@ -929,9 +1154,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
 // was cut, 11.6 us for 64 tokens; twice as many: 2 us more for the head_dim 256 prompts.)
 constexpr int kJoinThreads = 256, kJoinAhead = 4;   // parts that are read before they can be weighed
 
-template <int D>
+template <int D, int QT>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ QcacheAttentionParams p) {
-    using C = Shape<D>;
+    using C = Shape<D, QT>;
     constexpr int kJoinRows = C::kRows / 16, kColumns = kJoinThreads / kJoinRows, kVecs = D / 4 > kColumns ? D / 4 / kColumns : 1;
     after_kernels_before();
     const QcacheSplit z = p.splits[blockIdx.x];
@@ -987,32 +1212,37 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     for (int v = 0; v < kVecs; ++v) write_row(p, w, z.row_tile * C::kRows + row, (column + v * kColumns) * 4, acc[v], m, l, kHeadroom);
 }
 
-template <int D, int FORMAT, bool TREE>
+template <int D, int FORMAT, bool TREE, int QT>
 cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream) {
-    using C = Shape<D>;
+    using C = Shape<D, QT>;
     // more than half of an SM's shared memory: one block per SM, which holds all of its tensor memory
     const size_t smem = C::kSmem > 120 * 1024 ? C::kSmem : 120 * 1024;
     static std::atomic<uint64_t> allowed{0};   // devices on which the shared memory limit is raised
     if (device >= 64 || !(allowed.load() >> device & 1)) {
-        const cudaError_t e = cudaFuncSetAttribute(prefill_kernel<D, FORMAT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = cudaFuncSetAttribute(prefill_kernel<D, FORMAT, TREE, QT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         if (device < 64) allowed.fetch_or(1ull << device);
     }
-    const cudaError_t e = launch_behind(prefill_kernel<D, FORMAT, TREE>, dim3(num_sms), kThreads, smem, stream, p);
-    return e != cudaSuccess ? e : launch_behind(join_kernel<D>, dim3(num_sms, 16), kJoinThreads, 0, stream, p);
+    const cudaError_t e = launch_behind(prefill_kernel<D, FORMAT, TREE, QT>, dim3(num_sms), kThreads, smem, stream, p);
+    return e != cudaSuccess ? e : launch_behind(join_kernel<D, QT>, dim3(num_sms, 16), kJoinThreads, 0, stream, p);
+}
+
+template <int D, bool TREE, int QT>
+cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream) {
+    return p.format == CM_QCACHE_E4M3 ? launch<D, CM_QCACHE_E4M3, TREE, QT>(p, num_sms, device, stream)
+                                      : launch<D, CM_QCACHE_INT8, TREE, QT>(p, num_sms, device, stream);
 }
 
 }  // namespace
 
 size_t qcache_prefill_part_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
 
-cudaError_t launch_qcache_prefill(const QcacheAttentionParams &p, int num_sms, int device, cudaStream_t stream) {
+cudaError_t launch_qcache_prefill(const QcacheAttentionParams &p, int rows_per_request, int num_sms, int device, cudaStream_t stream) {
 #define CM_LAUNCH(D) \
     if (p.head_dim == D) { \
-        if (p.tree) return p.format == CM_QCACHE_E4M3 ? launch<D, CM_QCACHE_E4M3, true>(p, num_sms, device, stream) \
-                                                      : launch<D, CM_QCACHE_INT8, true>(p, num_sms, device, stream); \
-        return p.format == CM_QCACHE_E4M3 ? launch<D, CM_QCACHE_E4M3, false>(p, num_sms, device, stream) \
-                                          : launch<D, CM_QCACHE_INT8, false>(p, num_sms, device, stream); \
+        constexpr int kTiles = Shape<D>::kQTiles; \
+        if (!p.tree) return launch<D, false, kTiles>(p, num_sms, device, stream); \
+        return rows_per_request <= 128 ? launch<D, true, 1>(p, num_sms, device, stream) : launch<D, true, kTiles>(p, num_sms, device, stream); \
     }
     CM_LAUNCH(32) CM_LAUNCH(64) CM_LAUNCH(128) CM_LAUNCH(256)
 #undef CM_LAUNCH

@@ -371,7 +371,7 @@ def test_attend_large_trees(ctx, nodes, max_nodes, group, d):
     _attend_case(ctx, [77, 0], [nodes, 3], 2, group, d, "int8", max_nodes=max_nodes, seed=nodes)
 
 
-@pytest.mark.parametrize("max_new", [1, 100])                   # either kernel
+@pytest.mark.parametrize("max_new", [1, 20, 100])               # few rows, one tile of queries, two
 @pytest.mark.parametrize("d", [64, 128])
 def test_attend_any_masks(ctx, max_new, d):
     """Masks that no tree has: nothing at all, later rows, bits beyond the rows, all."""
@@ -380,7 +380,7 @@ def test_attend_any_masks(ctx, max_new, d):
     _attend_case(ctx, [0, 33, 0], [5, 12, 1], 2, 2, d, "e4m3", max_nodes=64, masks=masks, max_new=max_new)
 
 
-@pytest.mark.parametrize("max_new", [1, 100])
+@pytest.mark.parametrize("max_new", [1, 20, 100])
 def test_attend_rows_without_tokens(ctx, max_new):
     """Fewer tokens than rows: row i of n is token kv - n + i, and the first ones are not there."""
     cache, batch, tree, q, out, lse = _attend_case(ctx, [-3, -4], [6, 4], 1, 2, 64, "int8", kv=[3, 0], max_nodes=32,
@@ -388,14 +388,14 @@ def test_attend_rows_without_tokens(ctx, max_new):
     assert bool((out[6:] == 0).all()) and bool((lse[6:] == -math.inf).all())
 
 
-@pytest.mark.parametrize("max_new", [1, 100])
+@pytest.mark.parametrize("max_new", [1, 20, 100])
 def test_attend_requests_that_were_cut(ctx, max_new):
     """context_lens says where the rows of a request begin whose table ended before them."""
     _attend_case(ctx, [20, 10], [9, 7], 1, 2, 128, "e4m3", kv=[24, 17], cut=[20, -1], max_new=max_new,
                  masks=[0b1, 0b11, 0b111, 0b1111, 0b11111, 0b111111111, 0, 0b100000000, 0b10] + [1, 3, 5, 9, 17, 33, 65], max_nodes=9)
 
 
-@pytest.mark.parametrize("max_new", [1, 100])
+@pytest.mark.parametrize("max_new", [1, 20, 100])
 @pytest.mark.parametrize("scale", [-0.3, 0.0])
 def test_attend_scales(ctx, max_new, scale):
     _attend_case(ctx, [50], [11], 2, 2, 64, "e4m3", max_new=max_new, scale=scale)
@@ -437,7 +437,7 @@ def test_attend_leaves_rows_of_no_request_and_ignores_junk(ctx):
 
 def test_attend_missing_blocks(ctx):
     """Tokens whose table entry names no block are not attended, in the context or among the rows."""
-    for max_new in (1, 100):
+    for max_new in (1, 40, 200):
         cache, batch, tree, q, _, _ = _attend_case(ctx, [60], [20], 1, 1, 64, "e4m3", seed=12, max_new=max_new)
         batch.block_table[0, 1] = -1
         batch.block_table[0, 4] = 10 ** 6                      # tokens 64 .. 79: rows 4 on
