@@ -21,7 +21,9 @@ namespace cm {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kHeld = 4;                      // vectors of a lane that are read before they are written
+constexpr int kPairs = 2;                     // (layer, head) that a warp moves at a time, K and V of each
+constexpr int kHeld = 1;                      // vectors of a lane of each that are read before they are written
+constexpr int kBlocksPerSm = 3;
 
 // What entry i of a request's path names: places of the row's present and new slot, negative if there are none.
 struct Place {
@@ -54,58 +56,88 @@ __device__ __forceinline__ uint4 rescale(const uint4 &x, float ratio) {
     return make_uint4(shrink<FORMAT>(x.x, ratio), shrink<FORMAT>(x.y, ratio), shrink<FORMAT>(x.z, ratio), shrink<FORMAT>(x.w, ratio));
 }
 
-// One (layer, head) of K or V of a request by a warp.
+// K and V of up to kPairs (layer, head) of a request by a warp: their rows lie alike, so that they are read together.
 template <int FORMAT>
-__device__ __forceinline__ void move_rows(const QcacheKeepParams &p, int kv, int64_t layer, int64_t head, const Place *from, const Place *to,
-                                          int begin, int end) {
+__device__ __forceinline__ void move_rows(const QcacheKeepParams &p, int pair0, const Place *from, const Place *to, int begin, int end) {
+    constexpr int kTasks = 2 * kPairs;
     const int lane = threadIdx.x % 32;
     const int log2_vecs = 31 - __clz(p.head_dim) - 4, row = lane >> log2_vecs, rows = 32 >> log2_vecs;
-    uint8_t *codes = p.codes[kv] + layer * p.stride_layer + head * p.stride_head + (lane & ((1 << log2_vecs) - 1)) * 16;
-    float *scales = p.scales[kv] + layer * p.scale_stride_layer + head * p.scale_stride_head;
-    auto code_at = [&](int block, int at) { return reinterpret_cast<uint4 *>(codes + block * p.stride_block + at * p.stride_token); };
+    uint8_t *codes[kTasks];
+    float *scales[kTasks];
+    const int tasks = 2 * min(kPairs, p.layers * p.heads - pair0);
+#pragma unroll
+    for (int u = 0; u < kTasks; ++u) {
+        const int pair = pair0 + (u < tasks ? u / 2 : 0);
+        const int64_t layer = pair / p.heads, head = pair - layer * p.heads;
+        codes[u] = p.codes[u % 2] + layer * p.stride_layer + head * p.stride_head + (lane & ((1 << log2_vecs) - 1)) * 16;
+        scales[u] = p.scales[u % 2] + layer * p.scale_stride_layer + head * p.scale_stride_head;
+    }
+    auto code_at = [&](int u, int64_t offset) { return reinterpret_cast<uint4 *>(codes[u] + offset); };
+    auto place_at = [&](const Place &x, int more) { return x.block * p.stride_block + (x.at + more) * p.stride_token; };
     for (int i0 = begin; i0 < end;) {
         const Place first = to[i0];
         const int i1 = min(end, i0 + (1 << p.log2_block) - first.at);
-        float *scale = scales + first.block * p.scale_stride_block;
+        const int64_t scale_at = first.block * p.scale_stride_block;
         // the first rows are on their way while the scales are looked at
-        uint4 x[kHeld];
-        float s[kHeld];
+        uint4 x[kTasks][kHeld];
+        float s[kTasks][kHeld], old[kTasks], now[kTasks];
         auto load = [&](int base) {
 #pragma unroll
             for (int j = 0; j < kHeld; ++j) {
                 const int i = base + j * rows + row;
                 if (i < i1) {
                     const Place f = from[i];
-                    x[j] = *code_at(f.block, f.at);
-                    s[j] = scales[f.block * p.scale_stride_block];
+                    const int64_t at = place_at(f, 0), scale = f.block * p.scale_stride_block;
+#pragma unroll
+                    for (int u = 0; u < kTasks; ++u)
+                        if (u < tasks) {
+                            x[u][j] = *code_at(u, at);
+                            s[u][j] = scales[u][scale];
+                        }
                 }
             }
         };
         load(i0);
-        const float old = first.at ? *scale : 0.f;
-        float now = old;
-        for (int i = i0 + lane; i < i1; i += 32) now = fmaxf(now, scales[from[i].block * p.scale_stride_block]);
 #pragma unroll
-        for (int d = 16; d; d /= 2) now = fmaxf(now, __shfl_xor_sync(~0u, now, d));
+        for (int u = 0; u < kTasks; ++u) now[u] = old[u] = first.at && u < tasks ? scales[u][scale_at] : 0.f;
+        for (int i = i0 + lane; i < i1; i += 32) {
+            const int64_t scale = from[i].block * p.scale_stride_block;
+#pragma unroll
+            for (int u = 0; u < kTasks; ++u)
+                if (u < tasks) now[u] = fmaxf(now[u], scales[u][scale]);
+        }
+#pragma unroll
+        for (int u = 0; u < kTasks; ++u)
+#pragma unroll
+            for (int d = 16; d; d /= 2) now[u] = fmaxf(now[u], __shfl_xor_sync(~0u, now[u], d));
         for (int base = i0; base < i1; base += kHeld * rows) {
             if (base != i0) load(base);
             __syncwarp();                     // all of them are read before one is written over
 #pragma unroll
             for (int j = 0; j < kHeld; ++j) {
                 const int i = base + j * rows + row;
-                if (i < i1) *code_at(first.block, first.at + i - i0) = rescale<FORMAT>(x[j], s[j] == now ? 1.f : __fdiv_rn(s[j], now));
+                if (i < i1) {
+                    const int64_t at = place_at(first, i - i0);
+#pragma unroll
+                    for (int u = 0; u < kTasks; ++u)
+                        if (u < tasks) *code_at(u, at) = rescale<FORMAT>(x[u][j], s[u][j] == now[u] ? 1.f : __fdiv_rn(s[u][j], now[u]));
+                }
             }
         }
-        if (first.at && now > old) {          // the tokens that stay in the block
-            const float ratio = __fdiv_rn(old, now);
+#pragma unroll
+        for (int u = 0; u < kTasks; ++u)
+            if (first.at && now[u] > old[u]) {          // the tokens that stay in the block (old: 0 beyond the tasks, and now too)
+                const float ratio = __fdiv_rn(old[u], now[u]);
 #pragma unroll 2
-            for (int t = row; t < first.at; t += rows) {
-                uint4 *at = code_at(first.block, t);
-                *at = rescale<FORMAT>(*at, ratio);
+                for (int t = row; t < first.at; t += rows) {
+                    uint4 *at = code_at(u, first.block * p.stride_block + t * p.stride_token);
+                    *at = rescale<FORMAT>(*at, ratio);
+                }
             }
-        }
         __syncwarp();                         // every lane has read the scales
-        if (lane == 0) *scale = now;
+#pragma unroll
+        for (int u = 0; u < kTasks; ++u)
+            if (u < tasks && lane == u) scales[u][scale_at] = now[u];
         __syncwarp();
         i0 = i1;
     }
@@ -155,7 +187,7 @@ __device__ __forceinline__ void count_blocks(const QcacheKeepParams &p) {
 }
 
 template <int FORMAT>
-__global__ void __launch_bounds__(kThreads) keep_kernel(const __grid_constant__ QcacheKeepParams p) {
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) keep_kernel(const __grid_constant__ QcacheKeepParams p) {
     __shared__ Place from[kTreeMaxNodes], to[kTreeMaxNodes];
     __shared__ int first_moved, first_wrong;
     after_kernels_before();
@@ -183,19 +215,17 @@ __global__ void __launch_bounds__(kThreads) keep_kernel(const __grid_constant__ 
     __syncthreads();
     const int begin = first_moved, end = min(most, first_wrong);
     if (begin >= end) return;
-    const int tasks = p.layers * p.heads * 2;
-    for (int task = chunk * kWarps + threadIdx.x / 32; task < tasks; task += p.chunks * kWarps) {
-        const int which = task & 1, at = task >> 1;
-        move_rows<FORMAT>(p, which, at / p.heads, at % p.heads, from, to, begin, end);
-    }
+    for (int pair = (chunk * kWarps + threadIdx.x / 32) * kPairs; pair < p.layers * p.heads; pair += p.chunks * kWarps * kPairs)
+        move_rows<FORMAT>(p, pair, from, to, begin, end);
 }
 
 }  // namespace
 
 cudaError_t launch_qcache_keep(QcacheKeepParams p, int num_sms, cudaStream_t stream) {
-    const int64_t warps = ((int64_t)p.layers * p.heads * 2 + kWarps - 1) / kWarps;      // thread blocks of one task a warp
-    const int64_t fair = p.requests ? (8ll * num_sms + p.requests - 1) / p.requests : 1;
-    p.chunks = (int)(warps < fair ? warps : fair);
+    // thread blocks of a request: no more than its (layer, head) can use, nor, together, than run at a time
+    const int64_t most = ((int64_t)p.layers * p.heads + kWarps * kPairs - 1) / (kWarps * kPairs);
+    const int64_t fair = p.requests ? ((int64_t)kBlocksPerSm * num_sms + p.requests - 1) / p.requests : 1;
+    p.chunks = (int)(most < fair ? most : fair);
     const dim3 grid((unsigned)(p.requests * p.chunks + 1));
     return p.format == CM_QCACHE_E4M3 ? launch_behind(keep_kernel<CM_QCACHE_E4M3>, grid, kThreads, 0, stream, p)
                                       : launch_behind(keep_kernel<CM_QCACHE_INT8>, grid, kThreads, 0, stream, p);
