@@ -149,9 +149,7 @@ cm_status cm_tree_verify(cm_context *ctx, const cm_tree_drafts *drafts, cm_strea
         p.vocab = drafts->vocab;
         p.max_nodes = drafts->max_nodes;
         p.type = drafts->type;
-        return on_device(ctx, "verification launch", [&] {
-            return cm::launch_tree_verify(p, cm::context_num_sms(ctx), reinterpret_cast<cudaStream_t>(stream));
-        });
+        return on_device(ctx, "verification launch", [&] { return cm::launch_tree_verify(p, reinterpret_cast<cudaStream_t>(stream)); });
     });
 }
 

@@ -48,7 +48,7 @@ struct TreeVerifyParams {
     int32_t *path, *kept, *next_token;
     int32_t requests, total_rows, vocab, max_nodes, type;
 };
-cudaError_t launch_tree_verify(const TreeVerifyParams &p, int num_sms, cudaStream_t stream);
+cudaError_t launch_tree_verify(const TreeVerifyParams &p, cudaStream_t stream);
 
 // ---------------------------------------------------------------- accepted rows to the front
 struct QcacheKeepParams {

@@ -26,24 +26,34 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kMaxVocab = 1 << 20;
-constexpr int kMaxSteps = kMaxVocab / (32 * 4 * kWarps) + 1;   // of a warp, if one block has the whole row
+constexpr int kMaxVocab = 1 << 20, kAlone = 4096;              // elements that one block takes alone
+constexpr int kMaxSteps = kMaxVocab / (32 * 4 * 8 * kMaxCluster) + 1;   // of a warp, with eight of them to a block
+static_assert(kAlone / (32 * 4 * 8) + 1 <= kMaxSteps, "a smaller cluster's warps have no more");
+constexpr int kThreads = 256, kWarps = kThreads / 32;   // four blocks to an SM: 64 requests with a cluster of eight each are there at once
+constexpr int kAhead = 3, kSlot = 2 * kThreads * 16;    // vectors of each row that a thread has on their way, 24 KB of a block
 constexpr double kUnit = 0x1p-42;
 
-__device__ __forceinline__ float clean(float x) { return fminf(fmaxf(x, 0.f), 1.f); }      // a NaN becomes 0
+__device__ __forceinline__ float clean(float x) { return __saturatef(x); }      // to [0, 1], a NaN to 0
+
+// max(w - q z, 0) of values in [0, 1], each operation rounded.
+__device__ __forceinline__ float less(float w, float q, float z) {
+    const float product = __fmul_rn(q, z);
+    float rest;
+    asm("sub.rn.sat.f32 %0, %1, %2;" : "=f"(rest) : "f"(w), "f"(product));
+    return rest;
+}
 
 template <int TYPE>
 struct Row;
 template <>
 struct Row<CM_PROB_F32> {
     using Element = float;
-    static constexpr int kVec = 4;
+    static constexpr int kVec = 4;            // elements of a vector
     static __device__ __forceinline__ float one(const float *p) { return clean(*p); }
-    static __device__ __forceinline__ void vec(const float *p, float (&x)[4]) {
-        const float4 v = *reinterpret_cast<const float4 *>(p);
-        x[0] = clean(v.x); x[1] = clean(v.y); x[2] = clean(v.z); x[3] = clean(v.w);
+    static __device__ __forceinline__ void unpack(const uint4 &v, float (&x)[4]) {
+        x[0] = clean(__uint_as_float(v.x)); x[1] = clean(__uint_as_float(v.y));
+        x[2] = clean(__uint_as_float(v.z)); x[3] = clean(__uint_as_float(v.w));
     }
 };
 template <>
@@ -51,8 +61,7 @@ struct Row<CM_PROB_BF16> {
     using Element = uint16_t;
     static constexpr int kVec = 8;
     static __device__ __forceinline__ float one(const uint16_t *p) { return clean(__uint_as_float((uint32_t)*p << 16)); }
-    static __device__ __forceinline__ void vec(const uint16_t *p, float (&x)[8]) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(p);
+    static __device__ __forceinline__ void unpack(const uint4 &v, float (&x)[8]) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -62,19 +71,103 @@ struct Row<CM_PROB_BF16> {
     }
 };
 
-// The whole multiples of 2^-42 in x, 0 <= x <= 1, as hi * 2^21 + lo: additions that round towards zero leave
-// floor(x * 2^21) in the low bits of 4 + x, then the same of what is left.
+// The whole multiples of 2^-42 in x, 0 <= x <= 1, are hi * 2^21 + lo: additions that round towards zero leave
+// floor(x * 2^21) in the low bits of 4 + x, then the same of what is left. Both come with kBits of 4 on top, which a sum
+// takes off at its end (modulo 2^32).
+constexpr uint32_t kBits = 0x40800000u;
 __device__ __forceinline__ void split(float x, uint32_t &hi, uint32_t &lo) {
     const float y = __fadd_rz(x, 4.f);
-    hi = __float_as_uint(y) - 0x40800000u;
-    const float rest = __fmul_rn(__fsub_rn(x, __fsub_rn(y, 4.f)), 0x1p21f);
-    lo = __float_as_uint(__fadd_rz(rest, 4.f)) - 0x40800000u;
+    hi = __float_as_uint(y);
+    lo = __float_as_uint(__fmaf_rz(__fsub_rn(x, __fsub_rn(y, 4.f)), 0x1p21f, 4.f));
+}
+template <int N>
+__device__ __forceinline__ uint64_t whole(const float (&x)[N]) {
+    uint32_t hi = 0, lo = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        uint32_t a, b;
+        split(x[i], a, b);
+        hi += a;
+        lo += b;
+    }
+    return ((uint64_t)(hi - N * kBits) << 21) + (lo - N * kBits);
 }
 __device__ __forceinline__ uint64_t whole(float x) {
-    uint32_t hi, lo;
-    split(x, hi, lo);
-    return ((uint64_t)hi << 21) + lo;
+    const float one[1] = {x};
+    return whole(one);
 }
+
+// Two elements in a 64-bit register, for the two-wide instructions.
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+    return v;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+
+// less() of both, the factor negated.
+__device__ __forceinline__ uint64_t less2(uint64_t w, uint64_t q, uint64_t minus_z) {
+    uint64_t product, rest;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(product) : "l"(q), "l"(minus_z));
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(rest) : "l"(w), "l"(product));
+    float a, b;
+    unpair(rest, a, b);
+    return pair(fmaxf(a, 0.f), fmaxf(b, 0.f));
+}
+
+// split() of both, added up.
+__device__ __forceinline__ void split2(uint64_t x, uint32_t &hi, uint32_t &lo) {
+    const uint64_t four = pair(4.f, 4.f), minus_four = pair(-4.f, -4.f), minus_one = pair(-1.f, -1.f), up = pair(0x1p21f, 0x1p21f);
+    uint64_t y, t, rest, z;
+    asm("add.rz.f32x2 %0, %1, %2;" : "=l"(y) : "l"(x), "l"(four));
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(t) : "l"(y), "l"(minus_four));
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(rest) : "l"(t), "l"(minus_one), "l"(x));
+    asm("fma.rz.f32x2 %0, %1, %2, %3;" : "=l"(z) : "l"(rest), "l"(up), "l"(four));
+    hi += (uint32_t)y + (uint32_t)(y >> 32);
+    lo += (uint32_t)z + (uint32_t)(z >> 32);
+}
+
+__device__ __forceinline__ void copy16(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ uint4 load16(uint32_t from) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from) : "memory");
+    return v;
+}
+
+// A row and what the rejections at it leave of it.
+template <int TYPE>
+struct Rest {
+    using E = typename Row<TYPE>::Element;
+    static constexpr int kVec = Row<TYPE>::kVec;
+    const E *target, *draft;      // draft may be null
+    int vocab, levels;
+    bool wide;                    // both rows begin alike within a vector
+    const float *level;           // z of each rejection, with a draft
+    const int32_t *out;           // tokens taken out, without
+
+    // Elements e, e + 1, ... (0 outside the row) where speed does not count, and their sum.
+    __device__ __forceinline__ uint64_t get(int e, float (&w)[kVec]) const {
+        const bool drawn = draft && levels > 0;
+        float q[kVec];
+        if (wide && e >= 0 && e + kVec <= vocab) {
+            Row<TYPE>::unpack(*reinterpret_cast<const uint4 *>(target + e), w);
+            if (drawn) Row<TYPE>::unpack(*reinterpret_cast<const uint4 *>(draft + e), q);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) {
+                const bool there = e + k >= 0 && e + k < vocab;
+                w[k] = there ? Row<TYPE>::one(target + e + k) : 0.f;
+                q[k] = there && drawn ? Row<TYPE>::one(draft + e + k) : 0.f;
+            }
+        }
+        for (int l = 0; l < levels; ++l)
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) w[k] = drawn ? less(w[k], q[k], level[l]) : out[l] == e + k ? 0.f : w[k];
+        return whole(w);
+    }
+};
 
 // Where the walk is, in shared memory.
 struct Walk {
@@ -86,10 +179,12 @@ struct Walk {
 };
 
 template <int TYPE>
-__global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant__ TreeVerifyParams p) {
+__global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_constant__ TreeVerifyParams p) {
     using R = Row<TYPE>;
     using E = typename R::Element;
     constexpr int kVec = R::kVec;
+    extern __shared__ __align__(16) unsigned char copies[];   // [kAhead][target, draft][thread] vectors
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(copies) + threadIdx.x * 16;
     __shared__ int16_t parent[kTreeMaxNodes], walked[kTreeMaxNodes];
     __shared__ int32_t token[kTreeMaxNodes];
     __shared__ float target_at[kTreeMaxNodes], draft_at[kTreeMaxNodes], accept_at[kTreeMaxNodes];
@@ -113,6 +208,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
         }
         return;
     }
+    const float sample = p.sample[r];
     cluster.barrier_arrive();                   // waited for before the first write to another block's memory
     for (int i = tid; i < n; i += kThreads) {
         int a = p.parents[rows.first + i];
@@ -169,7 +265,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
                 double bar;
                 if (draft) {
                     const float q = draft_at[c], z = (float)((double)w.z * kUnit);
-                    for (int k = 0; k < w.levels; ++k) have = fmaxf(__fsub_rn(have, __fmul_rn(q, level[k])), 0.f);
+                    for (int k = 0; k < w.levels; ++k) have = less(have, q, level[k]);
                     bar = __dmul_rn(__dmul_rn((double)accept_at[c], (double)q), (double)z);
                 } else {
                     for (int k = 0; k < w.levels; ++k)
@@ -207,57 +303,76 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
         const E *t_row = target + node * p.target_stride, *d_row = draft ? draft + node * p.draft_stride : nullptr;
         const int skew = (int)((reinterpret_cast<uintptr_t>(t_row) / sizeof(E)) % kVec);
         const bool wide = !d_row || (int)((reinterpret_cast<uintptr_t>(d_row) / sizeof(E)) % kVec) == skew;
-        int levels = walk.levels;
-        // element e of the row is number e + skew of its vectors
-        auto weights = [&](int at, float (&w)[kVec]) {
-            const int e = at - skew;
-            float q[kVec];
-            if (wide && e >= 0 && e + kVec <= p.vocab) {
-                R::vec(t_row + e, w);
-                if (d_row && levels) R::vec(d_row + e, q);
-            } else {
-#pragma unroll
-                for (int k = 0; k < kVec; ++k) {
-                    const bool there = e + k >= 0 && e + k < p.vocab;
-                    w[k] = there ? R::one(t_row + e + k) : 0.f;
-                    q[k] = there && d_row && levels ? R::one(d_row + e + k) : 0.f;
-                }
-            }
-            if (d_row) {
-                for (int l = 0; l < levels; ++l) {
-                    const float z = level[l];
-#pragma unroll
-                    for (int k = 0; k < kVec; ++k) w[k] = fmaxf(__fsub_rn(w[k], __fmul_rn(q[k], z)), 0.f);
-                }
-            } else {
-                for (int l = 0; l < levels; ++l)
-#pragma unroll
-                    for (int k = 0; k < kVec; ++k)
-                        if (out[l] == e + k) w[k] = 0.f;
-            }
-        };
-        auto vector_sum = [&](const float (&w)[kVec]) {
-            uint32_t hi = 0, lo = 0;
-#pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                uint32_t x, y;
-                split(w[k], x, y);
-                hi += x;
-                lo += y;
-            }
-            return ((uint64_t)hi << 21) + lo;
-        };
+        Rest<TYPE> rest{t_row, d_row, p.vocab, walk.levels, wide, level, out};
         uint64_t total, before;                 // of the whole row; of the blocks in front of this one
         auto sum_row = [&] {
-            uint64_t sum = 0;
-#pragma unroll 4
-            for (int s = 0; s < warp_steps; ++s) {
-                const int at = begin + (warp * warp_steps + s) * kStep + lane * kVec;
-                if (at - skew >= p.vocab) break;
-                float w[kVec];
-                weights(at, w);
-                sum += vector_sum(w);
+            // the warp's piece: from step s0 to s1 every lane's vector is within the row
+            const int first = begin + warp * warp_steps * kStep - skew;
+            const int s1 = wide ? min(warp_steps, max(p.vocab - first, 0) / kStep) : 0, s0 = min(first < 0 ? 1 : 0, s1);
+            const bool drawn = d_row && rest.levels > 0;
+            const E *t_at = t_row + first + lane * kVec, *d_at = drawn ? d_row + first + lane * kVec : t_at;
+            const float minus_z = drawn ? -level[0] : 0.f;
+            uint32_t hi = 0, lo = 0;            // less kBits for each element, modulo 2^32
+            // vectors on their way lie in shared memory, each for the thread that asked for it
+            const int n = max(s1 - s0, 0);
+            t_at += s0 * kStep;
+            d_at += s0 * kStep;
+            int asked = 0;
+            uint32_t to = ring, from = ring;
+            auto ask = [&] {
+                if (asked < n) {
+                    copy16(to, t_at);
+                    if (drawn) copy16(to + kThreads * 16, d_at);
+                }
+                ++asked;
+                t_at += kStep;
+                d_at += kStep;
+                to = to == ring + (kAhead - 1) * kSlot ? ring : to + kSlot;
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
+            for (int i = 0; i < kAhead; ++i) ask();
+#pragma unroll 1
+            for (int s = 0; s < n; ++s) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+                float w[kVec], q[kVec];
+                R::unpack(load16(from), w);
+                uint64_t x[kVec / 2];
+#pragma unroll
+                for (int k = 0; k < kVec / 2; ++k) x[k] = pair(w[2 * k], w[2 * k + 1]);
+                if (drawn) {
+                    R::unpack(load16(from + kThreads * 16), q);
+                    float z = minus_z;
+                    for (int l = 1;; ++l) {
+#pragma unroll
+                        for (int k = 0; k < kVec / 2; ++k) x[k] = less2(x[k], pair(q[2 * k], q[2 * k + 1]), pair(z, z));
+                        if (l == rest.levels) break;
+                        z = -level[l];
+                    }
+                }
+                from = from == ring + (kAhead - 1) * kSlot ? ring : from + kSlot;
+#pragma unroll
+                for (int k = 0; k < kVec / 2; ++k) split2(x[k], hi, lo);
+                ask();
             }
+            const uint32_t elements = (uint32_t)(n * kVec);
+            uint64_t sum = ((uint64_t)(hi - elements * kBits) << 21) + (lo - elements * kBits);
+            // the row's ends, or all of rows that do not begin alike
+            auto slowly = [&](int from, int to) {
+#pragma unroll 1
+                for (int s = from; s < to; ++s) {
+                    const int e = first + s * kStep + lane * kVec;
+                    float w[kVec];
+                    if (e < p.vocab) sum += rest.get(e, w);
+                }
+            };
+            slowly(0, s0);
+            slowly(s1, warp_steps);
+            // without draft rows the steps above have counted the tokens that are taken out
+            if (!d_row)
+                for (int l = 0; l < rest.levels; ++l) {
+                    const int at = out[l] - first, step = at / kStep;
+                    if (at >= 0 && step >= s0 && step < s1 && at % kStep / kVec == lane) sum -= whole(R::one(t_row + out[l]));
+                }
 #pragma unroll
             for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
             if (lane == 0) warp_sum[warp] = sum;
@@ -276,16 +391,20 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
             }
             ++pass;
         };
-        sum_row();
-        if (total == 0 && levels > 0) {
+        bool taken_back = false;
+        while (true) {
+            sum_row();
+            if (total != 0 || rest.levels == 0 || taken_back) break;
             // a rejection that leaves nothing is taken back; without draft rows, all of them
-            levels = draft ? levels - 1 : 0;
-            if (ends) sum_row();
-            else if (tid == 0) walk.levels = levels;
-        } else if (!ends && tid == 0) {
-            walk.z = (int64_t)total;
+            rest.levels = draft ? rest.levels - 1 : 0;
+            taken_back = true;
+            if (!ends) break;
         }
         if (!ends) {
+            if (tid == 0) {
+                if (taken_back) walk.levels = rest.levels;
+                else walk.z = (int64_t)total;
+            }
             __syncwarp();
             continue;
         }
@@ -298,7 +417,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
                 if (total == 0) p.next_token[r] = -1;
             }
         }
-        const double number = (double)fminf(fmaxf(p.sample[r], 0.f), 1.f) * 0x1p32;
+        const double number = (double)clean(sample) * 0x1p32;
         uint64_t point = __umul64hi(total, min((uint64_t)number, (uint64_t)0xffffffffu) << 32);
         if (total == 0 || point < before) return;
         point -= before;
@@ -306,36 +425,44 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
         while (piece < kWarps && point >= warp_sum[piece]) point -= warp_sum[piece++];
         if (piece == kWarps) return;            // another block's
         // its steps, shared by the block's warps
-        const int piece_begin = begin + piece * warp_steps * kStep;
+        const int first = begin + piece * warp_steps * kStep + lane * kVec - skew;   // this lane's
+        float w[kVec];
         for (int s = warp; s < warp_steps; s += kWarps) {
-            float w[kVec];
-            weights(piece_begin + s * kStep + lane * kVec, w);
-            uint64_t sum = vector_sum(w);
+            uint64_t sum = rest.get(first + s * kStep, w);
 #pragma unroll
             for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
             if (lane == 0) step_sum[s] = sum;
         }
         __syncthreads();
         if (warp != 0) return;
-        int s = 0;
-        while (s < warp_steps - 1 && point >= step_sum[s]) point -= step_sum[s++];
-        float w[kVec];
-        const int at = piece_begin + s * kStep + lane * kVec;
-        weights(at, w);
-        const uint64_t mine = vector_sum(w);
-        uint64_t upto = mine;
+        // the step, its lane, its element: where the sum passes the point
+        auto scan = [&](uint64_t x) {
 #pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const uint64_t x = __shfl_up_sync(~0u, upto, d);
-            if (lane >= d) upto += x;
-        }
-        if (point < upto && point >= upto - mine) {
-            point -= upto - mine;
-            int k = 0;
+            for (int d = 1; d < 32; d *= 2) {
+                const uint64_t y = __shfl_up_sync(~0u, x, d);
+                if (lane >= d) x += y;
+            }
+            return x;
+        };
+        for (int s0 = 0; s0 < warp_steps; s0 += 32) {
+            const uint64_t mine = s0 + lane < warp_steps ? step_sum[s0 + lane] : 0, upto = scan(mine);
+            const unsigned passed = __ballot_sync(~0u, point < upto);
+            if (!passed) {
+                point -= __shfl_sync(~0u, upto, 31);
+                continue;
+            }
+            const int l = __ffs(passed) - 1, e = first + (s0 + l) * kStep;
+            point -= __shfl_sync(~0u, upto - mine, l);
+            const uint64_t own = rest.get(e, w), all = scan(own);
+            if (point < all && point >= all - own) {
+                point -= all - own;
+                int k = 0;
 #pragma unroll
-            for (int i = 0; i < kVec - 1; ++i)
-                if (k == i && point >= whole(w[i])) point -= whole(w[i]), ++k;
-            p.next_token[r] = at - skew + k;
+                for (int i = 0; i < kVec - 1; ++i)
+                    if (k == i && point >= whole(w[i])) point -= whole(w[i]), ++k;
+                p.next_token[r] = e + k;
+            }
+            return;
         }
         return;
     }
@@ -351,6 +478,7 @@ cudaError_t launch(const TreeVerifyParams &p, int blocks, cudaStream_t stream) {
     cudaLaunchConfig_t config{};
     config.gridDim = dim3((unsigned)p.requests * blocks);
     config.blockDim = dim3(kThreads);
+    config.dynamicSmemBytes = kAhead * kSlot;
     config.stream = stream;
     config.attrs = attrs;
     config.numAttrs = 2;
@@ -359,10 +487,9 @@ cudaError_t launch(const TreeVerifyParams &p, int blocks, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_tree_verify(const TreeVerifyParams &p, int num_sms, cudaStream_t stream) {
-    (void)num_sms;
+cudaError_t launch_tree_verify(const TreeVerifyParams &p, cudaStream_t stream) {
     int blocks = 1;
-    while (blocks < kMaxCluster && p.vocab > 4096 * blocks) blocks *= 2;
+    while (blocks < kMaxCluster && p.vocab > kAlone * blocks) blocks *= 2;
     return p.type == CM_PROB_F32 ? launch<CM_PROB_F32>(p, blocks, stream) : launch<CM_PROB_BF16>(p, blocks, stream);
 }
 
