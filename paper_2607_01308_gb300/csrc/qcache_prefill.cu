@@ -896,8 +896,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                 // is waited for is waited for with those that were asked for after it.
                 constexpr int kWarpsOf = C::kTileWarps, kTurns = kLoadWarps / kWarpsOf, kStep = 32 * kWarpsOf / kPerRow;   // tokens between a thread's loads
                 constexpr int kLoads = kTile / kStep;
+                const int64_t step8 = 8 * p.stride_token;
                 const int turn = warp % kLoadWarps / kWarpsOf, row = (warp % kWarpsOf * 32 + lane) / kPerRow;
-                const uint8_t *plane = head - (lt / kPerRow) % 16 * p.stride_token;       // at the thread's columns, a block's first token
+                static_assert(kStep == 8 || kStep == 16, "a thread's tokens lie alike in every block");
+                const uint8_t *plane = head + ((kStep == 8 ? row : row % 16) - lt / kPerRow % 16) * p.stride_token;   // of the thread's first token and columns
                 unsigned char *to = (is_v ? v_smem : k_smem) + d / 64 * C::kKvPanel + row * 128;
                 const int x0 = (at16 ^ (row & 7)) * 16, x1 = ((at16 ^ 1) ^ (row & 7)) * 16;
                 uint4 x[kLoads];
@@ -906,14 +908,19 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                     const uint32_t n = n_tile + i;
                     // those looked up together are there together
                     if (i == turn || n / kEntryTiles != (n - kTurns) / kEntryTiles) wait.warp(&bars.entry_full[n % C::kEntryStages], n / C::kEntryStages & 1);
-                    const int64_t *offset = entries[n % C::kEntryStages].offset;
-                    const int left = w.kv - (w.t0 + i) * kTile;
+                    int64_t at[kBlocks];
+#pragma unroll
+                    for (int g = 0; g < kBlocks; g += 2) {
+                        const longlong2 y = *reinterpret_cast<const longlong2 *>(entries[n % C::kEntryStages].offset + g);
+                        at[g] = y.x;
+                        at[g + 1] = y.y;
+                    }
+                    const int left = w.kv - (w.t0 + i) * kTile - row;
 #pragma unroll
                     for (int c = 0; c < kLoads; ++c) {
-                        const int r = row + c * kStep;
-                        const int64_t at = offset[r / 16];
+                        const int g = c * kStep / 16;
                         x[c] = make_uint4(0, 0, 0, 0);
-                        if (at >= 0 && r < left) x[c] = load_codes(plane + at + r % 16 * p.stride_token);
+                        if (at[g] >= 0 && c * kStep < left) x[c] = load_codes(plane + at[g] + (c * kStep % 16 ? step8 : 0));
                     }
                 };
                 if (turn < tiles) ask(turn);
