@@ -915,12 +915,17 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                         at[g] = y.x;
                         at[g + 1] = y.y;
                     }
-                    const int left = w.kv - (w.t0 + i) * kTile - row;
+                    const int left = w.kv - (w.t0 + i) * kTile;
+                    if (left >= kTile && (at[0] | at[1] | at[2] | at[3]) >= 0) {     // as a rule
+#pragma unroll
+                        for (int c = 0; c < kLoads; ++c) x[c] = load_codes(plane + at[c * kStep / 16] + (c * kStep % 16 ? step8 : 0));
+                        return;
+                    }
 #pragma unroll
                     for (int c = 0; c < kLoads; ++c) {
                         const int g = c * kStep / 16;
                         x[c] = make_uint4(0, 0, 0, 0);
-                        if (at[g] >= 0 && c * kStep < left) x[c] = load_codes(plane + at[g] + (c * kStep % 16 ? step8 : 0));
+                        if (at[g] >= 0 && c * kStep + row < left) x[c] = load_codes(plane + at[g] + (c * kStep % 16 ? step8 : 0));
                     }
                 };
                 if (turn < tiles) ask(turn);
