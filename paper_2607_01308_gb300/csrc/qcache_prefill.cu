@@ -1051,9 +1051,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         __syncwarp();
       };
       // The same for a stream of one query tile: every second kv tile, K of one beside V of the stream's second before it. Steps of both
-      // streams lie in turn in the stages.
-      auto issue_stream = [&](auto which) {
-        constexpr int S = decltype(which)::value;
+      // streams lie in turn in the stages. (One code for both: with two the block's loops do not fit the instruction caches, 64
+      // trees 170 us against 163.)
+      auto issue_stream = [&](const int S) {
         constexpr uint32_t s_instruction = instruction(128, kTile, false), o_instruction = instruction(128, D, true);
         const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
         const uint32_t leader = elect();
@@ -1115,7 +1115,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
       using First = std::integral_constant<int, 0>;
       using Second = std::integral_constant<int, 1>;
       using All = std::integral_constant<int, C::kQTiles>;
-      if (warp == kEntryWarp) {
+      if (C::kStreams == 2 && (warp == kMmaWarp || warp == kSecondMmaWarp)) {
+        if constexpr (C::kStreams == 2) issue_stream(__shfl_sync(~0u, warp == kSecondMmaWarp, 0));
+      } else if (warp == kEntryWarp) {
         // ------------------------------------------------ blocks and scales, kEntryTiles tiles at a time
         uint32_t n_tile = 0;
         const bool withheld = p.withhold == kQcacheWithholdEntries && blockIdx.x == 0;
@@ -1143,12 +1145,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             }
         }
       } else if (warp == kMmaWarp) {
-        if constexpr (C::kStreams == 2) issue_stream(First{});
-        else if constexpr (C::kIssuers == 2) issue(First{}, Second{});
+        if constexpr (C::kIssuers == 2) issue(First{}, Second{});
         else issue(First{}, All{});
       } else if (warp == kSecondMmaWarp) {
-        if constexpr (C::kStreams == 2) issue_stream(Second{});
-        else if constexpr (C::kIssuers == 2) issue(Second{}, All{});
+        if constexpr (C::kIssuers == 2) issue(Second{}, All{});
       }
     }
     fence_before();
