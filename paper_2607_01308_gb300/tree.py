@@ -113,6 +113,15 @@ class QTree:
         return self
 
 
+_ROWS = "q and k must be bf16 [rows, heads, head_dim] of the same rows and head_dim, contiguous in it, on the context's device"
+
+
+def _weight(t, bf16, d: int, device: int) -> int:
+    if t.dtype is not bf16 or t.dim() != 1 or t.numel() != d or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError("weights must be contiguous bf16 [head_dim] on the context's device")
+    return t.data_ptr()
+
+
 def rotate_qk(ctx: Context, q, k, positions, q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None, k_out=None,
               stream=None) -> Tuple[object, object]:
     """(q_out, k_out): every head's row of q and k (bf16 CUDA tensors [rows, heads, head_dim], head_dim contiguous; views of a
@@ -120,38 +129,41 @@ def rotate_qk(ctx: Context, q, k, positions, q_weight=None, k_weight=None, eps: 
     positions [rows] (int32), as the keys of a fragment are, with the context's rope_theta. Either of q and k may be None. q_out
     and k_out are made if not given, on `stream`; they may be q and k themselves."""
     import torch
-    bf16, device = torch.bfloat16, ctx.device
-    like = q if q is not None else k
-    _require(like is not None, "q or k must be given")
-    rows, d = like.shape[0], like.shape[-1]
-    if positions.dtype is not torch.int32 or positions.dim() != 1 or not positions.is_contiguous() or positions.numel() != rows or positions.get_device() != device:
+    _require(q is not None or k is not None, "q or k must be given")
+    bf16, device, shape = torch.bfloat16, ctx.device, (k if q is None else q).shape
+    rows, d = shape[0], shape[-1]
+    if (positions.dtype is not torch.int32 or positions.dim() != 1 or not positions.is_contiguous() or positions.numel() != rows or
+            positions.get_device() != device):
         raise ValueError("positions must be a contiguous int32 vector with one for each row, on the context's device")
-    pointers, strides, heads, outs = [], [], [], []
-    for x, out, weight in ((q, q_out, q_weight), (k, k_out, k_weight)):
-        if x is None:
-            _require(out is None and weight is None, "an output or a weight without its rows")
-            pointers.append((0, 0, 0))
-            strides.append((0, 0, 0, 0))
-            heads.append(0)
-            outs.append(None)
-            continue
-        shape = x.shape
-        if x.dtype is not bf16 or len(shape) != 3 or shape[0] != rows or shape[2] != d or x.stride(2) != 1 or x.get_device() != device:
-            raise ValueError("q and k must be bf16 [rows, heads, head_dim] of the same rows and head_dim, contiguous in it, on the context's device")
-        if out is None:
-            out = _new_on(stream, x)
-        elif out.dtype is not bf16 or out.shape != shape or out.stride(2) != 1 or out.get_device() != device:
-            raise ValueError("q_out and k_out must be like q and k")
-        if weight is not None and (weight.dtype is not bf16 or weight.dim() != 1 or weight.numel() != d or not weight.is_contiguous() or
-                                   weight.get_device() != device):
-            raise ValueError("weights must be contiguous bf16 [head_dim] on the context's device")
-        pointers.append((x.data_ptr(), out.data_ptr(), 0 if weight is None else weight.data_ptr()))
-        strides.append(_strides(x, 2, 8) + _strides(out, 2, 8))
-        heads.append(shape[1])
-        outs.append(out)
-    (qp, qo, qw), (kp, ko, kw) = pointers
-    qs, ks = strides
-    desc = _pack_rows(qp, kp, qo, ko, qw, kw, positions.data_ptr(), qs[0], qs[1], ks[0], ks[1], qs[2], qs[3], ks[2], ks[3], rows,
-                      heads[0], heads[1], d, eps, 0)
-    _check(lib.cm_qk_rotate(ctx.handle, desc, _stream_handle(stream)))
-    return outs[0], outs[1]
+    q_in = q_to = qw = q_row = q_head = q_to_row = q_to_head = q_heads = 0
+    k_in = k_to = kw = k_row = k_head = k_to_row = k_to_head = k_heads = 0
+    if q is not None:
+        if q.dtype is not bf16 or len(shape) != 3 or q.stride(2) != 1 or q.get_device() != device:
+            raise ValueError(_ROWS)
+        if q_out is None:
+            q_out = _new_on(stream, q)
+        elif q_out.dtype is not bf16 or q_out.shape != shape or q_out.stride(2) != 1 or q_out.get_device() != device:
+            raise ValueError("q_out must be like q")
+        if q_weight is not None:
+            qw = _weight(q_weight, bf16, d, device)
+        q_in, q_to, q_heads = q.data_ptr(), q_out.data_ptr(), shape[1]
+        (q_row, q_head), (q_to_row, q_to_head) = _strides(q, 2, 8), _strides(q_out, 2, 8)
+    else:
+        _require(q_out is None and q_weight is None, "q_out or q_weight without q")
+    if k is not None:
+        shape = k.shape
+        if k.dtype is not bf16 or len(shape) != 3 or shape[0] != rows or shape[2] != d or k.stride(2) != 1 or k.get_device() != device:
+            raise ValueError(_ROWS)
+        if k_out is None:
+            k_out = _new_on(stream, k)
+        elif k_out.dtype is not bf16 or k_out.shape != shape or k_out.stride(2) != 1 or k_out.get_device() != device:
+            raise ValueError("k_out must be like k")
+        if k_weight is not None:
+            kw = _weight(k_weight, bf16, d, device)
+        k_in, k_to, k_heads = k.data_ptr(), k_out.data_ptr(), shape[1]
+        (k_row, k_head), (k_to_row, k_to_head) = _strides(k, 2, 8), _strides(k_out, 2, 8)
+    else:
+        _require(k_out is None and k_weight is None, "k_out or k_weight without k")
+    _check(lib.cm_qk_rotate(ctx.handle, _pack_rows(q_in, k_in, q_to, k_to, qw, kw, positions.data_ptr(), q_row, q_head, k_row, k_head, q_to_row,
+                                                   q_to_head, k_to_row, k_to_head, rows, q_heads, k_heads, d, eps, 0), _stream_handle(stream)))
+    return q_out, k_out
