@@ -223,6 +223,19 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
             if (b.block < 0) continue;
             const unsigned char *k_at = ring + stage * C::kStageBytes, *v_at = k_at + 16 * D;
 
+            // what of the request's own rows the rows see, in its last tiles: on its way while the scores are computed
+            uint32_t seen[NT][2];
+            if (TREE && token + 16 > least) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int n = w.row_tile * C::kRows + nt * 8 + 2 * t + b;
+                        seen[nt][b] = 0;
+                        if (n < w.rows)
+                            seen[nt][b] = tree_window(p.tree + (int64_t)(w.row0 + n / p.group) * p.tree_words, p.tree_words, token - w.first);
+                    }
+            }
             float s[NT][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
@@ -252,14 +265,10 @@ __global__ void __launch_bounds__(kThreads, Decode<D, FORMAT, NT>::kBlocksPerSm)
                 s[nt][2] = fmaf(s[nt][2], f0, b.v_log2);
                 s[nt][3] = fmaf(s[nt][3], f1, b.v_log2);
                 if (TREE && token + 16 > least) {
-                    // rare (the last tiles of a request), so that nothing of it is kept in registers
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        const int n = w.row_tile * C::kRows + nt * 8 + 2 * t + b;
-                        uint32_t seen = 0;
-                        if (n < w.rows) seen = tree_window(p.tree + (int64_t)(w.row0 + n / p.group) * p.tree_words, p.tree_words, token - w.first);
-                        if (!(seen >> g & 1) || token + g >= w.kv) s[nt][b] = -INFINITY;
-                        if (!(seen >> (g + 8) & 1) || token + g + 8 >= w.kv) s[nt][2 + b] = -INFINITY;
+                        if (!(seen[nt][b] >> g & 1) || token + g >= w.kv) s[nt][b] = -INFINITY;
+                        if (!(seen[nt][b] >> (g + 8) & 1) || token + g + 8 >= w.kv) s[nt][2 + b] = -INFINITY;
                     }
                 } else if (token + 16 > least) {
                     if (token + g >= limit[nt][0]) s[nt][0] = -INFINITY;
