@@ -593,7 +593,7 @@ cm_status cm_qcache_workspace(cm_context *ctx, int32_t head_dim, int64_t *out_by
  * The rows of request r are row_starts[r] .. row_starts[r + 1] - 1 of a batch. Its row 0 is the root, the token that
  * the step before has chosen; parents[row] is the place, among its request's rows, of the row that it was drafted behind: before its
  * own, or it counts as having none (negative: behind the context alone). All of these calls enqueue one kernel
- * (cm_qcache_attend_tree: as cm_qcache_attend), allocate nothing, and can be captured in a CUDA graph. As
+ * (cm_qcache_attend_tree two where cm_qcache_attend does, at head_dim 128 from 17 rows on too), allocate nothing, and can be captured in a CUDA graph. As
  * with the calls above the host never reads DEVICE arrays, entries that name nothing are left out rather than followed, and distinct
  * arguments must not overlap unless said otherwise. */
 

@@ -12,7 +12,9 @@
 // (layer, head, K or V) of a request block by block, and reads 16 rows or so before it writes them, never reads what it
 // has written. A thread block looks up where a request's rows lie once, for several layers and heads. One more thread
 // block adds up the lengths and lists the blocks given back. Bound by the chain of dependent reads (lengths, path,
-// table, codes and scales): a step of a few accepted rows moves little.
+// table, codes and scales), then by the tokens that stay in a block whose scale grows, which are most of the traffic: 64 requests,
+// 36 layers of 8 heads of 128, about two rows moved in each: 10.0 us; four heads to a warp 9.9 there, but 4.4 instead of 3.5
+// for 6 requests of 4 layers; one head 10.9.
 #include "cm_tree_kernels.h"
 
 #include "cm_qcache_codes.h"

@@ -19,7 +19,14 @@
 // always have a tile at hand while the tensor cores take the last one's weights. Products of 128 x 64 leave
 // a third of the tensor cores' time to the operands' way from shared memory; with tiles of 128 tokens, for
 // which there is one buffer, softmax and products wait for each other (513 us against 464 for the chunk
-// below). The softmax warps take registers over from the others. Work is cut as in qcache_attention.cu, over
+// below). The softmax warps take registers over from the others.
+//
+// Trees, which have few rows to a kv head, mostly have one query tile, and a second one's place and half of the softmax warps to spare: these take
+// every second kv tile (two streams, each with scores, maximum, sum and output of its own, joined when a segment
+// ends), and a tile is loaded by one or two warps. 32 requests of 4,096 tokens, 64 rows, 8 kv heads: head_dim 128 89 us instead of
+// 118 with the other half idle, 64 69 instead of 93, 32 63 instead of 79. 64 trees over 600 to 12,000 tokens: 163 us (202).
+//
+// Work is cut as in qcache_attention.cu, over
 // kv tiles that the rows of a tile may see at all; a second, small kernel joins the ranges that were cut
 // between thread blocks, over the whole GPU (one thread block alone took 95 us for 256 rows in 19 parts).
 //
@@ -893,7 +900,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             if constexpr (C::kStreams == 2) {
                 // A tile for a warp (head_dim 128: for two) in turn, so that what a tile costs besides its codes (three waits, a fence) is
                 // not spent by each of four. The next tile's codes are asked for together, when all of this one have been used: a load that
-                // is waited for is waited for with those that were asked for after it.
+                // is waited for is waited for with those that were asked for after it. (64 rows of head_dim 128 as above, at the time of
+                // 96 us: refilled one by one 115; 16 loads a thread, a warp to a tile at head_dim 128 too, 111, as they pass the instruction
+                // caches; asynchronous copies through shared memory, 48 KB of them on their way, 101.)
                 constexpr int kWarpsOf = C::kTileWarps, kTurns = kLoadWarps / kWarpsOf, kStep = 32 * kWarpsOf / kPerRow;   // tokens between a thread's loads
                 constexpr int kLoads = kTile / kStep;
                 const int64_t step8 = 8 * p.stride_token;
@@ -947,7 +956,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
                     }
                     fence_async_smem();
                     end_step(step);
-                    asm volatile("" ::: "memory");
+                    asm volatile("" ::: "memory");                // the loads below stay below
                     if (i + kTurns < tiles) ask(i + kTurns);
                 }
                 if (!is_v)
@@ -1249,12 +1258,17 @@ cudaError_t launch(const QcacheAttentionParams &p, int num_sms, int device, cuda
 
 size_t qcache_prefill_part_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
 
+// Trees: query tiles of 128 rows with two streams, or of 256, by the rows that a request is expected to have. 32 requests of 4,096 tokens:
+//   head_dim 128   256 rows 155 us in tiles of 256, 171 of 128 (64 rows: 118 and 89), so a last tile that is half empty makes those of
+//                  128 the faster ones up to 7 of them
+//   head_dim 64    256 rows 127 and 129 us, 32 114 and 117; five requests with 328 to 512 rows 154 and 141: always those of 128
 cudaError_t launch_qcache_prefill(const QcacheAttentionParams &p, int rows_per_request, int num_sms, int device, cudaStream_t stream) {
+    const int tiles = (int)(((int64_t)rows_per_request + 127) / 128);
 #define CM_LAUNCH(D) \
     if (p.head_dim == D) { \
         constexpr int kTiles = Shape<D>::kQTiles; \
         if (!p.tree) return launch<D, false, kTiles>(p, num_sms, device, stream); \
-        return rows_per_request <= 128 ? launch<D, true, 1>(p, num_sms, device, stream) : launch<D, true, kTiles>(p, num_sms, device, stream); \
+        return D < 128 || (tiles % 2 && tiles < 8) ? launch<D, true, 1>(p, num_sms, device, stream) : launch<D, true, kTiles>(p, num_sms, device, stream); \
     }
     CM_LAUNCH(32) CM_LAUNCH(64) CM_LAUNCH(128) CM_LAUNCH(256)
 #undef CM_LAUNCH
