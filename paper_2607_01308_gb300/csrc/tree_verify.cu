@@ -12,16 +12,16 @@
 // are fp32, each operation rounded alone; a sum adds the whole multiples of 2^-42 that its elements reach, in 64-bit
 // integers (up to 2^20 elements of at most 1: below 2^62), and is exact. Tests multiply in fp64.
 //
-// A cluster of thread blocks has a request. Each block reads, at once, what the walk may ask of single
-// elements (the probabilities of every drafted token at its parent) and walks for itself, so that blocks only meet
+// A cluster of thread blocks has a request. What the walk may ask of single elements (the probabilities of every
+// drafted token at its parent) is read at once, and each block walks for itself, so that blocks only meet
 // where a whole row has to be summed: after a rejection, and at the end. Then each takes a share of the vocabulary,
 // and the shares' sums are put into every block's shared memory. The last share's sums lead to the token: the block,
 // its warp's piece, and the element within it, read once more.
 //
 // Bound by issue while all requests sum their first rows (some eleven instructions an element, which is as long as
 // its two rows take from HBM), then by the chain of a walk with several rejections: 64 trees over 152,000 tokens, up to four
-// rows to sum one after another, 42 us (1.2 pairs of rows a request are read: 92 MB); one such tree 19 us; 16 chains over 32,003
-// tokens without draft rows 7.6 us. Tried and no faster: four or six vectors on their way instead of three; blocks of 512 threads, which
+// rows to sum one after another, 43 us (1.2 pairs of rows a request are read: 92 MB); one such tree 19 us; 16 chains over 32,003
+// tokens without draft rows 7.7 us. Tried and no faster: four or six vectors on their way instead of three; blocks of 512 threads, which
 // leave less than a third of the requests room to walk (55 us).
 #include "cm_tree_kernels.h"
 
@@ -198,15 +198,47 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
     __shared__ int32_t out[kTreeMaxNodes];              // tokens taken out, without draft rows
     __shared__ uint64_t warp_sum[kWarps], block_sum[2][kMaxCluster], step_sum[kMaxSteps];
     __shared__ Walk walk;
+    __shared__ RequestRows rows_here;
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), r = blockIdx.x / blocks;
     after_kernels_before();
 
-    const RequestRows rows = request_rows(p.row_starts, r, p.total_rows);
+    // The first block reads what the walk goes by and puts it into each block's memory: the blocks' barriers only meet if all
+    // walk alike, whatever happens to the inputs meanwhile. (Every block reading for itself is no faster.)
+    cluster.barrier_arrive();                   // waited for before the first write to another block's memory
+    RequestRows given{};
+    if (rank == 0) given = request_rows(p.row_starts, r, p.total_rows);
+    const int m = min(given.n, p.max_nodes);
+    struct Node {
+        int parent, token;
+        float target, draft, accept;
+    };
+    auto read = [&](int i) {
+        const int a = p.parents[given.first + i], t = p.tokens[given.first + i];
+        if (a < 0 || a >= i || t < 0 || t >= p.vocab) return Node{-1, t, 0.f, 1.f, 0.f};
+        return Node{a, t, R::one(static_cast<const E *>(p.target) + (given.first + a) * p.target_stride + t),
+                    p.draft ? R::one(static_cast<const E *>(p.draft) + (given.first + a) * p.draft_stride + t) : 1.f, p.accept[given.first + i]};
+    };
+    auto put = [&](int i, const Node &x) {
+        for (int b = 0; b < blocks; ++b) {
+            cluster.map_shared_rank(parent, b)[i] = (int16_t)x.parent;
+            cluster.map_shared_rank(token, b)[i] = x.token;
+            cluster.map_shared_rank(target_at, b)[i] = x.target;
+            cluster.map_shared_rank(draft_at, b)[i] = x.draft;
+            cluster.map_shared_rank(accept_at, b)[i] = x.accept;
+        }
+    };
+    Node mine{};
+    if (tid < m) mine = read(tid);
+    cluster.barrier_wait();
+    if (tid < m) put(tid, mine);
+    for (int i = tid + kThreads; i < m; i += kThreads) put(i, read(i));
+    if (rank == 0 && tid < blocks) *cluster.map_shared_rank(&rows_here, tid) = given;
+    const float sample = p.sample[r];
+    cluster.sync();
+    const RequestRows rows = rows_here;
     const int n = min(rows.n, p.max_nodes);
-    const E *target = static_cast<const E *>(p.target) + rows.first * p.target_stride;
-    const E *draft = p.draft ? static_cast<const E *>(p.draft) + rows.first * p.draft_stride : nullptr;
     if (n == 0) {
         if (rank == 0 && tid == 0) {
             p.kept[r] = 0;
@@ -214,21 +246,8 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
         }
         return;
     }
-    const float sample = p.sample[r];
-    cluster.barrier_arrive();                   // waited for before the first write to another block's memory
-    for (int i = tid; i < n; i += kThreads) {
-        int a = p.parents[rows.first + i];
-        const int t = p.tokens[rows.first + i];
-        if (a < 0 || a >= i || t < 0 || t >= p.vocab) a = -1;
-        parent[i] = (int16_t)a;
-        token[i] = t;
-        if (a >= 0) {
-            target_at[i] = R::one(target + a * p.target_stride + t);
-            draft_at[i] = draft ? R::one(draft + a * p.draft_stride + t) : 1.f;
-            accept_at[i] = p.accept[rows.first + i];
-        }
-    }
-    __syncthreads();
+    const E *target = static_cast<const E *>(p.target) + rows.first * p.target_stride;
+    const E *draft = p.draft ? static_cast<const E *>(p.draft) + rows.first * p.draft_stride : nullptr;
     if (warp == 0) {
         int child = -1;
         for (int base = 1; base < n && child < 0; base += 32) {
@@ -241,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
         }
         __syncwarp();
     }
-    cluster.barrier_wait();
+    __syncthreads();
 
     // The block's share of a row, and its warps' pieces of it, one behind the other, in steps of 32 vectors. (A row
     // may begin within a vector.)
