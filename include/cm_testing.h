@@ -34,6 +34,12 @@ cm_status cm_testing_qcache_attend_withheld(cm_context *ctx, const cm_qcache *ca
                                             void *workspace, int64_t workspace_bytes, int32_t what,
                                             cm_stream_t stream);
 
+/* The same of cm_qcache_attend_tree. */
+cm_status cm_testing_qcache_attend_tree_withheld(cm_context *ctx, const cm_qcache *cache, int32_t layer,
+                                                 const cm_qcache_batch *batch, const cm_qcache_query *query,
+                                                 const uint32_t *mask, int32_t words, void *workspace, int64_t workspace_bytes,
+                                                 int32_t what, cm_stream_t stream);
+
 /* Bounds-checked builds of the library (compiled with -DCM_DEBUG_BOUNDS; build.py --bounds
  * writes libcm_bounds.so) test every global access of the render, content-address
  * and byte-comparison kernels against the buffer it belongs to (a fragment, an output, a level of the hash

@@ -112,7 +112,9 @@ cm_status attend(cm_context *ctx, const cm_qcache *cache, int32_t layer, const c
         const int64_t rows = (int64_t)(query->max_rows_per_request ? query->max_rows_per_request : query->total_rows) * group;
         return on_device(ctx, "attention launch", [&] {
             const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-            if (extras.withhold) return cm::launch_qcache_prefill(p, INT32_MAX, num_sms, cm::context_device(ctx), s);
+            if (extras.withhold)   // a tree's kernel goes by the rows, the others' is the one of long prompts
+                return cm::launch_qcache_prefill(p, (int)(extras.trees && rows < INT32_MAX ? rows : INT32_MAX), num_sms,
+                                                 cm::context_device(ctx), s);
             return cm::launch_qcache_attention(p, (int)(rows < INT32_MAX ? rows : INT32_MAX), num_sms,
                                                cm::context_device(ctx), s);
         });
@@ -244,6 +246,15 @@ cm_status cm_testing_qcache_attend_withheld(cm_context *ctx, const cm_qcache *ca
     if (what != cm::kQcacheWithholdQueries && what != cm::kQcacheWithholdEntries)
         return fail(CM_ERR_INVALID_ARG, "nothing that can be withheld");
     return attend(ctx, cache, layer, batch, query, workspace, workspace_bytes, stream, Extras{what, false, nullptr, 0});
+}
+
+cm_status cm_testing_qcache_attend_tree_withheld(cm_context *ctx, const cm_qcache *cache, int32_t layer,
+                                                 const cm_qcache_batch *batch, const cm_qcache_query *query,
+                                                 const uint32_t *mask, int32_t words, void *workspace, int64_t workspace_bytes,
+                                                 int32_t what, cm_stream_t stream) {
+    if (what != cm::kQcacheWithholdQueries && what != cm::kQcacheWithholdEntries)
+        return fail(CM_ERR_INVALID_ARG, "nothing that can be withheld");
+    return attend(ctx, cache, layer, batch, query, workspace, workspace_bytes, stream, Extras{what, true, mask, words});
 }
 
 cm_status cm_qcache_workspace(cm_context *ctx, int32_t head_dim, int64_t *out_bytes) {

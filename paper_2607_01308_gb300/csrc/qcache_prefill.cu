@@ -512,6 +512,7 @@ struct Barriers {
     uint64_t s_full[2][2], p_full[2][2];      // query tile, score buffer
     uint64_t o_done[2];                       // all but the segment's last tile is in the output
     uint64_t drained[2];                      // all that an issuing warp has issued is done
+    uint64_t halves;                          // the softmax warps of both streams
 };
 
 template <int D, int FORMAT, bool TREE, int QT>
@@ -580,6 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             bar_init(&bars.drained[i], 1);
         }
         for (int i = 0; i < C::kEntryGroups; ++i) bar_init(&bars.entry_empty[i], C::kIssuers);
+        bar_init(&bars.halves, kSoftmaxWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
     }
@@ -648,9 +650,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
         uint32_t o_phase = 0, done = 0;
         Parity scored;
         if constexpr (C::kStreams == 2) {
-            auto both_halves = [] {
+            uint32_t met = 0;
+            auto both_halves = [&] {
                 fence_before();
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(&bars.halves);
+                wait.warp(&bars.halves, met);
+                met ^= 1;
                 fence_after();
             };
             while (walk.next(p)) {
@@ -1268,7 +1274,8 @@ cudaError_t launch_qcache_prefill(const QcacheAttentionParams &p, int rows_per_r
     if (p.head_dim == D) { \
         constexpr int kTiles = Shape<D>::kQTiles; \
         if (!p.tree) return launch<D, false, kTiles>(p, num_sms, device, stream); \
-        return D < 128 || (tiles % 2 && tiles < 8) ? launch<D, true, 1>(p, num_sms, device, stream) : launch<D, true, kTiles>(p, num_sms, device, stream); \
+        if (D < 128 || (tiles % 2 && tiles < 8)) return launch<D, true, 1>(p, num_sms, device, stream); \
+        return launch<D, true, D < 128 ? 1 : kTiles>(p, num_sms, device, stream); \
     }
     CM_LAUNCH(32) CM_LAUNCH(64) CM_LAUNCH(128) CM_LAUNCH(256)
 #undef CM_LAUNCH

@@ -169,6 +169,38 @@ def test_streams(ctx):
             assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("what", [1, 2])
+@pytest.mark.parametrize("d,nodes", [(32, 40), (64, 40), (128, 40), (128, 150), (256, 40)])
+def test_waits_of_tree_attention_that_run_out(ctx, d, nodes, what):
+    """An arrival that never comes, in one thread block: the call ends, the host learns of it once, and the next call is right."""
+    block, tokens, heads = 16, 3000, 2
+    n = -(-tokens // block)
+    g = torch.Generator(device=DEV).manual_seed(d)
+    cache = cm.QCache(ctx, n, block, 1, heads, d)
+    batch = cm.QBatch(ctx, 1, n, nodes, block)
+    tree = cm.QTree(batch, nodes)
+    batch.block_table.copy_(torch.arange(n)[None].int())
+    batch.row_starts.copy_(_i32([0, nodes]))
+    batch.kv_lens.fill_(tokens)
+    batch.max_new = nodes
+    rows = torch.randn((1, heads, tokens, d), generator=g, device=DEV).bfloat16()
+    cache.append(rows, rows, torch.arange(tokens, device=DEV))
+    tree.plan(_i32([-1] + [i // 2 for i in range(nodes - 1)]), _i32([tokens - nodes]))
+    q = torch.randn((nodes, heads, d), generator=g, device=DEV).bfloat16()
+    want, _ = cache.attend(q, batch, tree=tree)
+    out = torch.zeros_like(q)
+    query = cm.cm_qcache_query(q=q.data_ptr(), out=out.data_ptr(), q_stride_row=heads * d, q_stride_head=d, out_stride_row=heads * d,
+                               out_stride_head=d, total_rows=nodes, num_q_heads=heads, max_rows_per_request=nodes, softmax_scale=d ** -0.5)
+    assert cm.lib.cm_testing_qcache_attend_tree_withheld(ctx.handle, cache._ref, 0, batch._ref, bytes(query), tree.mask.data_ptr(), tree.mask.shape[1],
+                                                         batch._workspace_ptr, batch._workspace_bytes, what,
+                                                         torch.cuda.current_stream().cuda_stream or None) == cm.Status.OK
+    with pytest.raises(cm.CMError) as e:
+        ctx.check()
+    assert e.value.status == cm.Status.ERR_TIMEOUT
+    assert torch.equal(cache.attend(q, batch, tree=tree)[0], want)
+    ctx.check()
+
+
 def test_repeated_calls_give_the_same_bits(ctx):
     runs = []
     for _ in range(3):
