@@ -18,11 +18,13 @@
 // and the shares' sums are put into every block's shared memory. The last share's sums lead to the token: the block,
 // its warp's piece, and the element within it, read once more.
 //
-// Bound by issue while all requests sum their first rows (some eleven instructions an element, which is as long as
-// its two rows take from HBM), then by the chain of a walk with several rejections: 64 trees over 152,000 tokens, up to four
-// rows to sum one after another, 43 us (1.2 pairs of rows a request are read: 92 MB); one such tree 19 us; 16 chains over 32,003
-// tokens without draft rows 7.7 us. Tried and no faster: four or six vectors on their way instead of three; blocks of 512 threads, which
-// leave less than a third of the requests room to walk (55 us).
+// While all requests sum their first rows, that takes as long as the rows take from HBM (and some eleven instructions an
+// element just as long); then it is the chain of a walk with several rejections, 4 us for each, in which a thread's own chain
+// through its share counts: two vectors at once take 5,900 cycles where one after the other takes 6,550. 64 trees over 152,000
+// tokens, up to four rows to sum one after another, 42 us (1.2 pairs of rows a request are read: 92 MB); one such tree 18 us; 16 chains
+// over 32,003 tokens without draft rows 7.3 us (7.6 with fp64 products for the children asked first: that pipe is slow).
+// Tried and no faster: more vectors on their way; blocks of 512 threads, which leave less than a third of the requests
+// room to walk (55 us).
 #include "cm_tree_kernels.h"
 
 #include <cooperative_groups.h>
@@ -37,7 +39,7 @@ constexpr int kMaxVocab = 1 << 20, kAlone = 4096;              // elements that 
 constexpr int kMaxSteps = kMaxVocab / (32 * 4 * 8 * kMaxCluster) + 1;   // of a warp, with eight of them to a block
 static_assert(kAlone / (32 * 4 * 8) + 1 <= kMaxSteps, "a smaller cluster's warps have no more");
 constexpr int kThreads = 256, kWarps = kThreads / 32;   // four blocks to an SM: 64 requests with a cluster of eight each are there at once
-constexpr int kAhead = 3, kSlot = 2 * kThreads * 16;    // vectors of each row that a thread has on their way, 24 KB of a block
+constexpr int kSlot = 2 * kThreads * 16;                // a vector of each row for every thread
 constexpr double kUnit = 0x1p-42;
 
 __device__ __forceinline__ float clean(float x) { return __saturatef(x); }      // to [0, 1], a NaN to 0
@@ -50,12 +52,20 @@ __device__ __forceinline__ float less(float w, float q, float z) {
     return rest;
 }
 
+// u q < w without rounding, for q and w in [0, 1]. A product that rounds to another value than w is on the same side of
+// it; else its rounding's error says. 2^60 keeps that error above the least fp32 value, unless w is 0.
+__device__ __forceinline__ bool product_below(float u, float q, float w) {
+    const float a = q * 0x1p60f, b = w * 0x1p60f, product = __fmul_rn(u, a);
+    return product < b || (product == b && __fmaf_rn(u, a, -product) < 0.f) || (u < 0.f && q > 0.f);
+}
+
 template <int TYPE>
 struct Row;
 template <>
 struct Row<CM_PROB_F32> {
     using Element = float;
     static constexpr int kVec = 4;            // elements of a vector
+    static constexpr int kAtOnce = 2, kAhead = 2;   // vectors of each row that a thread takes at once, and of those on their way (32 KB of a block)
     static __device__ __forceinline__ float one(const float *p) { return clean(*p); }
     static __device__ __forceinline__ void unpack(const uint4 &v, float (&x)[4]) {
         x[0] = clean(__uint_as_float(v.x)); x[1] = clean(__uint_as_float(v.y));
@@ -65,7 +75,7 @@ struct Row<CM_PROB_F32> {
 template <>
 struct Row<CM_PROB_BF16> {
     using Element = uint16_t;
-    static constexpr int kVec = 8;
+    static constexpr int kVec = 8, kAtOnce = 1, kAhead = 3;
     static __device__ __forceinline__ float one(const uint16_t *p) { return clean(__uint_as_float((uint32_t)*p << 16)); }
     static __device__ __forceinline__ void unpack(const uint4 &v, float (&x)[8]) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -101,6 +111,14 @@ __device__ __forceinline__ uint64_t whole(const float (&x)[N]) {
 __device__ __forceinline__ uint64_t whole(float x) {
     const float one[1] = {x};
     return whole(one);
+}
+
+// Sum over a warp's lanes of numbers below 2^59.
+__device__ __forceinline__ uint64_t over_warp(uint64_t x) {
+    constexpr uint32_t kLow = (1u << 27) - 1;
+    const uint32_t a = __reduce_add_sync(~0u, (uint32_t)x & kLow), b = __reduce_add_sync(~0u, (uint32_t)(x >> 27) & kLow),
+                   c = __reduce_add_sync(~0u, (uint32_t)(x >> 54));
+    return a + ((uint64_t)b << 27) + ((uint64_t)c << 54);
 }
 
 // Two elements in a 64-bit register, for the two-wide instructions.
@@ -177,7 +195,7 @@ struct Rest {
 
 // Where the walk is, in shared memory.
 struct Walk {
-    int node, child;              // the row, and its next child (-1: none)
+    int node, child;              // the row, and its next child (kTreeMaxNodes: none)
     int levels;                   // of z, with draft rows; tokens taken out, without
     int depth;                    // rows accepted so far, the first among them
     int64_t z;                    // in multiples of 2^-42
@@ -188,13 +206,15 @@ template <int TYPE>
 __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_constant__ TreeVerifyParams p) {
     using R = Row<TYPE>;
     using E = typename R::Element;
-    constexpr int kVec = R::kVec;
-    extern __shared__ __align__(16) unsigned char copies[];   // [kAhead][target, draft][thread] vectors
+    constexpr int kVec = R::kVec, kAtOnce = R::kAtOnce, kAhead = R::kAhead, kRing = kAhead * kAtOnce * kSlot;
+    extern __shared__ __align__(16) unsigned char copies[];   // [kAhead][kAtOnce][target, draft][thread] vectors
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(copies) + threadIdx.x * 16;
     __shared__ int16_t parent[kTreeMaxNodes], walked[kTreeMaxNodes];
     __shared__ int32_t token[kTreeMaxNodes];
     __shared__ float target_at[kTreeMaxNodes], draft_at[kTreeMaxNodes], accept_at[kTreeMaxNodes];
     __shared__ float level[kTreeMaxNodes];              // z of each subtraction at this node
+    __shared__ int32_t first_child[kTreeMaxNodes];      // kTreeMaxNodes: none
+    __shared__ bool accepted[kTreeMaxNodes];            // where nothing was rejected at its parent
     __shared__ int32_t out[kTreeMaxNodes];              // tokens taken out, without draft rows
     __shared__ uint64_t warp_sum[kWarps], block_sum[2][kMaxCluster], step_sum[kMaxSteps];
     __shared__ Walk walk;
@@ -206,6 +226,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
 
     // The first block reads what the walk goes by and puts it into each block's memory: the blocks' barriers only meet if all
     // walk alike, whatever happens to the inputs meanwhile. (Every block reading for itself is no faster.)
+    for (int i = tid; i < p.max_nodes; i += kThreads) first_child[i] = kTreeMaxNodes;
     cluster.barrier_arrive();                   // waited for before the first write to another block's memory
     RequestRows given{};
     if (rank == 0) given = request_rows(p.row_starts, r, p.total_rows);
@@ -248,18 +269,14 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
     }
     const E *target = static_cast<const E *>(p.target) + rows.first * p.target_stride;
     const E *draft = p.draft ? static_cast<const E *>(p.draft) + rows.first * p.draft_stride : nullptr;
-    if (warp == 0) {
-        int child = -1;
-        for (int base = 1; base < n && child < 0; base += 32) {
-            const unsigned found = __ballot_sync(~0u, base + lane < n && parent[min(base + lane, n - 1)] == 0);
-            if (found) child = base + __ffs(found) - 1;
-        }
-        if (lane == 0) {
-            walk = {0, child, 0, 1, (int64_t)1 << 42, false};
-            walked[0] = 0;
-        }
-        __syncwarp();
+    for (int i = tid; i < n; i += kThreads) {
+        const int a = parent[i];
+        if (a >= 0 && i < first_child[a]) atomicMin(&first_child[a], i);
+        accepted[i] = product_below(accept_at[i], draft_at[i], target_at[i]);
     }
+    if (tid == 0) walked[0] = 0;
+    __syncthreads();
+    if (tid == 0) walk = {0, first_child[0], 0, 1, (int64_t)1 << 42, false};
     __syncthreads();
 
     // The block's share of a row, and its warps' pieces of it, one behind the other, in steps of 32 vectors. (A row
@@ -278,36 +295,37 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
                     const unsigned found = __ballot_sync(~0u, base + lane < n && parent[min(base + lane, n - 1)] == w.node);
                     if (found) return base + __ffs(found) - 1;
                 }
-                return -1;
+                return kTreeMaxNodes;
             };
             while (true) {
                 const int c = w.child;
-                if (c < 0) {
+                if (c == kTreeMaxNodes) {
                     w.ends = true;
                     break;
                 }
                 float have = target_at[c];
-                double bar;
-                if (draft) {
+                bool yes;
+                if (w.levels == 0) {
+                    yes = accepted[c];          // z is 1
+                } else if (draft) {
                     const float q = draft_at[c], z = (float)((double)w.z * kUnit);
                     for (int k = 0; k < w.levels; ++k) have = less(have, q, level[k]);
-                    bar = __dmul_rn(__dmul_rn((double)accept_at[c], (double)q), (double)z);
+                    yes = __dmul_rn(__dmul_rn((double)accept_at[c], (double)q), (double)z) < (double)have;
                 } else {
                     for (int k = 0; k < w.levels; ++k)
                         if (out[k] == token[c]) have = 0.f;
-                    bar = __dmul_rn((double)accept_at[c], (double)w.z * kUnit);
+                    yes = __dmul_rn((double)accept_at[c], (double)w.z * kUnit) < (double)have;
                 }
-                if (bar < (double)have) {
+                if (yes) {
                     if (lane == 0) walked[w.depth] = (int16_t)c;
-                    w = {c, -1, 0, w.depth + 1, (int64_t)1 << 42, false};
-                    w.child = next_child(c);
+                    w = {c, first_child[c], 0, w.depth + 1, (int64_t)1 << 42, false};
                     continue;
                 }
                 w.child = next_child(c);
                 if (draft) {
                     if (lane == 0) level[w.levels] = (float)((double)w.z * kUnit);
                     ++w.levels;
-                    w.ends = w.child < 0;
+                    w.ends = w.child == kTreeMaxNodes;
                     break;                      // what is left of the row has to be summed
                 }
                 if (have > 0.f) {
@@ -337,6 +355,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
             const bool drawn = d_row && rest.levels > 0;
             const E *t_at = t_row + first + lane * kVec, *d_at = drawn ? d_row + first + lane * kVec : t_at;
             const float minus_z = drawn ? -level[0] : 0.f;
+            uint64_t sum = 0;
             uint32_t hi = 0, lo = 0;            // less kBits for each element, modulo 2^32
             // vectors on their way lie in shared memory, each for the thread that asked for it
             const int n = max(s1 - s0, 0);
@@ -345,61 +364,70 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
             int asked = 0;
             uint32_t to = ring, from = ring;
             auto ask = [&] {
-                if (asked < n) {
-                    copy16(to, t_at);
-                    if (drawn) copy16(to + kThreads * 16, d_at);
-                }
-                ++asked;
-                t_at += kStep;
-                d_at += kStep;
-                to = to == ring + (kAhead - 1) * kSlot ? ring : to + kSlot;
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (asked + j < n) {
+                        copy16(to + j * kSlot, t_at + j * kStep);
+                        if (drawn) copy16(to + j * kSlot + kThreads * 16, d_at + j * kStep);
+                    }
+                asked += kAtOnce;
+                t_at += kAtOnce * kStep;
+                d_at += kAtOnce * kStep;
+                to = to == ring + kRing - kAtOnce * kSlot ? ring : to + kAtOnce * kSlot;
                 asm volatile("cp.async.commit_group;" ::: "memory");
             };
             for (int i = 0; i < kAhead; ++i) ask();
+            // the row's ends, or all of rows that do not begin alike
 #pragma unroll 1
-            for (int s = 0; s < n; ++s) {
+            for (int i = 0; i < s0 + warp_steps - s1; ++i) {
+                const int e = first + (i < s0 ? i : s1 + i - s0) * kStep + lane * kVec;
+                float w[kVec];
+                if (e < p.vocab) sum += rest.get(e, w);
+            }
+            int taken = 0;
+#pragma unroll 1
+            for (; taken < n; taken += kAtOnce) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
-                float w[kVec], q[kVec];
-                R::unpack(load16(from), w);
-                uint64_t x[kVec / 2];
+                uint64_t x[kAtOnce][kVec / 2];
+                float w[kAtOnce][kVec], q[kAtOnce][kVec];
+                auto unpack = [&](int j, int row, float (&v)[kVec]) {   // zeros behind the last
+                    R::unpack(taken + j < n ? load16(from + j * kSlot + row * kThreads * 16) : make_uint4(0, 0, 0, 0), v);
+                };
 #pragma unroll
-                for (int k = 0; k < kVec / 2; ++k) x[k] = pair(w[2 * k], w[2 * k + 1]);
+                for (int j = 0; j < kAtOnce; ++j) {
+                    unpack(j, 0, w[j]);
+#pragma unroll
+                    for (int k = 0; k < kVec / 2; ++k) x[j][k] = pair(w[j][2 * k], w[j][2 * k + 1]);
+                }
                 if (drawn) {
-                    R::unpack(load16(from + kThreads * 16), q);
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j) unpack(j, 1, q[j]);
                     float z = minus_z;
                     for (int l = 1;; ++l) {
 #pragma unroll
-                        for (int k = 0; k < kVec / 2; ++k) x[k] = less2(x[k], pair(q[2 * k], q[2 * k + 1]), pair(z, z));
+                        for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+                            for (int k = 0; k < kVec / 2; ++k) x[j][k] = less2(x[j][k], pair(q[j][2 * k], q[j][2 * k + 1]), pair(z, z));
                         if (l == rest.levels) break;
                         z = -level[l];
                     }
                 }
-                from = from == ring + (kAhead - 1) * kSlot ? ring : from + kSlot;
+                from = from == ring + kRing - kAtOnce * kSlot ? ring : from + kAtOnce * kSlot;
 #pragma unroll
-                for (int k = 0; k < kVec / 2; ++k) split2(x[k], hi, lo);
+                for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+                    for (int k = 0; k < kVec / 2; ++k) split2(x[j][k], hi, lo);
                 ask();
             }
-            const uint32_t elements = (uint32_t)(n * kVec);
-            uint64_t sum = ((uint64_t)(hi - elements * kBits) << 21) + (lo - elements * kBits);
-            // the row's ends, or all of rows that do not begin alike
-            auto slowly = [&](int from, int to) {
-#pragma unroll 1
-                for (int s = from; s < to; ++s) {
-                    const int e = first + s * kStep + lane * kVec;
-                    float w[kVec];
-                    if (e < p.vocab) sum += rest.get(e, w);
-                }
-            };
-            slowly(0, s0);
-            slowly(s1, warp_steps);
+            const uint32_t elements = (uint32_t)(taken * kVec);
+            sum += ((uint64_t)(hi - elements * kBits) << 21) + (lo - elements * kBits);
             // without draft rows the steps above have counted the tokens that are taken out
             if (!d_row)
                 for (int l = 0; l < rest.levels; ++l) {
                     const int at = out[l] - first, step = at / kStep;
                     if (at >= 0 && step >= s0 && step < s1 && at % kStep / kVec == lane) sum -= whole(R::one(t_row + out[l]));
                 }
-#pragma unroll
-            for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+            sum = over_warp(sum);
             if (lane == 0) warp_sum[warp] = sum;
             __syncthreads();
             if (tid < blocks) {
@@ -442,20 +470,29 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
                 if (total == 0) p.next_token[r] = -1;
             }
         }
-        const double number = (double)clean(sample) * 0x1p32;
-        uint64_t point = __umul64hi(total, min((uint64_t)number, (uint64_t)0xffffffffu) << 32);
+        uint64_t point = __umul64hi(total, (uint64_t)__float2uint_rz(clean(sample) * 0x1p32f) << 32);
         if (total == 0 || point < before) return;
         point -= before;
         int piece = 0;
-        while (piece < kWarps && point >= warp_sum[piece]) point -= warp_sum[piece++];
+        uint64_t sums[kWarps];
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) sums[i] = warp_sum[i];
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i)
+            if (piece == i && point >= sums[i]) point -= sums[i], ++piece;
         if (piece == kWarps) return;            // another block's
         // its steps, shared by the block's warps
         const int first = begin + piece * warp_steps * kStep + lane * kVec - skew;   // this lane's
         float w[kVec];
         for (int s = warp; s < warp_steps; s += kWarps) {
-            uint64_t sum = rest.get(first + s * kStep, w);
-#pragma unroll
-            for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+            const int e = first + s * kStep;
+            if (e >= 0 && e < p.vocab) {        // all of them on their way before the first is waited for
+                asm volatile("prefetch.global.L1 [%0];" ::"l"(t_row + e));
+                if (draft) asm volatile("prefetch.global.L1 [%0];" ::"l"(d_row + e));
+            }
+        }
+        for (int s = warp; s < warp_steps; s += kWarps) {
+            const uint64_t sum = over_warp(rest.get(first + s * kStep, w));
             if (lane == 0) step_sum[s] = sum;
         }
         __syncthreads();
@@ -503,7 +540,7 @@ cudaError_t launch(const TreeVerifyParams &p, int blocks, cudaStream_t stream) {
     cudaLaunchConfig_t config{};
     config.gridDim = dim3((unsigned)p.requests * blocks);
     config.blockDim = dim3(kThreads);
-    config.dynamicSmemBytes = kAhead * kSlot;
+    config.dynamicSmemBytes = Row<TYPE>::kAhead * Row<TYPE>::kAtOnce * kSlot;
     config.stream = stream;
     config.attrs = attrs;
     config.numAttrs = 2;
