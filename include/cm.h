@@ -619,7 +619,7 @@ typedef struct cm_qk_rows {
     const int32_t *positions;                  /* DEVICE [num_rows], any int32 */
     int64_t q_stride_row, q_stride_head;       /* elements, multiples of 8 */
     int64_t k_stride_row, k_stride_head;
-    int64_t q_out_stride_row, q_out_stride_head;   /* head_dim at least where there are several */
+    int64_t q_out_stride_row, q_out_stride_head;   /* head_dim at least where there are several, the wider beyond all that the other reaches */
     int64_t k_out_stride_row, k_out_stride_head;
     int64_t num_rows;                          /* below 2^31 */
     int32_t num_q_heads, num_kv_heads;         /* 0 to 65535 */

@@ -18,6 +18,13 @@ bool overlap(const void *a, int64_t n, const void *b, int64_t m) {
     return a && b && n > 0 && m > 0 && x < y + (uintptr_t)m && y < x + (uintptr_t)n;
 }
 
+// Whether the wider of two strides (d at least, of several each) steps over all that the other reaches: rows of d elements do not meet then.
+bool apart(int64_t stride_a, int64_t n_a, int64_t stride_b, int64_t n_b, int64_t d) {
+    const bool a_first = stride_a < stride_b;
+    const int64_t inner = a_first ? stride_a : stride_b, outer = a_first ? stride_b : stride_a, n = a_first ? n_a : n_b;
+    return inner <= (outer - d) / (n - 1);
+}
+
 }  // namespace
 
 extern "C" {
@@ -78,9 +85,17 @@ cm_status cm_qk_rotate(cm_context *ctx, const cm_qk_rows *rows, cm_stream_t stre
         }
         const int64_t heads[2] = {rows->num_q_heads, rows->num_kv_heads};
         const int64_t out_row[2] = {rows->q_out_stride_row, rows->k_out_stride_row}, out_head[2] = {rows->q_out_stride_head, rows->k_out_stride_head};
-        for (int i = 0; i < 2; ++i)
-            if ((heads[i] && rows->num_rows > 1 && out_row[i] < rows->head_dim) || (heads[i] > 1 && out_head[i] < rows->head_dim))
+        const int64_t in_row[2] = {rows->q_stride_row, rows->k_stride_row}, in_head[2] = {rows->q_stride_head, rows->k_stride_head};
+        const void *in[2] = {rows->q, rows->k}, *out[2] = {rows->q_out, rows->k_out};
+        for (int i = 0; i < 2; ++i) {
+            const int64_t n_row = heads[i] ? rows->num_rows : 0, n_head = heads[i];
+            const bool some_rows = n_row > 1, some_heads = n_head > 1;
+            if ((some_rows && out_row[i] < rows->head_dim) || (some_heads && out_head[i] < rows->head_dim) ||
+                (some_rows && some_heads && !apart(out_row[i], n_row, out_head[i], n_head, rows->head_dim)))
                 return fail(CM_ERR_INVALID_ARG, "rows of an output lie on one another");
+            if (in[i] == out[i] && ((some_rows && in_row[i] != out_row[i]) || (some_heads && in_head[i] != out_head[i])))
+                return fail(CM_ERR_INVALID_ARG, "in place, the strides must be alike");
+        }
         cm::RotateParams p{};
         p.in[0] = static_cast<const uint16_t *>(rows->q);
         p.in[1] = static_cast<const uint16_t *>(rows->k);

@@ -850,14 +850,24 @@ def test_refusals_of_the_library(ctx):
             setattr(r, name, value)
         cm.cm_qk_rotate(ctx.handle, r)
 
+    elsewhere = torch.zeros(2048, dtype=torch.bfloat16, device=DEV)
+    other = elsewhere.data_ptr()
     rows()
+    rows(q_out=other, q_out_stride_row=64, q_out_stride_head=320)
+    rows(q_out=other, q_out_stride_row=136, q_out_stride_head=72)
+    rows(num_rows=1, q_out_stride_row=0)
+    rows(num_q_heads=1, q_out_stride_head=0)
     for status, kw in ((S.ERR_INVALID_ARG, {"head_dim": 96}), (S.ERR_INVALID_ARG, {"head_dim": 8}), (S.ERR_INVALID_ARG, {"head_dim": 1024}),
                        (S.ERR_INVALID_ARG, {"reserved": 1}), (S.ERR_INVALID_ARG, {"num_rows": -1}), (S.ERR_INVALID_ARG, {"num_rows": 2 ** 31}),
                        (S.ERR_INVALID_ARG, {"eps": -1.0}), (S.ERR_INVALID_ARG, {"eps": float("nan")}), (S.ERR_INVALID_ARG, {"eps": float("inf")}),
                        (S.ERR_INVALID_ARG, {"num_kv_heads": 1}), (S.ERR_INVALID_ARG, {"q_out": None}), (S.ERR_INVALID_ARG, {"positions": None}),
                        (S.ERR_ALIGNMENT, {"q": q.data_ptr() + 2}), (S.ERR_ALIGNMENT, {"q_stride_row": 132}), (S.ERR_INVALID_ARG, {"q_stride_head": -64}),
                        (S.ERR_ALIGNMENT, {"q_weight": q.data_ptr() + 8}), (S.ERR_INVALID_ARG, {"q_out_stride_head": 32}),
-                       (S.ERR_INVALID_ARG, {"q_out_stride_row": 0}), (S.ERR_INVALID_ARG, {"num_q_heads": 65536})):
+                       (S.ERR_INVALID_ARG, {"q_out_stride_row": 0}), (S.ERR_INVALID_ARG, {"num_q_heads": 65536}),
+                       # rows that lie on one another, in place with other strides
+                       (S.ERR_INVALID_ARG, {"q_out": other, "q_out_stride_row": 64}), (S.ERR_INVALID_ARG, {"q_out": other, "q_out_stride_row": 120}),
+                       (S.ERR_INVALID_ARG, {"q_out": other, "q_out_stride_row": 64, "q_out_stride_head": 312}),
+                       (S.ERR_INVALID_ARG, {"q_out_stride_row": 136}), (S.ERR_INVALID_ARG, {"q_out_stride_head": 72, "q_out_stride_row": 136})):
         refused(status, lambda: rows(**kw))
 
     p = torch.zeros((5, 10), device=DEV)
