@@ -24,7 +24,7 @@
 // Trees, which have few rows to a kv head, mostly have one query tile, and a second one's place and half of the softmax warps to spare: these take
 // every second kv tile (two streams, each with scores, maximum, sum and output of its own, joined when a segment
 // ends), and a tile is loaded by one or two warps. 32 requests of 4,096 tokens, 64 rows, 8 kv heads: head_dim 128 89 us instead of
-// 118 with the other half idle, 64 69 instead of 93, 32 63 instead of 79. 64 trees over 600 to 12,000 tokens: 163 us (202).
+// 118 with the other half idle, 64 69 instead of 93, 32 63 instead of 79. 64 trees over 600 to 12,000 tokens: 165 us (202).
 //
 // Work is cut as in qcache_attention.cu, over
 // kv tiles that the rows of a tile may see at all; a second, small kernel joins the ranges that were cut
@@ -581,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const __grid_const
             bar_init(&bars.drained[i], 1);
         }
         for (int i = 0; i < C::kEntryGroups; ++i) bar_init(&bars.entry_empty[i], C::kIssuers);
-        bar_init(&bars.halves, kSoftmaxWarps);
+        if (C::kStreams == 2) bar_init(&bars.halves, kSoftmaxWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
     }
