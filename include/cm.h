@@ -689,8 +689,9 @@ cm_status cm_tree_verify(cm_context *ctx, const cm_tree_drafts *drafts, cm_strea
  *   context_lens    [R]: as given to cm_qcache_schedule (negative counts as 0)
  *   lens_out        [R]: context_lens[r] + the rows of its path; none of the arrays that are read. batch is not changed: its tables go
  *                   on naming the blocks that are given back, until cm_qcache_schedule writes others over them
- *   freed           [max_freed]: the blocks of which no token is left, ceil(lens_out / B) .. ceil(kv_len / B) - 1 of
- *                   each request's table row, in the requests' order; -1 behind the last. requests + total_rows / B are enough
+ *   freed           [max_freed]: the blocks of which no token is left, those that entries ceil(lens_out / B) .. ceil(kv_len / B) - 1 of
+ *                   each request's table row name, in the requests' order; -1 behind the last. An entry that names no block of the pool
+ *                   (cm_qcache_schedule writes -1 where the free list has ended) is none of them. requests + total_rows / B are enough
  *   freed_count     [1]: their number (freed holds as many as fit)
  * A block must not be named by two requests where one of them moves rows in it. Limits: R <= 16384. */
 cm_status cm_qcache_keep(cm_context *ctx, const cm_qcache *cache, const cm_qcache_batch *batch, const int32_t *context_lens,

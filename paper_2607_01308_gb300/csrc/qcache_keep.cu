@@ -145,14 +145,17 @@ __device__ __forceinline__ void move_rows(const QcacheKeepParams &p, int pair0, 
     }
 }
 
-// The last thread block: new lengths, and the blocks that no token is left in, in the requests' order.
+// The last thread block: new lengths, and the blocks of the pool that no token is left in, in the requests' order. (A table has entries
+// that name none where the free list was too short; on a free list they would be handed out in place of blocks that are there.)
 __device__ __forceinline__ void count_blocks(const QcacheKeepParams &p) {
     __shared__ int64_t warp_sum[kWarps];
     const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     int64_t total = 0;
     for (int r0 = 0; r0 < p.requests; r0 += kThreads) {
         const int r = r0 + tid;
-        int64_t begin = 0, n = 0;
+        int64_t n = 0, given = 0;              // table entries behind the last that is needed; those that name a block
+        const int32_t *entries = nullptr;
+        auto named = [&](int32_t b) { return b >= 0 && b < p.num_blocks; };
         if (r < p.requests) {
             const Request q = request(p, r);
             const int most = min(min(max(p.kept[r], 0), q.n), kTreeMaxNodes);
@@ -164,10 +167,12 @@ __device__ __forceinline__ void count_blocks(const QcacheKeepParams &p) {
             }
             const int64_t length = q.context + kept, mask = ((int64_t)1 << p.log2_block) - 1;
             p.lens_out[r] = (int32_t)min(length, (int64_t)INT32_MAX);
-            begin = (length + mask) >> p.log2_block;
+            const int64_t begin = (length + mask) >> p.log2_block;
             n = max(((q.kv + mask) >> p.log2_block) - begin, (int64_t)0);
+            entries = p.block_table + r * p.table_width + begin;
+            for (int64_t j = 0; j < n; ++j) given += named(entries[j]);
         }
-        int64_t upto = n;
+        int64_t upto = given;
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) {
             const int64_t x = __shfl_up_sync(~0u, upto, d);
@@ -175,13 +180,16 @@ __device__ __forceinline__ void count_blocks(const QcacheKeepParams &p) {
         }
         if (lane == 31) warp_sum[warp] = upto;
         __syncthreads();
-        int64_t at = total + upto - n;
+        int64_t at = total + upto - given;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             if (w < warp) at += warp_sum[w];
             total += warp_sum[w];
         }
-        for (int64_t j = 0; j < n && at + j < p.max_freed; ++j) p.freed[at + j] = p.block_table[r * p.table_width + begin + j];
+        for (int64_t j = 0; j < n && at < p.max_freed; ++j) {
+            const int32_t b = entries[j];
+            if (named(b)) p.freed[at++] = b;
+        }
         __syncthreads();
     }
     for (int64_t j = total + tid; j < p.max_freed; j += kThreads) p.freed[j] = -1;
