@@ -692,7 +692,9 @@ cm_status cm_tree_verify(cm_context *ctx, const cm_tree_drafts *drafts, cm_strea
  *   freed           [max_freed]: the blocks of which no token is left, those that entries ceil(lens_out / B) .. ceil(kv_len / B) - 1 of
  *                   each request's table row name, in the requests' order; -1 behind the last. An entry that names no block of the pool
  *                   (cm_qcache_schedule writes -1 where the free list has ended) is none of them. requests + total_rows / B are enough
- *   freed_count     [1]: their number (freed holds as many as fit)
+ *                   where all rows had room: cm_qcache_schedule takes blocks for those that max_rows cuts off too, and with
+ *                   them there are up to requests * table_width
+ *   freed_count     [1]: their number; freed holds as many as fit, the tables go on naming the others
  * A block must not be named by two requests where one of them moves rows in it. Limits: R <= 16384. */
 cm_status cm_qcache_keep(cm_context *ctx, const cm_qcache *cache, const cm_qcache_batch *batch, const int32_t *context_lens,
                          const int32_t *path, const int32_t *kept, int32_t total_rows, int32_t *lens_out, int32_t *freed,

@@ -22,7 +22,12 @@ class QTree:
       lens [R] int32, freed [max_freed] int32, freed_count [1] int64: written by QCache.keep(), the tokens that
       each request holds then, the blocks that none is left in (-1 behind the last) and their number
 
-    max_nodes: the most rows of one request, to 256; rows behind it are seen by none and never accepted. A program with masks or
+    max_nodes: the most rows of one request, to 256; rows behind it are seen by none and never accepted. max_freed: entries of
+    freed, if not one for each request and one for each block_size rows of the batch. Those hold the blocks of any step whose rows
+    all had room in the batch. schedule() takes blocks for the rows that max_rows cuts off too, which keep() gives back:
+    a program whose steps may be cut asks for num_requests * table_width, which is always enough. freed_count counts
+    what there was no room for as well; those blocks are still named by the table, behind what lens needs, until schedule()
+    writes others over them. A program with masks or
     paths of its own writes into these tensors instead. One tree is used by one stream at a time; its memory is
     given back as a QBatch's is."""
 
@@ -30,15 +35,16 @@ class QTree:
     next_token, lens = _fixed("_next_token"), _fixed("_lens")
     freed, freed_count = _fixed("_freed"), _fixed("_freed_count")
 
-    def __init__(self, batch: QBatch, max_nodes: int):
+    def __init__(self, batch: QBatch, max_nodes: int, max_freed: Optional[int] = None):
         import torch
         _require(1 <= max_nodes <= 256, "max_nodes must be in [1, 256]")
+        _require(max_freed is None or 0 <= max_freed < 1 << 31, "max_freed must be in [0, 2^31 - 1]")
         dev = batch.row_starts.device
         rows, n = batch.slot_map.numel(), batch._num_requests
         self.batch, self.ctx = batch, batch.ctx
         self.max_nodes = max_nodes
         self._device, self._max_rows, self._num_requests = batch._device, rows, n
-        self._words, self._max_freed = (max_nodes + 31) // 32, n + rows // batch._c.block_size
+        self._words, self._max_freed = (max_nodes + 31) // 32, n + rows // batch._c.block_size if max_freed is None else max_freed
         self._int32, self._fp32, self._bf16 = torch.int32, torch.float32, torch.bfloat16
 
         def whole(*shape, fill=-1, dtype=torch.int32):

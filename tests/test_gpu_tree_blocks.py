@@ -1,5 +1,5 @@
 """What a step over trees gives back of the cache's blocks, and that none is lost: blocks that the free list did not have, table
-entries that name none of the pool's. Blocks and lengths are compared exactly."""
+entries that name none of the pool's, requests that were cut short. Blocks and lengths are compared exactly."""
 import numpy as np
 import pytest
 import torch
@@ -100,3 +100,38 @@ def test_no_block_is_lost_where_the_free_list_is_too_short(ctx, seed):
             free = torch.cat([free, _i32(table[r][:-(-context[r] // block)])])
             context[r] = 0
     assert short >= 2
+
+
+@pytest.mark.parametrize("old,new,rows,block,width", [
+    ([0], [160], 16, 16, 12), ([5, 0, 40], [30, 100, 20], 40, 16, 8), ([0, 17, 3, 9], [70, 70, 70, 70], 1, 16, 8),
+    ([3, 60, 20], [500, 40, 1], 90, 16, 6), ([10, 0], [33, 64], 200, 32, 4)])
+def test_blocks_of_rows_that_were_cut_are_given_back(ctx, old, new, rows, block, width):
+    """What a step has taken is held or given back, also for rows that had no room in the batch or in the table."""
+    R = len(old)
+    cache = cm.QCache(ctx, R * width + 5, block, 1, 1, 16)
+    pool = np.random.default_rng(rows).permutation(R * width).tolist()
+    table = []
+    for c in old:
+        need = -(-c // block)
+        table.append(pool[:need] + [-1] * (width - need))
+        pool = pool[need:]
+    batch = cm.QBatch(ctx, R, width, rows, block)
+    batch.block_table.copy_(_i32(table))
+    tree, few = cm.QTree(batch, 256, max_freed=R * width), cm.QTree(batch, 256)
+    assert tree.freed.numel() == R * width and few.freed.numel() == R + rows // block
+    batch.schedule(_i32(old), _i32(new), _i32(pool))
+    starts = batch.row_starts.tolist()
+    paths = [list(range(0, min(n, 256), 2)) for n in np.diff(starts)]
+    for t in (tree, few):
+        _put(t, starts, paths)
+        cache.keep(batch, t, _i32(old))
+    table, taken, count = batch.block_table.tolist(), pool[:int(batch.counts[0])], int(tree.freed_count)
+    lens = tree.lens.tolist()
+    assert all(c <= n <= c + len(p) for c, n, p in zip(old, lens, paths))
+    held = [b for t, c, n in zip(table, old, lens) for b in t[-(-c // block):-(-n // block)]]
+    freed = tree.freed.tolist()
+    assert sorted(held + freed[:count]) == sorted(taken) and freed[count:] == [-1] * (R * width - count)
+    # a list that is too short holds the first of them, and the number of all
+    assert few.freed_count.item() == count and few.freed.tolist() == (freed + [-1] * few.freed.numel())[:few.freed.numel()]
+    if sum(new) <= rows:
+        assert count <= few.freed.numel()
