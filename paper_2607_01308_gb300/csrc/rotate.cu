@@ -37,6 +37,32 @@ __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
     return make_uint4(to_bf16(x[0], x[1]), to_bf16(x[2], x[3]), to_bf16(x[4], x[5]), to_bf16(x[6], x[7]));
 }
 
+constexpr uint32_t kLeastMean = (127 - 60) << 23, kLargestMean = (127 + 100) << 23;   // as bits
+
+// x / sqrt(mean x^2 + eps) of a row whose mean, eps with it, is too small or too large for sums of its squares: these
+// are taken of x times 2^80 or 2^-70. Small: eps and all elements are below 2^-25, their squares below 2^110, and at 2^-106 or more
+// (bf16 ends at 2^-133). Large: squares to 2^116, of which those that vanish are below the mean's rounding. All lanes of the warp come here,
+// `odd`: those whose row it is.
+template <int D>
+__device__ __forceinline__ void normed_far(float (&a)[8], float (&b)[8], float mean, float eps, bool odd) {
+    const bool small = mean < 1.f;
+    const float by = small ? 0x1p80f : 0x1p-70f;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = a[i] * by, y = b[i] * by;
+        sum = fmaf(x, x, fmaf(y, y, sum));
+    }
+#pragma unroll
+    for (int d = D / 32; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+    if (!odd) return;
+    const float scaled = sum * (1.f / D) + eps * by * by, root = scaled == 0.f ? 0.f : rsqrtf(scaled);
+    // small elements are made larger, large ones meet a smaller factor: neither passes fp32's ends on the way
+    const float first = small ? by : 1.f, second = small ? root : root * by;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = a[i] * first * second, b[i] = b[i] * first * second;
+}
+
 // D: head_dim. Tokens [blockIdx.x * tokens, + tokens).
 template <int D>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm) rotate_kernel(const __grid_constant__ RotateParams p, int tokens) {
@@ -91,8 +117,15 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) rotate_kernel(const __
             for (int i = 0; i < 8; ++i) sum = fmaf(a[i], a[i], fmaf(b[i], b[i], sum));
 #pragma unroll
             for (int d = kLanes / 2; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+            const float mean = sum * (1.f / D) + p.eps;
+            float f = rsqrtf(mean);
+            // outside of [2^-60, 2^100] (or NaN): squares that fp32 does not hold
+            const bool odd = p.weight[which] && __float_as_uint(mean) - kLeastMean > kLargestMean - kLeastMean;
+            if (__any_sync(~0u, odd)) {
+                normed_far<D>(a, b, mean, p.eps, odd);
+                if (odd) f = 1.f;
+            }
             if (p.weight[which]) {
-                const float mean = sum * (1.f / D) + p.eps, f = mean == 0.f ? 0.f : rsqrtf(mean);
                 float wa[8], wb[8];
                 unpack(which ? wl[1] : wl[0], wa);
                 unpack(which ? wh[1] : wh[0], wb);
