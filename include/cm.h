@@ -629,8 +629,9 @@ typedef struct cm_qk_rows {
 } cm_qk_rows;
 
 /* q_out and k_out: every head's row x of q and k, y = x / sqrt(mean x^2 + eps) * weight (0 where the root is 0), rotated to its
- * row's position as the keys of a fragment are: (y_j, y_{j + head_dim / 2}) by position * theta^(-2j / head_dim), theta the
- * context's. fp32, rounded once to bf16; angles are exact to some 2^-24 turns at any position, and rows of any size are normed as
+ * row's position by the angles of a fragment's keys: (y_j, y_{j + head_dim / 2}) by position * theta^(-2j / head_dim), theta the
+ * context's. fp32, rounded once to bf16 (a fragment's keys, which are fp64 before they are rounded, may be the next bf16 number);
+ * angles are exact to some 2^-24 turns at any position, and rows of any size are normed as
  * exactly, with eps 0 too. q_out may be q, with the same strides, and k_out k. */
 cm_status cm_qk_rotate(cm_context *ctx, const cm_qk_rows *rows, cm_stream_t stream);
 

@@ -9,12 +9,13 @@
 // so a value that moves is rounded once more at most, and not at all if the scales are alike.
 //
 // path_i >= i, so what a block takes comes from itself or from later blocks, and a warp that goes through one
-// (layer, head, K or V) of a request block by block, and reads 16 rows or so before it writes them, never reads what it
-// has written. A thread block looks up where a request's rows lie once, for several layers and heads. One more thread
-// block adds up the lengths and lists the blocks given back. Bound by the chain of dependent reads (lengths, path,
-// table, codes and scales), then by the tokens that stay in a block whose scale grows, which are most of the traffic: 64 requests,
-// 36 layers of 8 heads of 128, about two rows moved in each: 10.0 us; four heads to a warp 9.9 there, but 4.4 instead of 3.5
-// for 6 requests of 4 layers; one head 10.9.
+// (layer, head, K or V) of a request block by block, and reads some rows (kHeld * 512 / head_dim of them) before it writes
+// them, never reads what it has written. A thread block looks up where a request's rows lie once, for several layers and
+// heads. One more thread block adds up the lengths and lists the blocks given back. Bound by the chain of dependent reads:
+// lengths, path and table, then for each pair of heads that a warp takes codes and scales, and, where a scale grows, the tokens that
+// stay, some rows after another. 64 requests, 36 layers of 8 heads of 128, two to three such rounds to a warp, about two rows moved in
+// each: 10.0 us again and again on one cache, whose scales have grown then; 13 where codes and scales are not in L2, 33 there where some
+// 4,100 scales grow. Four heads to a warp 9.9 instead of 10.0, but 4.4 instead of 3.5 for 6 requests of 4 layers; one head 10.9.
 #include "cm_tree_kernels.h"
 
 #include "cm_qcache_codes.h"

@@ -132,7 +132,7 @@ def rotate_qk(ctx: Context, q, k, positions, q_weight=None, k_weight=None, eps: 
               stream=None) -> Tuple[object, object]:
     """(q_out, k_out): every head's row of q and k (bf16 CUDA tensors [rows, heads, head_dim], head_dim contiguous; views of a
     fused projection, say), normed (x / sqrt(mean x^2 + eps) * weight; a weight of None: not) and rotated to
-    positions [rows] (int32), as the keys of a fragment are, with the context's rope_theta. Either of q and k may be None. q_out
+    positions [rows] (int32) by the angles of a fragment's keys, with the context's rope_theta, in fp32. Either of q and k may be None. q_out
     and k_out are made if not given, on `stream`; they may be q and k themselves."""
     import torch
     _require(q is not None or k is not None, "q or k must be given")
